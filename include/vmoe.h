@@ -78,7 +78,8 @@ typedef enum { VMOE_F32 = 0, VMOE_BF16 = 1 } vmoe_dtype;
 enum {
     VMOE_LOGITS_IN = 1u << 0, /* vmoe_route reads `logits` instead of computing them */
     VMOE_NO_RENORM = 1u << 1, /* gate = softmax probability (V-MoE); default renormalises over top-k */
-    VMOE_GELU_TANH = 1u << 2  /* tanh-approximate GELU; default is the exact erf form */
+    VMOE_GELU_TANH = 1u << 2, /* tanh-approximate GELU; default is the exact erf form */
+    VMOE_DLOGITS_ADD = 1u << 3 /* vmoe_router_bwd adds to the gradients that `dlogits` holds */
 };
 
 /* The problem statement: T tasks, each with N tokens of width d_model, its own
@@ -301,6 +302,154 @@ int vmoe_router_bwd(const vmoe_problem *p, const void *x, const float *w_router,
                     const int32_t *slot, const void *dy, const void *ye, float *dgate,
                     float *dlogits, float *dw_router, float *dbias, void *dx,
                     void *cuda_stream);
+
+/* Balance losses of the routers, with per-expert counts (they keep what an
+ * uneven router would send to a full expert, Challenge #1, from being dropped).
+ * Per task t, over the M tokens that take part, with p = softmax(logits):
+ *   count[t,e]  = choices j of tokens n with expert_idx[t,n,j] = e, before the
+ *                 capacity drops any
+ *   excess[t,e] = sum_n p[n,e] - M / E, the expert's importance above an even share
+ *   loss[t,0]   = E / (k M^2) sum_e count_e sum_n p[n,e]     (1 for an even load)
+ *   loss[t,1]   = E / M^2 sum_e excess_e^2    (squared coefficient of variation of
+ *                 the importances)
+ *   loss[t,2]   = 1 / M sum_n lse_n^2, lse_n = log sum_e exp(logits[n,e])
+ * A token takes part unless its token_mask is 0 or all its logits are -inf; one
+ * that does not reaches no output, whatever its logits and choices hold.  A task
+ * without tokens gets zeros.  Single logits of -inf are experts of probability 0.
+ * An index outside [0, E) is not counted; a NaN or +inf logit of a token that
+ * takes part makes its task's excess and losses NaN.
+ *   logits [T,N,E] fp32, expert_idx [T,N,k] (from vmoe_route), token_mask [T,N]
+ *   uint8 nullable; count [T,E] int32, tokens [T] int32 (= M), excess [T,E] fp32,
+ *   loss [T,3] fp32 out (every element written).
+ *   workspace: caller-owned device scratch of vmoe_balance_workspace_size(p)
+ *   bytes or more (else VMOE_ERR_INVALID), 16-byte aligned, its contents clobbered.
+ * p->d_model, d_ff, the capacity, the dtype and the flags are not used.  Sums in
+ * fp32 and in fixed orders; the counts are whole numbers. */
+int vmoe_balance(const vmoe_problem *p, const float *logits, const int32_t *expert_idx,
+                 const uint8_t *token_mask, int32_t *count, int32_t *tokens, float *excess, float *loss,
+                 void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Device bytes of scratch vmoe_balance needs for `p`, or 0 if `p` is invalid.  Host only. */
+size_t vmoe_balance_workspace_size(const vmoe_problem *p);
+
+/* Gradient of sum_t,i dloss[t,i] loss[t,i] by the logits (the counts have none):
+ *   c_e = dloss[t,0] E / (k M^2) count_e + dloss[t,1] 2 E / M^2 excess_e,
+ *   dlogits[t,n,e] = p_e (c_e - sum_i p_i c_i + dloss[t,2] 2 / M lse_n),
+ * 0 for a token that does not take part.  logits and token_mask as given to
+ * vmoe_balance; count, tokens and excess as it wrote them; dloss [T,3] fp32 on the
+ * device; dlogits [T,N,E] fp32 out (every element written), which may be logits
+ * itself.  Give it to vmoe_router_bwd with VMOE_DLOGITS_ADD. */
+int vmoe_balance_bwd(const vmoe_problem *p, const float *logits, const uint8_t *token_mask,
+                     const int32_t *count, const int32_t *tokens, const float *excess,
+                     const float *dloss, float *dlogits, void *cuda_stream);
+
+enum {
+    VMOE_NORM_RMS = 1u << 0,  /* root-mean-square norms (no mean); default is the layer norm */
+    VMOE_NORM_POST = 1u << 1  /* a norm on the branch y */
+};
+
+/* The norms around a layer: norm(v) = (v - mean) / sqrt(var + eps) * weight + bias
+ * over the d channels of a token (mean 0 with VMOE_NORM_RMS). */
+typedef struct {
+    float eps;            /* > 0 */
+    float residual_scale; /* rho */
+    uint32_t flags;
+} vmoe_norm;
+
+/* A transformer block's residual around its expert layer (Section 2.1), in one
+ * pass over the tokens:
+ *   w = norm(y; post_w, post_b) with VMOE_NORM_POST, else y
+ *   z = rho x + gate * w             rounded to p->dtype
+ *   u = norm(z; pre_w, pre_b)        of z as stored: the next layer's input
+ * y NULL: no branch, u = norm(x); z, gate, post_* are NULL then.  u NULL: z alone;
+ * pre_* are NULL then.  At least one of y and u is given.
+ *   x, y, z, u [T,N,d] p->dtype; post_w, post_b, gate, pre_w, pre_b [T,d] fp32,
+ *   each nullable (weights and gate 1, biases 0); post_stat, pre_stat [T,N,2]
+ *   fp32 out, nullable: each norm's mean and 1 / sqrt(var + eps), for the backward.
+ * z may be x itself; no other output may overlap an input.  d_model <= 8192 and
+ * T*N < 2^31 (else VMOE_ERR_UNSUPPORTED).  Statistics and sums in fp32. */
+int vmoe_block_norm(const vmoe_problem *p, const vmoe_norm *norm, const void *x, const void *y,
+                    const float *post_w, const float *post_b, const float *gate, const float *pre_w,
+                    const float *pre_b, void *z, void *u, float *post_stat, float *pre_stat,
+                    void *cuda_stream);
+
+/* Device bytes of scratch vmoe_block_norm_bwd needs for `p`, or 0 if `p` is
+ * invalid or unsupported.  Host only. */
+size_t vmoe_block_norm_bwd_workspace_size(const vmoe_problem *p);
+
+/* Backward of vmoe_block_norm for the gradients dz of z and du of u (either may
+ * be NULL: zero), with dzt = dz + (d u / d z)^T du:
+ *   dx = rho dzt (dzt where y is NULL),  dy = (d w / d y)^T (gate * dzt),
+ *   dpost_w = sum_n gate * dzt * yhat,  dpost_b = sum_n gate * dzt,  dgate = sum_n dzt * w,
+ *   dpre_w = sum_n du * zhat,  dpre_b = sum_n du,
+ * yhat and zhat the normalised y and z (yhat = y without VMOE_NORM_POST).
+ *   y as given to the forward (NULL: no branch; dy, post_*, gate and their
+ *   gradients are NULL then); z as it was stored, or x without a branch, needed
+ *   with du; post_stat (with y and VMOE_NORM_POST) and pre_stat (with du) from the
+ *   forward; the parameters as given to it.  du NULL: pre_* and their gradients
+ *   are NULL.  dx, dy [T,N,d] p->dtype out; the parameters' gradients [T,d] fp32
+ *   out, each nullable, NULL where its parameter is.
+ *   workspace: caller-owned device scratch of
+ *   vmoe_block_norm_bwd_workspace_size(p) bytes or more (else VMOE_ERR_INVALID),
+ *   16-byte aligned, its contents clobbered.
+ * dx may be dz itself; no other output may overlap an input.  Sums in fp32 and in
+ * fixed orders; no atomics. */
+int vmoe_block_norm_bwd(const vmoe_problem *p, const vmoe_norm *norm, const void *y, const void *z,
+                        const float *post_stat, const float *pre_stat, const float *post_w,
+                        const float *post_b, const float *gate, const float *pre_w, const void *dz,
+                        const void *du, void *dx, void *dy, float *dpost_w, float *dpost_b,
+                        float *dgate, float *dpre_w, float *dpre_b, void *workspace,
+                        size_t workspace_bytes, void *cuda_stream);
+
+typedef enum {
+    VMOE_STATE_F32 = 0,  /* m and v in fp32 */
+    VMOE_STATE_E4M3 = 1  /* m and sqrt(v) in 8 bits, a scale for each 256 elements */
+} vmoe_adamw_state;
+
+/* One tensor of vmoe_adamw; device pointers, 16-byte aligned (the scales: 4). */
+typedef struct {
+    void *param;       /* [numel], updated in place */
+    const void *grad;  /* [numel] */
+    void *m, *v;       /* moments, [numel]: fp32, or e4m3 with VMOE_STATE_E4M3 */
+    float *m_scale, *v_scale; /* [ceil(numel / 256)] with VMOE_STATE_E4M3, else NULL */
+    float *master;     /* [numel] fp32 copy of bf16 parameters that the update works on, nullable */
+    int64_t numel;     /* 0: the tensor is passed over */
+    int32_t param_dtype, grad_dtype; /* vmoe_dtype; fp32 parameters have fp32 gradients */
+    int32_t state;     /* vmoe_adamw_state */
+    float lr_scale, weight_decay;
+} vmoe_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps; /* lr finite, betas in [0, 1), eps > 0 (as fp32 too) */
+    int32_t step;            /* t, 1 for the first update */
+    uint32_t seed;           /* of the 8-bit moments' rounding */
+    const int32_t *step_dev; /* device, nullable: t = step + *step_dev (at least 1) */
+    const float *lr_dev;     /* device, nullable: the learning rate is lr times *lr_dev */
+    const float *grad_scale; /* device, nullable: gradients are taken times it */
+} vmoe_adamw_config;
+
+/* One AdamW update of n tensors (the adaptation of Section 3.1) in one launch for
+ * up to 380 of them, with r = lr lr_scale:
+ *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+ *   p = p (1 - r weight_decay) - r (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps),
+ * in fp32; bf16 parameters are rounded to nearest from the master copy, or from
+ * their own updated value where there is none.  `tensors` and `config` are host
+ * memory, read before the call returns; step, lr and seed of a captured call stay
+ * what they were, so a graph that is replayed takes step_dev and lr_dev.
+ * A grad_scale that is infinite or NaN leaves everything as it was.
+ * VMOE_STATE_E4M3: element i is held as m = m_scale[i / 256] * m[i] and sqrt(v) =
+ * v_scale[i / 256] * v[i]; a new scale is its block's largest magnitude / 448 (0
+ * below 2^-100, where the block's moments become 0), and a value a = |m| / scale
+ * becomes grid * floor(a / grid + (16 R + 8) / 2^20), at most 448, grid the step of
+ * e4m3 at a: rounded up or down at random, a in the mean.  R is the low (m) or the
+ * high (v) half of mix(0x51f6db5b i + 0x5e4087b3 place + 0x339cd49b t + 0xe32a5e87
+ * seed) mod 2^32, place the tensor's index in the call, with mix(h): h = (h ^ h >>
+ * 16) * 0x9e4a8af7, h = (h ^ h >> 15) * 0xa6bd2c99, h ^ h >> 16.  An infinite
+ * moment makes its block's moments NaN.
+ * The tensors' arrays may not overlap (not checked here; one array given twice is a
+ * race).  numel < 2^38.  Asynchronous on `cuda_stream`; no workspace. */
+int vmoe_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_config *config,
+               void *cuda_stream);
 
 /* Cross-task slice planner (Section 3.2.1, fragmentation-aware expert
  * grouping; host code, no GPU).  Items (experts) i = 0..n-1 have a memory

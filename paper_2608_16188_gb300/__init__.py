@@ -30,6 +30,13 @@ VMOE_BF16 = 1
 VMOE_LOGITS_IN = 1 << 0
 VMOE_NO_RENORM = 1 << 1
 VMOE_GELU_TANH = 1 << 2
+VMOE_DLOGITS_ADD = 1 << 3
+
+VMOE_NORM_RMS = 1 << 0
+VMOE_NORM_POST = 1 << 1
+
+VMOE_STATE_F32 = 0
+VMOE_STATE_E4M3 = 1
 
 # Every symbol include/vmoe.h declares.
 EXPORTS = ("vmoe_version", "vmoe_status_string", "vmoe_problem_capacity", "vmoe_route",
@@ -37,6 +44,8 @@ EXPORTS = ("vmoe_version", "vmoe_status_string", "vmoe_problem_capacity", "vmoe_
            "vmoe_expert_bwd_min_workspace_size",
            "vmoe_expert_bwd", "vmoe_expert_bwd_static_scratch", "vmoe_combine", "vmoe_router_bwd", "vmoe_plan_slices", "vmoe_plan_shares",
            "vmoe_attn_expert_fwd", "vmoe_attn_expert_bwd", "vmoe_attn_expert_bwd_workspace_size",
+           "vmoe_balance", "vmoe_balance_workspace_size", "vmoe_balance_bwd", "vmoe_block_norm", "vmoe_block_norm_bwd",
+           "vmoe_block_norm_bwd_workspace_size", "vmoe_adamw",
            "vmoe_device_status", "vmoe_selftest_bounded_wait", "vmoe_trace_enable",
            "vmoe_trace_disable", "vmoe_trace_get")
 
@@ -53,6 +62,27 @@ class VmoeProblem(ctypes.Structure):
                 ("d_ff", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32),
                 ("capacity_factor", ctypes.c_double), ("capacity", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class VmoeNorm(ctypes.Structure):
+    """Mirror of ``vmoe_norm`` in include/vmoe.h."""
+    _fields_ = [("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class VmoeAdamwTensor(ctypes.Structure):
+    """Mirror of ``vmoe_adamw_tensor`` in include/vmoe.h."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("master", ctypes.c_void_p), ("numel", ctypes.c_int64), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("state", ctypes.c_int32), ("lr_scale", ctypes.c_float),
+                ("weight_decay", ctypes.c_float)]
+
+
+class VmoeAdamwConfig(ctypes.Structure):
+    """Mirror of ``vmoe_adamw_config`` in include/vmoe.h."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int32), ("seed", ctypes.c_uint32),
+                ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
 _lib = None
@@ -85,6 +115,13 @@ def library():
             "vmoe_attn_expert_fwd": (ctypes.c_int, [PP, ctypes.c_int] + [_P] * 9),
             "vmoe_attn_expert_bwd_workspace_size": (ctypes.c_size_t, [PP, ctypes.c_int]),
             "vmoe_attn_expert_bwd": (ctypes.c_int, [PP, ctypes.c_int] + [_P] * 12 + [ctypes.c_size_t, _P]),
+            "vmoe_balance_workspace_size": (ctypes.c_size_t, [PP]),
+            "vmoe_balance": (ctypes.c_int, [PP] + [_P] * 8 + [ctypes.c_size_t, _P]),
+            "vmoe_balance_bwd": (ctypes.c_int, [PP] + [_P] * 8),
+            "vmoe_block_norm": (ctypes.c_int, [PP, ctypes.POINTER(VmoeNorm)] + [_P] * 12),
+            "vmoe_block_norm_bwd_workspace_size": (ctypes.c_size_t, [PP]),
+            "vmoe_block_norm_bwd": (ctypes.c_int, [PP, ctypes.POINTER(VmoeNorm)] + [_P] * 18 + [ctypes.c_size_t, _P]),
+            "vmoe_adamw": (ctypes.c_int, [ctypes.c_int, _P, ctypes.POINTER(VmoeAdamwConfig), _P]),
             "vmoe_plan_slices": (ctypes.c_int, [ctypes.c_int, _P, _P, ctypes.c_int64,
                                                 ctypes.c_double, ctypes.c_double, _P, _P]),
             "vmoe_plan_shares": (ctypes.c_int, [ctypes.c_int, _P, _P, _P, ctypes.c_int32, _P]),
@@ -252,6 +289,153 @@ def vmoe_router_bwd(p, x, w_router, logits, expert_idx, gate, slot, dy, ye, dgat
         ctypes.byref(p), _ptr(x), _ptr(w_router), _ptr(logits), _ptr(expert_idx), _ptr(gate),
         _ptr(slot), _ptr(dy), _ptr(ye), _ptr(dgate), _ptr(dlogits), _ptr(dw_router), _ptr(dbias),
         _ptr(dx), _stream(stream)), "vmoe_router_bwd")
+
+
+_DTYPES = None
+
+
+def _dtypes():
+    """The torch dtypes that the checks below compare with, looked up once."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {"f32": torch.float32, "i32": torch.int32, "u8": torch.uint8, "fp8": torch.float8_e4m3fn,
+                   VMOE_F32: torch.float32, VMOE_BF16: torch.bfloat16}
+    return _DTYPES
+
+
+def _arrays(where, *args):
+    """Device pointers of (tensor, dtype, elements) triples.
+
+    A tensor has to be contiguous, on the current device, of that dtype and of as many
+    elements: one that is not would be read as something else, or past its end.  None and
+    raw pointers are handed on."""
+    import torch
+    kinds, device, out = _dtypes(), -1, []
+    for t, dtype, n in args:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        if device < 0:
+            device = torch.cuda.current_device() if t.is_cuda else -2
+        if not t.is_cuda or t.get_device() != device or t.dtype != kinds[dtype] or t.numel() != n or not t.is_contiguous():
+            raise VmoeError(VMOE_ERR_INVALID, "%s: a tensor of %s, %s on %s, where %d contiguous elements of %s are read on "
+                            "the current device" % (where, tuple(t.shape), t.dtype, t.device, n, kinds[dtype]))
+        out.append(t.data_ptr())
+    return out
+
+
+def _workspace(where, t, nbytes):
+    if t is None or isinstance(t, int):
+        return t, int(nbytes or 0)
+    have = t.numel() * t.element_size()
+    if not t.is_cuda or not t.is_contiguous() or (nbytes is not None and nbytes > have):
+        raise VmoeError(VMOE_ERR_INVALID, where)
+    return t.data_ptr(), have if nbytes is None else int(nbytes)
+
+
+def vmoe_balance_workspace_size(p) -> int:
+    return int(library().vmoe_balance_workspace_size(ctypes.byref(p)))
+
+
+def vmoe_balance(p, logits, expert_idx, token_mask, count, tokens, excess, loss, workspace, workspace_bytes=None,
+                 stream=None):
+    """Balance losses of the routers and per-expert counts (see include/vmoe.h)."""
+    te, tn = p.T * p.E, p.T * p.N
+    a = _arrays("vmoe_balance", (logits, "f32", tn * p.E), (expert_idx, "i32", tn * p.k), (token_mask, "u8", tn),
+                (count, "i32", te), (tokens, "i32", p.T), (excess, "f32", te), (loss, "f32", 3 * p.T))
+    ws, nbytes = _workspace("vmoe_balance", workspace, workspace_bytes)
+    _check(library().vmoe_balance(ctypes.byref(p), *a, ws, nbytes, _stream(stream)), "vmoe_balance")
+
+
+def vmoe_balance_bwd(p, logits, token_mask, count, tokens, excess, dloss, dlogits, stream=None):
+    """Gradient of the weighted balance losses by the logits (see include/vmoe.h)."""
+    te, tn = p.T * p.E, p.T * p.N
+    a = _arrays("vmoe_balance_bwd", (logits, "f32", tn * p.E), (token_mask, "u8", tn), (count, "i32", te),
+                (tokens, "i32", p.T), (excess, "f32", te), (dloss, "f32", 3 * p.T), (dlogits, "f32", tn * p.E))
+    _check(library().vmoe_balance_bwd(ctypes.byref(p), *a, _stream(stream)), "vmoe_balance_bwd")
+
+
+def norm_config(rms=False, post=True, eps=1e-6, residual_scale=1.0):
+    """Build a VmoeNorm: layer or root-mean-square norms, with or without one on the branch."""
+    return VmoeNorm(float(eps), float(residual_scale), (VMOE_NORM_RMS if rms else 0) | (VMOE_NORM_POST if post else 0))
+
+
+def vmoe_block_norm(p, norm, x, y, post_w, post_b, gate, pre_w, pre_b, z, u, post_stat=None, pre_stat=None, stream=None):
+    """z = rho x + gate * norm(y) and u = norm(z) (see include/vmoe.h)."""
+    n, td, st = p.T * p.N * p.d_model, p.T * p.d_model, 2 * p.T * p.N
+    a = _arrays("vmoe_block_norm", (x, p.dtype, n), (y, p.dtype, n), (post_w, "f32", td), (post_b, "f32", td),
+                (gate, "f32", td), (pre_w, "f32", td), (pre_b, "f32", td), (z, p.dtype, n), (u, p.dtype, n),
+                (post_stat, "f32", st), (pre_stat, "f32", st))
+    _check(library().vmoe_block_norm(ctypes.byref(p), ctypes.byref(norm), *a, _stream(stream)), "vmoe_block_norm")
+
+
+def vmoe_block_norm_bwd_workspace_size(p) -> int:
+    return int(library().vmoe_block_norm_bwd_workspace_size(ctypes.byref(p)))
+
+
+def vmoe_block_norm_bwd(p, norm, y, z, post_stat, pre_stat, post_w, post_b, gate, pre_w, dz, du, dx, dy, dpost_w, dpost_b,
+                        dgate, dpre_w, dpre_b, workspace, workspace_bytes=None, stream=None):
+    """Backward of vmoe_block_norm (see include/vmoe.h)."""
+    n, td, st = p.T * p.N * p.d_model, p.T * p.d_model, 2 * p.T * p.N
+    a = _arrays("vmoe_block_norm_bwd", (y, p.dtype, n), (z, p.dtype, n), (post_stat, "f32", st), (pre_stat, "f32", st),
+                (post_w, "f32", td), (post_b, "f32", td), (gate, "f32", td), (pre_w, "f32", td), (dz, p.dtype, n),
+                (du, p.dtype, n), (dx, p.dtype, n), (dy, p.dtype, n), (dpost_w, "f32", td), (dpost_b, "f32", td),
+                (dgate, "f32", td), (dpre_w, "f32", td), (dpre_b, "f32", td))
+    ws, nbytes = _workspace("vmoe_block_norm_bwd", workspace, workspace_bytes)
+    _check(library().vmoe_block_norm_bwd(ctypes.byref(p), ctypes.byref(norm), *a, ws, nbytes, _stream(stream)),
+           "vmoe_block_norm_bwd")
+
+
+def adamw_tensors(tensors):
+    """The host table of vmoe_adamw, built once for a set of tensors.
+
+    ``tensors``: dicts with param, grad, m, v (torch tensors; fp32 moments, or
+    float8_e4m3fn ones with m_scale and v_scale), and optionally master, lr_scale and
+    weight_decay.  The table keeps the tensors alive.  One array in two places is refused:
+    its update would be a race."""
+    tensors = [dict(t) for t in tensors]
+    table = (VmoeAdamwTensor * max(1, len(tensors)))()
+    kinds = _dtypes()
+    code = {kinds[VMOE_F32]: VMOE_F32, kinds[VMOE_BF16]: VMOE_BF16}
+    written, read = [], []
+    for e, t in zip(table, tensors):
+        param, n = t["param"], t["param"].numel()
+        if param.dtype not in code or t["grad"].dtype not in code:
+            raise VmoeError(VMOE_ERR_INVALID, "adamw_tensors")
+        e.param_dtype, e.grad_dtype, e.numel = code[param.dtype], code[t["grad"].dtype], n
+        eight = t["m"].dtype == kinds["fp8"]
+        e.state = VMOE_STATE_E4M3 if eight else VMOE_STATE_F32
+        state, blocks = "fp8" if eight else "f32", (n + 255) // 256
+        if not eight and (t.get("m_scale") is not None or t.get("v_scale") is not None):
+            raise VmoeError(VMOE_ERR_INVALID, "adamw_tensors: scales of fp32 moments")
+        if eight and (t.get("m_scale") is None or t.get("v_scale") is None):
+            raise VmoeError(VMOE_ERR_INVALID, "adamw_tensors: 8-bit moments without scales")
+        names = ("param", "grad", "m", "v", "m_scale", "v_scale", "master")
+        sizes = (e.param_dtype, n), (e.grad_dtype, n), (state, n), (state, n), ("f32", blocks), ("f32", blocks), ("f32", n)
+        ptrs = _arrays("adamw_tensors", *((t.get(k), *s) for k, s in zip(names, sizes)))
+        for name, ptr in zip(names, ptrs):
+            setattr(e, name, ptr)
+            if ptr and t[name].numel():
+                span = (ptr, ptr + t[name].numel() * t[name].element_size())
+                (read if name == "grad" else written).append(span)
+        e.lr_scale, e.weight_decay = float(t.get("lr_scale", 1.0)), float(t.get("weight_decay", 0.0))
+    spans = sorted([(b, e, True) for b, e in written] + [(b, e, False) for b, e in read])
+    end, last_write = 0, 0  # of all arrays so far, and of the written ones
+    for b, e, w in spans:
+        if b < (end if w else last_write):
+            raise VmoeError(VMOE_ERR_INVALID, "adamw_tensors: two arrays overlap")
+        end, last_write = max(end, e), max(last_write, e) if w else last_write
+    table.tensors, table.count = tensors, len(tensors)
+    return table
+
+
+def vmoe_adamw(table, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, step_dev=None, lr_dev=None, grad_scale=None,
+               stream=None):
+    """One AdamW update of the tensors of ``table`` (adamw_tensors; see include/vmoe.h)."""
+    a = _arrays("vmoe_adamw", (step_dev, "i32", 1), (lr_dev, "f32", 1), (grad_scale, "f32", 1))
+    c = VmoeAdamwConfig(lr, beta1, beta2, eps, step, seed & 0xffffffff, *a)
+    _check(library().vmoe_adamw(table.count, table, ctypes.byref(c), _stream(stream)), "vmoe_adamw")
 
 
 def vmoe_plan_slices(weight, lifespan, capacity: int, eta: float = 0.0, budget: float = 0.0):

@@ -134,7 +134,7 @@ static int check_problem(const vmoe_problem *p, Dims *d) {
     if (p->capacity < 0) return VMOE_ERR_INVALID;
     if (p->capacity == 0 && !(p->capacity_factor > 0.0 && isfinite(p->capacity_factor)))
         return VMOE_ERR_INVALID;
-    if (p->flags & ~(uint32_t)(VMOE_LOGITS_IN | VMOE_NO_RENORM | VMOE_GELU_TANH))
+    if (p->flags & ~(uint32_t)(VMOE_LOGITS_IN | VMOE_NO_RENORM | VMOE_GELU_TANH | VMOE_DLOGITS_ADD))
         return VMOE_ERR_INVALID;
     if (p->E > 256) return VMOE_ERR_UNSUPPORTED;
     if ((long long)p->T * p->E > 1024) return VMOE_ERR_UNSUPPORTED;
@@ -355,6 +355,121 @@ int vmoe_attn_expert_bwd(const vmoe_problem *p, int heads, const void *xe, const
                                   (const __nv_bfloat16 *)wo, (const __nv_bfloat16 *)dye, load,
                                   (__nv_bfloat16 *)dxe, (__nv_bfloat16 *)dwqkv, (__nv_bfloat16 *)dwo,
                                   workspace, (cudaStream_t)cuda_stream);
+}
+
+size_t vmoe_balance_workspace_size(const vmoe_problem *p) {
+    Dims d;
+    return check_problem(p, &d) == VMOE_OK ? balance_workspace(d) : 0;
+}
+
+int vmoe_balance(const vmoe_problem *p, const float *logits, const int32_t *expert_idx,
+                 const uint8_t *token_mask, int32_t *count, int32_t *tokens, float *excess, float *loss,
+                 void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    Dims d;
+    int st = check_problem(p, &d);
+    if (st != VMOE_OK) return st;
+    if (!dev_ok(logits) || !dev_ok(expert_idx) || !opt_ok(token_mask) || !dev_ok(count) || !dev_ok(tokens) ||
+        !dev_ok(excess) || !dev_ok(loss) || !dev_ok(workspace) || workspace_bytes < balance_workspace(d))
+        return VMOE_ERR_INVALID;
+    return launch_balance(d, logits, expert_idx, token_mask, count, tokens, excess, loss, (float *)workspace,
+                          (cudaStream_t)cuda_stream);
+}
+
+int vmoe_balance_bwd(const vmoe_problem *p, const float *logits, const uint8_t *token_mask,
+                     const int32_t *count, const int32_t *tokens, const float *excess,
+                     const float *dloss, float *dlogits, void *cuda_stream) {
+    Dims d;
+    int st = check_problem(p, &d);
+    if (st != VMOE_OK) return st;
+    if (!dev_ok(logits) || !opt_ok(token_mask) || !dev_ok(count) || !dev_ok(tokens) || !dev_ok(excess) ||
+        !dev_ok(dloss) || !dev_ok(dlogits))
+        return VMOE_ERR_INVALID;
+    return launch_balance_bwd(d, logits, token_mask, count, tokens, excess, dloss, dlogits, (cudaStream_t)cuda_stream);
+}
+
+// The problem and the norm's description; d <= 8192 (32 warps of 256 channels hold a row).
+static int check_norm(const vmoe_problem *p, const vmoe_norm *n, Dims *d) {
+    int st = check_problem(p, d);
+    if (st != VMOE_OK) return st;
+    if (n && (!(n->eps > 0.0f) || !isfinite(n->eps) || !isfinite(n->residual_scale) ||
+              (n->flags & ~(uint32_t)(VMOE_NORM_RMS | VMOE_NORM_POST))))
+        return VMOE_ERR_INVALID;
+    if (d->d > 8192 || (long long)d->T * d->N >= (1LL << 31)) return VMOE_ERR_UNSUPPORTED;
+    return VMOE_OK;
+}
+
+int vmoe_block_norm(const vmoe_problem *p, const vmoe_norm *norm, const void *x, const void *y,
+                    const float *post_w, const float *post_b, const float *gate, const float *pre_w,
+                    const float *pre_b, void *z, void *u, float *post_stat, float *pre_stat,
+                    void *cuda_stream) {
+    Dims d;
+    if (!norm) return VMOE_ERR_INVALID;
+    int st = check_norm(p, norm, &d);
+    if (st != VMOE_OK) return st;
+    if (!dev_ok(x) || !opt_ok(y) || !opt_ok(post_w) || !opt_ok(post_b) || !opt_ok(gate) || !opt_ok(pre_w) ||
+        !opt_ok(pre_b) || !opt_ok(z) || !opt_ok(u) || !opt_ok(post_stat) || !opt_ok(pre_stat))
+        return VMOE_ERR_INVALID;
+    const bool post = y && (norm->flags & VMOE_NORM_POST);
+    if ((!y && !u) || (y != nullptr) != (z != nullptr) || (!y && gate) || (!post && (post_w || post_b || post_stat)) ||
+        (!u && (pre_w || pre_b || pre_stat)))
+        return VMOE_ERR_INVALID;
+    return launch_block_norm(d, norm, x, y, post_w, post_b, gate, pre_w, pre_b, z, u, post_stat, pre_stat,
+                             (cudaStream_t)cuda_stream);
+}
+
+size_t vmoe_block_norm_bwd_workspace_size(const vmoe_problem *p) {
+    Dims d;
+    return check_norm(p, nullptr, &d) == VMOE_OK ? norm_bwd_workspace(d) : 0;
+}
+
+int vmoe_block_norm_bwd(const vmoe_problem *p, const vmoe_norm *norm, const void *y, const void *z,
+                        const float *post_stat, const float *pre_stat, const float *post_w,
+                        const float *post_b, const float *gate, const float *pre_w, const void *dz,
+                        const void *du, void *dx, void *dy, float *dpost_w, float *dpost_b,
+                        float *dgate, float *dpre_w, float *dpre_b, void *workspace,
+                        size_t workspace_bytes, void *cuda_stream) {
+    Dims d;
+    if (!norm) return VMOE_ERR_INVALID;
+    int st = check_norm(p, norm, &d);
+    if (st != VMOE_OK) return st;
+    if (!opt_ok(y) || !opt_ok(z) || !opt_ok(post_stat) || !opt_ok(pre_stat) || !opt_ok(post_w) || !opt_ok(post_b) ||
+        !opt_ok(gate) || !opt_ok(pre_w) || !opt_ok(dz) || !opt_ok(du) || !dev_ok(dx) || !opt_ok(dy) || !opt_ok(dpost_w) ||
+        !opt_ok(dpost_b) || !opt_ok(dgate) || !opt_ok(dpre_w) || !opt_ok(dpre_b) || !dev_ok(workspace))
+        return VMOE_ERR_INVALID;
+    const bool post = y && (norm->flags & VMOE_NORM_POST);
+    if ((!dz && !du) || (!y && !du) || (y != nullptr) != (dy != nullptr) || (!y && gate) ||
+        (!post && (post_w || post_b)) || (post && !post_stat) || (du ? !z || !pre_stat : pre_w || dpre_w || dpre_b) ||
+        (dpost_w && !post_w) || (dpost_b && !post_b) || (dgate && !gate) || (dpre_w && !pre_w) ||
+        workspace_bytes < norm_bwd_workspace(d))
+        return VMOE_ERR_INVALID;
+    return launch_block_norm_bwd(d, norm, y, z, post_stat, pre_stat, post_w, post_b, gate, pre_w, dz, du, dx, dy,
+                                 dpost_w, dpost_b, dgate, dpre_w, dpre_b, (float *)workspace,
+                                 (cudaStream_t)cuda_stream);
+}
+
+int vmoe_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_config *config, void *cuda_stream) {
+    if (n < 0 || (n > 0 && !tensors) || !config) return VMOE_ERR_INVALID;
+    const vmoe_adamw_config &c = *config;
+    if (!isfinite(c.lr) || !isfinite((float)c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
+        !((float)c.eps > 0.0f) || !isfinite((float)c.eps) || c.step < (c.step_dev ? 0 : 1))
+        return VMOE_ERR_INVALID;
+    if (((uintptr_t)c.step_dev & 3u) || ((uintptr_t)c.lr_dev & 3u) || ((uintptr_t)c.grad_scale & 3u)) return VMOE_ERR_INVALID;
+    bool supported = true;
+    for (int i = 0; i < n; ++i) {
+        const vmoe_adamw_tensor &t = tensors[i];
+        if (t.numel < 0 || (t.param_dtype != VMOE_F32 && t.param_dtype != VMOE_BF16) ||
+            (t.grad_dtype != VMOE_F32 && t.grad_dtype != VMOE_BF16) ||
+            (t.state != VMOE_STATE_F32 && t.state != VMOE_STATE_E4M3) || !isfinite(t.lr_scale) || !isfinite(t.weight_decay))
+            return VMOE_ERR_INVALID;
+        if (t.numel == 0) continue;
+        const bool eight = t.state == VMOE_STATE_E4M3;
+        if (!dev_ok(t.param) || !dev_ok(t.grad) || !dev_ok(t.m) || !dev_ok(t.v) || !opt_ok(t.master) ||
+            (t.m_scale != nullptr) != eight || (t.v_scale != nullptr) != eight || ((uintptr_t)t.m_scale & 3u) ||
+            ((uintptr_t)t.v_scale & 3u))
+            return VMOE_ERR_INVALID;
+        supported &= t.numel < (1LL << 38) && (t.param_dtype == VMOE_BF16 || (t.grad_dtype == VMOE_F32 && !t.master));
+    }
+    return supported ? launch_adamw(n, tensors, config, (cudaStream_t)cuda_stream) : VMOE_ERR_UNSUPPORTED;
 }
 
 int vmoe_device_status(int reset) {
