@@ -161,18 +161,12 @@ __device__ __forceinline__ float sqrt_approx(float v) {
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float rcp_approx(float v) {
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-
 // The scale of a block whose largest magnitude in this lane is `top`, and 1 / scale.
 // Below 2^-100 the block is zero: 448 / top would overflow.
 __device__ __forceinline__ float2 block_scale(float top) {
     top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
     if (top < 7.888609052210118e-31f) return make_float2(0.0f, 0.0f);
-    return make_float2(top * (1.0f / 448.0f), 448.0f * rcp_approx(top));
+    return make_float2(top / 448.0f, 448.0f / top);
 }
 
 template <typename P, typename G, bool EIGHT, bool MASTER>

@@ -25,7 +25,9 @@ namespace vmoe {
 
 namespace {
 
-// Eight consecutive elements as they lie in memory, and as floats.
+// Eight consecutive elements as they lie in memory, and as four pairs of floats: the
+// arithmetic runs on packed fp32 instructions, two elements each (60 instructions an
+// element without them bound the forward at half the memory's rate, 30 do not).
 template <typename T>
 struct Raw8;
 template <>
@@ -33,46 +35,55 @@ struct Raw8<__nv_bfloat16> {
     uint4 v;
     __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void get(float (&o)[8]) const { bf16x8_to_f32(v, o); }
-    // rounds in[] to what is stored
-    __device__ __forceinline__ void set(float (&in)[8]) {
-        v = f32_to_bf16x8(in);
-        bf16x8_to_f32(v, in);
+    __device__ __forceinline__ void get(f32x2 (&o)[4]) const {
+        o[0] = bf16x2_to_f32x2(v.x);
+        o[1] = bf16x2_to_f32x2(v.y);
+        o[2] = bf16x2_to_f32x2(v.z);
+        o[3] = bf16x2_to_f32x2(v.w);
+    }
+    __device__ __forceinline__ void set(const f32x2 (&in)[4]) {
+        v = make_uint4(f32x2_to_bf16x2(in[0]), f32x2_to_bf16x2(in[1]), f32x2_to_bf16x2(in[2]), f32x2_to_bf16x2(in[3]));
     }
     __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = v; }
 };
 template <>
 struct Raw8<float> {
-    float4 a, b;
+    ulonglong2 a, b;
     __device__ __forceinline__ void load(const float *p) {
-        a = reinterpret_cast<const float4 *>(p)[0];
-        b = reinterpret_cast<const float4 *>(p)[1];
+        a = reinterpret_cast<const ulonglong2 *>(p)[0];
+        b = reinterpret_cast<const ulonglong2 *>(p)[1];
     }
-    __device__ __forceinline__ void zero() { a = b = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
-    __device__ __forceinline__ void get(float (&o)[8]) const {
-        o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-        o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+    __device__ __forceinline__ void zero() { a = b = make_ulonglong2(0, 0); }
+    __device__ __forceinline__ void get(f32x2 (&o)[4]) const {
+        o[0] = a.x;
+        o[1] = a.y;
+        o[2] = b.x;
+        o[3] = b.y;
     }
-    __device__ __forceinline__ void set(float (&in)[8]) {
-        a = make_float4(in[0], in[1], in[2], in[3]);
-        b = make_float4(in[4], in[5], in[6], in[7]);
+    __device__ __forceinline__ void set(const f32x2 (&in)[4]) {
+        a = make_ulonglong2(in[0], in[1]);
+        b = make_ulonglong2(in[2], in[3]);
     }
     __device__ __forceinline__ void store(float *p) const {
-        reinterpret_cast<float4 *>(p)[0] = a;
-        reinterpret_cast<float4 *>(p)[1] = b;
+        reinterpret_cast<ulonglong2 *>(p)[0] = a;
+        reinterpret_cast<ulonglong2 *>(p)[1] = b;
     }
 };
 
 // Eight values of a [T, d] parameter, or a constant where there is none.
-__device__ __forceinline__ void param8(const float *p, long long at, float none, float (&o)[8]) {
+__device__ __forceinline__ void param8(const float *p, long long at, float none, f32x2 (&o)[4]) {
+    Raw8<float> r;
     if (p) {
-        const float4 a = __ldg(reinterpret_cast<const float4 *>(p + at)), b = __ldg(reinterpret_cast<const float4 *>(p + at) + 1);
-        o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-        o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+        r.load(p + at);
+        r.get(o);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = none;
+        o[0] = o[1] = o[2] = o[3] = pk2(none);
     }
+}
+
+__device__ __forceinline__ float sum2(f32x2 v) {
+    const float2 f = unpk2(v);
+    return f.x + f.y;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -81,19 +92,26 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// The sum over the W warps of a row, the same in every thread.
-template <int W>
-__device__ __forceinline__ float group_sum(float v, float *buf) {
-    v = warp_sum(v);
-    if (W == 1) return v;
-    __syncthreads();  // the last sum's readers are done
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) v += buf[w];
-    return v;
+// How rows lie on a CTA, forward and backward: W = ceil(d / 256) warps hold a row, 8
+// columns a thread, so that a thread keeps its columns' parameters (and, in the
+// backward, their gradients) in registers over all rows of the CTA's slice of a task.
+// `groups` such rows, R at a time, with the next ones' loads in flight meanwhile.
+int row_warps(int d) { return (d + 255) / 256; }
+int row_groups(int d) { return std::max(1, 4 / row_warps(d)); }
+// Slices of a task's tokens: enough CTAs for `regs` registers a thread to fill 152 SMs
+// once, and `least` steps for each.
+int slices_of(const Dims &p, int R, int regs, int least) {
+    const int groups = row_groups(p.d), threads = 32 * row_warps(p.d) * groups, rows = least * R * groups;
+    const int resident = 152 * std::max(1, 65536 / (regs * threads));
+    return std::max(1, std::min((p.N + rows - 1) / rows, resident / p.T));
 }
+
+// Rows at a time and CTAs of 128 threads an SM, for 1 to 4 warps a row.  Forward: two
+// bf16 rows and five CTAs; 34 us at 17 x 1576 tokens of 768 channels and 64.5 at 8 x
+// 6304 of 1024 without a post-norm, where four rows and four CTAs took 31 and 73, two
+// rows and six CTAs 39 and 69.  Backward: two rows and three CTAs, 52 us at the former
+// size; one row and three to five CTAs 56 to 60.
+constexpr int FR = 2, FB = 5, BR = 2, BB = 3;
 
 struct FwdArgs {
     const void *x, *y;
@@ -104,101 +122,185 @@ struct FwdArgs {
     bool rms, post;
 };
 
-// mean and rstd of the NV x 8 values a thread holds of a row.
-template <int NV, int W>
-__device__ __forceinline__ float2 stats(const float (&v)[NV][8], const bool (&have)[NV], int d, bool rms, float eps, float *buf) {
-    float mean = 0.0f;
-    if (!rms) {
-        float s = 0.0f;
+// Totals of R values over the W warps of a row, the same in every thread.  The first
+// halvings of the butterfly sum two values at once; `buf` alternates between two
+// halves, so one barrier a call is enough.
+template <int WC, int R>
+struct Totals {
+    float (*buf)[32][R];
+    int first, flip;  // first warp of the group
+    int W;            // WC, or where that is 0 the number of warps
+    __device__ __forceinline__ void operator()(float (&v)[R]) {
+        const int lane = threadIdx.x & 31;
+        int mine = 0;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+        for (int h = R / 2, o = 16; h > 0; h >>= 1, o >>= 1) {
+            const bool up = (lane & o) != 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += v[j][i];
-        mean = group_sum<W>(s, buf) / (float)d;
-    }
-    float q = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (!have[j]) continue;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = v[j][i] - mean;
-            q = fmaf(c, c, q);
+            for (int i = 0; i < h; ++i) {
+                const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+            mine += up ? h : 0;
         }
+#pragma unroll
+        for (int o = 16 / R; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        float sum = v[0];
+        if (WC != 1) {
+            if (lane % (32 / R) == 0) buf[flip][threadIdx.x >> 5][mine] = sum;
+            __syncthreads();
+            sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < (WC ? WC : W); ++w) sum += buf[flip][first + w][mine];
+            flip ^= 1;
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = __shfl_sync(0xffffffffu, sum, i * (32 / R));
     }
-    q = group_sum<W>(q, buf) / (float)d;
-    return make_float2(mean, 1.0f / sqrtf(q + eps));
+};
+
+// mean and rstd of R rows.
+template <typename T, int WC, int R>
+__device__ __forceinline__ void stats(const Raw8<T> (&raw)[R], bool have, const FwdArgs &a, float share, Totals<WC, R> &totals,
+                                      float2 (&s)[R]) {
+    float m[R], q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) m[r] = 0.0f;
+    if (!a.rms) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x2 v[4];
+            raw[r].get(v);
+            m[r] = sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+        }
+        totals(m);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        f32x2 v[4], sq = 0;
+        raw[r].get(v);
+        m[r] *= share;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = add2(v[i], pk2(-m[r]));
+            sq = fma2(v[i], v[i], sq);
+        }
+        q[r] = have ? sum2(sq) : 0.0f;
+    }
+    totals(q);
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = make_float2(m[r], rsqrtf(fmaf(q[r], share, a.eps)));
 }
 
-// Forward: W warps a row, NV vectors of 8 a thread.  With W = 1 the eight warps of a
-// CTA take a row each.
-template <typename T, int NV, int W>
-__global__ void __launch_bounds__(W == 1 ? 256 : 32 * W)
-norm_fwd_kernel(Dims p, FwdArgs a) {
-    __shared__ float buf[32];
-    constexpr int GROUPS = W == 1 ? 8 : 1, TH = 32 * W;
-    const int th = threadIdx.x % TH, d = p.d;
-    const long long row = (long long)blockIdx.x * GROUPS + threadIdx.x / TH;
+// The R rows' statistics, row by row of threads.
+template <int R>
+__device__ __forceinline__ void store_stats(float2 *out, const float2 (&s)[R], int th, int rows) {
+    if (out == nullptr || th >= R || th >= rows) return;
+    float2 o = s[0];
+#pragma unroll
+    for (int r = 1; r < R; ++r)
+        if (th == r) o = s[r];
+    out[th] = o;
+}
+
+template <typename T, int WC, int MAXT, int MINB, int R, bool AHEAD>
+__global__ void __launch_bounds__(MAXT, MINB)
+norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
+    __shared__ float buf[2][32][R];
+    const int W = WC ? WC : warps;
+    const int warp = threadIdx.x >> 5, group = warp / W, th = threadIdx.x - group * 32 * W;
+    const int t = blockIdx.y, N = p.N, d = p.d, c = 8 * th;
+    const int beg = (int)((long long)N * blockIdx.x / gridDim.x), end = (int)((long long)N * (blockIdx.x + 1) / gridDim.x);
+    const bool have = c < d;
+    const float share = 1.0f / (float)d;
+    Totals<WC, R> totals = {buf, group * W, 0, W};
     pdl_wait();
-    if (row >= (long long)p.T * p.N) return;  // whole groups
-    const long long par = row / p.N * d, at = row * d;
-    float v[NV][8];
-    bool have[NV];
+    const long long par = (long long)t * d + c, base = (long long)t * N;
+    f32x2 post_w[4], post_b[4], pre_w[4], pre_b[4];
+    {
+        f32x2 gate[4];
+        param8(have ? a.gate : nullptr, par, 1.0f, gate);
+        param8(have ? a.post_w : nullptr, par, 1.0f, post_w);
+        param8(have ? a.post_b : nullptr, par, 0.0f, post_b);
+        param8(have ? a.pre_w : nullptr, par, 1.0f, pre_w);
+        param8(have ? a.pre_b : nullptr, par, 0.0f, pre_b);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (th + j * TH) * 8;
-        have[j] = c < d;
-        Raw8<T> r;
-        r.zero();
-        if (have[j]) r.load((const T *)(a.y ? a.y : a.x) + at + c);
-        r.get(v[j]);
-    }
-    if (a.y) {
-        float2 s = make_float2(0.0f, 1.0f);
-        if (a.post) {
-            s = stats<NV, W>(v, have, d, a.rms, a.eps, buf);
-            if (a.post_stat && th == 0) a.post_stat[row] = s;
-        }
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (!have[j]) continue;
-            const int c = (th + j * TH) * 8;
-            float x[8], g[8], w[8], b[8];
-            Raw8<T> r;
-            r.load((const T *)a.x + at + c);
-            r.get(x);
-            param8(a.gate, par + c, 1.0f, g);
-            param8(a.post_w, par + c, 1.0f, w);
-            param8(a.post_b, par + c, 0.0f, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[j][i] = fmaf(g[i], fmaf((v[j][i] - s.x) * s.y, w[i], b[i]), a.rho * x[i]);
-            r.set(v[j]);
-            r.store((T *)a.z + at + c);
+        for (int i = 0; i < 4; ++i) {  // behind the last column z stays 0, for the sums
+            post_w[i] = have ? mul2(post_w[i], gate[i]) : 0;
+            post_b[i] = mul2(post_b[i], gate[i]);
         }
     }
-    if (!a.u) return;
-    const float2 s = stats<NV, W>(v, have, d, a.rms, a.eps, buf);
-    if (a.pre_stat && th == 0) a.pre_stat[row] = s;
+    Raw8<T> nx[R], ny[R];
+    auto fetch = [&](int n0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        if (!have[j]) continue;
-        const int c = (th + j * TH) * 8;
-        float w[8], b[8];
-        Raw8<T> r;
-        param8(a.pre_w, par + c, 1.0f, w);
-        param8(a.pre_b, par + c, 0.0f, b);
+        for (int r = 0; r < R; ++r) {
+            const int n = n0 + group * R + r;
+            const long long at = (base + n) * d + c;
+            nx[r].zero();
+            ny[r].zero();
+            if (have && n < end) {
+                nx[r].load((const T *)a.x + at);
+                if (a.y) ny[r].load((const T *)a.y + at);
+            }
+        }
+    };
+    if (AHEAD) fetch(beg);
+    for (int n0 = beg; n0 < end; n0 += groups * R) {
+        if (!AHEAD) fetch(n0);
+        Raw8<T> x[R], y[R];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[j][i] = fmaf((v[j][i] - s.x) * s.y, w[i], b[i]);
-        r.set(v[j]);
-        r.store((T *)a.u + at + c);
+        for (int r = 0; r < R; ++r) {
+            x[r] = nx[r];
+            y[r] = ny[r];
+        }
+        if (AHEAD && n0 + groups * R < end) fetch(n0 + groups * R);
+        float2 s[R];
+        const int n = n0 + group * R, rows = have ? end - n : 0;
+        const long long at = (base + n) * d + c;
+        if (a.y) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r] = make_float2(0.0f, 1.0f);
+            if (a.post) {
+                stats<T, WC, R>(y, have, a, share, totals, s);
+                store_stats<R>(a.post_stat ? a.post_stat + base + n : nullptr, s, th, end - n);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                f32x2 v[4], o[4];
+                y[r].get(v);
+                x[r].get(o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    o[i] = fma2(mul2(add2(v[i], pk2(-s[r].x)), pk2(s[r].y)), post_w[i], fma2(pk2(a.rho), o[i], post_b[i]));
+                x[r].set(o);
+                if (r < rows) x[r].store((T *)a.z + at + (long long)r * d);
+            }
+        }
+        if (!a.u) continue;
+        stats<T, WC, R>(x, have, a, share, totals, s);
+        store_stats<R>(a.pre_stat ? a.pre_stat + base + n : nullptr, s, th, end - n);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x2 v[4];
+            x[r].get(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = fma2(mul2(add2(v[i], pk2(-s[r].x)), pk2(s[r].y)), pre_w[i], pre_b[i]);
+            x[r].set(v);
+            if (r < rows) x[r].store((T *)a.u + at + (long long)r * d);
+        }
     }
 }
 
 // ---------------------------------------------------------------------------
-// Backward.  W = ceil(d / 256) warps hold a row, 8 columns a thread; a CTA walks a
-// slice of one task's rows with GROUPS such groups and keeps the four column sums in
-// registers.  Its sums go to `parts` [T][slices][4][d]: A, B, dpre_w, dpre_b.
+// Backward.  The four column sums stay in registers; a CTA's go to `parts`
+// [T][slices][4][d]: A, B, dpre_w, dpre_b.
+//
+// With g = du . pre_w, e = dz + r_z g and aw = gate . post_w, the gradient behind the
+// pre-norm is dzt = e - r_z (m1 + m2 zhat), m1 = sum g / d, m2 = sum g zhat / d, and what
+// the post-norm needs of q = dzt . aw follows from sums over e, zhat and yhat:
+//   sum q      = sum e aw - r_z (m1 sum aw + m2 sum zhat aw)
+//   sum q yhat = sum e aw yhat - r_z (m1 sum aw yhat + m2 sum zhat aw yhat),
+// so seven sums a row, taken together, replace two rounds of two that wait for one another.
 struct BwdArgs {
     const void *y, *z;
     const float2 *post_stat, *pre_stat;
@@ -210,159 +312,204 @@ struct BwdArgs {
     bool rms, post;
 };
 
-int bwd_warps(int d) { return (d + 255) / 256; }
-int bwd_groups(int d) { return std::max(1, 8 / bwd_warps(d)); }
+int bwd_rows(const Dims &p) { return p.bf16 && row_warps(p.d) <= 4 ? BR : 1; }
 int bwd_slices(const Dims &p) {
-    const int rows = 4 * bwd_groups(p.d);
-    return std::max(1, std::min((p.N + rows - 1) / rows, (456 + p.T - 1) / p.T));  // 152 SMs x 3
+    const int W = row_warps(p.d);
+    return slices_of(p, bwd_rows(p), W <= 4 ? 512 / BB : W <= 16 ? 128 : 64, 2);
 }
 
-// Sums of two values over the warps of each group.
-__device__ __forceinline__ float2 rows_sum(float a, float b, int W, int group, float2 *buf) {
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (W == 1) return make_float2(a, b);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = make_float2(a, b);
-    __syncthreads();
-    float2 s = make_float2(0.0f, 0.0f);
-    for (int w = 0; w < W; ++w) {
-        const float2 o = buf[group * W + w];
-        s.x += o.x;
-        s.y += o.y;
+// Totals over a warp of M (8 or 16) values a lane: each halving step sums two lanes'
+// values and keeps half of them, 16 shuffles for 16 totals.  Lane l ends with value l % M.
+template <int M>
+__device__ __forceinline__ float warp_totals(float (&v)[16]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = M / 2; h > 0; h >>= 1) {
+        const bool up = (lane & h) != 0;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+        }
     }
-    return s;
+#pragma unroll
+    for (int o = M; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
 }
 
-template <typename T, int MAXT>
-__global__ void __launch_bounds__(MAXT)
-norm_bwd_kernel(Dims p, BwdArgs a, int W, int groups) {
-    __shared__ float2 buf[32];
-    extern __shared__ float join[];  // [groups - 1][4][d], where there are several groups
-    const int th = threadIdx.x % (32 * W), group = threadIdx.x / (32 * W);
+template <typename T>
+struct BwdRow {
+    Raw8<T> y, z, dz, du;
+    float2 py, pz;  // mean, rstd
+    __device__ __forceinline__ void load(const BwdArgs &a, long long row, long long at, bool in) {
+        y.zero();
+        z.zero();
+        dz.zero();
+        du.zero();
+        py = pz = make_float2(0.0f, in ? 1.0f : 0.0f);
+        if (!in) return;
+        if (a.du) {
+            du.load((const T *)a.du + at);
+            z.load((const T *)a.z + at);
+            pz = a.pre_stat[row];
+        }
+        if (a.dz) dz.load((const T *)a.dz + at);
+        if (a.y) {
+            y.load((const T *)a.y + at);
+            if (a.post) py = a.post_stat[row];
+        }
+    }
+};
+
+template <typename T, int WC, int MAXT, int MINB, int R, bool AHEAD>
+__global__ void __launch_bounds__(MAXT, MINB)
+norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
+    __shared__ float totals[2][32][16];
+    extern __shared__ __align__(16) float join[];  // [groups - 1][4][d], where there are several groups
+    const int W = WC ? WC : warps;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, th = threadIdx.x - group * 32 * W;
     const int t = blockIdx.y, N = p.N, d = p.d, c = 8 * th;
     const int beg = (int)((long long)N * blockIdx.x / gridDim.x), end = (int)((long long)N * (blockIdx.x + 1) / gridDim.x);
     const bool have = c < d;
     const float share = 1.0f / (float)d, centre = a.rms ? 0.0f : share;
     pdl_wait();
-    float pw[8], aw[8];  // pre_w; gate . post_w
+    f32x2 pw[4], aw[4];  // pre_w; gate . post_w
+    float sum_aw;
     {
         const long long par = (long long)t * d + c;
-        float g[8];
+        f32x2 g[4];
         param8(have ? a.pre_w : nullptr, par, 1.0f, pw);
         param8(have ? a.gate : nullptr, par, 1.0f, g);
         param8(have ? a.post_w : nullptr, par, 1.0f, aw);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) aw[i] *= g[i];
+        for (int i = 0; i < 4; ++i) aw[i] = have ? mul2(aw[i], g[i]) : 0;
+        sum_aw = warp_sum(sum2(add2(add2(aw[0], aw[1]), add2(aw[2], aw[3]))));
+        if (WC != 1) {
+            if (lane == 0) totals[0][warp][0] = sum_aw;
+            __syncthreads();
+            sum_aw = 0.0f;
+            for (int w = 0; w < W; ++w) sum_aw += totals[0][group * W + w][0];
+            __syncthreads();
+        }
     }
-    float A[8] = {}, B[8] = {}, Pw[8] = {}, Pb[8] = {};
-    for (int n0 = beg; n0 < end; n0 += groups) {
-        const int n = n0 + group;
-        const bool in = have && n < end;
-        const long long row = (long long)t * N + min(n, end - 1), at = row * d + c;
-        Raw8<T> ry, rz, rdz, rdu;
-        ry.zero();
-        rz.zero();
-        rdz.zero();
-        rdu.zero();
-        if (in) {
-            if (a.dz) rdz.load((const T *)a.dz + at);
-            if (a.du) {
-                rdu.load((const T *)a.du + at);
-                rz.load((const T *)a.z + at);
-            }
-            if (a.y) ry.load((const T *)a.y + at);
+    f32x2 A[4] = {}, B[4] = {}, Pw[4] = {}, Pb[4] = {};
+    BwdRow<T> next[R];
+    const long long base = (long long)t * N;
+    auto fetch = [&](int n0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int n = n0 + group * R + r;
+            next[r].load(a, base + n, (base + n) * d + c, have && n < end);
         }
-        float dz[8];
-        rdz.get(dz);
-        if (a.du) {
-            const float2 s = a.pre_stat[row];
-            float zh[8], du[8];
-            rz.get(zh);
-            rdu.get(du);
-            float s1 = 0.0f, s2 = 0.0f;
+    };
+    if (AHEAD) fetch(beg);
+    int flip = 0;
+    for (int n0 = beg; n0 < end; n0 += groups * R, flip ^= 1) {
+        if (!AHEAD) fetch(n0);
+        f32x2 e[R][4], zh[R][4], yh[R][4];
+        float rz[R], ry[R], v[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                zh[i] = in ? (zh[i] - s.x) * s.y : 0.0f;
-                Pw[i] = fmaf(du[i], zh[i], Pw[i]);
-                Pb[i] += du[i];
-                du[i] *= pw[i];
-                s1 += du[i];
-                s2 = fmaf(du[i], zh[i], s2);
+        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            rz[r] = next[r].pz.y;
+            ry[r] = next[r].py.y;
+            const f32x2 mz = pk2(-next[r].pz.x), my = pk2(-next[r].py.x);
+            f32x2 du[4], s[7] = {};
+            next[r].dz.get(e[r]);
+            next[r].du.get(du);
+            next[r].z.get(zh[r]);
+            next[r].y.get(yh[r]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                zh[r][i] = mul2(add2(zh[r][i], mz), pk2(rz[r]));
+                yh[r][i] = mul2(add2(yh[r][i], my), pk2(ry[r]));
+                Pw[i] = fma2(du[i], zh[r][i], Pw[i]);
+                Pb[i] = add2(Pb[i], du[i]);
+                const f32x2 g = mul2(du[i], pw[i]);
+                e[r][i] = fma2(pk2(rz[r]), g, e[r][i]);
+                const f32x2 ea = mul2(e[r][i], aw[i]), za = mul2(zh[r][i], aw[i]);
+                s[0] = add2(s[0], g);
+                s[1] = fma2(g, zh[r][i], s[1]);
+                s[2] = add2(s[2], ea);
+                s[3] = fma2(ea, yh[r][i], s[3]);
+                s[4] = add2(s[4], za);
+                s[5] = fma2(aw[i], yh[r][i], s[5]);
+                s[6] = fma2(za, yh[r][i], s[6]);
             }
-            const float2 q = rows_sum(s1, s2, W, group, buf);
-            const float m1 = q.x * centre, m2 = q.y * share;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dz[i] = fmaf(s.y, (du[i] - m1) - zh[i] * m2, dz[i]);
+            for (int i = 0; i < 7; ++i) v[8 * r + i] = sum2(s[i]);
         }
-        if (a.y) {
-            const float2 s = a.post ? a.post_stat[row] : make_float2(0.0f, 1.0f);
-            float yh[8], g[8], s1 = 0.0f, s2 = 0.0f;
-            ry.get(yh);
+        if (AHEAD && n0 + groups * R < end) fetch(n0 + groups * R);
+        float sum = warp_totals<8 * R>(v);
+        if (WC != 1) {
+            if (lane < 8 * R) totals[flip][warp][lane] = sum;
+            __syncthreads();  // the other half is written next: one barrier a step
+            sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!in) dz[i] = 0.0f;
-                yh[i] = in ? (yh[i] - s.x) * s.y : 0.0f;
-                A[i] = fmaf(dz[i], yh[i], A[i]);
-                B[i] += dz[i];
-                g[i] = dz[i] * aw[i];
-                s1 += g[i];
-                s2 = fmaf(g[i], yh[i], s2);
-            }
-            if (a.post) {
-                const float2 q = rows_sum(s1, s2, W, group, buf);
-                const float m1 = q.x * centre, m2 = q.y * share;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = s.y * ((g[i] - m1) - yh[i] * m2);
-            }
-            if (in) {
-                Raw8<T> r;
-                r.set(g);
-                r.store((T *)a.dy + at);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) dz[i] *= a.rho;
+            for (int w = 0; w < (WC ? WC : W); ++w) sum += totals[flip][group * W + w][lane & (8 * R - 1)];
         }
-        if (in) {
-            Raw8<T> r;
-            r.set(dz);
-            r.store((T *)a.dx + at);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float s[7];
+#pragma unroll
+            for (int i = 0; i < 7; ++i) s[i] = __shfl_sync(0xffffffffu, sum, 8 * r + i);
+            const int n = n0 + group * R + r;
+            const float z1 = a.du ? rz[r] : 0.0f, m1 = z1 * centre * s[0], m2 = z1 * share * s[1];
+            const float k1 = a.post ? centre * (s[2] - m1 * sum_aw - m2 * s[4]) : 0.0f;
+            const float k2 = a.post ? share * (s[3] - m1 * s[5] - m2 * s[6]) : 0.0f;
+            f32x2 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[r][i] = fma2(pk2(-m2), zh[r][i], add2(e[r][i], pk2(-m1)));
+                A[i] = fma2(e[r][i], yh[r][i], A[i]);
+                B[i] = add2(B[i], e[r][i]);
+                q[i] = mul2(pk2(ry[r]), fma2(pk2(-k2), yh[r][i], fma2(e[r][i], aw[i], pk2(-k1))));
+                if (a.y) e[r][i] = mul2(e[r][i], pk2(a.rho));
+            }
+            if (have && n < end) {
+                const long long at = (base + n) * d + c;
+                Raw8<T> o;
+                o.set(e[r]);
+                o.store((T *)a.dx + at);
+                if (a.y) {
+                    o.set(q);
+                    o.store((T *)a.dy + at);
+                }
+            }
         }
     }
     // the groups' sums, in their order
     __syncthreads();
-    if (group > 0 && have) {
-        float *o = join + (long long)(group - 1) * 4 * d + c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            o[i] = A[i];
-            o[d + i] = B[i];
-            o[2 * d + i] = Pw[i];
-            o[3 * d + i] = Pb[i];
-        }
-    }
+    Raw8<float> r;
+    auto put = [&](float *o) {
+        r.set(A);
+        r.store(o);
+        r.set(B);
+        r.store(o + d);
+        r.set(Pw);
+        r.store(o + 2 * d);
+        r.set(Pb);
+        r.store(o + 3 * d);
+    };
+    if (group > 0 && have) put(join + (long long)(group - 1) * 4 * d + c);
     __syncthreads();
     if (group > 0 || !have) return;
     for (int g = 1; g < groups; ++g) {
         const float *o = join + (long long)(g - 1) * 4 * d + c;
+        auto add = [&](f32x2 (&to)[4], const float *from) {
+            f32x2 f[4];
+            r.load(from);
+            r.get(f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            A[i] += o[i];
-            B[i] += o[d + i];
-            Pw[i] += o[2 * d + i];
-            Pb[i] += o[3 * d + i];
-        }
+            for (int i = 0; i < 4; ++i) to[i] = add2(to[i], f[i]);
+        };
+        add(A, o);
+        add(B, o + d);
+        add(Pw, o + 2 * d);
+        add(Pb, o + 3 * d);
     }
-    float *o = a.parts + ((long long)t * gridDim.x + blockIdx.x) * 4 * d + c;
-    Raw8<float> r;
-    r.set(A);
-    r.store(o);
-    r.set(B);
-    r.store(o + d);
-    r.set(Pw);
-    r.store(o + 2 * d);
-    r.set(Pb);
-    r.store(o + 3 * d);
+    put(a.parts + ((long long)t * gridDim.x + blockIdx.x) * 4 * d + c);
 }
 
 struct JoinArgs {
@@ -370,16 +517,18 @@ struct JoinArgs {
     float *dpost_w, *dpost_b, *dgate, *dpre_w, *dpre_b;
 };
 
-// The slices' column sums joined: 32 columns a CTA, eight threads a column, each a run
+// The slices' column sums joined: 32 columns a CTA, JOIN threads a column, each a run
 // of the slices.
-__global__ void __launch_bounds__(256)
+constexpr int JOIN = 16;
+__global__ void __launch_bounds__(32 * JOIN)
 norm_join_kernel(Dims p, JoinArgs a, int slices) {
-    __shared__ float part[8][4][32];
+    __shared__ float part[JOIN][4][32];
     const int lane = threadIdx.x & 31, q = threadIdx.x >> 5, d = p.d, t = blockIdx.y, c = blockIdx.x * 32 + lane;
-    const int beg = slices * q / 8, end = slices * (q + 1) / 8;
+    const int beg = slices * q / JOIN, end = slices * (q + 1) / JOIN;
     pdl_wait();
     float s[4] = {};
     if (c < d)
+#pragma unroll 4
         for (int i = beg; i < end; ++i) {
             const float *in = a.parts + ((long long)t * slices + i) * 4 * d + c;
 #pragma unroll
@@ -393,7 +542,7 @@ norm_join_kernel(Dims p, JoinArgs a, int slices) {
     for (int j = 0; j < 4; ++j) {
         s[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[j] += part[i][j][lane];
+        for (int i = 0; i < JOIN; ++i) s[j] += part[i][j][lane];
     }
     const long long at = (long long)t * d + c;
     const float g = a.gate ? a.gate[at] : 1.0f, w = a.post_w ? a.post_w[at] : 1.0f, b = a.post_b ? a.post_b[at] : 0.0f;
@@ -404,30 +553,41 @@ norm_join_kernel(Dims p, JoinArgs a, int slices) {
     if (a.dpre_b) a.dpre_b[at] = s[3];
 }
 
-template <typename T, int NV, int W>
-int launch_fwd(const Dims &p, const FwdArgs &a, cudaStream_t s) {
-    const long long rows = (long long)p.T * p.N, groups = W == 1 ? 8 : 1;
-    return launch_kernel(norm_fwd_kernel<T, NV, W>, dim3((unsigned)((rows + groups - 1) / groups)), dim3(W == 1 ? 256 : 32 * W),
-                         0, s, p, a);
-}
 template <typename T>
 int run_fwd(const Dims &p, const FwdArgs &a, cudaStream_t s) {
-    if (p.d <= 256) return launch_fwd<T, 1, 1>(p, a, s);
-    if (p.d <= 512) return launch_fwd<T, 2, 1>(p, a, s);
-    if (p.d <= 768) return launch_fwd<T, 3, 1>(p, a, s);
-    if (p.d <= 1024) return launch_fwd<T, 4, 1>(p, a, s);
-    if (p.d <= 2048) return launch_fwd<T, 4, 2>(p, a, s);
-    if (p.d <= 4096) return launch_fwd<T, 4, 4>(p, a, s);
-    return launch_fwd<T, 4, 8>(p, a, s);
+    constexpr int R = sizeof(T) == 2 ? FR : FR / 2;
+    const int W = row_warps(p.d), groups = row_groups(p.d), threads = 32 * W * groups;
+    auto go = [&](auto kern, int rows, int regs) {
+        return launch_kernel(kern, dim3(slices_of(p, rows, regs, 1), p.T), dim3(threads), 0, s, p, a, W, groups);
+    };
+    switch (W) {
+        case 1: return go(norm_fwd_kernel<T, 1, 128, FB, R, true>, R, 512 / FB);
+        case 2: return go(norm_fwd_kernel<T, 2, 128, FB, R, true>, R, 512 / FB);
+        case 3: return go(norm_fwd_kernel<T, 3, 96, FB * 4 / 3, R, true>, R, 512 / FB);
+        case 4: return go(norm_fwd_kernel<T, 4, 128, FB, R, true>, R, 512 / FB);
+    }
+    if (W <= 8) return go(norm_fwd_kernel<T, 0, 256, 2, R, true>, R, 128);
+    if (W <= 16) return go(norm_fwd_kernel<T, 0, 512, 1, R, true>, R, 128);
+    return go(norm_fwd_kernel<T, 0, 1024, 1, 1, false>, 1, 64);
 }
 
 template <typename T>
 int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
-    const int W = bwd_warps(p.d), groups = bwd_groups(p.d), threads = 32 * W * groups;
+    constexpr int R = sizeof(T) == 2 ? BR : 1;
+    const int W = row_warps(p.d), groups = row_groups(p.d);
     const size_t smem = (size_t)(groups - 1) * 4 * p.d * sizeof(float);
-    const dim3 grid(bwd_slices(p), p.T);
-    if (threads <= 256) return launch_kernel(norm_bwd_kernel<T, 256>, grid, dim3(threads), smem, s, p, a, W, groups);
-    return launch_kernel(norm_bwd_kernel<T, 1024>, grid, dim3(threads), smem, s, p, a, W, groups);
+    auto go = [&](auto kern) {
+        return launch_kernel(kern, dim3(bwd_slices(p), p.T), dim3(32 * W * groups), smem, s, p, a, W, groups);
+    };
+    switch (W) {
+        case 1: return go(norm_bwd_kernel<T, 1, 128, BB, R, true>);
+        case 2: return go(norm_bwd_kernel<T, 2, 128, BB, R, true>);
+        case 3: return go(norm_bwd_kernel<T, 3, 96, BB * 4 / 3, R, true>);
+        case 4: return go(norm_bwd_kernel<T, 4, 128, BB, R, true>);
+    }
+    if (W <= 8) return go(norm_bwd_kernel<T, 0, 256, 2, 1, true>);
+    if (W <= 16) return go(norm_bwd_kernel<T, 0, 512, 1, 1, true>);
+    return go(norm_bwd_kernel<T, 0, 1024, 1, 1, false>);
 }
 
 }  // namespace
@@ -457,7 +617,7 @@ int launch_block_norm_bwd(const Dims &p, const vmoe_norm *n, const void *y, cons
     if (st != VMOE_OK || !(dpost_w || dpost_b || dgate || dpre_w || dpre_b)) return st;
     const JoinArgs j = {parts, post_w, post_b, gate, dpost_w, dpost_b, dgate, dpre_w, dpre_b};
     trace_before(s, "block_norm_join");
-    st = launch_kernel(norm_join_kernel, dim3((p.d + 31) / 32, p.T), dim3(256), 0, s, p, j, bwd_slices(p));
+    st = launch_kernel(norm_join_kernel, dim3((p.d + 31) / 32, p.T), dim3(32 * JOIN), 0, s, p, j, bwd_slices(p));
     trace_after(s);
     return st;
 }
