@@ -420,7 +420,7 @@ typedef struct {
 } vmoe_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2, eps; /* lr finite, betas in [0, 1), eps > 0 (as fp32 too) */
+    double lr, beta1, beta2, eps; /* lr finite, betas in [0, 1), eps >= FLT_MIN */
     int32_t step;            /* t, 1 for the first update */
     uint32_t seed;           /* of the 8-bit moments' rounding */
     const int32_t *step_dev; /* device, nullable: t = step + *step_dev (at least 1) */

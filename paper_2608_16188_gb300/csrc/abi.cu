@@ -451,7 +451,7 @@ int vmoe_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_config 
     if (n < 0 || (n > 0 && !tensors) || !config) return VMOE_ERR_INVALID;
     const vmoe_adamw_config &c = *config;
     if (!isfinite(c.lr) || !isfinite((float)c.lr) || !(c.beta1 >= 0.0 && c.beta1 < 1.0) || !(c.beta2 >= 0.0 && c.beta2 < 1.0) ||
-        !((float)c.eps > 0.0f) || !isfinite((float)c.eps) || c.step < (c.step_dev ? 0 : 1))
+        !((float)c.eps >= 1.17549435e-38f) || !isfinite((float)c.eps) || c.step < (c.step_dev ? 0 : 1))
         return VMOE_ERR_INVALID;
     if (((uintptr_t)c.step_dev & 3u) || ((uintptr_t)c.lr_dev & 3u) || ((uintptr_t)c.grad_scale & 3u)) return VMOE_ERR_INVALID;
     bool supported = true;

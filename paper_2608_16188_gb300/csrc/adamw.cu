@@ -13,11 +13,16 @@
 // rather than v: e4m3's range, 2^17 from the block's largest value down, then covers
 // the gradients' range and not its square root.
 //
-// A warp takes a block of 256 elements, 8 a lane: 16-byte loads of bf16, the block's
-// largest magnitude by one warp reduction, one pass over everything.
+// A warp takes two blocks of 256 elements, 8 a lane of each: 16-byte loads of bf16, all
+// in flight at once, a block's largest magnitude by one warp reduction, one pass over
+// everything.  With 8-bit moments (10 bytes an element) the instructions weigh as much
+// as the bytes: 54 an element fill the card's issue slots at the memory's rate.  So the
+// arithmetic is packed, and what only rare blocks need is behind a warp-wide branch: the
+// rounding below e4m3's normal range, NaN, and square roots of subnormal numbers.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -26,6 +31,9 @@ namespace vmoe {
 namespace {
 
 constexpr int AT = 256;  // threads a CTA
+// CTAs an SM, 128 registers a thread: fp32 moments 164 us for 38 M bf16 elements with a
+// master copy (three CTAs 180, one 187), 8-bit ones 606 us for 302 M (707 with spills, 745).
+constexpr int AB = 2;
 
 struct Entry {
     void *param;
@@ -39,12 +47,12 @@ struct Entry {
 };
 enum { P32 = 1, G32 = 2, S8 = 4, MST = 8 };
 
-// The tensors of a launch, passed by value: `first` is the first block of 256 of each,
+// The tensors of a launch, passed by value: `first` is the first pair of blocks of each,
 // counted over the launch.
 template <int MAX>
 struct Table {
     int n;
-    uint32_t blocks;
+    uint32_t pairs;
     uint32_t first[MAX];
     Entry e[MAX];
 };
@@ -63,226 +71,452 @@ struct Rates {
     uint32_t key;
 };
 
+// Eight elements as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, bool full, int have, float (&o)[8]);
+struct Raw8;
 template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, bool full, int have, float (&o)[8]) {
-    if (full) {
-        bf16x8_to_f32(*reinterpret_cast<const uint4 *>(p), o);
+struct Raw8<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(f32x2 (&o)[4]) const {
+        o[0] = bf16x2_to_f32x2(v.x);
+        o[1] = bf16x2_to_f32x2(v.y);
+        o[2] = bf16x2_to_f32x2(v.z);
+        o[3] = bf16x2_to_f32x2(v.w);
+    }
+};
+template <>
+struct Raw8<float> {
+    ulonglong2 a, b;
+    __device__ __forceinline__ void load(const float *p) {
+        a = reinterpret_cast<const ulonglong2 *>(p)[0];
+        b = reinterpret_cast<const ulonglong2 *>(p)[1];
+    }
+    __device__ __forceinline__ void get(f32x2 (&o)[4]) const {
+        o[0] = a.x;
+        o[1] = a.y;
+        o[2] = b.x;
+        o[3] = b.y;
+    }
+};
+
+// Eight elements of an array as four pairs of floats; `have` of them where !FULL.
+template <bool FULL>
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, int have, f32x2 (&o)[4]) {
+    if (FULL) {
+        Raw8<__nv_bfloat16> r;
+        r.load(p);
+        r.get(o);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = i < have ? __bfloat162float(p[i]) : 0.0f;
+        for (int i = 0; i < 4; ++i)
+            o[i] = pk2(2 * i < have ? __bfloat162float(p[2 * i]) : 0.0f, 2 * i + 1 < have ? __bfloat162float(p[2 * i + 1]) : 0.0f);
     }
 }
-template <>
-__device__ __forceinline__ void load8<float>(const float *p, bool full, int have, float (&o)[8]) {
-    if (full) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-        o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+template <bool FULL>
+__device__ __forceinline__ void load8(const float *p, int have, f32x2 (&o)[4]) {
+    if (FULL) {
+        Raw8<float> r;
+        r.load(p);
+        r.get(o);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = i < have ? p[i] : 0.0f;
+        for (int i = 0; i < 4; ++i) o[i] = pk2(2 * i < have ? p[2 * i] : 0.0f, 2 * i + 1 < have ? p[2 * i + 1] : 0.0f);
     }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T *p, bool full, int have, const float (&v)[8]);
-template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 *p, bool full, int have, const float (&v)[8]) {
-    if (full) {
-        *reinterpret_cast<uint4 *>(p) = f32_to_bf16x8(v);
+template <bool FULL>
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, int have, const f32x2 (&v)[4]) {
+    if (FULL) {
+        *reinterpret_cast<uint4 *>(p) =
+            make_uint4(f32x2_to_bf16x2(v[0]), f32x2_to_bf16x2(v[1]), f32x2_to_bf16x2(v[2]), f32x2_to_bf16x2(v[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 two = unpk2(v[i >> 1]);
+            if (i < have) p[i] = __float2bfloat16_rn(i & 1 ? two.y : two.x);
+        }
+    }
+}
+template <bool FULL>
+__device__ __forceinline__ void store8(float *p, int have, const f32x2 (&v)[4]) {
+    if (FULL) {
+        reinterpret_cast<ulonglong2 *>(p)[0] = make_ulonglong2(v[0], v[1]);
+        reinterpret_cast<ulonglong2 *>(p)[1] = make_ulonglong2(v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 two = unpk2(v[i >> 1]);
+            if (i < have) p[i] = i & 1 ? two.y : two.x;
+        }
+    }
+}
+template <bool FULL>
+__device__ __forceinline__ uint2 load_codes(const uint8_t *p, int have) {
+    if (FULL) return *reinterpret_cast<const uint2 *>(p);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < have) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+template <bool FULL>
+__device__ __forceinline__ void store_codes(uint8_t *p, int have, uint2 v) {
+    if (FULL) {
+        *reinterpret_cast<uint2 *>(p) = v;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < have) p[i] = __float2bfloat16_rn(v[i]);
-    }
-}
-template <>
-__device__ __forceinline__ void store8<float>(float *p, bool full, int have, const float (&v)[8]) {
-    if (full) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) p[i] = v[i];
+            if (i < have) p[i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
     }
 }
 
 // Eight e4m3 values times `scale`.
-__device__ __forceinline__ void load_e4m3(const uint8_t *p, bool full, int have, float scale, float (&o)[8]) {
-    uint32_t w[2] = {0, 0};
-    if (full) {
-        const uint2 r = *reinterpret_cast<const uint2 *>(p);
-        w[0] = r.x;
-        w[1] = r.y;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-    }
+__device__ __forceinline__ void decode(uint2 c, float scale, f32x2 (&o)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint16_t two = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-        uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
+        const uint16_t two = (uint16_t)((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
         float lo, hi;
-        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(lo), "=f"(hi) : "r"(h));
-        o[2 * i] = lo * scale;
-        o[2 * i + 1] = hi * scale;
+        asm("{\n .reg .b32 t;\n .reg .b16 l, h;\n cvt.rn.f16x2.e4m3x2 t, %2;\n mov.b32 {l, h}, t;\n"
+            " cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
+            : "=f"(lo), "=f"(hi)
+            : "h"(two));
+        o[i] = mul2(pk2(lo, hi), pk2(scale));
     }
 }
 
-__device__ __forceinline__ uint16_t e4m3x2(float lo, float hi) {
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+__device__ __forceinline__ uint32_t e4m3x4(const float (&q)[4]) {
+    uint32_t r;
+    asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n"
+        " mov.b32 %0, {l, h};\n}"
+        : "=r"(r)
+        : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
     return r;
 }
 
-// |v| inv rounded to one of the two e4m3 neighbours, 20 bits of `bits` against the
-// distance to the lower one.  The bits of the mantissa that e4m3 does not have are cut
-// off after the random number is added; below 2^-6, where e4m3's steps stay 2^-9, that is
-// done at 2^-6 higher, where fp32's first three bits have the same steps.  NaN stays NaN.
-__device__ __forceinline__ float dither(float v, float inv, uint32_t bits) {
-    const float a = fabsf(v) * inv;
-    const float low = a < 0.015625f ? 0.015625f : 0.0f * a;
-    const uint32_t cut = (__float_as_uint(a + low) + bits) & 0xfff00000u;
-    return copysignf(__uint_as_float(cut) - low, v);
+// a rounded to one of the two e4m3 neighbours, `bits` + 8 of 2^20 against the distance to
+// the lower one: the bits of the mantissa that e4m3 does not have are cut off after the
+// random number is added (to the magnitude: the sign is the top bit).
+__device__ __forceinline__ float dither(float a, uint32_t bits) {
+    return __uint_as_float((__float_as_uint(a) + bits + 8u) & 0xfff00000u);
+}
+// The same for any a.  Below 2^-6, where e4m3's steps stay 2^-9, it is done at 2^-6
+// higher, where fp32's first three bits have the same steps.  NaN stays NaN.
+__device__ __forceinline__ float dither_any(float a, uint32_t bits) {
+    if (a != a) return a;
+    if (fabsf(a) >= 0.015625f) return dither(a, bits);
+    return copysignf(dither(fabsf(a) + 0.015625f, bits) - 0.015625f, a);
 }
 
+// The hash but for its last step, h ^ h >> 16, which is taken with the half it is for:
+// 16 times the low or the high half of the result, a multiple of 16 below 2^20.
 __device__ __forceinline__ uint32_t mix(uint32_t h) {
     h = (h ^ (h >> 16)) * 0x9e4a8af7u;
-    h = (h ^ (h >> 15)) * 0xa6bd2c99u;
-    return h ^ (h >> 16);
+    return (h ^ (h >> 15)) * 0xa6bd2c99u;
+}
+template <bool HIGH>
+__device__ __forceinline__ uint32_t random20(uint32_t h) {
+    return (HIGH ? h >> 12 : (h << 4) ^ (h >> 12)) & 0xffff0u;
 }
 
-__device__ __forceinline__ float sqrt_approx(float v) {
+// Three-operand minimum and maximum of magnitudes; a NaN makes the result NaN.
+__device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// The scale of a block whose largest magnitude in this lane is `top`, and 1 / scale.
-// Below 2^-100 the block is zero: 448 / top would overflow.
-__device__ __forceinline__ float2 block_scale(float top) {
-    top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
-    if (top < 7.888609052210118e-31f) return make_float2(0.0f, 0.0f);
-    return make_float2(top / 448.0f, 448.0f / top);
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float r;
+    asm("min.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
-template <typename P, typename G, bool EIGHT, bool MASTER>
-__device__ __forceinline__ void update(const Entry &e, const Rates &r, const Consts &k, uint32_t block) {
-    const int lane = threadIdx.x & 31;
-    const long long at = (long long)block * 256 + lane * 8;
-    const int have = (int)max(0LL, min(8LL, e.numel - at));
-    const bool full = have == 8;
-    float p[8], g[8], m[8], v[8], root[8];
-    load8<G>((const G *)e.grad + at, full, have, g);
-    if (EIGHT) {
-        load_e4m3((const uint8_t *)e.m + at, full, have, e.m_scale[block], m);
-        load_e4m3((const uint8_t *)e.v + at, full, have, e.v_scale[block], v);
+// The codes of eight values `v` of a block, and the block's scale.
+template <bool HIGH>
+__device__ __forceinline__ uint2 encode(const f32x2 (&v)[4], const uint32_t (&h)[8], float &scale) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 two = unpk2(v[i]);
+        f[2 * i] = two.x;
+        f[2 * i + 1] = two.y;
+    }
+    float top = max3(f[0], f[1], f[2]), low = min3(f[0], f[1], f[2]);
+    top = max3(top, f[3], f[4]);
+    low = min3(low, f[3], f[4]);
+    top = max3(top, f[5], f[6]);
+    low = min3(low, f[5], f[6]);
+    top = max3(top, f[7], 0.0f);
+    low = min3(low, f[7], f[7]);
+    uint32_t t = __reduce_max_sync(0xffffffffu, __float_as_uint(top));  // NaN above infinity above the rest
+    if (t > 0x7f800000u) {  // the largest of the numbers
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
+        t = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+    }
+    // below 2^-100 the block is zero: 448 / top would overflow
+    const float big = __uint_as_float(t);
+    float inv = 0.0f;
+    scale = 0.0f;
+    if (big >= 7.888609052210118e-31f) {
+        // 448 / big: the approximate reciprocal and one Newton step on the quotient
+        float rcp;
+        asm("rcp.approx.f32 %0, %1;" : "=f"(rcp) : "f"(big));
+        inv = 448.0f * rcp;
+        if (t < 0x7e000000u) inv = fmaf(fmaf(-big, inv, 448.0f), rcp, inv);
+        scale = big * (1.0f / 448.0f);
+    }
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 two = unpk2(mul2(v[i], pk2(inv)));
+        q[2 * i] = two.x;
+        q[2 * i + 1] = two.y;
+    }
+    if (__any_sync(0xffffffffu, !(low * inv >= 0.015625f))) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = dither_any(q[i], random20<HIGH>(h[i]));
     } else {
-        load8<float>((const float *)e.m + at, full, have, m);
-        load8<float>((const float *)e.v + at, full, have, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = dither(q[i], random20<HIGH>(h[i]));
+    }
+    const float a[4] = {q[0], q[1], q[2], q[3]}, b[4] = {q[4], q[5], q[6], q[7]};
+    return make_uint2(e4m3x4(a), e4m3x4(b));
+}
+
+// Square roots within 2^-22.  The approximation takes subnormal numbers for zero: a warp
+// that gets a zero looks again.
+__device__ __forceinline__ void roots(const f32x2 (&v)[4], f32x2 (&o)[4]) {
+    float low = 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float2 a = unpk2(v[i]);
+        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.x));
+        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.y));
+        o[i] = pk2(a.x, a.y);
+        low = min3(low, a.x, a.y);
+    }
+    if (__any_sync(0xffffffffu, low == 0.0f)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 a = unpk2(v[i]);
+            asm("sqrt.approx.f32 %0, %0;" : "+f"(a.x));
+            asm("sqrt.approx.f32 %0, %0;" : "+f"(a.y));
+            o[i] = pk2(a.x, a.y);
+        }
+    }
+}
+
+// A block's update: p, g, and the moments as values; p, m and v become the new ones,
+// `root` sqrt(v).
+__device__ __forceinline__ void adam(f32x2 (&p)[4], const f32x2 (&g)[4], f32x2 (&m)[4], f32x2 (&v)[4], f32x2 (&root)[4],
+                                     const Rates &r, const Consts &k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 gi = mul2(g[i], pk2(r.gs));
+        m[i] = fma2(pk2(k.b1), m[i], mul2(pk2(k.c1), gi));
+        v[i] = fma2(pk2(k.b2), v[i], mul2(pk2(k.c2), mul2(gi, gi)));
+    }
+    roots(v, root);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 den = fma2(root[i], pk2(r.root_scale), pk2(k.eps));
+        p[i] = fma2(p[i], pk2(r.keep), mul2(mul2(m[i], pk2(-r.rate)), rcp2(den)));
+    }
+}
+
+// m and sqrt(v) of a block to memory in 8 bits.
+template <bool FULL>
+__device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, uint32_t block, int have, const f32x2 (&m)[4],
+                                              const f32x2 (&root)[4]) {
+    const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
+    uint32_t h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = mix(((uint32_t)at + i) * 0x51f6db5bu + r.key);
+    float scale_m, scale_v;
+    const uint2 om = encode<false>(m, h, scale_m), ov = encode<true>(root, h, scale_v);
+    store_codes<FULL>((uint8_t *)e.m + at, have, om);
+    store_codes<FULL>((uint8_t *)e.v + at, have, ov);
+    if ((threadIdx.x & 31) == 0) {
+        e.m_scale[block] = scale_m;
+        e.v_scale[block] = scale_v;
+    }
+}
+
+// One block of a tensor, the last and ragged one too.
+template <typename P, typename G, bool EIGHT, bool MASTER, bool FULL>
+__device__ __forceinline__ void update(const Entry &e, const Rates &r, const Consts &k, uint32_t block) {
+    const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
+    const int have = FULL ? 8 : (int)max(0LL, min(8LL, e.numel - at));
+    f32x2 p[4], g[4], m[4], v[4], root[4];
+    load8<FULL>((const G *)e.grad + at, have, g);
+    if (EIGHT) {
+        decode(load_codes<FULL>((const uint8_t *)e.m + at, have), e.m_scale[block], m);
+        decode(load_codes<FULL>((const uint8_t *)e.v + at, have), e.v_scale[block], v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
+    } else {
+        load8<FULL>((const float *)e.m + at, have, m);
+        load8<FULL>((const float *)e.v + at, have, v);
     }
     if (MASTER)
-        load8<float>(e.master + at, full, have, p);
+        load8<FULL>(e.master + at, have, p);
     else
-        load8<P>((const P *)e.param + at, full, have, p);
-    float top_m = 0.0f, top_v = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        g[i] *= r.gs;
-        if (EIGHT) v[i] *= v[i];
-        m[i] = fmaf(k.b1, m[i], k.c1 * g[i]);
-        v[i] = fmaf(k.b2, v[i], k.c2 * (g[i] * g[i]));
-        root[i] = sqrt_approx(v[i]);
-        const float den = fmaf(root[i], r.root_scale, k.eps);
-        p[i] = fmaf(p[i], r.keep, -r.rate * __fdividef(m[i], den));
-        if (EIGHT) {
-            top_m = fmaxf(top_m, fabsf(m[i]));
-            top_v = fmaxf(top_v, root[i]);
-        }
-    }
-    if (MASTER) store8<float>(e.master + at, full, have, p);
-    store8<P>((P *)e.param + at, full, have, p);
-    if (!EIGHT) {
-        store8<float>((float *)e.m + at, full, have, m);
-        store8<float>((float *)e.v + at, full, have, v);
-        return;
-    }
-    const float2 sm = block_scale(top_m), sv = block_scale(top_v);
-    if (lane == 0) {
-        e.m_scale[block] = sm.x;
-        e.v_scale[block] = sv.x;
-    }
-    const uint32_t h0 = (uint32_t)at * 0x51f6db5bu + r.key;
-    uint32_t wm[2], wv[2];
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        const uint32_t ha = mix(h0 + i * 0x51f6db5bu), hb = mix(h0 + (i + 1) * 0x51f6db5bu);
-        const uint32_t two_m = e4m3x2(dither(m[i], sm.y, ((ha & 0xffffu) << 4) + 8), dither(m[i + 1], sm.y, ((hb & 0xffffu) << 4) + 8));
-        const uint32_t two_v = e4m3x2(dither(root[i], sv.y, ((ha >> 16) << 4) + 8), dither(root[i + 1], sv.y, ((hb >> 16) << 4) + 8));
-        if (i % 4 == 0) {
-            wm[i >> 2] = two_m;
-            wv[i >> 2] = two_v;
-        } else {
-            wm[i >> 2] |= two_m << 16;
-            wv[i >> 2] |= two_v << 16;
-        }
-    }
-    uint8_t *om = (uint8_t *)e.m + at, *ov = (uint8_t *)e.v + at;
-    if (full) {
-        *reinterpret_cast<uint2 *>(om) = make_uint2(wm[0], wm[1]);
-        *reinterpret_cast<uint2 *>(ov) = make_uint2(wv[0], wv[1]);
+        load8<FULL>((const P *)e.param + at, have, p);
+    adam(p, g, m, v, root, r, k);
+    if (MASTER) store8<FULL>(e.master + at, have, p);
+    store8<FULL>((P *)e.param + at, have, p);
+    if (EIGHT) {
+        store_moments<FULL>(e, r, block, have, m, root);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < have) {
-                om[i] = (uint8_t)(wm[i >> 2] >> (8 * (i & 3)));
-                ov[i] = (uint8_t)(wv[i >> 2] >> (8 * (i & 3)));
-            }
+        store8<FULL>((float *)e.m + at, have, m);
+        store8<FULL>((float *)e.v + at, have, v);
     }
 }
 
-// Every warp walks blocks w, w + warps, ...; the tensor is found by bisection once and
-// followed from there.
+// A pair of blocks that the tensor ends within.
+template <typename P, typename G, bool EIGHT, bool MASTER>
+__device__ __forceinline__ void update_last(const Entry &e, const Rates &r, const Consts &k, uint32_t pair) {
+#pragma unroll 1
+    for (uint32_t b = 2 * pair; b < 2 * pair + 2 && (long long)b * 256 < e.numel; ++b)
+        update<P, G, EIGHT, MASTER, false>(e, r, k, b);
+}
+
+// A warp's way through the launch: pairs w, w + warps, ... of all tensors.  The tensor
+// is found by bisection once and followed from there.
 template <int MAX>
-__global__ void __launch_bounds__(AT)
+struct Walk {
+    const Table<MAX> &tab;
+    uint32_t b, warps;
+    int at;
+    __device__ __forceinline__ Walk(const Table<MAX> &t, uint32_t first, uint32_t step) : tab(t), b(first), warps(step), at(0) {
+        int hi = t.n;
+        while (hi - at > 1) {
+            const int mid = (at + hi) >> 1;
+            if (t.first[mid] <= b)
+                at = mid;
+            else
+                hi = mid;
+        }
+    }
+    __device__ __forceinline__ bool more() const { return b < tab.pairs; }
+    __device__ __forceinline__ void next() {
+        b += warps;
+        while (at + 1 < tab.n && tab.first[at + 1] <= b) ++at;
+    }
+    __device__ __forceinline__ const Entry &entry() const { return tab.e[at]; }
+    __device__ __forceinline__ uint32_t pair() const { return b - tab.first[at]; }
+    __device__ __forceinline__ bool whole() const { return ((long long)pair() + 1) * 512 <= entry().numel; }
+};
+
+struct Common {
+    float lr, inv_c1, root_scale, gs;
+    uint32_t key;
+    __device__ __forceinline__ Rates of(const Entry &e) const {
+        const float rate = lr * e.lr_scale;
+        return {1.0f - rate * e.decay, rate * inv_c1, root_scale, gs, key + e.key};
+    }
+};
+
+// What a pair of blocks with 8-bit moments is read as.
+template <typename P, typename G>
+struct Raw {
+    Raw8<P> p[2];
+    Raw8<G> g[2];
+    uint2 m[2], v[2];
+    float m_scale[2], v_scale[2];
+    __device__ __forceinline__ void load(const P *param, const Entry &e, uint32_t pair) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const long long at = (long long)pair * 512 + b * 256 + (threadIdx.x & 31) * 8;
+            p[b].load(param + at);
+            g[b].load((const G *)e.grad + at);
+            m[b] = *reinterpret_cast<const uint2 *>((const uint8_t *)e.m + at);
+            v[b] = *reinterpret_cast<const uint2 *>((const uint8_t *)e.v + at);
+            m_scale[b] = e.m_scale[2 * pair + b];
+            v_scale[b] = e.v_scale[2 * pair + b];
+        }
+    }
+};
+
+// 8-bit moments: whole pairs of one kind of tensors, the next one's loads in flight
+// while one is computed; leaves `w` at the first pair that is something else.
+template <typename P, typename G, bool MASTER, int MAX>
+__device__ __forceinline__ void run_eight(Walk<MAX> &w, const Common &c, const Consts &k, int kind) {
+    typedef std::conditional_t<MASTER, float, P> S;  // what the update works on
+    auto source = [](const Entry &e) { return (const S *)(MASTER ? (void *)e.master : e.param); };
+    if (!w.whole()) {
+        update_last<P, G, true, MASTER>(w.entry(), c.of(w.entry()), k, w.pair());
+        w.next();
+        return;
+    }
+    Raw<S, G> raw;
+    raw.load(source(w.entry()), w.entry(), w.pair());
+    for (bool go = true; go;) {
+        const Entry &e = w.entry();
+        const uint32_t pair = w.pair();
+        const Rates r = c.of(e);
+        const Raw<S, G> now = raw;
+        w.next();
+        go = w.more() && w.entry().kind == kind && w.whole();
+        if (go) raw.load(source(w.entry()), w.entry(), w.pair());
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const long long at = (long long)pair * 512 + b * 256 + (threadIdx.x & 31) * 8;
+            f32x2 p[4], g[4], m[4], v[4], root[4];
+            now.p[b].get(p);
+            now.g[b].get(g);
+            decode(now.m[b], now.m_scale[b], m);
+            decode(now.v[b], now.v_scale[b], v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
+            adam(p, g, m, v, root, r, k);
+            if (MASTER) store8<true>(e.master + at, 8, p);
+            store8<true>((P *)e.param + at, 8, p);
+            store_moments<true>(e, r, 2 * pair + b, 8, m, root);
+        }
+    }
+}
+
+template <typename P, typename G, bool MASTER, int MAX>
+__device__ __forceinline__ void run_f32(Walk<MAX> &w, const Common &c, const Consts &k) {
+    const Entry &e = w.entry();
+    const Rates r = c.of(e);
+    if (w.whole()) {
+        update<P, G, false, MASTER, true>(e, r, k, 2 * w.pair());
+        update<P, G, false, MASTER, true>(e, r, k, 2 * w.pair() + 1);
+    } else {
+        update_last<P, G, false, MASTER>(e, r, k, w.pair());
+    }
+    w.next();
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(AT, AB)
 adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
     pdl_wait();
-    const float gs = k.grad_scale ? *k.grad_scale : 1.0f;
-    if (!isfinite(gs)) return;  // an overflowed gradient: the step is left out
+    Common c;
+    c.gs = k.grad_scale ? *k.grad_scale : 1.0f;
+    if (!isfinite(c.gs)) return;  // an overflowed gradient: the step is left out
     const int t = max(1, k.step + (k.step_dev ? *k.step_dev : 0));
-    const float lr = k.lr * (k.lr_dev ? *k.lr_dev : 1.0f);
-    const float inv_c1 = -1.0f / expm1f((float)t * k.log_b1), root_scale = 1.0f / sqrtf(-expm1f((float)t * k.log_b2));
-    const uint32_t key = k.seed_key + (uint32_t)t * 0x339cd49bu;
-    const uint32_t warps = gridDim.x * (AT / 32);
-    uint32_t b = blockIdx.x * (AT / 32) + (threadIdx.x >> 5);
-    int lo = 0, hi = tab.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tab.first[mid] <= b)
-            lo = mid;
-        else
-            hi = mid;
-    }
-    for (; b < tab.blocks; b += warps) {
-        while (lo + 1 < tab.n && tab.first[lo + 1] <= b) ++lo;
-        const Entry &e = tab.e[lo];
-        const float rate = lr * e.lr_scale;
-        const Rates r = {1.0f - rate * e.decay, rate * inv_c1, root_scale, gs, key + e.key};
-        const uint32_t block = b - tab.first[lo];
-        switch (e.kind) {
-            case P32 | G32: update<float, float, false, false>(e, r, k, block); break;
-            case P32 | G32 | S8: update<float, float, true, false>(e, r, k, block); break;
-            case 0: update<__nv_bfloat16, __nv_bfloat16, false, false>(e, r, k, block); break;
-            case S8: update<__nv_bfloat16, __nv_bfloat16, true, false>(e, r, k, block); break;
-            case MST: update<__nv_bfloat16, __nv_bfloat16, false, true>(e, r, k, block); break;
-            case MST | S8: update<__nv_bfloat16, __nv_bfloat16, true, true>(e, r, k, block); break;
-            case G32: update<__nv_bfloat16, float, false, false>(e, r, k, block); break;
-            case G32 | S8: update<__nv_bfloat16, float, true, false>(e, r, k, block); break;
-            case G32 | MST: update<__nv_bfloat16, float, false, true>(e, r, k, block); break;
-            default: update<__nv_bfloat16, float, true, true>(e, r, k, block); break;  // G32 | S8 | MST
+    c.lr = k.lr * (k.lr_dev ? *k.lr_dev : 1.0f);
+    c.inv_c1 = -1.0f / expm1f((float)t * k.log_b1);
+    c.root_scale = 1.0f / sqrtf(-expm1f((float)t * k.log_b2));
+    c.key = k.seed_key + (uint32_t)t * 0x339cd49bu;
+    typedef __nv_bfloat16 H;
+    for (Walk<MAX> w(tab, blockIdx.x * (AT / 32) + (threadIdx.x >> 5), gridDim.x * (AT / 32)); w.more();) {
+        const int kind = w.entry().kind;
+        switch (kind) {
+            case P32 | G32: run_f32<float, float, false>(w, c, k); break;
+            case 0: run_f32<H, H, false>(w, c, k); break;
+            case MST: run_f32<H, H, true>(w, c, k); break;
+            case G32: run_f32<H, float, false>(w, c, k); break;
+            case G32 | MST: run_f32<H, float, true>(w, c, k); break;
+            case P32 | G32 | S8: run_eight<float, float, false>(w, c, k, kind); break;
+            case S8: run_eight<H, H, false>(w, c, k, kind); break;
+            case MST | S8: run_eight<H, H, true>(w, c, k, kind); break;
+            case G32 | S8: run_eight<H, float, false>(w, c, k, kind); break;
+            default: run_eight<H, float, true>(w, c, k, kind); break;  // G32 | S8 | MST
         }
     }
 }
@@ -290,17 +524,17 @@ adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
 static_assert(sizeof(Table<380>) + sizeof(Consts) <= 32764, "a launch's arguments");
 
 template <int MAX>
-int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t blocks, const Consts &k, cudaStream_t s) {
+int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pairs, const Consts &k, cudaStream_t s) {
     Table<MAX> tab;
     tab.n = 0;
-    tab.blocks = blocks;
+    tab.pairs = pairs;
     uint32_t at = 0;
     for (int i = 0; i < n; ++i) {
         const vmoe_adamw_tensor &x = tensors[i];
         if (x.numel == 0) continue;
         Entry &e = tab.e[tab.n];
         tab.first[tab.n++] = at;
-        at += (uint32_t)((x.numel + 255) / 256);
+        at += (uint32_t)((x.numel + 511) / 512);
         e.param = x.param;
         e.grad = x.grad;
         e.m = x.m;
@@ -315,8 +549,8 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t blo
         e.kind = (x.param_dtype == VMOE_F32 ? P32 : 0) | (x.grad_dtype == VMOE_F32 ? G32 : 0) |
                  (x.state == VMOE_STATE_E4M3 ? S8 : 0) | (x.master ? MST : 0);
     }
-    const long long ctas = ((long long)blocks + AT / 32 - 1) / (AT / 32);
-    return launch_kernel(adamw_kernel<MAX>, dim3((unsigned)std::min<long long>(ctas, 4LL * num_sms())), dim3(AT), 0, s, tab, k);
+    const long long ctas = ((long long)pairs + AT / 32 - 1) / (AT / 32);
+    return launch_kernel(adamw_kernel<MAX>, dim3((unsigned)std::min<long long>(ctas, (long long)AB * num_sms())), dim3(AT), 0, s, tab, k);
 }
 
 }  // namespace
@@ -339,17 +573,17 @@ int launch_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_confi
     constexpr int SMALL = 40, LARGE = 380;  // tables of 3.4 and 32 KB; a launch takes at most 32764 B
     for (int base = 0; base < n;) {
         int m = 0;
-        uint64_t blocks = 0;
+        uint64_t pairs = 0;
         while (base + m < n && m < LARGE) {
-            const uint64_t more = ((uint64_t)tensors[base + m].numel + 255) / 256;
-            if (blocks + more > 0x7fffffffu) break;
-            blocks += more;
+            const uint64_t more = ((uint64_t)tensors[base + m].numel + 511) / 512;
+            if (pairs + more > 0x7fffffffu) break;
+            pairs += more;
             ++m;
         }
-        if (blocks) {
+        if (pairs) {
             trace_before(s, "adamw");
-            const int st = m <= SMALL ? launch_table<SMALL>(tensors + base, m, base, (uint32_t)blocks, k, s)
-                                      : launch_table<LARGE>(tensors + base, m, base, (uint32_t)blocks, k, s);
+            const int st = m <= SMALL ? launch_table<SMALL>(tensors + base, m, base, (uint32_t)pairs, k, s)
+                                      : launch_table<LARGE>(tensors + base, m, base, (uint32_t)pairs, k, s);
             trace_after(s);
             if (st != VMOE_OK) return st;
         }
