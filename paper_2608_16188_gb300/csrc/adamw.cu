@@ -31,8 +31,9 @@ namespace vmoe {
 namespace {
 
 constexpr int AT = 256;  // threads a CTA
-// CTAs an SM, 128 registers a thread: fp32 moments 164 us for 38 M bf16 elements with a
-// master copy (three CTAs 180, one 187), 8-bit ones 606 us for 302 M (707 with spills, 745).
+// CTAs an SM, 128 registers a thread: 538 us for 302 M bf16 elements with 8-bit moments
+// (83% of the measured copy rate), 168 us for 38 M with fp32 moments and a master copy
+// (99%).  Three CTAs of 128 threads: 594 and 162; five, at 102 registers: 646 and 178.
 constexpr int AB = 2;
 
 struct Entry {
@@ -170,8 +171,8 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int have, uint2 v) {
     }
 }
 
-// Eight e4m3 values times `scale`.
-__device__ __forceinline__ void decode(uint2 c, float scale, f32x2 (&o)[4]) {
+// Eight e4m3 values.
+__device__ __forceinline__ void decode(uint2 c, f32x2 (&o)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint16_t two = (uint16_t)((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
@@ -180,31 +181,43 @@ __device__ __forceinline__ void decode(uint2 c, float scale, f32x2 (&o)[4]) {
             " cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
             : "=f"(lo), "=f"(hi)
             : "h"(two));
-        o[i] = mul2(pk2(lo, hi), pk2(scale));
+        o[i] = pk2(lo, hi);
     }
 }
 
-__device__ __forceinline__ uint32_t e4m3x4(const float (&q)[4]) {
+// (scale v)^2
+__device__ __forceinline__ void square(f32x2 (&v)[4], float scale) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = mul2(v[i], pk2(scale));
+        v[i] = mul2(v[i], v[i]);
+    }
+}
+
+__device__ __forceinline__ uint32_t e4m3x4(f32x2 lo, f32x2 hi) {
+    const float2 a = unpk2(lo), b = unpk2(hi);
     uint32_t r;
     asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n"
         " mov.b32 %0, {l, h};\n}"
         : "=r"(r)
-        : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
 
 // a rounded to one of the two e4m3 neighbours, `bits` + 8 of 2^20 against the distance to
-// the lower one: the bits of the mantissa that e4m3 does not have are cut off after the
-// random number is added (to the magnitude: the sign is the top bit).
+// the lower one.  The bits of the mantissa that e4m3 does not have, 20, would be cut off
+// after the random number is added (to the magnitude: the sign is the top bit); half of
+// them less is added here, and the conversion to e4m3 rounds to nearest.
 __device__ __forceinline__ float dither(float a, uint32_t bits) {
-    return __uint_as_float((__float_as_uint(a) + bits + 8u) & 0xfff00000u);
+    return __uint_as_float(__float_as_uint(a) + bits + (8u - (1u << 19)));
 }
 // The same for any a.  Below 2^-6, where e4m3's steps stay 2^-9, it is done at 2^-6
 // higher, where fp32's first three bits have the same steps.  NaN stays NaN.
 __device__ __forceinline__ float dither_any(float a, uint32_t bits) {
     if (a != a) return a;
     if (fabsf(a) >= 0.015625f) return dither(a, bits);
-    return copysignf(dither(fabsf(a) + 0.015625f, bits) - 0.015625f, a);
+    const uint32_t cut = (__float_as_uint(fabsf(a) + 0.015625f) + bits + 8u) & 0xfff00000u;
+    return copysignf(__uint_as_float(cut) - 0.015625f, a);
 }
 
 // The hash but for its last step, h ^ h >> 16, which is taken with the half it is for:
@@ -230,9 +243,9 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
     return r;
 }
 
-// The codes of eight values `v` of a block, and the block's scale.
-template <bool HIGH>
-__device__ __forceinline__ uint2 encode(const f32x2 (&v)[4], const uint32_t (&h)[8], float &scale) {
+// The scale of a block of which this lane holds v, and 1 / scale; `low` is the least
+// magnitude here.
+__device__ __forceinline__ float2 block_scale(const f32x2 (&v)[4], float &low) {
     float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -240,13 +253,8 @@ __device__ __forceinline__ uint2 encode(const f32x2 (&v)[4], const uint32_t (&h)
         f[2 * i] = two.x;
         f[2 * i + 1] = two.y;
     }
-    float top = max3(f[0], f[1], f[2]), low = min3(f[0], f[1], f[2]);
-    top = max3(top, f[3], f[4]);
-    low = min3(low, f[3], f[4]);
-    top = max3(top, f[5], f[6]);
-    low = min3(low, f[5], f[6]);
-    top = max3(top, f[7], 0.0f);
-    low = min3(low, f[7], f[7]);
+    const float top = max3(max3(f[0], f[1], f[2]), max3(f[3], f[4], f[5]), max3(f[6], f[7], f[7]));
+    low = min3(min3(f[0], f[1], f[2]), min3(f[3], f[4], f[5]), min3(f[6], f[7], f[7]));
     uint32_t t = __reduce_max_sync(0xffffffffu, __float_as_uint(top));  // NaN above infinity above the rest
     if (t > 0x7f800000u) {  // the largest of the numbers
         float m = 0.0f;
@@ -254,92 +262,110 @@ __device__ __forceinline__ uint2 encode(const f32x2 (&v)[4], const uint32_t (&h)
         for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
         t = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
     }
-    // below 2^-100 the block is zero: 448 / top would overflow
     const float big = __uint_as_float(t);
-    float inv = 0.0f;
-    scale = 0.0f;
-    if (big >= 7.888609052210118e-31f) {
-        // 448 / big: the approximate reciprocal and one Newton step on the quotient
-        float rcp;
-        asm("rcp.approx.f32 %0, %1;" : "=f"(rcp) : "f"(big));
-        inv = 448.0f * rcp;
-        if (t < 0x7e000000u) inv = fmaf(fmaf(-big, inv, 448.0f), rcp, inv);
-        scale = big * (1.0f / 448.0f);
-    }
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 two = unpk2(mul2(v[i], pk2(inv)));
-        q[2 * i] = two.x;
-        q[2 * i + 1] = two.y;
-    }
-    if (__any_sync(0xffffffffu, !(low * inv >= 0.015625f))) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = dither_any(q[i], random20<HIGH>(h[i]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = dither(q[i], random20<HIGH>(h[i]));
-    }
-    const float a[4] = {q[0], q[1], q[2], q[3]}, b[4] = {q[4], q[5], q[6], q[7]};
-    return make_uint2(e4m3x4(a), e4m3x4(b));
+    if (big < 7.888609052210118e-31f) return make_float2(0.0f, 0.0f);  // 2^-100: 448 / big would overflow
+    // 448 / big: the approximate reciprocal and one Newton step on the quotient
+    float rcp, inv;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(rcp) : "f"(big));
+    inv = 448.0f * rcp;
+    if (t < 0x7e000000u) inv = fmaf(fmaf(-big, inv, 448.0f), rcp, inv);
+    return make_float2(big * (1.0f / 448.0f), inv);
 }
 
 // Square roots within 2^-22.  The approximation takes subnormal numbers for zero: a warp
 // that gets a zero looks again.
-__device__ __forceinline__ void roots(const f32x2 (&v)[4], f32x2 (&o)[4]) {
+template <int NB>
+__device__ __forceinline__ void roots(const f32x2 (&v)[NB][4], f32x2 (&o)[NB][4]) {
     float low = 1.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float2 a = unpk2(v[i]);
+    for (int i = 0; i < 4 * NB; ++i) {
+        float2 a = unpk2(v[i >> 2][i & 3]);
         asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.x));
         asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.y));
-        o[i] = pk2(a.x, a.y);
+        o[i >> 2][i & 3] = pk2(a.x, a.y);
         low = min3(low, a.x, a.y);
     }
     if (__any_sync(0xffffffffu, low == 0.0f)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float2 a = unpk2(v[i]);
+        for (int i = 0; i < 4 * NB; ++i) {
+            float2 a = unpk2(v[i >> 2][i & 3]);
             asm("sqrt.approx.f32 %0, %0;" : "+f"(a.x));
             asm("sqrt.approx.f32 %0, %0;" : "+f"(a.y));
-            o[i] = pk2(a.x, a.y);
+            o[i >> 2][i & 3] = pk2(a.x, a.y);
         }
     }
 }
 
-// A block's update: p, g, and the moments as values; p, m and v become the new ones,
-// `root` sqrt(v).
-__device__ __forceinline__ void adam(f32x2 (&p)[4], const f32x2 (&g)[4], f32x2 (&m)[4], f32x2 (&v)[4], f32x2 (&root)[4],
-                                     const Rates &r, const Consts &k) {
+// The update of NB blocks: p, g, and the moments as values, m still to be taken times
+// m_scale; p, m and v become the new ones, `root` sqrt(v).
+template <int NB>
+__device__ __forceinline__ void adam(f32x2 (&p)[NB][4], const f32x2 (&g)[NB][4], f32x2 (&m)[NB][4], const float (&m_scale)[NB],
+                                     f32x2 (&v)[NB][4], f32x2 (&root)[NB][4], const Rates &r, const Consts &k) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x2 gi = mul2(g[i], pk2(r.gs));
-        m[i] = fma2(pk2(k.b1), m[i], mul2(pk2(k.c1), gi));
-        v[i] = fma2(pk2(k.b2), v[i], mul2(pk2(k.c2), mul2(gi, gi)));
-    }
-    roots(v, root);
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x2 den = fma2(root[i], pk2(r.root_scale), pk2(k.eps));
-        p[i] = fma2(p[i], pk2(r.keep), mul2(mul2(m[i], pk2(-r.rate)), rcp2(den)));
-    }
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 gi = mul2(g[b][i], pk2(r.gs));
+            m[b][i] = fma2(pk2(k.c1), gi, mul2(pk2(k.b1 * m_scale[b]), m[b][i]));
+            v[b][i] = fma2(pk2(k.b2), v[b][i], mul2(pk2(k.c2), mul2(gi, gi)));
+        }
+    roots<NB>(v, root);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 den = fma2(root[b][i], pk2(r.root_scale), pk2(k.eps));
+            p[b][i] = fma2(p[b][i], pk2(r.keep), mul2(mul2(m[b][i], pk2(-r.rate)), rcp2(den)));
+        }
 }
 
-// m and sqrt(v) of a block to memory in 8 bits.
-template <bool FULL>
-__device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, uint32_t block, int have, const f32x2 (&m)[4],
-                                              const f32x2 (&root)[4]) {
+// m and sqrt(v) of NB blocks to memory in 8 bits.
+template <bool FULL, int NB>
+__device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, uint32_t block, int have, f32x2 (&m)[NB][4],
+                                              f32x2 (&root)[NB][4]) {
     const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
-    uint32_t h[8];
+    float2 sm[NB], sv[NB];
+    bool rare = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = mix(((uint32_t)at + i) * 0x51f6db5bu + r.key);
-    float scale_m, scale_v;
-    const uint2 om = encode<false>(m, h, scale_m), ov = encode<true>(root, h, scale_v);
-    store_codes<FULL>((uint8_t *)e.m + at, have, om);
-    store_codes<FULL>((uint8_t *)e.v + at, have, ov);
-    if ((threadIdx.x & 31) == 0) {
-        e.m_scale[block] = scale_m;
-        e.v_scale[block] = scale_v;
+    for (int b = 0; b < NB; ++b) {
+        float low_m, low_v;
+        sm[b] = block_scale(m[b], low_m);
+        sv[b] = block_scale(root[b], low_v);
+        rare |= !(low_m * sm[b].y >= 0.015625f) | !(low_v * sv[b].y >= 0.015625f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[b][i] = mul2(m[b][i], pk2(sm[b].y));
+            root[b][i] = mul2(root[b][i], pk2(sv[b].y));
+        }
+    }
+    uint32_t h[NB][8];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[b][i] = mix(((uint32_t)at + 256 * b + i) * 0x51f6db5bu + r.key);
+    auto all = [&](auto round) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 x = unpk2(m[b][i]), y = unpk2(root[b][i]);
+                const uint32_t h0 = h[b][2 * i], h1 = h[b][2 * i + 1];
+                m[b][i] = pk2(round(x.x, random20<false>(h0)), round(x.y, random20<false>(h1)));
+                root[b][i] = pk2(round(y.x, random20<true>(h0)), round(y.y, random20<true>(h1)));
+            }
+    };
+    if (__any_sync(0xffffffffu, rare))
+        all([](float a, uint32_t bits) { return dither_any(a, bits); });
+    else
+        all([](float a, uint32_t bits) { return dither(a, bits); });
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        store_codes<FULL>((uint8_t *)e.m + at + 256 * b, have, make_uint2(e4m3x4(m[b][0], m[b][1]), e4m3x4(m[b][2], m[b][3])));
+        store_codes<FULL>((uint8_t *)e.v + at + 256 * b, have, make_uint2(e4m3x4(root[b][0], root[b][1]), e4m3x4(root[b][2], root[b][3])));
+        if ((threadIdx.x & 31) == 0) {
+            e.m_scale[block + b] = sm[b].x;
+            e.v_scale[block + b] = sv[b].x;
+        }
     }
 }
 
@@ -348,29 +374,30 @@ template <typename P, typename G, bool EIGHT, bool MASTER, bool FULL>
 __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Consts &k, uint32_t block) {
     const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
     const int have = FULL ? 8 : (int)max(0LL, min(8LL, e.numel - at));
-    f32x2 p[4], g[4], m[4], v[4], root[4];
-    load8<FULL>((const G *)e.grad + at, have, g);
+    f32x2 p[1][4], g[1][4], m[1][4], v[1][4], root[1][4];
+    float m_scale[1] = {1.0f};
+    load8<FULL>((const G *)e.grad + at, have, g[0]);
     if (EIGHT) {
-        decode(load_codes<FULL>((const uint8_t *)e.m + at, have), e.m_scale[block], m);
-        decode(load_codes<FULL>((const uint8_t *)e.v + at, have), e.v_scale[block], v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
+        decode(load_codes<FULL>((const uint8_t *)e.m + at, have), m[0]);
+        decode(load_codes<FULL>((const uint8_t *)e.v + at, have), v[0]);
+        m_scale[0] = e.m_scale[block];
+        square(v[0], e.v_scale[block]);
     } else {
-        load8<FULL>((const float *)e.m + at, have, m);
-        load8<FULL>((const float *)e.v + at, have, v);
+        load8<FULL>((const float *)e.m + at, have, m[0]);
+        load8<FULL>((const float *)e.v + at, have, v[0]);
     }
     if (MASTER)
-        load8<FULL>(e.master + at, have, p);
+        load8<FULL>(e.master + at, have, p[0]);
     else
-        load8<FULL>((const P *)e.param + at, have, p);
-    adam(p, g, m, v, root, r, k);
-    if (MASTER) store8<FULL>(e.master + at, have, p);
-    store8<FULL>((P *)e.param + at, have, p);
+        load8<FULL>((const P *)e.param + at, have, p[0]);
+    adam<1>(p, g, m, m_scale, v, root, r, k);
+    if (MASTER) store8<FULL>(e.master + at, have, p[0]);
+    store8<FULL>((P *)e.param + at, have, p[0]);
     if (EIGHT) {
-        store_moments<FULL>(e, r, block, have, m, root);
+        store_moments<FULL, 1>(e, r, block, have, m, root);
     } else {
-        store8<FULL>((float *)e.m + at, have, m);
-        store8<FULL>((float *)e.v + at, have, v);
+        store8<FULL>((float *)e.m + at, have, m[0]);
+        store8<FULL>((float *)e.v + at, have, v[0]);
     }
 }
 
@@ -460,21 +487,23 @@ __device__ __forceinline__ void run_eight(Walk<MAX> &w, const Common &c, const C
         w.next();
         go = w.more() && w.entry().kind == kind && w.whole();
         if (go) raw.load(source(w.entry()), w.entry(), w.pair());
+        f32x2 p[2][4], g[2][4], m[2][4], v[2][4], root[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            now.p[b].get(p[b]);
+            now.g[b].get(g[b]);
+            decode(now.m[b], m[b]);
+            decode(now.v[b], v[b]);
+            square(v[b], now.v_scale[b]);
+        }
+        adam<2>(p, g, m, now.m_scale, v, root, r, k);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const long long at = (long long)pair * 512 + b * 256 + (threadIdx.x & 31) * 8;
-            f32x2 p[4], g[4], m[4], v[4], root[4];
-            now.p[b].get(p);
-            now.g[b].get(g);
-            decode(now.m[b], now.m_scale[b], m);
-            decode(now.v[b], now.v_scale[b], v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
-            adam(p, g, m, v, root, r, k);
-            if (MASTER) store8<true>(e.master + at, 8, p);
-            store8<true>((P *)e.param + at, 8, p);
-            store_moments<true>(e, r, 2 * pair + b, 8, m, root);
+            if (MASTER) store8<true>(e.master + at, 8, p[b]);
+            store8<true>((P *)e.param + at, 8, p[b]);
         }
+        store_moments<true, 2>(e, r, 2 * pair, 8, m, root);
     }
 }
 
