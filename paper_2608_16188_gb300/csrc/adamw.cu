@@ -59,7 +59,7 @@ struct Table {
 };
 
 struct Consts {
-    float lr, b1, b2, c1, c2, eps, log_b1, log_b2;  // c1 = 1 - b1, c2 = 1 - b2
+    float lr, b1, b2, c1, c2, eps, log_b1, log_b2, zero;  // c1 = 1 - b1, c2 = 1 - b2
     int step;
     uint32_t seed_key;
     const int32_t *step_dev;
@@ -171,8 +171,8 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int have, uint2 v) {
     }
 }
 
-// Eight e4m3 values.
-__device__ __forceinline__ void decode(uint2 c, f32x2 (&o)[4]) {
+// Eight e4m3 values times `scale`.
+__device__ __forceinline__ void decode(uint2 c, float scale, f32x2 (&o)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint16_t two = (uint16_t)((i < 2 ? c.x : c.y) >> (16 * (i & 1)));
@@ -181,17 +181,13 @@ __device__ __forceinline__ void decode(uint2 c, f32x2 (&o)[4]) {
             " cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}"
             : "=f"(lo), "=f"(hi)
             : "h"(two));
-        o[i] = pk2(lo, hi);
+        o[i] = mul2(pk2(lo, hi), pk2(scale));
     }
 }
 
-// (scale v)^2
-__device__ __forceinline__ void square(f32x2 (&v)[4], float scale) {
+__device__ __forceinline__ void square(f32x2 (&v)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[i] = mul2(v[i], pk2(scale));
-        v[i] = mul2(v[i], v[i]);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], v[i]);
 }
 
 __device__ __forceinline__ uint32_t e4m3x4(f32x2 lo, f32x2 hi) {
@@ -205,19 +201,26 @@ __device__ __forceinline__ uint32_t e4m3x4(f32x2 lo, f32x2 hi) {
 }
 
 // a rounded to one of the two e4m3 neighbours, `bits` + 8 of 2^20 against the distance to
-// the lower one.  The bits of the mantissa that e4m3 does not have, 20, would be cut off
-// after the random number is added (to the magnitude: the sign is the top bit); half of
-// them less is added here, and the conversion to e4m3 rounds to nearest.
+// the lower one: the bits of the mantissa that e4m3 does not have, 20, are cut off after
+// the random number is added (to the magnitude: the sign is the top bit).
 __device__ __forceinline__ float dither(float a, uint32_t bits) {
-    return __uint_as_float(__float_as_uint(a) + bits + (8u - (1u << 19)));
+    return __uint_as_float((__float_as_uint(a) + bits + 8u) & 0xfff00000u);
 }
 // The same for any a.  Below 2^-6, where e4m3's steps stay 2^-9, it is done at 2^-6
 // higher, where fp32's first three bits have the same steps.  NaN stays NaN.
 __device__ __forceinline__ float dither_any(float a, uint32_t bits) {
     if (a != a) return a;
     if (fabsf(a) >= 0.015625f) return dither(a, bits);
-    const uint32_t cut = (__float_as_uint(fabsf(a) + 0.015625f) + bits + 8u) & 0xfff00000u;
-    return copysignf(__uint_as_float(cut) - 0.015625f, a);
+    return copysignf(dither(fabsf(a) + 0.015625f, bits) - 0.015625f, a);
+}
+// dither of a positive a from 2^-6 on, with the high half of a hash and as a code: the
+// exponent and the first three bits of the mantissa, less the difference of the biases,
+// (127 - 7) << 3.  Shifted by 4 they are the top byte, modulo 256.
+__device__ __forceinline__ uint32_t dither_code(float a, uint32_t h) {
+    return (__float_as_uint(a) << 4) + (((h >> 8) & 0x00ffff00u) | 0x40000080u);
+}
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 
 // The hash but for its last step, h ^ h >> 16, which is taken with the half it is for:
@@ -264,50 +267,58 @@ __device__ __forceinline__ float2 block_scale(const f32x2 (&v)[4], float &low) {
     }
     const float big = __uint_as_float(t);
     if (big < 7.888609052210118e-31f) return make_float2(0.0f, 0.0f);  // 2^-100: 448 / big would overflow
-    // 448 / big: the approximate reciprocal and one Newton step on the quotient
-    float rcp, inv;
+    // 1 / big to nearest: the approximation and one Newton step, where that neither
+    // underflows (above 2^125) nor meets an infinity
+    float rcp;
     asm("rcp.approx.f32 %0, %1;" : "=f"(rcp) : "f"(big));
-    inv = 448.0f * rcp;
-    if (t < 0x7e000000u) inv = fmaf(fmaf(-big, inv, 448.0f), rcp, inv);
-    return make_float2(big * (1.0f / 448.0f), inv);
+    if (t < 0x7e000000u) rcp = fmaf(fmaf(-big, rcp, 1.0f), rcp, rcp);
+    return make_float2(big * (1.0f / 448.0f), 448.0f * rcp);
 }
 
-// Square roots within 2^-22.  The approximation takes subnormal numbers for zero: a warp
-// that gets a zero looks again.
+// Square roots, rounded to nearest: the approximate 1 / sqrt(v) and one Newton step on
+// v / sqrt(v).  Where that is no number (0, infinity) or the step underflows, sqrtf.
 template <int NB>
 __device__ __forceinline__ void roots(const f32x2 (&v)[NB][4], f32x2 (&o)[NB][4]) {
     float low = 1.0f;
 #pragma unroll
     for (int i = 0; i < 4 * NB; ++i) {
-        float2 a = unpk2(v[i >> 2][i & 3]);
-        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.x));
-        asm("sqrt.approx.ftz.f32 %0, %0;" : "+f"(a.y));
-        o[i >> 2][i & 3] = pk2(a.x, a.y);
-        low = min3(low, a.x, a.y);
+        const f32x2 x = v[i >> 2][i & 3];
+        float2 y = unpk2(x);
+        asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(y.x));
+        asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(y.y));
+        const f32x2 r = pk2(y.x, y.y), s = mul2(x, r), ns = mul2(s, pk2(-1.0f));
+        o[i >> 2][i & 3] = fma2(fma2(ns, s, x), mul2(r, pk2(0.5f)), s);
+        const float2 two = unpk2(o[i >> 2][i & 3]);
+        low = min3(low, two.x, two.y);
     }
-    if (__any_sync(0xffffffffu, low == 0.0f)) {
+    if (__any_sync(0xffffffffu, !(low >= 8.8817841970012523e-16f))) {  // 2^-50
 #pragma unroll
         for (int i = 0; i < 4 * NB; ++i) {
-            float2 a = unpk2(v[i >> 2][i & 3]);
-            asm("sqrt.approx.f32 %0, %0;" : "+f"(a.x));
-            asm("sqrt.approx.f32 %0, %0;" : "+f"(a.y));
-            o[i >> 2][i & 3] = pk2(a.x, a.y);
+            const float2 x = unpk2(v[i >> 2][i & 3]);
+            o[i >> 2][i & 3] = pk2(sqrtf(x.x), sqrtf(x.y));
         }
     }
 }
 
-// The update of NB blocks: p, g, and the moments as values, m still to be taken times
-// m_scale; p, m and v become the new ones, `root` sqrt(v).
+// a b, which the compiler cannot make one instruction with a sum that follows: it adds a
+// zero that it does not know (a product and a sum of packed instructions it does join,
+// although both say how they round).
+__device__ __forceinline__ f32x2 product(f32x2 a, f32x2 b, const Consts &k) { return fma2(a, b, pk2(k.zero)); }
+
+// The update of NB blocks: p, g, and the moments as values; p, m and v become the new
+// ones, `root` sqrt(v).  Every product and sum of the moments is rounded by itself, as a
+// sequence of elementary operations would: what an 8-bit moment is rounded to hangs on
+// the last bit now and then, and a reference for it is then easily written.
 template <int NB>
-__device__ __forceinline__ void adam(f32x2 (&p)[NB][4], const f32x2 (&g)[NB][4], f32x2 (&m)[NB][4], const float (&m_scale)[NB],
-                                     f32x2 (&v)[NB][4], f32x2 (&root)[NB][4], const Rates &r, const Consts &k) {
+__device__ __forceinline__ void adam(f32x2 (&p)[NB][4], const f32x2 (&g)[NB][4], f32x2 (&m)[NB][4], f32x2 (&v)[NB][4],
+                                     f32x2 (&root)[NB][4], const Rates &r, const Consts &k) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f32x2 gi = mul2(g[b][i], pk2(r.gs));
-            m[b][i] = fma2(pk2(k.c1), gi, mul2(pk2(k.b1 * m_scale[b]), m[b][i]));
-            v[b][i] = fma2(pk2(k.b2), v[b][i], mul2(pk2(k.c2), mul2(gi, gi)));
+            m[b][i] = add2(product(pk2(k.b1), m[b][i], k), product(pk2(k.c1), gi, k));
+            v[b][i] = add2(product(pk2(k.b2), v[b][i], k), product(pk2(k.c2), mul2(gi, gi), k));
         }
     roots<NB>(v, root);
 #pragma unroll
@@ -343,25 +354,40 @@ __device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, ui
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[b][i] = mix(((uint32_t)at + 256 * b + i) * 0x51f6db5bu + r.key);
-    auto all = [&](auto round) {
+    uint2 cm[NB], cv[NB];
+    if (__any_sync(0xffffffffu, rare)) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 x = unpk2(m[b][i]), y = unpk2(root[b][i]);
                 const uint32_t h0 = h[b][2 * i], h1 = h[b][2 * i + 1];
-                m[b][i] = pk2(round(x.x, random20<false>(h0)), round(x.y, random20<false>(h1)));
-                root[b][i] = pk2(round(y.x, random20<true>(h0)), round(y.y, random20<true>(h1)));
+                m[b][i] = pk2(dither_any(x.x, random20<false>(h0)), dither_any(x.y, random20<false>(h1)));
+                root[b][i] = pk2(dither_any(y.x, random20<true>(h0)), dither_any(y.y, random20<true>(h1)));
             }
-    };
-    if (__any_sync(0xffffffffu, rare))
-        all([](float a, uint32_t bits) { return dither_any(a, bits); });
-    else
-        all([](float a, uint32_t bits) { return dither(a, bits); });
+            cm[b] = make_uint2(e4m3x4(m[b][0], m[b][1]), e4m3x4(m[b][2], m[b][3]));
+            cv[b] = make_uint2(e4m3x4(root[b][0], root[b][1]), e4m3x4(root[b][2], root[b][3]));
+        }
+    } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 x = unpk2(m[b][i]), y = unpk2(root[b][i]);
+                const uint32_t h0 = h[b][2 * i], h1 = h[b][2 * i + 1];
+                m[b][i] = pk2(dither(x.x, random20<false>(h0)), dither(x.y, random20<false>(h1)));
+                w[2 * i] = dither_code(y.x, h0);
+                w[2 * i + 1] = dither_code(y.y, h1);
+            }
+            cm[b] = make_uint2(e4m3x4(m[b][0], m[b][1]), e4m3x4(m[b][2], m[b][3]));
+            cv[b] = make_uint2(top_bytes(w[0], w[1], w[2], w[3]), top_bytes(w[4], w[5], w[6], w[7]));
+        }
+    }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        store_codes<FULL>((uint8_t *)e.m + at + 256 * b, have, make_uint2(e4m3x4(m[b][0], m[b][1]), e4m3x4(m[b][2], m[b][3])));
-        store_codes<FULL>((uint8_t *)e.v + at + 256 * b, have, make_uint2(e4m3x4(root[b][0], root[b][1]), e4m3x4(root[b][2], root[b][3])));
+        store_codes<FULL>((uint8_t *)e.m + at + 256 * b, have, cm[b]);
+        store_codes<FULL>((uint8_t *)e.v + at + 256 * b, have, cv[b]);
         if ((threadIdx.x & 31) == 0) {
             e.m_scale[block + b] = sm[b].x;
             e.v_scale[block + b] = sv[b].x;
@@ -375,13 +401,11 @@ __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Con
     const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
     const int have = FULL ? 8 : (int)max(0LL, min(8LL, e.numel - at));
     f32x2 p[1][4], g[1][4], m[1][4], v[1][4], root[1][4];
-    float m_scale[1] = {1.0f};
     load8<FULL>((const G *)e.grad + at, have, g[0]);
     if (EIGHT) {
-        decode(load_codes<FULL>((const uint8_t *)e.m + at, have), m[0]);
-        decode(load_codes<FULL>((const uint8_t *)e.v + at, have), v[0]);
-        m_scale[0] = e.m_scale[block];
-        square(v[0], e.v_scale[block]);
+        decode(load_codes<FULL>((const uint8_t *)e.m + at, have), e.m_scale[block], m[0]);
+        decode(load_codes<FULL>((const uint8_t *)e.v + at, have), e.v_scale[block], v[0]);
+        square(v[0]);
     } else {
         load8<FULL>((const float *)e.m + at, have, m[0]);
         load8<FULL>((const float *)e.v + at, have, v[0]);
@@ -390,7 +414,7 @@ __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Con
         load8<FULL>(e.master + at, have, p[0]);
     else
         load8<FULL>((const P *)e.param + at, have, p[0]);
-    adam<1>(p, g, m, m_scale, v, root, r, k);
+    adam<1>(p, g, m, v, root, r, k);
     if (MASTER) store8<FULL>(e.master + at, have, p[0]);
     store8<FULL>((P *)e.param + at, have, p[0]);
     if (EIGHT) {
@@ -492,11 +516,11 @@ __device__ __forceinline__ void run_eight(Walk<MAX> &w, const Common &c, const C
         for (int b = 0; b < 2; ++b) {
             now.p[b].get(p[b]);
             now.g[b].get(g[b]);
-            decode(now.m[b], m[b]);
-            decode(now.v[b], v[b]);
-            square(v[b], now.v_scale[b]);
+            decode(now.m[b], now.m_scale[b], m[b]);
+            decode(now.v[b], now.v_scale[b], v[b]);
+            square(v[b]);
         }
-        adam<2>(p, g, m, now.m_scale, v, root, r, k);
+        adam<2>(p, g, m, v, root, r, k);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const long long at = (long long)pair * 512 + b * 256 + (threadIdx.x & 31) * 8;
@@ -594,6 +618,7 @@ int launch_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_confi
     k.eps = (float)c->eps;
     k.log_b1 = (float)log(c->beta1);
     k.log_b2 = (float)log(c->beta2);
+    k.zero = 0.0f;
     k.step = c->step;
     k.seed_key = c->seed * 0xe32a5e87u;
     k.step_dev = c->step_dev;
