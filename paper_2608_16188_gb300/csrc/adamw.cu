@@ -41,10 +41,11 @@ struct Entry {
     const void *grad;
     void *m, *v;
     float *m_scale, *v_scale, *master;
-    long long numel;
+    uint32_t whole, rest;  // pairs of whole blocks, and elements behind them
     float lr_scale, decay;
     uint32_t key;  // the tensor's place among the call's, hashed
     int kind;      // bits: fp32 parameters (1), fp32 gradients (2), 8-bit moments (4), master (8)
+    __device__ __forceinline__ long long numel() const { return (long long)whole * 512 + rest; }
 };
 enum { P32 = 1, G32 = 2, S8 = 4, MST = 8 };
 
@@ -215,9 +216,10 @@ __device__ __forceinline__ float dither_any(float a, uint32_t bits) {
 }
 // dither of a positive a from 2^-6 on, with the high half of a hash and as a code: the
 // exponent and the first three bits of the mantissa, less the difference of the biases,
-// (127 - 7) << 3.  Shifted by 4 they are the top byte, modulo 256.
+// (127 - 7) << 3.  Shifted by 4 they are the top byte, modulo 256, and the random number's
+// half is the two bytes in the middle.
 __device__ __forceinline__ uint32_t dither_code(float a, uint32_t h) {
-    return (__float_as_uint(a) << 4) + (((h >> 8) & 0x00ffff00u) | 0x40000080u);
+    return (__float_as_uint(a) << 4) + __byte_perm(h, 0x40000080u, 0x7324);
 }
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
@@ -246,9 +248,9 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
     return r;
 }
 
-// The scale of a block of which this lane holds v, and 1 / scale; `low` is the least
-// magnitude here.
-__device__ __forceinline__ float2 block_scale(const f32x2 (&v)[4], float &low) {
+// The largest magnitude of a block of which this lane holds v, the numbers among it;
+// `low` is the least one here (NaN where there is one).
+__device__ __forceinline__ uint32_t block_max(const f32x2 (&v)[4], float &low) {
     float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -259,12 +261,17 @@ __device__ __forceinline__ float2 block_scale(const f32x2 (&v)[4], float &low) {
     const float top = max3(max3(f[0], f[1], f[2]), max3(f[3], f[4], f[5]), max3(f[6], f[7], f[7]));
     low = min3(min3(f[0], f[1], f[2]), min3(f[3], f[4], f[5]), min3(f[6], f[7], f[7]));
     uint32_t t = __reduce_max_sync(0xffffffffu, __float_as_uint(top));  // NaN above infinity above the rest
-    if (t > 0x7f800000u) {  // the largest of the numbers
+    if (t > 0x7f800000u) {
         float m = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
         t = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
     }
+    return t;
+}
+
+// The scale of a block with this largest magnitude, and 1 / scale.
+__device__ __forceinline__ float2 scale_of(uint32_t t) {
     const float big = __uint_as_float(t);
     if (big < 7.888609052210118e-31f) return make_float2(0.0f, 0.0f);  // 2^-100: 448 / big would overflow
     // 1 / big to nearest: the approximation and one Newton step, where that neither
@@ -275,27 +282,28 @@ __device__ __forceinline__ float2 block_scale(const f32x2 (&v)[4], float &low) {
     return make_float2(big * (1.0f / 448.0f), 448.0f * rcp);
 }
 
-// Square roots, rounded to nearest: the approximate 1 / sqrt(v) and one Newton step on
-// v / sqrt(v).  Where that is no number (0, infinity) or the step underflows, sqrtf.
+// The negative square roots of -v, rounded to nearest: the approximate 1 / sqrt(v) and one
+// Newton step on v / sqrt(v).  Where that is no number (0, infinity) or the step
+// underflows, sqrtf.  `nv` is -v: with the signs turned the step needs no negation.
 template <int NB>
-__device__ __forceinline__ void roots(const f32x2 (&v)[NB][4], f32x2 (&o)[NB][4]) {
+__device__ __forceinline__ void roots(const f32x2 (&nv)[NB][4], f32x2 (&o)[NB][4]) {
     float low = 1.0f;
 #pragma unroll
     for (int i = 0; i < 4 * NB; ++i) {
-        const f32x2 x = v[i >> 2][i & 3];
+        const f32x2 x = nv[i >> 2][i & 3];
         float2 y = unpk2(x);
-        asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(y.x));
-        asm("rsqrt.approx.ftz.f32 %0, %0;" : "+f"(y.y));
-        const f32x2 r = pk2(y.x, y.y), s = mul2(x, r), ns = mul2(s, pk2(-1.0f));
-        o[i >> 2][i & 3] = fma2(fma2(ns, s, x), mul2(r, pk2(0.5f)), s);
+        asm("{\n .reg .f32 t;\n neg.f32 t, %0;\n rsqrt.approx.ftz.f32 %0, t;\n}" : "+f"(y.x));
+        asm("{\n .reg .f32 t;\n neg.f32 t, %0;\n rsqrt.approx.ftz.f32 %0, t;\n}" : "+f"(y.y));
+        const f32x2 r = pk2(y.x, y.y), ns = mul2(x, r);
+        o[i >> 2][i & 3] = fma2(fma2(ns, ns, x), mul2(r, pk2(0.5f)), ns);
         const float2 two = unpk2(o[i >> 2][i & 3]);
         low = min3(low, two.x, two.y);
     }
     if (__any_sync(0xffffffffu, !(low >= 8.8817841970012523e-16f))) {  // 2^-50
 #pragma unroll
         for (int i = 0; i < 4 * NB; ++i) {
-            const float2 x = unpk2(v[i >> 2][i & 3]);
-            o[i >> 2][i & 3] = pk2(sqrtf(x.x), sqrtf(x.y));
+            const float2 x = unpk2(nv[i >> 2][i & 3]);
+            o[i >> 2][i & 3] = pk2(-sqrtf(-x.x), -sqrtf(-x.y));
         }
     }
 }
@@ -305,8 +313,8 @@ __device__ __forceinline__ void roots(const f32x2 (&v)[NB][4], f32x2 (&o)[NB][4]
 // although both say how they round).
 __device__ __forceinline__ f32x2 product(f32x2 a, f32x2 b, const Consts &k) { return fma2(a, b, pk2(k.zero)); }
 
-// The update of NB blocks: p, g, and the moments as values; p, m and v become the new
-// ones, `root` sqrt(v).  Every product and sum of the moments is rounded by itself, as a
+// The update of NB blocks: p, g, and the moments as values; p and m become the new ones,
+// v becomes -v and `root` -sqrt(v).  Every product and sum of the moments is rounded by itself, as a
 // sequence of elementary operations would: what an 8-bit moment is rounded to hangs on
 // the last bit now and then, and a reference for it is then easily written.
 template <int NB>
@@ -318,35 +326,47 @@ __device__ __forceinline__ void adam(f32x2 (&p)[NB][4], const f32x2 (&g)[NB][4],
         for (int i = 0; i < 4; ++i) {
             const f32x2 gi = mul2(g[b][i], pk2(r.gs));
             m[b][i] = add2(product(pk2(k.b1), m[b][i], k), product(pk2(k.c1), gi, k));
-            v[b][i] = add2(product(pk2(k.b2), v[b][i], k), product(pk2(k.c2), mul2(gi, gi), k));
+            v[b][i] = add2(product(pk2(-k.b2), v[b][i], k), product(pk2(-k.c2), mul2(gi, gi), k));
         }
     roots<NB>(v, root);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const f32x2 den = fma2(root[b][i], pk2(r.root_scale), pk2(k.eps));
+            const f32x2 den = fma2(root[b][i], pk2(-r.root_scale), pk2(k.eps));
             p[b][i] = fma2(p[b][i], pk2(r.keep), mul2(mul2(m[b][i], pk2(-r.rate)), rcp2(den)));
         }
 }
 
-// m and sqrt(v) of NB blocks to memory in 8 bits.
+// m and sqrt(v), given as its negative, of NB blocks to memory in 8 bits.
 template <bool FULL, int NB>
 __device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, uint32_t block, int have, f32x2 (&m)[NB][4],
                                               f32x2 (&root)[NB][4]) {
-    const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
-    float2 sm[NB], sv[NB];
+    const int lane = threadIdx.x & 31;
+    const long long at = (long long)block * 256 + lane * 8;
     bool rare = false;
+    {
+        // lane i computes scale i of the blocks' 2 NB, m's and v's in turn, and stores it
+        float low[2 * NB];
+        uint32_t top = 0;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        float low_m, low_v;
-        sm[b] = block_scale(m[b], low_m);
-        sv[b] = block_scale(root[b], low_v);
-        rare |= !(low_m * sm[b].y >= 0.015625f) | !(low_v * sv[b].y >= 0.015625f);
+        for (int i = 0; i < 2 * NB; ++i) {
+            const uint32_t t = i & 1 ? block_max(root[i >> 1], low[i]) : block_max(m[i >> 1], low[i]);
+            if (lane == i) top = t;
+        }
+        const float2 mine = scale_of(top);
+        if (lane < 2 * NB) (lane & 1 ? e.v_scale : e.m_scale)[block + (lane >> 1)] = mine.x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m[b][i] = mul2(m[b][i], pk2(sm[b].y));
-            root[b][i] = mul2(root[b][i], pk2(sv[b].y));
+        for (int i = 0; i < 2 * NB; ++i) {
+            const float inv = __shfl_sync(0xffffffffu, mine.y, i);
+            rare |= !(low[i] * inv >= 0.015625f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (i & 1)
+                    root[i >> 1][j] = mul2(root[i >> 1][j], pk2(-inv));
+                else
+                    m[i >> 1][j] = mul2(m[i >> 1][j], pk2(inv));
+            }
         }
     }
     uint32_t h[NB][8];
@@ -388,10 +408,6 @@ __device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, ui
     for (int b = 0; b < NB; ++b) {
         store_codes<FULL>((uint8_t *)e.m + at + 256 * b, have, cm[b]);
         store_codes<FULL>((uint8_t *)e.v + at + 256 * b, have, cv[b]);
-        if ((threadIdx.x & 31) == 0) {
-            e.m_scale[block + b] = sm[b].x;
-            e.v_scale[block + b] = sv[b].x;
-        }
     }
 }
 
@@ -399,7 +415,7 @@ __device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, ui
 template <typename P, typename G, bool EIGHT, bool MASTER, bool FULL>
 __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Consts &k, uint32_t block) {
     const long long at = (long long)block * 256 + (threadIdx.x & 31) * 8;
-    const int have = FULL ? 8 : (int)max(0LL, min(8LL, e.numel - at));
+    const int have = FULL ? 8 : (int)max(0LL, min(8LL, e.numel() - at));
     f32x2 p[1][4], g[1][4], m[1][4], v[1][4], root[1][4];
     load8<FULL>((const G *)e.grad + at, have, g[0]);
     if (EIGHT) {
@@ -420,6 +436,8 @@ __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Con
     if (EIGHT) {
         store_moments<FULL, 1>(e, r, block, have, m, root);
     } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[0][i] = mul2(v[0][i], pk2(-1.0f));
         store8<FULL>((float *)e.m + at, have, m[0]);
         store8<FULL>((float *)e.v + at, have, v[0]);
     }
@@ -429,7 +447,7 @@ __device__ __forceinline__ void update(const Entry &e, const Rates &r, const Con
 template <typename P, typename G, bool EIGHT, bool MASTER>
 __device__ __forceinline__ void update_last(const Entry &e, const Rates &r, const Consts &k, uint32_t pair) {
 #pragma unroll 1
-    for (uint32_t b = 2 * pair; b < 2 * pair + 2 && (long long)b * 256 < e.numel; ++b)
+    for (uint32_t b = 2 * pair; b < 2 * pair + 2 && (long long)b * 256 < e.numel(); ++b)
         update<P, G, EIGHT, MASTER, false>(e, r, k, b);
 }
 
@@ -457,7 +475,7 @@ struct Walk {
     }
     __device__ __forceinline__ const Entry &entry() const { return tab.e[at]; }
     __device__ __forceinline__ uint32_t pair() const { return b - tab.first[at]; }
-    __device__ __forceinline__ bool whole() const { return ((long long)pair() + 1) * 512 <= entry().numel; }
+    __device__ __forceinline__ bool whole() const { return pair() < entry().whole; }
 };
 
 struct Common {
@@ -574,7 +592,8 @@ adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
     }
 }
 
-static_assert(sizeof(Table<380>) + sizeof(Consts) <= 32764, "a launch's arguments");
+constexpr int SMALL = 40, LARGE = 380;  // tables of 3.4 and 32 KB; a launch takes at most 32764 B
+static_assert(sizeof(Table<LARGE>) + sizeof(Consts) <= 32764, "a launch's arguments");
 
 template <int MAX>
 int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pairs, const Consts &k, cudaStream_t s) {
@@ -595,7 +614,8 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pai
         e.m_scale = x.m_scale;
         e.v_scale = x.v_scale;
         e.master = x.master;
-        e.numel = x.numel;
+        e.whole = (uint32_t)(x.numel / 512);
+        e.rest = (uint32_t)(x.numel % 512);
         e.lr_scale = x.lr_scale;
         e.decay = x.weight_decay;
         e.key = (uint32_t)(base + i) * 0x5e4087b3u;
@@ -624,7 +644,6 @@ int launch_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_confi
     k.step_dev = c->step_dev;
     k.lr_dev = c->lr_dev;
     k.grad_scale = c->grad_scale;
-    constexpr int SMALL = 40, LARGE = 380;  // tables of 3.4 and 32 KB; a launch takes at most 32764 B
     for (int base = 0; base < n;) {
         int m = 0;
         uint64_t pairs = 0;
