@@ -15,7 +15,8 @@
 // reduction; the dX update reads W_r[t] transposed from shared memory, staged
 // once per task segment of a persistent CTA.  With renormalised gates dlogit
 // has k non-zeros, so the update is k scaled columns of W_r, not an E-term
-// contraction.
+// contraction.  With VMOE_DLOGITS_ADD it is added to the dense gradient of other
+// losses that dlogits holds, and the update is an E-term one.
 //
 // Kernel 2 (router_dw), bf16 problems: dW_r = x^T dlogit on the tensor cores,
 // tcgen05 for E = 32 or 64 and d a multiple of 128 (router_dw_tc.cu), else the
@@ -89,8 +90,9 @@ constexpr int RG_THREADS = 512;
 constexpr int RG_WARPS = RG_THREADS / 32;
 constexpr int RG_UNROLL = 2;
 constexpr size_t RG_SMEM_CAP = 200 * 1024;
+constexpr unsigned RG_DENSE = VMOE_NO_RENORM | VMOE_DLOGITS_ADD;  // dlogit rows without zeros
 
-// Shared memory: per-warp dlogit rows (VMOE_NO_RENORM), then W_r[t]^T, one row
+// Shared memory: per-warp dlogit rows (dense ones), then W_r[t]^T, one row
 // per expert with pitch wt_pitch(d) floats.  Within each block of 256 columns the
 // columns are permuted so that the 8 columns 8L..8L+7 a lane reads sit at 4L..4L+3
 // and 128+4L..128+4L+3: the lanes of a warp then read two runs of consecutive
@@ -104,7 +106,7 @@ __device__ __forceinline__ int wt_col8(int v) {  // first half of columns v..v+7
     return (v & ~255) + ((v & 255) >> 1);
 }
 inline size_t rg_smem_rows(const Dims &p) {
-    return (p.flags & VMOE_NO_RENORM) ? (size_t)RG_WARPS * p.E * sizeof(float) : 0;
+    return (p.flags & RG_DENSE) ? (size_t)RG_WARPS * p.E * sizeof(float) : 0;
 }
 inline size_t rg_smem_w(const Dims &p) { return (size_t)p.E * wt_pitch(p.d) * sizeof(float); }
 
@@ -151,10 +153,10 @@ __device__ __noinline__ void stage_wt(const float *__restrict__ wrt, float *WT, 
 //
 // gate_backward: reduces the lane partials of dgate_j (fixed butterfly), writes
 // dgate and the dlogit row, and returns in c[j] the dlogit of expert e_j
-// (renormalised gates; VMOE_NO_RENORM leaves the dense row in dlrow).  Returns
+// (renormalised gates; a dense row is left in dlrow instead).  Returns
 // whether the dX update has any non-zero term.
 template <int KMAX>
-__device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, int lane, long long tn,
+__device__ __forceinline__ bool gate_backward(int k, int E, unsigned flags, int lane, long long tn,
                                               float (&dg)[KMAX], const float (&gt)[KMAX],
                                               const int (&ei)[KMAX], const float *logits,
                                               float *dgate, float *dlogits, float *dlrow,
@@ -181,15 +183,21 @@ __device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, int l
         c[j] = j < k ? gt[j] * (dg[j] - s) : 0.0f;
         any |= c[j] != 0.0f;
     }
-    if (!norenorm) {
+    if (!(flags & VMOE_NO_RENORM)) {
+        const bool add = (flags & VMOE_DLOGITS_ADD) != 0;
         for (int e = lane; e < E; e += 32) {
             float v = 0.0f;
 #pragma unroll
             for (int j = 0; j < KMAX; ++j)
                 if (j < k && ei[j] == e) v = c[j];
+            if (add) {
+                v += dl[e];
+                dlrow[e] = v;
+            }
             dl[e] = v;
         }
-        return any;
+        if (add) __syncwarp();
+        return any || add;
     }
     const float *l = logits + tn * E;
     float mx = -INFINITY;
@@ -205,7 +213,8 @@ __device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, int l
 #pragma unroll
         for (int j = 0; j < KMAX; ++j)
             if (j < k && ei[j] == e) g = dg[j];
-        const float v = expf(__ldg(l + e) - mx) / sum * (g - s);
+        float v = expf(__ldg(l + e) - mx) / sum * (g - s);
+        if (flags & VMOE_DLOGITS_ADD) v += dl[e];
         dl[e] = v;
         dlrow[e] = v;
     }
@@ -214,9 +223,9 @@ __device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, int l
 }
 
 // dx_terms: r[0..7] = sum over the dX terms of dlogit_e * W_r[v + q][e] for the
-// 8 columns v..v+7: the k chosen experts (renormalised gates) or all E.
+// 8 columns v..v+7: the k chosen experts (renormalised gates) or all E (dense).
 template <int KMAX, bool WSMEM>
-__device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool norenorm,
+__device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool dense,
                                          const float *dlrow, const int (&ei)[KMAX],
                                          const float (&c)[KMAX], const float *WT, int dp,
                                          const float *wrt, int E) {
@@ -225,7 +234,7 @@ __device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool nore
     for (int jj = 0; jj < ne; ++jj) {
         int e = jj;
         float cj = 0.0f;
-        if (norenorm) {
+        if (dense) {
             cj = dlrow[jj];
         } else {
 #pragma unroll
@@ -264,10 +273,10 @@ router_grad_kernel(Dims p, const T *__restrict__ dy, const T *__restrict__ ye,
     extern __shared__ __align__(16) float rg_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int d = p.d, E = p.E, k = p.k, N = p.N;
-    const bool norenorm = (p.flags & VMOE_NO_RENORM) != 0;
+    const bool dense = (p.flags & RG_DENSE) != 0;
     const int dp = wt_pitch(d);
     float *dlrow = rg_smem + warp * E;
-    float *WT = rg_smem + (norenorm ? RG_WARPS * E : 0);
+    float *WT = rg_smem + (dense ? RG_WARPS * E : 0);
     const long long TN = (long long)p.T * N;
     const long long beg = TN * blockIdx.x / gridDim.x;
     const long long end = TN * (blockIdx.x + 1) / gridDim.x;
@@ -310,22 +319,22 @@ router_grad_kernel(Dims p, const T *__restrict__ dy, const T *__restrict__ ye,
                 }
             }
             float c[KMAX];
-            const bool any = gate_backward<KMAX>(k, E, norenorm, lane, tn, dg, gt, ei, logits,
+            const bool any = gate_backward<KMAX>(k, E, p.flags, lane, tn, dg, gt, ei, logits,
                                                  dgate, dlogits, dlrow, c);
             // dX += W_r dlogit, summed in fp32 and added to dX with one rounding
             if (dx != nullptr && any) {
                 T *xr = dx + tn * d;
-                const int ne = norenorm ? E : k;
+                const int ne = dense ? E : k;
                 for (int v = lane * 8; v < d; v += 256) {
                     float r[8], o[8];
-                    dx_terms<KMAX, WSMEM>(r, v, ne, norenorm, dlrow, ei, c, WT, dp, wrt, E);
+                    dx_terms<KMAX, WSMEM>(r, v, ne, dense, dlrow, ei, c, WT, dp, wrt, E);
                     load8_rw<T>(xr + v, o);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) o[q] += r[q];
                     store8<T>(xr + v, o);
                 }
             }
-            if (norenorm) __syncwarp();  // dlrow is rewritten by the next token
+            if (dense) __syncwarp();  // dlrow is rewritten by the next token
         }
         seg = seg_end;
     }
@@ -346,10 +355,10 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
     extern __shared__ __align__(16) float rg_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int d = p.d, E = p.E, k = p.k, N = p.N;
-    const bool norenorm = (p.flags & VMOE_NO_RENORM) != 0;
+    const bool dense = (p.flags & RG_DENSE) != 0;
     const int dp = wt_pitch(d);
     float *dlrow = rg_smem + warp * E;
-    float *WT = rg_smem + (norenorm ? RG_WARPS * E : 0);
+    float *WT = rg_smem + (dense ? RG_WARPS * E : 0);
     const long long TN = (long long)p.T * N;
     const long long beg = TN * blockIdx.x / gridDim.x;
     const long long end = TN * (blockIdx.x + 1) / gridDim.x;
@@ -432,23 +441,23 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
                 }
             }
             float c[KMAX];
-            const bool any = gate_backward<KMAX>(k, E, norenorm, lane, tn, dg, gt, ei, logits,
+            const bool any = gate_backward<KMAX>(k, E, p.flags, lane, tn, dg, gt, ei, logits,
                                                  dgate, dlogits, dlrow, c);
             if (dx != nullptr && any) {
-                const int ne = norenorm ? E : k;
+                const int ne = dense ? E : k;
 #pragma unroll
                 for (int ch = 0; ch < NCH; ++ch) {
                     const int v = lane * 8 + 256 * ch;
                     if (v >= d) continue;
                     float r[8], o[8];
-                    dx_terms<KMAX, WSMEM>(r, v, ne, norenorm, dlrow, ei, c, WT, dp, wrt, E);
+                    dx_terms<KMAX, WSMEM>(r, v, ne, dense, dlrow, ei, c, WT, dp, wrt, E);
                     bf16x8_to_f32(xo[ch], o);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) o[q] += r[q];
                     *reinterpret_cast<uint4 *>(dx + tn * d + v) = f32_to_bf16x8(o);
                 }
             }
-            if (norenorm) __syncwarp();
+            if (dense) __syncwarp();
 #pragma unroll
             for (int j = 0; j < KMAX; ++j) {
                 ei[j] = ei2[j];

@@ -3,7 +3,8 @@
 Plumbing only: torch allocates the caller-owned device buffers the C ABI writes
 into, and ``StepRunner`` issues the seven library calls of one step in order on
 one stream -- eight with the router backward (``router_grad=True``), which adds
-the gradient of the gating network.  No arithmetic of the method happens here.
+the gradient of the gating network, ten with the balance losses.  No arithmetic of
+the method happens here.
 """
 from __future__ import annotations
 
@@ -11,7 +12,8 @@ import copy
 
 import torch
 
-from . import (VMOE_BF16, _stream, vmoe_combine, vmoe_dispatch, vmoe_expert_bwd,
+from . import (VMOE_BF16, VMOE_DLOGITS_ADD, VmoeProblem, _stream, vmoe_balance, vmoe_balance_bwd,
+               vmoe_balance_workspace_size, vmoe_combine, vmoe_dispatch, vmoe_expert_bwd,
                vmoe_expert_bwd_workspace_size, vmoe_expert_fwd, vmoe_problem_capacity, vmoe_route,
                vmoe_router_bwd)
 
@@ -51,24 +53,61 @@ class Buffers:
                                      device=device)
 
 
+class BalanceBuffers:
+    """Outputs of the balance losses of problem ``p``, and the losses' weights.
+
+    ``weights``: three numbers (balance, importance, router z-loss), the same for every
+    task, or a [T, 3] fp32 device tensor: the gradient of the whole loss by each task's
+    three, which the caller may change between steps."""
+
+    def __init__(self, p, weights, device="cuda"):
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+        self.count = new(p.T, p.E, dtype=torch.int32)
+        self.tokens = new(p.T, dtype=torch.int32)
+        self.excess = new(p.T, p.E)
+        self.loss = new(p.T, 3)
+        self.workspace = new(vmoe_balance_workspace_size(p), dtype=torch.uint8)
+        if not isinstance(weights, torch.Tensor):
+            weights = torch.tensor([[float(w) for w in weights]], device=device).repeat(p.T, 1)
+        if tuple(weights.shape) != (p.T, 3) or weights.dtype != torch.float32:
+            raise ValueError("balance weights: three numbers, or [T, 3] in fp32")
+        self.dloss = weights.contiguous()
+
+
 class StepRunner:
     """Issues the library calls of one forward + backward step.
 
     ``inputs`` holds device tensors x, dy [T,N,d], w_router [T,d,E], bias [T,E]
     or None, w1 [T,E,d,f], w2 [T,E,f,d].  With ``router_grad`` the backward also
-    produces dW_r and dbias and adds the router's share to dX.
+    produces dW_r and dbias and adds the router's share to dX.  With ``balance``
+    (the losses' weights, see BalanceBuffers; needs ``router_grad``) the forward
+    computes the balance losses and counts into ``self.balance`` and the router's
+    gradient is that of <dY, y> plus the weighted losses; ``inputs`` may then hold
+    token_mask [T,N] uint8, 0 for padding that they leave out.
     """
 
-    def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False):
+    def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False, balance=None):
         self.p = p
         self.inp = inputs
         self.router_grad = router_grad
         self.b = bufs if bufs is not None else Buffers(p, inputs["x"].device)
+        self.balance = balance
+        if balance is not None:
+            if not router_grad:
+                raise ValueError("the balance losses act on the router: router_grad=True")
+            if not isinstance(balance, BalanceBuffers):
+                self.balance = BalanceBuffers(p, balance, inputs["x"].device)
+            self.p_add = VmoeProblem.from_buffer_copy(p)
+            self.p_add.flags |= VMOE_DLOGITS_ADD
 
     def forward(self, stream=None):
         p, i, b, stream = self.p, self.inp, self.b, _stream(stream)
         vmoe_route(p, i["x"], i["w_router"], i.get("bias"), b.logits, b.idx, b.gate, b.slot,
                    b.load, stream)
+        if self.balance is not None:
+            o = self.balance
+            vmoe_balance(p, b.logits, b.idx, i.get("token_mask"), o.count, o.tokens, o.excess, o.loss, o.workspace,
+                         stream=stream)
         vmoe_dispatch(p, i["x"], None, b.idx, b.slot, b.load, b.xe, stream)
         vmoe_expert_fwd(p, b.xe, i["w1"], i["w2"], b.load, b.h, b.a, b.ye, stream)
         vmoe_combine(p, b.ye, b.gate, b.idx, b.slot, b.y, stream)
@@ -84,6 +123,10 @@ class StepRunner:
 
     def router_backward(self, stream=None):
         p, i, b = self.p, self.inp, self.b
+        if self.balance is not None:
+            o, p = self.balance, self.p_add
+            vmoe_balance_bwd(p, b.logits, i.get("token_mask"), o.count, o.tokens, o.excess, o.dloss, b.dlogits,
+                             stream=stream)
         vmoe_router_bwd(p, i["x"], i["w_router"], b.logits, b.idx, b.gate, b.slot, i["dy"], b.ye,
                         b.dgate, b.dlogits, b.dw_router, b.dbias, b.dx, stream)
 
@@ -105,9 +148,11 @@ class HostPipeline:
     """
 
     def __init__(self, p, weights, bufs: Buffers | None = None, device="cuda",
-                 router_grad: bool = False):
+                 router_grad: bool = False, balance=None):
         self.p = p
         base = bufs if bufs is not None else Buffers(p, device)
+        if balance is not None and not isinstance(balance, BalanceBuffers):
+            balance = BalanceBuffers(p, balance, device)
         self.slots = []
         for _ in range(2):
             b = copy.copy(base)
@@ -116,7 +161,7 @@ class HostPipeline:
             inp = dict(weights)
             inp["x"] = torch.empty_like(base.y)
             inp["dy"] = torch.empty_like(base.y)
-            self.slots.append(StepRunner(p, inp, b, router_grad=router_grad))
+            self.slots.append(StepRunner(p, inp, b, router_grad=router_grad, balance=balance))
         self.copy_stream = torch.cuda.Stream(device)
         ev = lambda: [torch.cuda.Event() for _ in range(2)]  # noqa: E731
         self.h2d, self.fwd, self.done, self.d2h = ev(), ev(), ev(), ev()
