@@ -15,8 +15,11 @@
 // reduction; the dX update reads W_r[t] transposed from shared memory, staged
 // once per task segment of a persistent CTA.  With renormalised gates dlogit
 // has k non-zeros, so the update is k scaled columns of W_r, not an E-term
-// contraction.  With VMOE_DLOGITS_ADD it is added to the dense gradient of other
-// losses that dlogits holds, and the update is an E-term one.
+// contraction.
+//
+// With VMOE_DLOGITS_ADD, dlogit is added to the gradient of other losses that
+// dlogits holds, which is dense: kernel 1 then leaves dX alone and router_dx adds
+// W_r dlogit as a tiled product.
 //
 // Kernel 2 (router_dw), bf16 problems: dW_r = x^T dlogit on the tensor cores,
 // tcgen05 for E = 32 or 64 and d a multiple of 128 (router_dw_tc.cu), else the
@@ -90,9 +93,8 @@ constexpr int RG_THREADS = 512;
 constexpr int RG_WARPS = RG_THREADS / 32;
 constexpr int RG_UNROLL = 2;
 constexpr size_t RG_SMEM_CAP = 200 * 1024;
-constexpr unsigned RG_DENSE = VMOE_NO_RENORM | VMOE_DLOGITS_ADD;  // dlogit rows without zeros
 
-// Shared memory: per-warp dlogit rows (dense ones), then W_r[t]^T, one row
+// Shared memory: per-warp dlogit rows (VMOE_NO_RENORM), then W_r[t]^T, one row
 // per expert with pitch wt_pitch(d) floats.  Within each block of 256 columns the
 // columns are permuted so that the 8 columns 8L..8L+7 a lane reads sit at 4L..4L+3
 // and 128+4L..128+4L+3: the lanes of a warp then read two runs of consecutive
@@ -106,7 +108,7 @@ __device__ __forceinline__ int wt_col8(int v) {  // first half of columns v..v+7
     return (v & ~255) + ((v & 255) >> 1);
 }
 inline size_t rg_smem_rows(const Dims &p) {
-    return (p.flags & RG_DENSE) ? (size_t)RG_WARPS * p.E * sizeof(float) : 0;
+    return (p.flags & VMOE_NO_RENORM) ? (size_t)RG_WARPS * p.E * sizeof(float) : 0;
 }
 inline size_t rg_smem_w(const Dims &p) { return (size_t)p.E * wt_pitch(p.d) * sizeof(float); }
 
@@ -153,10 +155,11 @@ __device__ __noinline__ void stage_wt(const float *__restrict__ wrt, float *WT, 
 //
 // gate_backward: reduces the lane partials of dgate_j (fixed butterfly), writes
 // dgate and the dlogit row, and returns in c[j] the dlogit of expert e_j
-// (renormalised gates; a dense row is left in dlrow instead).  Returns
-// whether the dX update has any non-zero term.
+// (renormalised gates; VMOE_NO_RENORM leaves the dense row in dlrow).  Returns
+// whether the dX update has any non-zero term.  `add`: the row is added to what
+// dlogits holds (and dX is not updated by the caller).
 template <int KMAX>
-__device__ __forceinline__ bool gate_backward(int k, int E, unsigned flags, int lane, long long tn,
+__device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, bool add, int lane, long long tn,
                                               float (&dg)[KMAX], const float (&gt)[KMAX],
                                               const int (&ei)[KMAX], const float *logits,
                                               float *dgate, float *dlogits, float *dlrow,
@@ -183,21 +186,16 @@ __device__ __forceinline__ bool gate_backward(int k, int E, unsigned flags, int 
         c[j] = j < k ? gt[j] * (dg[j] - s) : 0.0f;
         any |= c[j] != 0.0f;
     }
-    if (!(flags & VMOE_NO_RENORM)) {
-        const bool add = (flags & VMOE_DLOGITS_ADD) != 0;
+    if (!norenorm) {
         for (int e = lane; e < E; e += 32) {
             float v = 0.0f;
 #pragma unroll
             for (int j = 0; j < KMAX; ++j)
                 if (j < k && ei[j] == e) v = c[j];
-            if (add) {
-                v += dl[e];
-                dlrow[e] = v;
-            }
+            if (add) v += dl[e];
             dl[e] = v;
         }
-        if (add) __syncwarp();
-        return any || add;
+        return any;
     }
     const float *l = logits + tn * E;
     float mx = -INFINITY;
@@ -214,7 +212,7 @@ __device__ __forceinline__ bool gate_backward(int k, int E, unsigned flags, int 
         for (int j = 0; j < KMAX; ++j)
             if (j < k && ei[j] == e) g = dg[j];
         float v = expf(__ldg(l + e) - mx) / sum * (g - s);
-        if (flags & VMOE_DLOGITS_ADD) v += dl[e];
+        if (add) v += dl[e];
         dl[e] = v;
         dlrow[e] = v;
     }
@@ -223,9 +221,9 @@ __device__ __forceinline__ bool gate_backward(int k, int E, unsigned flags, int 
 }
 
 // dx_terms: r[0..7] = sum over the dX terms of dlogit_e * W_r[v + q][e] for the
-// 8 columns v..v+7: the k chosen experts (renormalised gates) or all E (dense).
+// 8 columns v..v+7: the k chosen experts (renormalised gates) or all E.
 template <int KMAX, bool WSMEM>
-__device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool dense,
+__device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool norenorm,
                                          const float *dlrow, const int (&ei)[KMAX],
                                          const float (&c)[KMAX], const float *WT, int dp,
                                          const float *wrt, int E) {
@@ -234,7 +232,7 @@ __device__ __forceinline__ void dx_terms(float (&r)[8], int v, int ne, bool dens
     for (int jj = 0; jj < ne; ++jj) {
         int e = jj;
         float cj = 0.0f;
-        if (dense) {
+        if (norenorm) {
             cj = dlrow[jj];
         } else {
 #pragma unroll
@@ -273,10 +271,10 @@ router_grad_kernel(Dims p, const T *__restrict__ dy, const T *__restrict__ ye,
     extern __shared__ __align__(16) float rg_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int d = p.d, E = p.E, k = p.k, N = p.N;
-    const bool dense = (p.flags & RG_DENSE) != 0;
+    const bool norenorm = (p.flags & VMOE_NO_RENORM) != 0, add = (p.flags & VMOE_DLOGITS_ADD) != 0;
     const int dp = wt_pitch(d);
     float *dlrow = rg_smem + warp * E;
-    float *WT = rg_smem + (dense ? RG_WARPS * E : 0);
+    float *WT = rg_smem + (norenorm ? RG_WARPS * E : 0);
     const long long TN = (long long)p.T * N;
     const long long beg = TN * blockIdx.x / gridDim.x;
     const long long end = TN * (blockIdx.x + 1) / gridDim.x;
@@ -319,22 +317,22 @@ router_grad_kernel(Dims p, const T *__restrict__ dy, const T *__restrict__ ye,
                 }
             }
             float c[KMAX];
-            const bool any = gate_backward<KMAX>(k, E, p.flags, lane, tn, dg, gt, ei, logits,
+            const bool any = gate_backward<KMAX>(k, E, norenorm, add, lane, tn, dg, gt, ei, logits,
                                                  dgate, dlogits, dlrow, c);
             // dX += W_r dlogit, summed in fp32 and added to dX with one rounding
             if (dx != nullptr && any) {
                 T *xr = dx + tn * d;
-                const int ne = dense ? E : k;
+                const int ne = norenorm ? E : k;
                 for (int v = lane * 8; v < d; v += 256) {
                     float r[8], o[8];
-                    dx_terms<KMAX, WSMEM>(r, v, ne, dense, dlrow, ei, c, WT, dp, wrt, E);
+                    dx_terms<KMAX, WSMEM>(r, v, ne, norenorm, dlrow, ei, c, WT, dp, wrt, E);
                     load8_rw<T>(xr + v, o);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) o[q] += r[q];
                     store8<T>(xr + v, o);
                 }
             }
-            if (dense) __syncwarp();  // dlrow is rewritten by the next token
+            if (norenorm) __syncwarp();  // dlrow is rewritten by the next token
         }
         seg = seg_end;
     }
@@ -355,10 +353,10 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
     extern __shared__ __align__(16) float rg_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int d = p.d, E = p.E, k = p.k, N = p.N;
-    const bool dense = (p.flags & RG_DENSE) != 0;
+    const bool norenorm = (p.flags & VMOE_NO_RENORM) != 0, add = (p.flags & VMOE_DLOGITS_ADD) != 0;
     const int dp = wt_pitch(d);
     float *dlrow = rg_smem + warp * E;
-    float *WT = rg_smem + (dense ? RG_WARPS * E : 0);
+    float *WT = rg_smem + (norenorm ? RG_WARPS * E : 0);
     const long long TN = (long long)p.T * N;
     const long long beg = TN * blockIdx.x / gridDim.x;
     const long long end = TN * (blockIdx.x + 1) / gridDim.x;
@@ -441,23 +439,23 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
                 }
             }
             float c[KMAX];
-            const bool any = gate_backward<KMAX>(k, E, p.flags, lane, tn, dg, gt, ei, logits,
+            const bool any = gate_backward<KMAX>(k, E, norenorm, add, lane, tn, dg, gt, ei, logits,
                                                  dgate, dlogits, dlrow, c);
             if (dx != nullptr && any) {
-                const int ne = dense ? E : k;
+                const int ne = norenorm ? E : k;
 #pragma unroll
                 for (int ch = 0; ch < NCH; ++ch) {
                     const int v = lane * 8 + 256 * ch;
                     if (v >= d) continue;
                     float r[8], o[8];
-                    dx_terms<KMAX, WSMEM>(r, v, ne, dense, dlrow, ei, c, WT, dp, wrt, E);
+                    dx_terms<KMAX, WSMEM>(r, v, ne, norenorm, dlrow, ei, c, WT, dp, wrt, E);
                     bf16x8_to_f32(xo[ch], o);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) o[q] += r[q];
                     *reinterpret_cast<uint4 *>(dx + tn * d + v) = f32_to_bf16x8(o);
                 }
             }
-            if (dense) __syncwarp();
+            if (norenorm) __syncwarp();
 #pragma unroll
             for (int j = 0; j < KMAX; ++j) {
                 ei[j] = ei2[j];
@@ -467,6 +465,185 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
         }
         seg = seg_end;
     }
+}
+
+// ---------------------------------------------------------------------------
+// Kernel 1b (VMOE_DLOGITS_ADD), bf16 problems: dX += dlogit W_r^T for dense rows, on
+// mma.sync tensor cores: K = E is short, and what bounds it is dX, read and written once.
+// Both fp32 factors are taken as two bf16 parts each, hi hi + hi lo + lo hi: 2^-16 of the
+// products, against dX's own rounding of 2^-8.  A CTA holds 64 columns of W_r^T in shared
+// memory in the order of the fragments, one 16-byte read for a lane's k16 x n8 parts, and
+// its warps walk tiles of 16 tokens, whose dlogit rows come straight from global memory.
+// The columns are dealt so that a lane's results are 16 neighbouring ones of a row.
+// All of vmoe_router_bwd at 17 x 1576 tokens, 768 channels and 32 experts: 83 us, 134 us
+// with kernel 1's dense update; 8 x 1576, 1024, 64: 64 us against 2.7 ms.
+constexpr int RX_COLS = 64, RX_TOKENS = 512, RX_THREADS = 256;
+
+__device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
+    hi = pack_bf16x2(a, b);
+    const float2 h = unpk2(bf16x2_to_f32x2(hi));
+    lo = pack_bf16x2(a - h.x, b - h.y);
+}
+// Elements k and k + 1 of a row of E values, 0 behind its end.
+template <bool EVEN>
+__device__ __forceinline__ float2 two_of(const float *row, int k, int E) {
+    if (EVEN) return k < E ? __ldg(reinterpret_cast<const float2 *>(row + k)) : make_float2(0.0f, 0.0f);
+    return make_float2(k < E ? __ldg(row + k) : 0.0f, k + 1 < E ? __ldg(row + k + 1) : 0.0f);
+}
+
+template <bool EVEN>
+__global__ void __launch_bounds__(RX_THREADS)
+router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, __nv_bfloat16 *dx) {
+    extern __shared__ __align__(16) uint4 rx_w[];  // [k16 steps][8 column tiles][32 lanes]: hi k, hi k + 8, lo, lo
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int t = blockIdx.z, d = p.d, E = p.E, N = p.N, d0 = blockIdx.x * RX_COLS, steps = (E + 15) / 16;
+    pdl_wait();
+    // column c of tile j, c = 2 q + b as a lane's result has it, is column 16 q + 2 j + b
+    for (int i = warp; i < steps * 8; i += RX_THREADS / 32) {
+        const int c = d0 + 16 * (g >> 1) + 2 * (i & 7) + (g & 1), k = 16 * (i >> 3) + 2 * q;
+        float2 w0 = make_float2(0.0f, 0.0f), w1 = w0;
+        if (c < d) {
+            const float *row = wr + ((long long)t * d + c) * E;
+            w0 = two_of<EVEN>(row, k, E);
+            w1 = two_of<EVEN>(row, k + 8, E);
+        }
+        uint4 v;
+        split2(w0.x, w0.y, v.x, v.z);
+        split2(w1.x, w1.y, v.y, v.w);
+        rx_w[i * 32 + lane] = v;
+    }
+    __syncthreads();
+    const int c0 = d0 + 16 * q, stop = min(N, (int)(blockIdx.y + 1) * RX_TOKENS);
+    for (int n0 = blockIdx.y * RX_TOKENS + warp * 16; n0 < stop; n0 += RX_THREADS / 2) {
+        const int na = n0 + g, nb = n0 + g + 8;
+        const long long ra = (long long)t * N + min(na, N - 1), rb = (long long)t * N + min(nb, N - 1);
+        __nv_bfloat16 *pa = dx + ra * d + c0, *pb = dx + rb * d + c0;
+        uint4 xa[2], xb[2];  // d and c0 are multiples of 8: a half's columns all are, or none
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            xa[h] = xb[h] = make_uint4(0, 0, 0, 0);
+            if (c0 + 8 * h < d) {
+                if (na < N) xa[h] = *reinterpret_cast<const uint4 *>(pa + 8 * h);
+                if (nb < N) xb[h] = *reinterpret_cast<const uint4 *>(pb + 8 * h);
+            }
+        }
+        float acc[8][4] = {};
+        for (int ks = 0; ks < steps; ++ks) {
+            const int k = 16 * ks + 2 * q;
+            uint32_t ah[4], al[4];
+            const float2 a0 = two_of<EVEN>(dl + ra * E, k, E), a1 = two_of<EVEN>(dl + rb * E, k, E);
+            const float2 a2 = two_of<EVEN>(dl + ra * E, k + 8, E), a3 = two_of<EVEN>(dl + rb * E, k + 8, E);
+            split2(a0.x, a0.y, ah[0], al[0]);
+            split2(a1.x, a1.y, ah[1], al[1]);
+            split2(a2.x, a2.y, ah[2], al[2]);
+            split2(a3.x, a3.y, ah[3], al[3]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint4 w = rx_w[(ks * 8 + j) * 32 + lane];
+                mma_bf16_16816(acc[j], ah[0], ah[1], ah[2], ah[3], w.x, w.y);
+                mma_bf16_16816(acc[j], ah[0], ah[1], ah[2], ah[3], w.z, w.w);
+                mma_bf16_16816(acc[j], al[0], al[1], al[2], al[3], w.x, w.y);
+            }
+        }
+        // results 0, 1 of tile j: columns c0 + 2 j, + 1 of row g; 2, 3 of row g + 8
+        auto add = [](uint32_t x, float lo, float hi) {
+            const float2 f = unpk2(bf16x2_to_f32x2(x));
+            return pack_bf16x2(f.x + lo, f.y + hi);
+        };
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (c0 + 8 * h >= d) continue;
+            const float(*s)[4] = acc + 4 * h;
+            if (na < N)
+                *reinterpret_cast<uint4 *>(pa + 8 * h) = make_uint4(add(xa[h].x, s[0][0], s[0][1]), add(xa[h].y, s[1][0], s[1][1]),
+                                                                    add(xa[h].z, s[2][0], s[2][1]), add(xa[h].w, s[3][0], s[3][1]));
+            if (nb < N)
+                *reinterpret_cast<uint4 *>(pb + 8 * h) = make_uint4(add(xb[h].x, s[0][2], s[0][3]), add(xb[h].y, s[1][2], s[1][3]),
+                                                                    add(xb[h].z, s[2][2], s[2][3]), add(xb[h].w, s[3][2], s[3][3]));
+        }
+    }
+}
+
+// Kernel 1b, fp32 problems: the same on CUDA cores, 64 tokens x 128 columns a CTA, the
+// experts in chunks of 32 staged transposed; 4 tokens x 8 columns a thread.
+constexpr int RXF_N = 64, RXF_D = 128, RXF_E = 32;
+
+__global__ void __launch_bounds__(RX_THREADS)
+router_dx_simt_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, float *dx) {
+    __shared__ __align__(16) float ds[RXF_E][RXF_N + 4];
+    __shared__ __align__(16) float ws[RXF_E][RXF_D + 4];
+    const int tid = threadIdx.x, tn = tid / 16, td = tid % 16;
+    const int t = blockIdx.z, n0 = blockIdx.y * RXF_N, d0 = blockIdx.x * RXF_D, d = p.d, E = p.E, N = p.N;
+    // a warp copies 4 rows x 8 experts at a time: 32 banks, and whole sectors
+    const int e8 = tid & 7, r4 = (tid & 31) >> 3, warp = tid >> 5;
+    pdl_wait();
+    const float *dlt = dl + ((long long)t * N + n0) * E;
+    const float *wt = wr + ((long long)t * d + d0) * E;
+    f32x2 acc[4][4] = {};
+    for (int e0 = 0; e0 < E; e0 += RXF_E) {
+        if (e0) __syncthreads();
+#pragma unroll 4
+        for (int i = warp; i < RXF_N; i += 8) {  // (row group, expert group)
+            const int r = (i >> 2) * 4 + r4, e = (i & 3) * 8 + e8;
+            ds[e][r] = e0 + e < E && n0 + r < N ? dlt[(long long)r * E + e0 + e] : 0.0f;
+        }
+#pragma unroll 4
+        for (int i = warp; i < RXF_D; i += 8) {
+            const int r = (i >> 2) * 4 + r4, e = (i & 3) * 8 + e8;
+            ws[e][r] = e0 + e < E && d0 + r < d ? __ldg(wt + (long long)r * E + e0 + e) : 0.0f;
+        }
+        __syncthreads();
+        const int last = min(RXF_E, E - e0);
+#pragma unroll 4
+        for (int q = 0; q < last; ++q) {
+            const float4 a = *reinterpret_cast<const float4 *>(&ds[q][4 * tn]);
+            const ulonglong2 b0 = *reinterpret_cast<const ulonglong2 *>(&ws[q][4 * td]);
+            const ulonglong2 b1 = *reinterpret_cast<const ulonglong2 *>(&ws[q][64 + 4 * td]);
+            const f32x2 av[4] = {pk2(a.x), pk2(a.y), pk2(a.z), pk2(a.w)};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                acc[r][0] = fma2(av[r], b0.x, acc[r][0]);
+                acc[r][1] = fma2(av[r], b0.y, acc[r][1]);
+                acc[r][2] = fma2(av[r], b1.x, acc[r][2]);
+                acc[r][3] = fma2(av[r], b1.y, acc[r][3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int n = n0 + 4 * tn + r;
+        if (n >= N) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = d0 + 64 * h + 4 * td;
+            if (c >= d) continue;  // d is a multiple of 8, c of 4: all four or none
+            float4 *o = reinterpret_cast<float4 *>(dx + ((long long)t * N + n) * d + c);
+            const float2 lo = unpk2(acc[r][2 * h]), hi = unpk2(acc[r][2 * h + 1]);
+            const float4 v = *o;
+            *o = make_float4(v.x + lo.x, v.y + lo.y, v.z + hi.x, v.w + hi.y);
+        }
+    }
+}
+
+int launch_router_dx(const Dims &p, const float *dl, const float *wr, void *dx, cudaStream_t s) {
+    trace_before(s, "router_dx");
+    int st;
+    if (p.bf16) {
+        const size_t smem = (size_t)((p.E + 15) / 16) * 8 * 32 * sizeof(uint4);  // 64 KB for 256 experts
+        const dim3 grid((p.d + RX_COLS - 1) / RX_COLS, (p.N + RX_TOKENS - 1) / RX_TOKENS, p.T);
+        auto go = [&](auto kern, std::atomic<int>(&limit)[64]) {
+            if (smem > 48 * 1024)
+                if (const int e = raise_smem_limit((const void *)kern, limit, (int)smem)) return e;
+            return launch_kernel(kern, grid, dim3(RX_THREADS), smem, s, p, dl, wr, (__nv_bfloat16 *)dx);
+        };
+        static std::atomic<int> even[64], odd[64];
+        st = p.E % 2 == 0 ? go(router_dx_mma_kernel<true>, even) : go(router_dx_mma_kernel<false>, odd);
+    } else {
+        const dim3 grid((p.d + RXF_D - 1) / RXF_D, (p.N + RXF_N - 1) / RXF_N, p.T);
+        st = launch_kernel(router_dx_simt_kernel, grid, dim3(RX_THREADS), 0, s, p, dl, wr, (float *)dx);
+    }
+    trace_after(s);
+    return st;
 }
 
 // ---------------------------------------------------------------------------
@@ -955,6 +1132,11 @@ int run(const Dims &p, const void *x, const float *wr, const float *logits, cons
         const float *gate, const int32_t *slot, const void *dy, const void *ye, float *dgate,
         float *dlogits, float *dw, float *dbias, void *dx, cudaStream_t s) {
     const T *dyt = (const T *)dy, *yet = (const T *)ye;
+    void *dense_dx = nullptr;
+    if (p.flags & VMOE_DLOGITS_ADD) {
+        dense_dx = dx;
+        dx = nullptr;
+    }
     T *dxt = (T *)dx;
     int st;
     trace_before(s, "router_grad");
@@ -975,6 +1157,7 @@ int run(const Dims &p, const void *x, const float *wr, const float *logits, cons
         st = launch_grad_k<T, 8>(p, wr, logits, idx, gate, slot, dyt, yet, dgate, dlogits, dxt, s);
     trace_after(s);
     if (st != VMOE_OK) return st;
+    if (dense_dx && (st = launch_router_dx(p, dlogits, wr, dense_dx, s)) != VMOE_OK) return st;
     trace_before(s, "router_dw");
     if (p.bf16 && (st = launch_router_dw_tc(p, (const __nv_bfloat16 *)x, dlogits, dw, dbias, s)) !=
                       VMOE_ERR_UNSUPPORTED) {
