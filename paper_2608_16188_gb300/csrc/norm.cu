@@ -171,19 +171,19 @@ __device__ __forceinline__ void stats(const Raw8<T> (&raw)[R], bool have, const 
         for (int r = 0; r < R; ++r) {
             f32x2 v[4];
             raw[r].get(v);
-            m[r] = sum2(add2(add2(v[0], v[1]), add2(v[2], v[3])));
+            m[r] = have ? sum2(add2(add2(v[0], v[1]), add2(v[2], v[3]))) : 0.0f;
         }
         totals(m);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        f32x2 v[4], sq = 0;
+        f32x2 v[4], sq;
         raw[r].get(v);
         m[r] *= share;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[i] = add2(v[i], pk2(-m[r]));
-            sq = fma2(v[i], v[i], sq);
+            sq = i ? fma2(v[i], v[i], sq) : mul2(v[i], v[i]);
         }
         q[r] = have ? sum2(sq) : 0.0f;
     }
@@ -216,6 +216,8 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
     Totals<WC, R> totals = {buf, group * W, 0, W};
     pdl_wait();
     const long long par = (long long)t * d + c, base = (long long)t * N;
+    const T *x0 = (const T *)a.x + base * d, *y0 = (const T *)a.y + (a.y ? base * d : 0);
+    T *z0 = (T *)a.z + (a.z ? base * d : 0), *u0 = (T *)a.u + (a.u ? base * d : 0);
     f32x2 post_w[4], post_b[4], pre_w[4], pre_b[4];
     {
         f32x2 gate[4];
@@ -225,23 +227,24 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
         param8(have ? a.pre_w : nullptr, par, 1.0f, pre_w);
         param8(have ? a.pre_b : nullptr, par, 0.0f, pre_b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // behind the last column z stays 0, for the sums
-            post_w[i] = have ? mul2(post_w[i], gate[i]) : 0;
+        for (int i = 0; i < 4; ++i) {
+            post_w[i] = mul2(post_w[i], gate[i]);
             post_b[i] = mul2(post_b[i], gate[i]);
         }
     }
+    // Behind the last row and the last column others are read in their place, and what
+    // comes of them is left out of the sums and not stored: predicated loads would cost
+    // as many instructions again to zero their targets.  Offsets within a task fit 31 bits.
+    const int cc = have ? c : 0;
     Raw8<T> nx[R], ny[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) ny[r].zero();
     auto fetch = [&](int n0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int n = n0 + group * R + r;
-            const long long at = (base + n) * d + c;
-            nx[r].zero();
-            ny[r].zero();
-            if (have && n < end) {
-                nx[r].load((const T *)a.x + at);
-                if (a.y) ny[r].load((const T *)a.y + at);
-            }
+            const int at = min(n0 + group * R + r, end - 1) * d + cc;
+            nx[r].load(x0 + at);
+            if (a.y) ny[r].load(y0 + at);
         }
     };
     if (AHEAD) fetch(beg);
@@ -255,8 +258,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
         }
         if (AHEAD && n0 + groups * R < end) fetch(n0 + groups * R);
         float2 s[R];
-        const int n = n0 + group * R, rows = have ? end - n : 0;
-        const long long at = (base + n) * d + c;
+        const int n = n0 + group * R, rows = have ? end - n : 0, at = n * d + c;
         if (a.y) {
 #pragma unroll
             for (int r = 0; r < R; ++r) s[r] = make_float2(0.0f, 1.0f);
@@ -273,7 +275,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
                 for (int i = 0; i < 4; ++i)
                     o[i] = fma2(mul2(add2(v[i], pk2(-s[r].x)), pk2(s[r].y)), post_w[i], fma2(pk2(a.rho), o[i], post_b[i]));
                 x[r].set(o);
-                if (r < rows) x[r].store((T *)a.z + at + (long long)r * d);
+                if (r < rows) x[r].store(z0 + at + r * d);
             }
         }
         if (!a.u) continue;
@@ -286,7 +288,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = fma2(mul2(add2(v[i], pk2(-s[r].x)), pk2(s[r].y)), pre_w[i], pre_b[i]);
             x[r].set(v);
-            if (r < rows) x[r].store((T *)a.u + at + (long long)r * d);
+            if (r < rows) x[r].store(u0 + at + r * d);
         }
     }
 }
@@ -341,24 +343,6 @@ template <typename T>
 struct BwdRow {
     Raw8<T> y, z, dz, du;
     float2 py, pz;  // mean, rstd
-    __device__ __forceinline__ void load(const BwdArgs &a, long long row, long long at, bool in) {
-        y.zero();
-        z.zero();
-        dz.zero();
-        du.zero();
-        py = pz = make_float2(0.0f, in ? 1.0f : 0.0f);
-        if (!in) return;
-        if (a.du) {
-            du.load((const T *)a.du + at);
-            z.load((const T *)a.z + at);
-            pz = a.pre_stat[row];
-        }
-        if (a.dz) dz.load((const T *)a.dz + at);
-        if (a.y) {
-            y.load((const T *)a.y + at);
-            if (a.post) py = a.post_stat[row];
-        }
-    }
 };
 
 template <typename T, int WC, int MAXT, int MINB, int R, bool AHEAD>
@@ -382,7 +366,10 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
         param8(have ? a.gate : nullptr, par, 1.0f, g);
         param8(have ? a.post_w : nullptr, par, 1.0f, aw);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) aw[i] = have ? mul2(aw[i], g[i]) : 0;
+        for (int i = 0; i < 4; ++i) {  // behind the last column 0, for the sums
+            aw[i] = have ? mul2(aw[i], g[i]) : 0;
+            pw[i] = have ? pw[i] : 0;
+        }
         sum_aw = warp_sum(sum2(add2(add2(aw[0], aw[1]), add2(aw[2], aw[3]))));
         if (WC != 1) {
             if (lane == 0) totals[0][warp][0] = sum_aw;
@@ -393,13 +380,36 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
         }
     }
     f32x2 A[4] = {}, B[4] = {}, Pw[4] = {}, Pb[4] = {};
-    BwdRow<T> next[R];
+    // as in the forward, others are read in the place of what lies behind the end
+    const int cc = have ? c : 0;
     const long long base = (long long)t * N;
+    auto task = [&](const void *p) { return (const T *)p + (p ? base * d : 0); };
+    const T *y0 = task(a.y), *z0 = task(a.z), *dz0 = task(a.dz), *du0 = task(a.du);
+    T *dx0 = (T *)task(a.dx), *dy0 = (T *)task(a.dy);
+    const float2 *py0 = a.post_stat + (a.post_stat ? base : 0), *pz0 = a.pre_stat + (a.pre_stat ? base : 0);
+    BwdRow<T> next[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        next[r].y.zero();
+        next[r].z.zero();
+        next[r].dz.zero();
+        next[r].du.zero();
+        next[r].py = next[r].pz = make_float2(0.0f, 1.0f);
+    }
     auto fetch = [&](int n0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int n = n0 + group * R + r;
-            next[r].load(a, base + n, (base + n) * d + c, have && n < end);
+            const int n = min(n0 + group * R + r, end - 1), at = n * d + cc;
+            if (a.du) {
+                next[r].du.load(du0 + at);
+                next[r].z.load(z0 + at);
+                next[r].pz = pz0[n];
+            }
+            if (a.dz) next[r].dz.load(dz0 + at);
+            if (a.y) {
+                next[r].y.load(y0 + at);
+                if (a.post) next[r].py = py0[n];
+            }
         }
     };
     if (AHEAD) fetch(beg);
@@ -407,15 +417,16 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     for (int n0 = beg; n0 < end; n0 += groups * R, flip ^= 1) {
         if (!AHEAD) fetch(n0);
         f32x2 e[R][4], zh[R][4], yh[R][4];
-        float rz[R], ry[R], v[16];
+        float rz[R], ry[R], in[R], v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = 0.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            rz[r] = next[r].pz.y;
-            ry[r] = next[r].py.y;
+            in[r] = n0 + group * R + r < end ? 1.0f : 0.0f;
+            rz[r] = next[r].pz.y * in[r];
+            ry[r] = next[r].py.y * in[r];
             const f32x2 mz = pk2(-next[r].pz.x), my = pk2(-next[r].py.x);
-            f32x2 du[4], s[7] = {};
+            f32x2 du[4], s[7];
             next[r].dz.get(e[r]);
             next[r].du.get(du);
             next[r].z.get(zh[r]);
@@ -425,17 +436,17 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
                 zh[r][i] = mul2(add2(zh[r][i], mz), pk2(rz[r]));
                 yh[r][i] = mul2(add2(yh[r][i], my), pk2(ry[r]));
                 Pw[i] = fma2(du[i], zh[r][i], Pw[i]);
-                Pb[i] = add2(Pb[i], du[i]);
+                Pb[i] = fma2(du[i], pk2(in[r]), Pb[i]);
                 const f32x2 g = mul2(du[i], pw[i]);
                 e[r][i] = fma2(pk2(rz[r]), g, e[r][i]);
                 const f32x2 ea = mul2(e[r][i], aw[i]), za = mul2(zh[r][i], aw[i]);
-                s[0] = add2(s[0], g);
-                s[1] = fma2(g, zh[r][i], s[1]);
-                s[2] = add2(s[2], ea);
-                s[3] = fma2(ea, yh[r][i], s[3]);
-                s[4] = add2(s[4], za);
-                s[5] = fma2(aw[i], yh[r][i], s[5]);
-                s[6] = fma2(za, yh[r][i], s[6]);
+                s[0] = i ? add2(s[0], g) : g;
+                s[1] = i ? fma2(g, zh[r][i], s[1]) : mul2(g, zh[r][i]);
+                s[2] = i ? add2(s[2], ea) : ea;
+                s[3] = i ? fma2(ea, yh[r][i], s[3]) : mul2(ea, yh[r][i]);
+                s[4] = i ? add2(s[4], za) : za;
+                s[5] = i ? fma2(aw[i], yh[r][i], s[5]) : mul2(aw[i], yh[r][i]);
+                s[6] = i ? fma2(za, yh[r][i], s[6]) : mul2(za, yh[r][i]);
             }
 #pragma unroll
             for (int i = 0; i < 7; ++i) v[8 * r + i] = sum2(s[i]);
@@ -463,18 +474,18 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             for (int i = 0; i < 4; ++i) {
                 e[r][i] = fma2(pk2(-m2), zh[r][i], add2(e[r][i], pk2(-m1)));
                 A[i] = fma2(e[r][i], yh[r][i], A[i]);
-                B[i] = add2(B[i], e[r][i]);
+                B[i] = fma2(e[r][i], pk2(in[r]), B[i]);
                 q[i] = mul2(pk2(ry[r]), fma2(pk2(-k2), yh[r][i], fma2(e[r][i], aw[i], pk2(-k1))));
                 if (a.y) e[r][i] = mul2(e[r][i], pk2(a.rho));
             }
             if (have && n < end) {
-                const long long at = (base + n) * d + c;
+                const int at = n * d + c;
                 Raw8<T> o;
                 o.set(e[r]);
-                o.store((T *)a.dx + at);
+                o.store(dx0 + at);
                 if (a.y) {
                     o.set(q);
-                    o.store((T *)a.dy + at);
+                    o.store(dy0 + at);
                 }
             }
         }
