@@ -54,6 +54,7 @@ enum { P32 = 1, G32 = 2, S8 = 4, MST = 8 };
 template <int MAX>
 struct Table {
     int n;
+    bool runs;  // CTAs take runs of pairs
     uint32_t pairs;
     uint32_t first[MAX];
     Entry e[MAX];
@@ -451,14 +452,15 @@ __device__ __forceinline__ void update_last(const Entry &e, const Rates &r, cons
         update<P, G, EIGHT, MASTER, false>(e, r, k, b);
 }
 
-// A warp's way through the launch: pairs w, w + warps, ... of all tensors.  The tensor
-// is found by bisection once and followed from there.
+// A warp's way through the launch: every step-th pair up to an end.  The tensor is found
+// by bisection once and followed from there.
 template <int MAX>
 struct Walk {
     const Table<MAX> &tab;
-    uint32_t b, warps;
+    uint32_t b, step, end;
     int at;
-    __device__ __forceinline__ Walk(const Table<MAX> &t, uint32_t first, uint32_t step) : tab(t), b(first), warps(step), at(0) {
+    __device__ __forceinline__ Walk(const Table<MAX> &t, uint32_t first, uint32_t by, uint32_t stop)
+        : tab(t), b(first), step(by), end(stop), at(0) {
         int hi = t.n;
         while (hi - at > 1) {
             const int mid = (at + hi) >> 1;
@@ -468,9 +470,9 @@ struct Walk {
                 hi = mid;
         }
     }
-    __device__ __forceinline__ bool more() const { return b < tab.pairs; }
+    __device__ __forceinline__ bool more() const { return b < end; }
     __device__ __forceinline__ void next() {
-        b += warps;
+        b += step;
         while (at + 1 < tab.n && tab.first[at + 1] <= b) ++at;
     }
     __device__ __forceinline__ const Entry &entry() const { return tab.e[at]; }
@@ -575,7 +577,14 @@ adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
     c.root_scale = 1.0f / sqrtf(-expm1f((float)t * k.log_b2));
     c.key = k.seed_key + (uint32_t)t * 0x339cd49bu;
     typedef __nv_bfloat16 H;
-    for (Walk<MAX> w(tab, blockIdx.x * (AT / 32) + (threadIdx.x >> 5), gridDim.x * (AT / 32)); w.more();) {
+    const uint32_t warp = threadIdx.x >> 5;
+    uint32_t first = blockIdx.x * (AT / 32) + warp, step = gridDim.x * (AT / 32), end = tab.pairs;
+    if (tab.runs) {
+        first = (uint32_t)((uint64_t)tab.pairs * blockIdx.x / gridDim.x) + warp;
+        end = (uint32_t)((uint64_t)tab.pairs * (blockIdx.x + 1) / gridDim.x);
+        step = AT / 32;
+    }
+    for (Walk<MAX> w(tab, first, step, end); w.more();) {
         const int kind = w.entry().kind;
         switch (kind) {
             case P32 | G32: run_f32<float, float, false>(w, c, k); break;
@@ -601,9 +610,11 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pai
     tab.n = 0;
     tab.pairs = pairs;
     uint32_t at = 0;
+    bool eight = false;
     for (int i = 0; i < n; ++i) {
         const vmoe_adamw_tensor &x = tensors[i];
         if (x.numel == 0) continue;
+        eight |= x.state == VMOE_STATE_E4M3;
         Entry &e = tab.e[tab.n];
         tab.first[tab.n++] = at;
         at += (uint32_t)((x.numel + 511) / 512);
@@ -622,8 +633,13 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pai
         e.kind = (x.param_dtype == VMOE_F32 ? P32 : 0) | (x.grad_dtype == VMOE_F32 ? G32 : 0) |
                  (x.state == VMOE_STATE_E4M3 ? S8 : 0) | (x.master ? MST : 0);
     }
-    const long long ctas = ((long long)pairs + AT / 32 - 1) / (AT / 32);
-    return launch_kernel(adamw_kernel<MAX>, dim3((unsigned)std::min<long long>(ctas, (long long)AB * num_sms())), dim3(AT), 0, s, tab, k);
+    const long long ctas = std::min(((long long)pairs + AT / 32 - 1) / (AT / 32), (long long)AB * num_sms());
+    // Warps dealt over all pairs in turn stay in one part of every array; of short tensors
+    // each pair is another one's, and a CTA takes a run of pairs instead.  Tensors of 20000
+    // elements, fp32 moments: 30 us in runs, 36 dealt (300 of them); of 147000, with a
+    // master copy: 129 and 123 (192); 8-bit moments: 64 and 69; of 885000: 62 both.
+    tab.runs = pairs < (uint64_t)tab.n * (eight ? 1024 : 128);
+    return launch_kernel(adamw_kernel<MAX>, dim3((unsigned)ctas), dim3(AT), 0, s, tab, k);
 }
 
 }  // namespace
