@@ -346,8 +346,9 @@ def _workspace(where, t, nbytes):
     if t is None or isinstance(t, int):
         return t, int(nbytes or 0)
     have = t.numel() * t.element_size()
-    if not t.is_cuda or not t.is_contiguous() or (nbytes is not None and nbytes > have):
-        raise VmoeError(VMOE_ERR_INVALID, where)
+    at = t.get_device()
+    if at < 0 or at != _device() or not t.is_contiguous() or (nbytes is not None and nbytes > have):
+        raise VmoeError(VMOE_ERR_INVALID, "%s: the workspace" % where)
     return t.data_ptr(), have if nbytes is None else int(nbytes)
 
 

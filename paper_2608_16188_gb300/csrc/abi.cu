@@ -7,7 +7,7 @@
 
 #include <vector>
 
-#include "common.cuh"
+#include "around.cuh"
 
 namespace vmoe {
 

@@ -24,7 +24,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "common.cuh"
+#include "around.cuh"
 
 namespace vmoe {
 

@@ -25,7 +25,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "common.cuh"
+#include "around.cuh"
 
 namespace cg = cooperative_groups;
 

@@ -114,22 +114,6 @@ int launch_router_bwd(const Dims &p, const void *x, const float *w_router, const
                       const void *ye, float *dgate, float *dlogits, float *dw_router, float *dbias,
                       void *dx, cudaStream_t s);
 
-// What surrounds the layer: balance.cu, norm.cu, adamw.cu.
-size_t balance_workspace(const Dims &p);
-int launch_balance(const Dims &p, const float *logits, const int32_t *idx, const uint8_t *mask, int32_t *count,
-                   int32_t *tokens, float *excess, float *loss, float *parts, cudaStream_t s);
-int launch_balance_bwd(const Dims &p, const float *logits, const uint8_t *mask, const int32_t *count,
-                       const int32_t *tokens, const float *excess, const float *dloss, float *dlogits, cudaStream_t s);
-size_t norm_bwd_workspace(const Dims &p);
-int launch_block_norm(const Dims &p, const vmoe_norm *n, const void *x, const void *y, const float *post_w,
-                      const float *post_b, const float *gate, const float *pre_w, const float *pre_b, void *z, void *u,
-                      float *post_stat, float *pre_stat, cudaStream_t s);
-int launch_block_norm_bwd(const Dims &p, const vmoe_norm *n, const void *y, const void *z, const float *post_stat,
-                          const float *pre_stat, const float *post_w, const float *post_b, const float *gate,
-                          const float *pre_w, const void *dz, const void *du, void *dx, void *dy, float *dpost_w,
-                          float *dpost_b, float *dgate, float *dpre_w, float *dpre_b, float *parts, cudaStream_t s);
-int launch_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_config *c, cudaStream_t s);
-
 // Attention experts (attention.cu: the attention core; gemm_tc_fwd.cu /
 // gemm_tc_bwd.cu: the projections and their gradients).  Head dimension 64.
 bool attn_core_supported(int C, int head_dim);

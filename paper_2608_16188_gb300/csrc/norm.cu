@@ -19,7 +19,7 @@
 
 #include <algorithm>
 
-#include "common.cuh"
+#include "around.cuh"
 
 namespace vmoe {
 

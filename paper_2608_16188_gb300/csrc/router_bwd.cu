@@ -496,7 +496,7 @@ __global__ void __launch_bounds__(RX_THREADS)
 router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, __nv_bfloat16 *dx) {
     extern __shared__ __align__(16) uint4 rx_w[];  // [k16 steps][8 column tiles][32 lanes]: hi k, hi k + 8, lo, lo
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int t = blockIdx.z, d = p.d, E = p.E, N = p.N, d0 = blockIdx.x * RX_COLS, steps = (E + 15) / 16;
+    const int t = blockIdx.z, d = p.d, E = p.E, N = p.N, d0 = blockIdx.y * RX_COLS, steps = (E + 15) / 16;
     pdl_wait();
     // column c of tile j, c = 2 q + b as a lane's result has it, is column 16 q + 2 j + b
     for (int i = warp; i < steps * 8; i += RX_THREADS / 32) {
@@ -513,8 +513,8 @@ router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restri
         rx_w[i * 32 + lane] = v;
     }
     __syncthreads();
-    const int c0 = d0 + 16 * q, stop = min(N, (int)(blockIdx.y + 1) * RX_TOKENS);
-    for (int n0 = blockIdx.y * RX_TOKENS + warp * 16; n0 < stop; n0 += RX_THREADS / 2) {
+    const int c0 = d0 + 16 * q, stop = min(N, (int)(blockIdx.x + 1) * RX_TOKENS);
+    for (int n0 = blockIdx.x * RX_TOKENS + warp * 16; n0 < stop; n0 += RX_THREADS / 2) {
         const int na = n0 + g, nb = n0 + g + 8;
         const long long ra = (long long)t * N + min(na, N - 1), rb = (long long)t * N + min(nb, N - 1);
         __nv_bfloat16 *pa = dx + ra * d + c0, *pb = dx + rb * d + c0;
@@ -573,7 +573,7 @@ router_dx_simt_kernel(Dims p, const float *__restrict__ dl, const float *__restr
     __shared__ __align__(16) float ds[RXF_E][RXF_N + 4];
     __shared__ __align__(16) float ws[RXF_E][RXF_D + 4];
     const int tid = threadIdx.x, tn = tid / 16, td = tid % 16;
-    const int t = blockIdx.z, n0 = blockIdx.y * RXF_N, d0 = blockIdx.x * RXF_D, d = p.d, E = p.E, N = p.N;
+    const int t = blockIdx.z, n0 = blockIdx.x * RXF_N, d0 = blockIdx.y * RXF_D, d = p.d, E = p.E, N = p.N;
     // a warp copies 4 rows x 8 experts at a time: 32 banks, and whole sectors
     const int e8 = tid & 7, r4 = (tid & 31) >> 3, warp = tid >> 5;
     pdl_wait();
@@ -630,7 +630,7 @@ int launch_router_dx(const Dims &p, const float *dl, const float *wr, void *dx, 
     int st;
     if (p.bf16) {
         const size_t smem = (size_t)((p.E + 15) / 16) * 8 * 32 * sizeof(uint4);  // 64 KB for 256 experts
-        const dim3 grid((p.d + RX_COLS - 1) / RX_COLS, (p.N + RX_TOKENS - 1) / RX_TOKENS, p.T);
+        const dim3 grid((p.N + RX_TOKENS - 1) / RX_TOKENS, (p.d + RX_COLS - 1) / RX_COLS, p.T);
         auto go = [&](auto kern, std::atomic<int>(&limit)[64]) {
             if (smem > 48 * 1024)
                 if (const int e = raise_smem_limit((const void *)kern, limit, (int)smem)) return e;
@@ -639,7 +639,7 @@ int launch_router_dx(const Dims &p, const float *dl, const float *wr, void *dx, 
         static std::atomic<int> even[64], odd[64];
         st = p.E % 2 == 0 ? go(router_dx_mma_kernel<true>, even) : go(router_dx_mma_kernel<false>, odd);
     } else {
-        const dim3 grid((p.d + RXF_D - 1) / RXF_D, (p.N + RXF_N - 1) / RXF_N, p.T);
+        const dim3 grid((p.N + RXF_N - 1) / RXF_N, (p.d + RXF_D - 1) / RXF_D, p.T);
         st = launch_kernel(router_dx_simt_kernel, grid, dim3(RX_THREADS), 0, s, p, dl, wr, (float *)dx);
     }
     trace_after(s);
