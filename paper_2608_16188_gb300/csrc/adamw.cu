@@ -30,11 +30,11 @@ namespace vmoe {
 
 namespace {
 
-constexpr int AT = 256;  // threads a CTA
-// CTAs an SM, 128 registers a thread: 538 us for 302 M bf16 elements with 8-bit moments
-// (83% of the measured copy rate), 168 us for 38 M with fp32 moments and a master copy
-// (99%).  Three CTAs of 128 threads: 594 and 162; five, at 102 registers: 646 and 178.
-constexpr int AB = 2;
+// Most warps a CTA, and one CTA an SM, 128 registers a thread: 541 us for 302 M bf16
+// elements with 8-bit moments (83% of the measured copy rate), 165 us for 38 M with fp32
+// moments and a master copy.  Two CTAs of 8 warps: 577 and 166; one of 12 or 18: 581 and
+// 696; three of 6: 733.  Fewer pairs than 16 an SM are dealt over all SMs.
+constexpr int WARPS = 16;
 
 struct Entry {
     void *param;
@@ -565,7 +565,7 @@ __device__ __forceinline__ void run_f32(Walk<MAX> &w, const Common &c, const Con
 }
 
 template <int MAX>
-__global__ void __launch_bounds__(AT, AB)
+__global__ void __launch_bounds__(32 * WARPS, 1)
 adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
     pdl_wait();
     Common c;
@@ -577,12 +577,12 @@ adamw_kernel(const __grid_constant__ Table<MAX> tab, const Consts k) {
     c.root_scale = 1.0f / sqrtf(-expm1f((float)t * k.log_b2));
     c.key = k.seed_key + (uint32_t)t * 0x339cd49bu;
     typedef __nv_bfloat16 H;
-    const uint32_t warp = threadIdx.x >> 5;
-    uint32_t first = blockIdx.x * (AT / 32) + warp, step = gridDim.x * (AT / 32), end = tab.pairs;
+    const uint32_t warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    uint32_t first = blockIdx.x * warps + warp, step = gridDim.x * warps, end = tab.pairs;
     if (tab.runs) {
         first = (uint32_t)((uint64_t)tab.pairs * blockIdx.x / gridDim.x) + warp;
         end = (uint32_t)((uint64_t)tab.pairs * (blockIdx.x + 1) / gridDim.x);
-        step = AT / 32;
+        step = warps;
     }
     for (Walk<MAX> w(tab, first, step, end); w.more();) {
         const int kind = w.entry().kind;
@@ -633,13 +633,14 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pai
         e.kind = (x.param_dtype == VMOE_F32 ? P32 : 0) | (x.grad_dtype == VMOE_F32 ? G32 : 0) |
                  (x.state == VMOE_STATE_E4M3 ? S8 : 0) | (x.master ? MST : 0);
     }
-    const long long ctas = std::min(((long long)pairs + AT / 32 - 1) / (AT / 32), (long long)AB * num_sms());
+    const uint32_t sms = (uint32_t)num_sms(), warps = std::min<uint32_t>(WARPS, (pairs + sms - 1) / sms);
+    const uint32_t ctas = std::min((pairs + warps - 1) / warps, sms);
     // Warps dealt over all pairs in turn stay in one part of every array; of short tensors
     // each pair is another one's, and a CTA takes a run of pairs instead.  Tensors of 20000
     // elements, fp32 moments: 30 us in runs, 36 dealt (300 of them); of 147000, with a
     // master copy: 129 and 123 (192); 8-bit moments: 64 and 69; of 885000: 62 both.
     tab.runs = pairs < (uint64_t)tab.n * (eight ? 1024 : 128);
-    return launch_kernel(adamw_kernel<MAX>, dim3((unsigned)ctas), dim3(AT), 0, s, tab, k);
+    return launch_kernel(adamw_kernel<MAX>, dim3(ctas), dim3(32 * warps), 0, s, tab, k);
 }
 
 }  // namespace
