@@ -37,10 +37,11 @@ constexpr int BT = 256;      // threads a CTA
 constexpr int R = 4;         // rows a lane works on at a time
 constexpr int SUM_RUN = 16;  // steps of R rows a thread sums before it adds them to its total
 constexpr int CLUSTER = 8;   // CTAs that join their sums through distributed shared memory
-// Steps of a CTA of a cluster before two launches are faster: 16 steps in all took 4.9 to
-// 5.5 us as a cluster of eight and 5.8 to 6.5 in two launches, 32 steps 6.7 to 7.7 and 6.3
-// to 6.7 (one and eight tasks, 32 and 256 experts).
-constexpr int JOIN_STEPS = 2;
+// Steps of a CTA of a cluster before two launches are faster.  On the GPU 16 steps in all
+// took 4.9 to 5.5 us as a cluster of eight and 5.8 to 6.5 in two launches, 32 steps 6.7 to
+// 7.7 and 6.3 to 6.7 (one and eight tasks, 32 and 256 experts), 64 steps 10.1 to 11.6 and
+// 6.4 to 8.2; the second launch costs the host 1.9 us.
+constexpr int JOIN_STEPS = 4;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 int lanes_of(int E) {
