@@ -86,22 +86,25 @@ __device__ __forceinline__ float sum2(f32x2 v) {
     return f.x + f.y;
 }
 
-__device__ __forceinline__ float warp_sum(float v) {
+template <int L>
+__device__ __forceinline__ float lane_sum(float v) {  // over L neighbouring lanes
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// How rows lie on a CTA, forward and backward: W = ceil(d / 256) warps hold a row, 8
-// columns a thread, so that a thread keeps its columns' parameters (and, in the
-// backward, their gradients) in registers over all rows of the CTA's slice of a task.
-// `groups` such rows, R at a time, with the next ones' loads in flight meanwhile.
+// How rows lie on a CTA, forward and backward: W = ceil(d / 256) warps hold a row, or,
+// up to 128 channels, 8 or 16 lanes; 8 columns a thread, so that a thread keeps its
+// columns' parameters (and, in the backward, their gradients) in registers over all rows
+// of the CTA's slice of a task.  A CTA has `groups` of such threads, each taking R rows
+// at a time, with the next ones' loads in flight meanwhile.
 int row_warps(int d) { return (d + 255) / 256; }
-int row_groups(int d) { return std::max(1, 4 / row_warps(d)); }
+int row_threads(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32 * row_warps(d); }
+int row_groups(int d) { return std::max(1, 128 / row_threads(d)); }
 // Slices of a task's tokens: enough CTAs for `regs` registers a thread to fill 152 SMs
 // once, and `least` steps for each.
 int slices_of(const Dims &p, int R, int regs, int least) {
-    const int groups = row_groups(p.d), threads = 32 * row_warps(p.d) * groups, rows = least * R * groups;
+    const int groups = row_groups(p.d), threads = row_threads(p.d) * groups, rows = least * R * groups;
     const int resident = 152 * std::max(1, 65536 / (regs * threads));
     return std::max(1, std::min((p.N + rows - 1) / rows, resident / p.T));
 }
@@ -125,16 +128,16 @@ struct FwdArgs {
 // Totals of R values over the W warps of a row, the same in every thread.  The first
 // halvings of the butterfly sum two values at once; `buf` alternates between two
 // halves, so one barrier a call is enough.
-template <int WC, int R>
+template <int WC, int L, int R>
 struct Totals {
     float (*buf)[32][R];
     int first, flip;  // first warp of the group
     int W;            // WC, or where that is 0 the number of warps
     __device__ __forceinline__ void operator()(float (&v)[R]) {
-        const int lane = threadIdx.x & 31;
+        const int lane = threadIdx.x % L;
         int mine = 0;
 #pragma unroll
-        for (int h = R / 2, o = 16; h > 0; h >>= 1, o >>= 1) {
+        for (int h = R / 2, o = L / 2; h > 0; h >>= 1, o >>= 1) {
             const bool up = (lane & o) != 0;
 #pragma unroll
             for (int i = 0; i < h; ++i) {
@@ -144,10 +147,10 @@ struct Totals {
             mine += up ? h : 0;
         }
 #pragma unroll
-        for (int o = 16 / R; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+        for (int o = L / R / 2; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
         float sum = v[0];
         if (WC != 1) {
-            if (lane % (32 / R) == 0) buf[flip][threadIdx.x >> 5][mine] = sum;
+            if (lane % (L / R) == 0) buf[flip][threadIdx.x >> 5][mine] = sum;
             __syncthreads();
             sum = 0.0f;
 #pragma unroll
@@ -155,13 +158,13 @@ struct Totals {
             flip ^= 1;
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = __shfl_sync(0xffffffffu, sum, i * (32 / R));
+        for (int i = 0; i < R; ++i) v[i] = __shfl_sync(0xffffffffu, sum, i * (L / R), L);
     }
 };
 
 // mean and rstd of R rows.
-template <typename T, int WC, int R>
-__device__ __forceinline__ void stats(const Raw8<T> (&raw)[R], bool have, const FwdArgs &a, float share, Totals<WC, R> &totals,
+template <typename T, int WC, int L, int R>
+__device__ __forceinline__ void stats(const Raw8<T> (&raw)[R], bool have, const FwdArgs &a, float share, Totals<WC, L, R> &totals,
                                       float2 (&s)[R]) {
     float m[R], q[R];
 #pragma unroll
@@ -203,17 +206,17 @@ __device__ __forceinline__ void store_stats(float2 *out, const float2 (&s)[R], i
     out[th] = o;
 }
 
-template <typename T, int WC, int MAXT, int MINB, int R, bool AHEAD>
+template <typename T, int WC, int L, int MAXT, int MINB, int R, bool AHEAD>
 __global__ void __launch_bounds__(MAXT, MINB)
 norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
     __shared__ float buf[2][32][R];
     const int W = WC ? WC : warps;
-    const int warp = threadIdx.x >> 5, group = warp / W, th = threadIdx.x - group * 32 * W;
+    const int group = threadIdx.x / (L * W), th = threadIdx.x - group * (L * W);
     const int t = blockIdx.y, N = p.N, d = p.d, c = 8 * th;
     const int beg = (int)((long long)N * blockIdx.x / gridDim.x), end = (int)((long long)N * (blockIdx.x + 1) / gridDim.x);
     const bool have = c < d;
     const float share = 1.0f / (float)d;
-    Totals<WC, R> totals = {buf, group * W, 0, W};
+    Totals<WC, L, R> totals = {buf, group * W, 0, W};
     pdl_wait();
     const long long par = (long long)t * d + c, base = (long long)t * N;
     const T *x0 = (const T *)a.x + base * d, *y0 = (const T *)a.y + (a.y ? base * d : 0);
@@ -263,7 +266,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
 #pragma unroll
             for (int r = 0; r < R; ++r) s[r] = make_float2(0.0f, 1.0f);
             if (a.post) {
-                stats<T, WC, R>(y, have, a, share, totals, s);
+                stats<T, WC, L, R>(y, have, a, share, totals, s);
                 store_stats<R>(a.post_stat ? a.post_stat + base + n : nullptr, s, th, end - n);
             }
 #pragma unroll
@@ -279,7 +282,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
             }
         }
         if (!a.u) continue;
-        stats<T, WC, R>(x, have, a, share, totals, s);
+        stats<T, WC, L, R>(x, have, a, share, totals, s);
         store_stats<R>(a.pre_stat ? a.pre_stat + base + n : nullptr, s, th, end - n);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -320,23 +323,29 @@ int bwd_slices(const Dims &p) {
     return slices_of(p, bwd_rows(p), W <= 4 ? 512 / BB : W <= 16 ? 128 : 64, 2);
 }
 
-// Totals over a warp of M (8 or 16) values a lane: each halving step sums two lanes'
-// values and keeps half of them, 16 shuffles for 16 totals.  Lane l ends with value l % M.
-template <int M>
-__device__ __forceinline__ float warp_totals(float (&v)[16]) {
-    const int lane = threadIdx.x & 31;
+// Totals of 8 R values over L lanes: each halving step sums two lanes' values and keeps
+// half of them, 16 shuffles for 16 totals.  Lane l ends with value l % 8 R; eight lanes
+// with value l of each row.
+template <int L, int R>
+__device__ __forceinline__ void lane_totals(float (&v)[8 * R], float (&sum)[R]) {
+    constexpr int M = L < 8 * R ? 8 : 8 * R;
+    const int lane = threadIdx.x % L;
 #pragma unroll
-    for (int h = M / 2; h > 0; h >>= 1) {
-        const bool up = (lane & h) != 0;
+    for (int r = 0; r < 8 * R / M; ++r) {
+        float *x = v + M * r;
 #pragma unroll
-        for (int i = 0; i < h; ++i) {
-            const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+        for (int h = M / 2; h > 0; h >>= 1) {
+            const bool up = (lane & h) != 0;
+#pragma unroll
+            for (int i = 0; i < h; ++i) {
+                const float give = up ? x[i] : x[i + h], keep = up ? x[i + h] : x[i];
+                x[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+            }
         }
-    }
 #pragma unroll
-    for (int o = M; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-    return v[0];
+        for (int o = M; o < L; o <<= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+        sum[r] = x[0];
+    }
 }
 
 template <typename T>
@@ -347,13 +356,13 @@ struct BwdRow {
 
 // ALL: every input is there and the branch has a norm, known to the compiler (49 us at 17 x
 // 1576 tokens of 768 channels, 55 without).
-template <typename T, int WC, int MAXT, int MINB, int R, bool AHEAD, bool ALL>
+template <typename T, int WC, int L, int MAXT, int MINB, int R, bool AHEAD, bool ALL>
 __global__ void __launch_bounds__(MAXT, MINB)
 norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     __shared__ float totals[2][32][16];
     extern __shared__ __align__(16) float join[];  // [groups - 1][4][d], where there are several groups
     const int W = WC ? WC : warps;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / W, th = threadIdx.x - group * 32 * W;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x / (L * W), th = threadIdx.x - group * (L * W);
     const int t = blockIdx.y, N = p.N, d = p.d, c = 8 * th;
     const int beg = (int)((long long)N * blockIdx.x / gridDim.x), end = (int)((long long)N * (blockIdx.x + 1) / gridDim.x);
     const bool have = c < d;
@@ -374,7 +383,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             aw[i] = have ? mul2(aw[i], g[i]) : 0;
             pw[i] = have ? pw[i] : 0;
         }
-        sum_aw = warp_sum(sum2(add2(add2(aw[0], aw[1]), add2(aw[2], aw[3]))));
+        sum_aw = lane_sum<L>(sum2(add2(add2(aw[0], aw[1]), add2(aw[2], aw[3]))));
         if (WC != 1) {
             if (lane == 0) totals[0][warp][0] = sum_aw;
             __syncthreads();
@@ -421,9 +430,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     for (int n0 = beg; n0 < end; n0 += groups * R, flip ^= 1) {
         if (!AHEAD) fetch(n0);
         f32x2 e[R][4], zh[R][4], yh[R][4];
-        float rz[R], ry[R], in[R], v[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+        float rz[R], ry[R], in[R], v[8 * R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             in[r] = n0 + group * R + r < end ? 1.0f : 0.0f;
@@ -454,21 +461,23 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             }
 #pragma unroll
             for (int i = 0; i < 7; ++i) v[8 * r + i] = sum2(s[i]);
+            v[8 * r + 7] = 0.0f;
         }
         if (AHEAD && n0 + groups * R < end) fetch(n0 + groups * R);
-        float sum = warp_totals<8 * R>(v);
+        float sum[R];
+        lane_totals<L, R>(v, sum);
         if (WC != 1) {
-            if (lane < 8 * R) totals[flip][warp][lane] = sum;
+            if (lane < 8 * R) totals[flip][warp][lane] = sum[0];
             __syncthreads();  // the other half is written next: one barrier a step
-            sum = 0.0f;
+            sum[0] = 0.0f;
 #pragma unroll
-            for (int w = 0; w < (WC ? WC : W); ++w) sum += totals[flip][group * W + w][lane & (8 * R - 1)];
+            for (int w = 0; w < (WC ? WC : W); ++w) sum[0] += totals[flip][group * W + w][lane & (8 * R - 1)];
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float s[7];
 #pragma unroll
-            for (int i = 0; i < 7; ++i) s[i] = __shfl_sync(0xffffffffu, sum, 8 * r + i);
+            for (int i = 0; i < 7; ++i) s[i] = L < 8 * R ? __shfl_sync(0xffffffffu, sum[r], i, L) : __shfl_sync(0xffffffffu, sum[0], 8 * r + i, L);
             const int n = n0 + group * R + r;
             const float z1 = has_u ? rz[r] : 0.0f, m1 = z1 * centre * s[0], m2 = z1 * share * s[1];
             const float k1 = post ? centre * (s[2] - m1 * sum_aw - m2 * s[4]) : 0.0f;
@@ -571,39 +580,47 @@ norm_join_kernel(Dims p, JoinArgs a, int slices) {
 template <typename T>
 int run_fwd(const Dims &p, const FwdArgs &a, cudaStream_t s) {
     constexpr int R = sizeof(T) == 2 ? FR : FR / 2;
-    const int W = row_warps(p.d), groups = row_groups(p.d), threads = 32 * W * groups;
+    const int W = row_warps(p.d), groups = row_groups(p.d), threads = row_threads(p.d) * groups;
     auto go = [&](auto kern, int rows, int regs) {
         return launch_kernel(kern, dim3(slices_of(p, rows, regs, 1), p.T), dim3(threads), 0, s, p, a, W, groups);
     };
+    if (p.d <= 64) return go(norm_fwd_kernel<T, 1, 8, 128, FB, R, true>, R, 512 / FB);
+    if (p.d <= 128) return go(norm_fwd_kernel<T, 1, 16, 128, FB, R, true>, R, 512 / FB);
     switch (W) {
-        case 1: return go(norm_fwd_kernel<T, 1, 128, FB, R, true>, R, 512 / FB);
-        case 2: return go(norm_fwd_kernel<T, 2, 128, FB, R, true>, R, 512 / FB);
-        case 3: return go(norm_fwd_kernel<T, 3, 96, FB * 4 / 3, R, true>, R, 512 / FB);
-        case 4: return go(norm_fwd_kernel<T, 4, 128, FB, R, true>, R, 512 / FB);
+        case 1: return go(norm_fwd_kernel<T, 1, 32, 128, FB, R, true>, R, 512 / FB);
+        case 2: return go(norm_fwd_kernel<T, 2, 32, 128, FB, R, true>, R, 512 / FB);
+        case 3: return go(norm_fwd_kernel<T, 3, 32, 96, FB * 4 / 3, R, true>, R, 512 / FB);
+        case 4: return go(norm_fwd_kernel<T, 4, 32, 128, FB, R, true>, R, 512 / FB);
     }
-    if (W <= 8) return go(norm_fwd_kernel<T, 0, 256, 2, R, true>, R, 128);
-    if (W <= 16) return go(norm_fwd_kernel<T, 0, 512, 1, R, true>, R, 128);
-    return go(norm_fwd_kernel<T, 0, 1024, 1, 1, false>, 1, 64);
+    if (W <= 8) return go(norm_fwd_kernel<T, 0, 32, 256, 2, R, true>, R, 128);
+    if (W <= 16) return go(norm_fwd_kernel<T, 0, 32, 512, 1, R, true>, R, 128);
+    return go(norm_fwd_kernel<T, 0, 32, 1024, 1, 1, false>, 1, 64);
 }
 
+template <typename T, int WC, int L, int MAXT, int MINB, int R>
+int launch_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
+    const int W = row_warps(p.d), groups = row_groups(p.d);
+    const size_t smem = (size_t)(groups - 1) * 4 * p.d * sizeof(float);
+    const dim3 grid(bwd_slices(p), p.T), block(row_threads(p.d) * groups);
+    if (WC && a.du && a.dz && a.y && a.post)
+        return launch_kernel(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, WC != 0>, grid, block, smem, s, p, a, W, groups);
+    return launch_kernel(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, false>, grid, block, smem, s, p, a, W, groups);
+}
 template <typename T>
 int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
     constexpr int R = sizeof(T) == 2 ? BR : 1;
-    const int W = row_warps(p.d), groups = row_groups(p.d);
-    const size_t smem = (size_t)(groups - 1) * 4 * p.d * sizeof(float);
-    auto go = [&](auto kern) {
-        return launch_kernel(kern, dim3(bwd_slices(p), p.T), dim3(32 * W * groups), smem, s, p, a, W, groups);
-    };
-    const bool all = a.du && a.dz && a.y && a.post;
+    if (p.d <= 64) return launch_bwd<T, 1, 8, 128, BB, R>(p, a, s);
+    if (p.d <= 128) return launch_bwd<T, 1, 16, 128, BB, R>(p, a, s);
+    const int W = row_warps(p.d);
     switch (W) {
-        case 1: return all ? go(norm_bwd_kernel<T, 1, 128, BB, R, true, true>) : go(norm_bwd_kernel<T, 1, 128, BB, R, true, false>);
-        case 2: return all ? go(norm_bwd_kernel<T, 2, 128, BB, R, true, true>) : go(norm_bwd_kernel<T, 2, 128, BB, R, true, false>);
-        case 3: return all ? go(norm_bwd_kernel<T, 3, 96, BB * 4 / 3, R, true, true>) : go(norm_bwd_kernel<T, 3, 96, BB * 4 / 3, R, true, false>);
-        case 4: return all ? go(norm_bwd_kernel<T, 4, 128, BB, R, true, true>) : go(norm_bwd_kernel<T, 4, 128, BB, R, true, false>);
+        case 1: return launch_bwd<T, 1, 32, 128, BB, R>(p, a, s);
+        case 2: return launch_bwd<T, 2, 32, 128, BB, R>(p, a, s);
+        case 3: return launch_bwd<T, 3, 32, 96, BB * 4 / 3, R>(p, a, s);
+        case 4: return launch_bwd<T, 4, 32, 128, BB, R>(p, a, s);
     }
-    if (W <= 8) return go(norm_bwd_kernel<T, 0, 256, 2, 1, true, false>);
-    if (W <= 16) return go(norm_bwd_kernel<T, 0, 512, 1, 1, true, false>);
-    return go(norm_bwd_kernel<T, 0, 1024, 1, 1, false, false>);
+    if (W <= 8) return launch_bwd<T, 0, 32, 256, 2, 1>(p, a, s);
+    if (W <= 16) return launch_bwd<T, 0, 32, 512, 1, 1>(p, a, s);
+    return launch_bwd<T, 0, 32, 1024, 1, 1>(p, a, s);
 }
 
 }  // namespace

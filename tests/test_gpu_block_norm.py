@@ -95,9 +95,11 @@ def _check(s, o, dtype, part, post, rms, rho):
             assert np.all(err <= 1.2e-5 * mag[n] + 1e-30), (n, float((err / (mag[n] + 1e-30)).max()))
 
 
-# widths around each form's border (256 channels a warp, 1024 a warp's row, 8192 the most), odd counts of tokens
+# widths around each form's border (8 lanes a row up to 64 channels, 16 up to 128, a warp for each 256, 8192 the
+# most), odd counts of tokens
 SHAPES = [(1, 1, 8), (2, 3, 16), (1, 197, 384), (3, 50, 248), (2, 33, 264), (2, 40, 512), (2, 65, 768), (3, 77, 1000),
-          (1, 130, 1024), (2, 9, 1032), (1, 21, 2048), (2, 5, 2056), (1, 13, 4104), (1, 3, 8192), (5, 700, 96)]
+          (1, 130, 1024), (2, 9, 1032), (1, 21, 2048), (2, 5, 2056), (1, 13, 4104), (1, 3, 8192), (5, 700, 96),
+          (7, 5, 40), (4, 37, 64), (2, 611, 72), (3, 211, 128), (2, 90, 136)]
 
 
 @pytest.mark.parametrize("shape", SHAPES, ids=str)
