@@ -21,6 +21,9 @@
  *                  dW1 = Xe^T dH, dW2 = A^T dYe
  *   vmoe_combine   dX  = sum_j dXe[e_j, s_j]
  *   vmoe_router_bwd dgate, dlogits, dW_r, dbias; dX += dlogits W_r^T
+ * Around it, in training: vmoe_balance and vmoe_balance_bwd (the routers' balance
+ * losses), vmoe_block_norm and vmoe_block_norm_bwd (a block's norms, gate and
+ * residual), vmoe_adamw (the update).
  *
  * Conventions for every entry point:
  *  - Ownership: every array argument is caller-owned DEVICE memory (except
@@ -37,7 +40,7 @@
  *    to [0, C], and expert indices or slots out of range are undefined
  *    behaviour.
  *  - Determinism: results are bitwise reproducible run to run (no atomics in
- *    any reduction, fixed summation orders).
+ *    any reduction but of whole numbers, fixed summation orders).
  *  - Host threads: entry points may be called from several host threads at
  *    once, each with its own stream and arrays; the kernel trace is kept per
  *    host thread.  The exception is vmoe_expert_bwd_static_scratch, whose
