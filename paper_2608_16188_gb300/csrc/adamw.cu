@@ -638,7 +638,7 @@ int launch_table(const vmoe_adamw_tensor *tensors, int n, int base, uint32_t pai
     // Warps dealt over all pairs in turn stay in one part of every array; of short tensors
     // each pair is another one's, and a CTA takes a run of pairs instead.  Tensors of 20000
     // elements, fp32 moments: 30 us in runs, 36 dealt (300 of them); of 147000, with a
-    // master copy: 129 and 123 (192); 8-bit moments: 64 and 69; of 885000: 62 both.
+    // master copy: 127 and 123 (192); 8-bit moments: 60 and 66; of 885000: 59 both.
     tab.runs = pairs < (uint64_t)tab.n * (eight ? 1024 : 128);
     return launch_kernel(adamw_kernel<MAX>, dim3(ctas), dim3(32 * warps), 0, s, tab, k);
 }
