@@ -555,25 +555,6 @@ balance_bwd_kernel(Dims p, const float *logits, const uint8_t *__restrict__ mask
     }
 }
 
-// launch_kernel with `ranks` CTAs along x as a cluster.
-template <typename... KArgs, typename... Args>
-int launch_cluster(void (*kern)(KArgs...), dim3 grid, dim3 block, int ranks, cudaStream_t s, Args &&...args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ranks;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...) == cudaSuccess ? VMOE_OK : VMOE_ERR_CUDA;
-}
-
 // Calls f(L, V, VEC) as constants for a problem of E experts.
 template <int I>
 using Int = std::integral_constant<int, I>;
@@ -608,7 +589,7 @@ int launch_balance(const Dims &p, const float *logits, const int32_t *idx, const
     int st = with_layout(p.E, [&](auto L, auto V, auto vec) {
         auto kern = balance_kernel<L(), V(), vec()>;
         if (two) return launch_kernel(kern, dim3(slices, p.T), dim3(BT), 0, s, p, logits, idx, mask, parts, o);
-        return launch_cluster(kern, dim3(slices, p.T), dim3(BT), slices, s, p, logits, idx, mask, (float *)nullptr, o);
+        return launch_cluster(kern, dim3(slices, p.T), dim3(BT), 0, slices, s, p, logits, idx, mask, (float *)nullptr, o);
     });
     trace_after(s);
     if (st != VMOE_OK || !two) return st;

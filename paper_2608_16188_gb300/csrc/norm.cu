@@ -15,11 +15,14 @@
 // gate and weights do not depend on the token, so two sums a column carry the three
 // gradients behind the branch.  Variances are sums of squared distances to the mean
 // (two passes over registers), all sums fp32.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <algorithm>
 
 #include "around.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace vmoe {
 
@@ -250,7 +253,7 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
             if (a.y) ny[r].load(y0 + at);
         }
     };
-    if (AHEAD) fetch(beg);
+    if (AHEAD && beg < end) fetch(beg);
     for (int n0 = beg; n0 < end; n0 += groups * R) {
         if (!AHEAD) fetch(n0);
         Raw8<T> x[R], y[R];
@@ -306,20 +309,49 @@ norm_fwd_kernel(Dims p, FwdArgs a, int warps, int groups) {
 //   sum q      = sum e aw - r_z (m1 sum aw + m2 sum zhat aw)
 //   sum q yhat = sum e aw yhat - r_z (m1 sum aw yhat + m2 sum zhat aw yhat),
 // so seven sums a row, taken together, replace two rounds of two that wait for one another.
+// What the column sums of a task become.
+struct JoinArgs {
+    const float *parts, *post_w, *post_b, *gate;
+    float *dpost_w, *dpost_b, *dgate, *dpre_w, *dpre_b;
+    __device__ __forceinline__ void store(long long at, const float (&s)[4]) const {
+        const float g = gate ? gate[at] : 1.0f, w = post_w ? post_w[at] : 1.0f, b = post_b ? post_b[at] : 0.0f;
+        if (dpost_w) dpost_w[at] = g * s[0];
+        if (dpost_b) dpost_b[at] = g * s[1];
+        if (dgate) dgate[at] = fmaf(w, s[0], b * s[1]);
+        if (dpre_w) dpre_w[at] = s[2];
+        if (dpre_b) dpre_b[at] = s[3];
+    }
+};
+
 struct BwdArgs {
     const void *y, *z;
     const float2 *post_stat, *pre_stat;
     const float *post_w, *post_b, *gate, *pre_w;
     const void *dz, *du;
     void *dx, *dy;
-    float *parts;
+    float *parts;  // NULL: the slices are a cluster, which joins its sums itself
+    JoinArgs join;
     float rho;
     bool rms, post;
 };
 
 int bwd_rows(const Dims &p) { return p.bf16 && row_warps(p.d) <= 4 ? BR : 1; }
+// Short tasks are a cluster of up to CLUSTER CTAs with at most JOIN_STEPS steps each, which
+// joins its sums itself: one launch (the second costs the host 1.9 us).  On the GPU 4 to 8
+// steps in all took 3.7 to 4.7 us so and 4.7 to 5.1 in two launches, 16 steps 4.8 to 6.0 and
+// 4.6 to 5.0, 32 steps 6.1 to 8.1 and 4.8 to 6.1 (1 to 17 tasks, 128 to 1024 channels).
+constexpr int CLUSTER = 8, JOIN_STEPS = 2;
+bool bwd_cluster(const Dims &p) {
+    return p.d <= 1024 && (p.N + bwd_rows(p) * row_groups(p.d) - 1) / (bwd_rows(p) * row_groups(p.d)) <= CLUSTER * JOIN_STEPS;
+}
 int bwd_slices(const Dims &p) {
     const int W = row_warps(p.d);
+    if (bwd_cluster(p)) {
+        const int steps = (p.N + bwd_rows(p) * row_groups(p.d) - 1) / (bwd_rows(p) * row_groups(p.d));
+        int n = 1;  // no more than there are rows: a slice has one at least
+        while (n < CLUSTER && 2 * n <= steps) n *= 2;
+        return n;
+    }
     return slices_of(p, bwd_rows(p), W <= 4 ? 512 / BB : W <= 16 ? 128 : 64, 2);
 }
 
@@ -360,7 +392,7 @@ template <typename T, int WC, int L, int MAXT, int MINB, int R, bool AHEAD, bool
 __global__ void __launch_bounds__(MAXT, MINB)
 norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     __shared__ float totals[2][32][16];
-    extern __shared__ __align__(16) float join[];  // [groups - 1][4][d], where there are several groups
+    extern __shared__ __align__(16) float join[];  // [max(1, groups - 1)][4][d]: the groups' sums, then the CTA's
     const int W = WC ? WC : warps;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x / (L * W), th = threadIdx.x - group * (L * W);
     const int t = blockIdx.y, N = p.N, d = p.d, c = 8 * th;
@@ -425,7 +457,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             }
         }
     };
-    if (AHEAD) fetch(beg);
+    if (AHEAD && beg < end) fetch(beg);
     int flip = 0;
     for (int n0 = beg; n0 < end; n0 += groups * R, flip ^= 1) {
         if (!AHEAD) fetch(n0);
@@ -518,8 +550,8 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     };
     if (group > 0 && have) put(join + (long long)(group - 1) * 4 * d + c);
     __syncthreads();
-    if (group > 0 || !have) return;
-    for (int g = 1; g < groups; ++g) {
+    const bool first = group == 0 && have;
+    for (int g = 1; g < (first ? groups : 1); ++g) {
         const float *o = join + (long long)(g - 1) * 4 * d + c;
         auto add = [&](f32x2 (&to)[4], const float *from) {
             f32x2 f[4];
@@ -533,13 +565,25 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
         add(Pw, o + 2 * d);
         add(Pb, o + 3 * d);
     }
-    put(a.parts + ((long long)t * gridDim.x + blockIdx.x) * 4 * d + c);
+    if (a.parts != nullptr) {
+        if (first) put(a.parts + ((long long)t * gridDim.x + blockIdx.x) * 4 * d + c);
+        return;
+    }
+    if (first) put(join + c);  // a thread overwrites what it alone has read
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const int ranks = (int)cluster.num_blocks();
+    for (int i = (int)cluster.block_rank() * blockDim.x + threadIdx.x; i < d; i += ranks * blockDim.x) {
+        float s[4] = {};
+        for (int q = 0; q < ranks; ++q) {
+            const float *in = cluster.map_shared_rank(join, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] += in[j * d + i];
+        }
+        a.join.store((long long)t * d + i, s);
+    }
+    cluster.sync();  // the sums stay until they are read
 }
-
-struct JoinArgs {
-    const float *parts, *post_w, *post_b, *gate;
-    float *dpost_w, *dpost_b, *dgate, *dpre_w, *dpre_b;
-};
 
 // The slices' column sums joined: 32 columns a CTA, JOIN threads a column, each a run
 // of the slices.
@@ -568,13 +612,7 @@ norm_join_kernel(Dims p, JoinArgs a, int slices) {
 #pragma unroll
         for (int i = 0; i < JOIN; ++i) s[j] += part[i][j][lane];
     }
-    const long long at = (long long)t * d + c;
-    const float g = a.gate ? a.gate[at] : 1.0f, w = a.post_w ? a.post_w[at] : 1.0f, b = a.post_b ? a.post_b[at] : 0.0f;
-    if (a.dpost_w) a.dpost_w[at] = g * s[0];
-    if (a.dpost_b) a.dpost_b[at] = g * s[1];
-    if (a.dgate) a.dgate[at] = fmaf(w, s[0], b * s[1]);
-    if (a.dpre_w) a.dpre_w[at] = s[2];
-    if (a.dpre_b) a.dpre_b[at] = s[3];
+    a.store((long long)t * d + c, s);
 }
 
 template <typename T>
@@ -599,12 +637,14 @@ int run_fwd(const Dims &p, const FwdArgs &a, cudaStream_t s) {
 
 template <typename T, int WC, int L, int MAXT, int MINB, int R>
 int launch_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
-    const int W = row_warps(p.d), groups = row_groups(p.d);
-    const size_t smem = (size_t)(groups - 1) * 4 * p.d * sizeof(float);
-    const dim3 grid(bwd_slices(p), p.T), block(row_threads(p.d) * groups);
-    if (WC && a.du && a.dz && a.y && a.post)
-        return launch_kernel(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, WC != 0>, grid, block, smem, s, p, a, W, groups);
-    return launch_kernel(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, false>, grid, block, smem, s, p, a, W, groups);
+    const int W = row_warps(p.d), groups = row_groups(p.d), slices = bwd_slices(p);
+    const dim3 grid(slices, p.T), block(row_threads(p.d) * groups);
+    auto go = [&](auto kern) {
+        if (a.parts) return launch_kernel(kern, grid, block, (size_t)(groups - 1) * 4 * p.d * sizeof(float), s, p, a, W, groups);
+        return launch_cluster(kern, grid, block, (size_t)std::max(1, groups - 1) * 4 * p.d * sizeof(float), slices, s, p, a, W, groups);
+    };
+    if (WC && a.du && a.dz && a.y && a.post) return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, WC != 0>);
+    return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, false>);
 }
 template <typename T>
 int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
@@ -625,7 +665,9 @@ int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
 
 }  // namespace
 
-size_t norm_bwd_workspace(const Dims &p) { return (size_t)p.T * bwd_slices(p) * 4 * p.d * sizeof(float); }
+size_t norm_bwd_workspace(const Dims &p) {
+    return bwd_cluster(p) ? 16 : (size_t)p.T * bwd_slices(p) * 4 * p.d * sizeof(float);
+}
 
 int launch_block_norm(const Dims &p, const vmoe_norm *n, const void *x, const void *y, const float *post_w,
                       const float *post_b, const float *gate, const float *pre_w, const float *pre_b, void *z, void *u,
@@ -642,13 +684,15 @@ int launch_block_norm_bwd(const Dims &p, const vmoe_norm *n, const void *y, cons
                           const float *pre_stat, const float *post_w, const float *post_b, const float *gate,
                           const float *pre_w, const void *dz, const void *du, void *dx, void *dy, float *dpost_w,
                           float *dpost_b, float *dgate, float *dpre_w, float *dpre_b, float *parts, cudaStream_t s) {
+    const bool cluster = bwd_cluster(p);
+    const JoinArgs j = {parts, post_w, post_b, gate, dpost_w, dpost_b, dgate, dpre_w, dpre_b};
     const BwdArgs a = {y, z, (const float2 *)post_stat, (const float2 *)pre_stat, post_w, post_b, gate, pre_w, dz, du,
-                       dx, dy, parts, n->residual_scale, (n->flags & VMOE_NORM_RMS) != 0, (n->flags & VMOE_NORM_POST) != 0};
+                       dx, dy, cluster ? nullptr : parts, j, n->residual_scale, (n->flags & VMOE_NORM_RMS) != 0,
+                       (n->flags & VMOE_NORM_POST) != 0};
     trace_before(s, "block_norm_bwd");
     int st = p.bf16 ? run_bwd<__nv_bfloat16>(p, a, s) : run_bwd<float>(p, a, s);
     trace_after(s);
-    if (st != VMOE_OK || !(dpost_w || dpost_b || dgate || dpre_w || dpre_b)) return st;
-    const JoinArgs j = {parts, post_w, post_b, gate, dpost_w, dpost_b, dgate, dpre_w, dpre_b};
+    if (st != VMOE_OK || cluster || !(dpost_w || dpost_b || dgate || dpre_w || dpre_b)) return st;
     trace_before(s, "block_norm_join");
     st = launch_kernel(norm_join_kernel, dim3((p.d + 31) / 32, p.T), dim3(32 * JOIN), 0, s, p, j, bwd_slices(p));
     trace_after(s);
