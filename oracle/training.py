@@ -123,9 +123,9 @@ def mix(h):
     return h ^ (h >> np.uint64(16))
 
 
-def dither_bits(n, place, step, seed):
-    """(low, high) 16-bit halves of each element's hash."""
-    i = np.arange(n, dtype=np.uint64)
+def dither_bits(n, place, step, seed, first=0):
+    """(low, high) 16-bit halves of the hashes of elements first .. first + n - 1."""
+    i = np.arange(first, first + n, dtype=np.uint64) & np.uint64(0xffffffff)
     key = np.uint64((0x5e4087b3 * place + 0x339cd49b * step + 0xe32a5e87 * seed) & 0xffffffff)
     h = mix(i * np.uint64(0x51f6db5b) + key)
     return (h & np.uint64(0xffff)).astype(np.int64), (h >> np.uint64(16)).astype(np.int64)

@@ -113,11 +113,13 @@ int slices_of(const Dims &p, int R, int regs, int least) {
 }
 
 // Rows at a time and CTAs of 128 threads an SM, for 1 to 4 warps a row.  Forward: two
-// bf16 rows and five CTAs; 34 us at 17 x 1576 tokens of 768 channels and 64.5 at 8 x
-// 6304 of 1024 without a post-norm, where four rows and four CTAs took 31 and 73, two
-// rows and six CTAs 39 and 69.  Backward: two rows and three CTAs, 52 us at the former
-// size; one row and three to five CTAs 56 to 60.
-constexpr int FR = 2, FB = 5, BR = 2, BB = 3;
+// bf16 rows (one in fp32) and five CTAs; 33 us at 17 x 1576 tokens of 768 channels and 64
+// at 8 x 6304 of 1024 without a post-norm, where four rows and four CTAs took 31 and 73, two
+// rows and six CTAs 39 and 69.  Backward: two rows and three CTAs, 50 us at the former size
+// (one row and three to five CTAs 56 to 60, before other steps that took 3 off both); fp32
+// rows fill the registers of two CTAs: forward and backward of 3 x 1001 x 1000 26 us, 28 with
+// one row and three CTAs, 8 x 4096 x 1024 205 and 209.
+constexpr int FR = 2, FB = 5, BR = 2, BB = 3, BB32 = 2;
 
 struct FwdArgs {
     const void *x, *y;
@@ -335,7 +337,7 @@ struct BwdArgs {
     bool rms, post;
 };
 
-int bwd_rows(const Dims &p) { return p.bf16 && row_warps(p.d) <= 4 ? BR : 1; }
+int bwd_rows(const Dims &p) { return row_warps(p.d) <= 4 ? BR : 1; }
 // Short tasks are a cluster of up to CLUSTER CTAs with at most JOIN_STEPS steps each, which
 // joins its sums itself: one launch (the second costs the host 1.9 us).  On the GPU 4 to 8
 // steps in all took 3.7 to 4.7 us so and 4.7 to 5.1 in two launches, 16 steps 4.8 to 6.0 and
@@ -352,7 +354,7 @@ int bwd_slices(const Dims &p) {
         while (n < CLUSTER && 2 * n <= steps) n *= 2;
         return n;
     }
-    return slices_of(p, bwd_rows(p), W <= 4 ? 512 / BB : W <= 16 ? 128 : 64, 2);
+    return slices_of(p, bwd_rows(p), W <= 4 ? 512 / (p.bf16 ? BB : BB32) : W <= 16 ? 128 : 64, 2);
 }
 
 // Totals of 8 R values over L lanes: each halving step sums two lanes' values and keeps
@@ -648,15 +650,15 @@ int launch_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
 }
 template <typename T>
 int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
-    constexpr int R = sizeof(T) == 2 ? BR : 1;
-    if (p.d <= 64) return launch_bwd<T, 1, 8, 128, BB, R>(p, a, s);
-    if (p.d <= 128) return launch_bwd<T, 1, 16, 128, BB, R>(p, a, s);
+    constexpr int R = BR, B = sizeof(T) == 2 ? BB : BB32;
+    if (p.d <= 64) return launch_bwd<T, 1, 8, 128, B, R>(p, a, s);
+    if (p.d <= 128) return launch_bwd<T, 1, 16, 128, B, R>(p, a, s);
     const int W = row_warps(p.d);
     switch (W) {
-        case 1: return launch_bwd<T, 1, 32, 128, BB, R>(p, a, s);
-        case 2: return launch_bwd<T, 2, 32, 128, BB, R>(p, a, s);
-        case 3: return launch_bwd<T, 3, 32, 96, BB * 4 / 3, R>(p, a, s);
-        case 4: return launch_bwd<T, 4, 32, 128, BB, R>(p, a, s);
+        case 1: return launch_bwd<T, 1, 32, 128, B, R>(p, a, s);
+        case 2: return launch_bwd<T, 2, 32, 128, B, R>(p, a, s);
+        case 3: return launch_bwd<T, 3, 32, 96, B * 4 / 3, R>(p, a, s);
+        case 4: return launch_bwd<T, 4, 32, 128, B, R>(p, a, s);
     }
     if (W <= 8) return launch_bwd<T, 0, 32, 256, 2, 1>(p, a, s);
     if (W <= 16) return launch_bwd<T, 0, 32, 512, 1, 1>(p, a, s);
