@@ -26,7 +26,8 @@ class BlockStack:
 
     ``forward(x)`` returns z [T,N,d]; ``backward(dz)`` returns dx and leaves every parameter's
     gradient in ``grads[l][name]``.  Both run on the current stream, or on ``stream``, and write the
-    same buffers in every call.
+    same buffers in every call: an ``x`` that is one of them (the z or dx of an earlier call) is refused,
+    since the backward reads x again; give a copy.
     """
 
     def __init__(self, p, layers, norm=None, balance=None, token_mask=None, device="cuda"):
@@ -65,8 +66,10 @@ class BlockStack:
         return mine, [None] * 2 if after is None else [after.get("pre_w"), after.get("pre_b")]
 
     def forward(self, x, stream=None):
+        if any(x.data_ptr() == t.data_ptr() for t in (*self.z, self.dz)):
+            raise ValueError("x is a buffer of the stack, which its own calls overwrite: give a copy")
         p, stream = self.p, _stream(stream)
-        self.x = x  # the backward reads it again
+        self.x = x
         _, pre = self._norm_args(None, self.layers[0])
         vmoe_block_norm(p, self.norm, x, None, None, None, None, *pre, None, self.runners[0].inp["x"], None,
                         self.pre_stat[0], stream)

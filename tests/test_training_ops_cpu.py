@@ -130,3 +130,14 @@ def test_the_binding_refuses_tensors_it_would_misread():
 def test_dlogits_add_is_a_known_flag():
     p = vm.problem(2, 64, 128, 256, 4, 2, 1.25, "bf16", flags=vm.VMOE_DLOGITS_ADD)
     assert vm.vmoe_problem_capacity(p) == 40
+
+
+def test_a_stack_refuses_its_own_buffers_as_input():
+    """The backward reads x again: an x that the forward or the backward overwrites gives another gradient."""
+    p = vm.problem(2, 4, 8, 8, 2, 1, 1.0, "f32")
+    w = dict(w_router=torch.zeros(2, 8, 2), w1=torch.zeros(2, 2, 8, 8), w2=torch.zeros(2, 2, 8, 8))
+    st = vm.BlockStack(p, [w, w], device="cpu")
+    for x in (st.z[0], st.z[-1], st.z[-1].view(-1), st.dz):
+        with pytest.raises(ValueError, match="copy"):
+            st.forward(x)
+    assert st.x is None
