@@ -36,7 +36,7 @@ class AdamW:
             if eight:
                 t["m_scale"], t["v_scale"] = (torch.zeros((n + 255) // 256, device=dev) for _ in range(2))
             if master and p.dtype == torch.bfloat16:
-                t["master"] = p.float()
+                t["master"] = p.detach().float()
             self.tensors.append(t)
         self.table = adamw_tensors(self.tensors)
         self.step_dev = self.lr_factor = None

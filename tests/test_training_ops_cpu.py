@@ -141,3 +141,12 @@ def test_a_stack_refuses_its_own_buffers_as_input():
         with pytest.raises(ValueError, match="copy"):
             st.forward(x)
     assert st.x is None
+
+
+def test_states_of_a_parameter_that_requires_a_gradient_hold_no_graph(monkeypatch):
+    """The master copy of a leaf is plain memory: not a node of a graph that keeps the leaf's history."""
+    import paper_2608_16188_gb300.optim as optim
+    monkeypatch.setattr(optim, "adamw_tensors", lambda t: t)  # host tensors have no table
+    w = torch.zeros(512, dtype=torch.bfloat16, requires_grad=True)
+    o = vm.AdamW([dict(param=w, grad=torch.zeros_like(w))])
+    assert not o.tensors[0]["master"].requires_grad
