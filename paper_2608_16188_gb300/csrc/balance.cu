@@ -539,8 +539,9 @@ balance_bwd_kernel(Dims p, const float *logits, const uint8_t *__restrict__ mask
 #pragma unroll
             for (int j = 0; j < V; j += 4) {
                 const int e = column<L>(lane, j);
-                const f32x2 lo = mul2(mul2(x[r][j / 2], pk2(inv)), add2(c[j / 2], add));
-                const f32x2 hi = mul2(mul2(x[r][j / 2 + 1], pk2(inv)), add2(c[j / 2 + 1], add));
+                // 0 for a token that does not take part, also where c is no number
+                const f32x2 lo = inv == 0.0f ? 0 : mul2(mul2(x[r][j / 2], pk2(inv)), add2(c[j / 2], add));
+                const f32x2 hi = inv == 0.0f ? 0 : mul2(mul2(x[r][j / 2 + 1], pk2(inv)), add2(c[j / 2 + 1], add));
                 if (VEC) {
                     if (e < E) *reinterpret_cast<ulonglong2 *>(out + e) = make_ulonglong2(lo, hi);
                 } else {

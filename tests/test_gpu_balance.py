@@ -192,3 +192,20 @@ def test_losses_against_differences():
                 y[0, n, e] += h
                 v.append(float((_run(p, y.cuda(), idx, None, dl)["loss"].double() * dl.double()).sum()))
             assert abs((v[0] - v[1]) / 0.04 - grad[0, n, e]) < 2e-4
+
+
+@pytest.mark.parametrize("E", [7, 32, 256])
+def test_what_takes_no_part_gets_zero_whatever_its_task_holds(E):
+    """Padding and a token all at -inf, in a task with a NaN logit and in one whose losses have infinite weights."""
+    T, N, k = 3, 70, 2
+    x, idx, dloss = _inputs(T, N, E, k, seed=19)
+    mask = torch.ones(T, N, dtype=torch.uint8)
+    mask[:, 40:] = 0
+    x[:, 3] = float("-inf")
+    x[0, 5, 2] = float("nan")
+    dloss[1] = float("inf")
+    o = _run(_problem(T, N, E, k), x.cuda(), idx.cuda(), mask.cuda(), dloss.cuda())
+    d = o["dlogits"].cpu()
+    assert torch.isnan(o["excess"][0]).any() and not torch.isfinite(d[:2, :3]).all()
+    assert torch.all(d[:, 40:] == 0) and torch.all(d[:, 3] == 0)
+    _check({n: v[2:] for n, v in o.items()}, x[2:], idx[2:], mask[2:], dloss[2:])
