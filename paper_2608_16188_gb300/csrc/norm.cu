@@ -386,6 +386,13 @@ template <typename T>
 struct BwdRow {
     Raw8<T> y, z, dz, du;
     float2 py, pz;  // mean, rstd
+    __device__ __forceinline__ void zero() {
+        y.zero();
+        z.zero();
+        dz.zero();
+        du.zero();
+        py = pz = make_float2(0.0f, 0.0f);
+    }
 };
 
 // ALL: every input is there and the branch has a norm, known to the compiler (49 us at 17 x
@@ -427,7 +434,8 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
         }
     }
     f32x2 A[4] = {}, B[4] = {}, Pw[4] = {}, Pb[4] = {};
-    // as in the forward, others are read in the place of what lies behind the end
+    // as in the forward, others are read in the place of what lies behind the end; rows there
+    // become zeros before they are used (a branch that the last step of a slice takes)
     const int cc = have ? c : 0;
     const long long base = (long long)t * N;
     auto task = [&](const void *p) { return (const T *)p + (p ? base * d : 0); };
@@ -437,11 +445,8 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     BwdRow<T> next[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        next[r].y.zero();
-        next[r].z.zero();
-        next[r].dz.zero();
-        next[r].du.zero();
-        next[r].py = next[r].pz = make_float2(0.0f, 1.0f);
+        next[r].zero();
+        next[r].py.y = next[r].pz.y = 1.0f;
     }
     auto fetch = [&](int n0) {
 #pragma unroll
@@ -464,12 +469,16 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     for (int n0 = beg; n0 < end; n0 += groups * R, flip ^= 1) {
         if (!AHEAD) fetch(n0);
         f32x2 e[R][4], zh[R][4], yh[R][4];
-        float rz[R], ry[R], in[R], v[8 * R];
+        float rz[R], ry[R], v[8 * R];
+        if (n0 + groups * R > end) {  // zeros add nothing to the columns' sums
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (n0 + group * R + r >= end) next[r].zero();
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            in[r] = n0 + group * R + r < end ? 1.0f : 0.0f;
-            rz[r] = next[r].pz.y * in[r];
-            ry[r] = next[r].py.y * in[r];
+            rz[r] = next[r].pz.y;
+            ry[r] = next[r].py.y;
             const f32x2 mz = pk2(-next[r].pz.x), my = pk2(-next[r].py.x);
             f32x2 du[4], s[7];
             next[r].dz.get(e[r]);
@@ -481,7 +490,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
                 zh[r][i] = mul2(add2(zh[r][i], mz), pk2(rz[r]));
                 yh[r][i] = mul2(add2(yh[r][i], my), pk2(ry[r]));
                 Pw[i] = fma2(du[i], zh[r][i], Pw[i]);
-                Pb[i] = fma2(du[i], pk2(in[r]), Pb[i]);
+                Pb[i] = add2(Pb[i], du[i]);
                 const f32x2 g = mul2(du[i], pw[i]);
                 e[r][i] = fma2(pk2(rz[r]), g, e[r][i]);
                 const f32x2 ea = mul2(e[r][i], aw[i]), za = mul2(zh[r][i], aw[i]);
@@ -521,7 +530,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             for (int i = 0; i < 4; ++i) {
                 e[r][i] = fma2(pk2(-m2), zh[r][i], add2(e[r][i], pk2(-m1)));
                 A[i] = fma2(e[r][i], yh[r][i], A[i]);
-                B[i] = fma2(e[r][i], pk2(in[r]), B[i]);
+                B[i] = add2(B[i], e[r][i]);
                 q[i] = mul2(pk2(ry[r]), fma2(pk2(-k2), yh[r][i], fma2(e[r][i], aw[i], pk2(-k1))));
                 if (has_y) e[r][i] = mul2(e[r][i], pk2(a.rho));
             }

@@ -205,3 +205,18 @@ def test_no_dz_and_no_parameter_gradients():
                            None, None, None, None, None, ws)
     torch.cuda.synchronize()
     assert torch.equal(dx, a["dx"]) and torch.equal(dy, a["dy"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,d", [(1, 8), (5, 64), (3, 104), (7, 200), (1, 256), (33, 512), (101, 768), (5, 1024), (301, 1000), (3, 1304)])
+def test_an_infinite_gradient_in_the_last_token_stays_in_its_column(N, d, dtype):
+    """Sums of one infinity and numbers are that infinity, in its column alone: nothing is added for rows of a
+    step that lie behind the last token."""
+    for part, grad, name in (("post", "dz", "dpost_b"), ("pre", "du", "dpre_b")):
+        s = _make(2, N, d, dtype, part, True, False, seed=5)
+        s[grad][1, N - 1, 3] = float("inf")
+        o = _run(s, dtype, part, True, False, 1.0)
+        got = o[name].cpu()
+        assert got[1, 3] == float("inf"), (part, got[1, 3])
+        got[1, 3] = 0.0
+        assert torch.isfinite(got).all(), part
