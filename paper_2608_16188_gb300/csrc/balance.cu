@@ -298,8 +298,10 @@ balance_kernel(Dims p, const float *__restrict__ logits, const int32_t *__restri
     int tokens = 0;
     f32x2 next[R][V / 2];
     unsigned next_in = 0;
+    int next_e = -1;  // a lane's first of the choices of those rows, which lie one after the other
     auto fetch = [&](int n0) {  // the warp's G x R rows from n0 on
         next_in = 0;
+        next_e = wl < min(G * R, end - n0) * k ? it[(long long)n0 * k + wl] : -1;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int n = n0 + group * R + r;
@@ -319,6 +321,7 @@ balance_kernel(Dims p, const float *__restrict__ logits, const int32_t *__restri
         for (int i = 0; i < SUM_RUN && n0 < end; ++i, n0 += STEP) {
             f32x2 x[R][V / 2];
             unsigned live = next_in;
+            int e = next_e;
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -340,14 +343,13 @@ balance_kernel(Dims p, const float *__restrict__ logits, const int32_t *__restri
                 if (on) lse_run = fmaf(lse, lse, lse_run);
             }
             live_rows += __popc(live);
-            // the choices of the warp's rows lie one after the other
             const int choices = G * R * k;
             const int32_t *ip = it + (long long)n0 * k;
             for (int j = wl; j - wl < choices; j += 32) {
                 const int row = j / k;
                 const unsigned bits = __shfl_sync(0xffffffffu, live, min(row / R, G - 1) * L);
                 if (j < choices && (bits >> (row % R) & 1)) {
-                    const int e = ip[j];
+                    if (j >= 32) e = ip[j];
                     if ((unsigned)e < (unsigned)E) atomicAdd(&sums.count[e], 1);
                 }
             }
