@@ -444,11 +444,13 @@ typedef struct {
  * v_scale[i / 256] * v[i]; a new scale is its block's largest magnitude / 448 (0
  * below 2^-100, where the block's moments become 0), and a value a = |m| / scale
  * becomes grid * floor(a / grid + (16 R + 8) / 2^20), at most 448, grid the step of
- * e4m3 at a: rounded up or down at random, a in the mean.  R is the low (m) or the
- * high (v) half of mix(0x51f6db5b i + 0x5e4087b3 place + 0x339cd49b t + 0xe32a5e87
- * seed) mod 2^32, place the tensor's index in the call, with mix(h): h = (h ^ h >>
- * 16) * 0x9e4a8af7, h = (h ^ h >> 15) * 0xa6bd2c99, h ^ h >> 16.  An infinite
- * moment makes its block's moments NaN.
+ * e4m3 at a: rounded up or down at random, a in the mean, but for a positive sqrt(v)
+ * becoming 2^-9 at least, one step: at 0 the next update would be m over eps.  Elements
+ * whose gradients stay 2^17 below their block's largest so move less than with fp32
+ * moments.  R is the low (m) or the high (v) half of mix(0x51f6db5b i + 0x5e4087b3
+ * place + 0x339cd49b t + 0xe32a5e87 seed) mod 2^32, place the tensor's index in the
+ * call, with mix(h): h = (h ^ h >> 16) * 0x9e4a8af7, h = (h ^ h >> 15) * 0xa6bd2c99,
+ * h ^ h >> 16.  An infinite moment makes its block's moments NaN.
  * The tensors' arrays may not overlap (not checked here; one array given twice is a
  * race).  numel < 2^38.  Asynchronous on `cuda_stream`; no workspace. */
 int vmoe_adamw(int n, const vmoe_adamw_tensor *tensors, const vmoe_adamw_config *config,

@@ -131,8 +131,9 @@ def dither_bits(n, place, step, seed, first=0):
     return (h & np.uint64(0xffff)).astype(np.int64), (h >> np.uint64(16)).astype(np.int64)
 
 
-def e4m3_encode(v, bits):
-    """(values, scale of each 256, distance of the rounding from its border in steps)."""
+def e4m3_encode(v, bits, root=False):
+    """(values, scale of each 256, distance of the rounding from its border in steps, steps).  ``root``: v is
+    sqrt(v), which does not become 0 where it is positive and its block has a scale, but one step at least."""
     n = v.size
     nb = (n + 255) // 256
     pad = np.zeros(nb * 256)
@@ -144,6 +145,8 @@ def e4m3_encode(v, bits):
     grid = 2.0 ** (np.maximum(np.frexp(a)[1] - 1, -6) - 3)
     pos = a / grid + (16 * bits + 8) / 2.0 ** 20
     q = np.minimum(grid * np.floor(pos), 448)
+    if root:
+        q = np.where(a > 0, np.maximum(q, 2.0 ** -9), q)
     return np.copysign(q, v), scale, np.abs(pos - np.round(pos)), grid
 
 

@@ -11,7 +11,11 @@
 // it would stand still, so both are rounded up or down at random with the value as the
 // mean.  The random numbers are a hash of (seed, step, tensor, element).  sqrt(v)
 // rather than v: e4m3's range, 2^17 from the block's largest value down, then covers
-// the gradients' range and not its square root.
+// that range of gradients and not its square root.  Below it the two roundings, each on a
+// grid of its own, must not part: m becomes a whole step now and then, and over a sqrt(v)
+// of 0 that would be an update of m / eps.  So a positive sqrt(v) is never rounded to 0
+// but to a step at least, which bounds |m| / sqrt(v) by the block's own ratio of the two
+// scales; such elements take shorter steps than with fp32 moments.
 //
 // A warp takes two blocks of 256 elements, 8 a lane of each: 16-byte loads of bf16, all
 // in flight at once, a block's largest magnitude by one warp reduction, one pass over
@@ -214,6 +218,11 @@ __device__ __forceinline__ float dither_any(float a, uint32_t bits) {
     const float low = fabsf(a) < 0.015625f ? 0.015625f : 0.0f * a;  // NaN for NaN
     return copysignf(dither(fabsf(a) + low, bits) - low, a);
 }
+// sqrt(v): a positive a is one step of e4m3 at least.
+__device__ __forceinline__ float dither_root(float a, uint32_t bits) {
+    const float q = dither_any(a, bits);
+    return a > 0.0f ? fmaxf(q, 0.001953125f) : q;
+}
 // dither of a positive a from 2^-6 on, with the high half of a hash and as a code: the
 // exponent and the first three bits of the mantissa, less the difference of the biases,
 // (127 - 7) << 3.  Shifted by 4 they are the top byte, modulo 256, and the random number's
@@ -413,7 +422,7 @@ __device__ __forceinline__ void store_moments(const Entry &e, const Rates &r, ui
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 y = unpk2(root[b][i]);
-                    root[b][i] = pk2(dither_any(y.x, random20<true>(h[b][2 * i])), dither_any(y.y, random20<true>(h[b][2 * i + 1])));
+                    root[b][i] = pk2(dither_root(y.x, random20<true>(h[b][2 * i])), dither_root(y.y, random20<true>(h[b][2 * i + 1])));
                 }
                 cv[b] = make_uint2(e4m3x4(root[b][0], root[b][1]), e4m3x4(root[b][2], root[b][3]));
             } else {
