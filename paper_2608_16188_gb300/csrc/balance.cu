@@ -13,11 +13,11 @@
 //
 // A row of E logits lies in the registers of L neighbouring lanes, V to a lane, and is
 // read once; L is the smallest power of two that holds it, and a lane works on R rows
-// at a time, with the next R rows' loads in flight.  exp(x - c) is taken with c the
-// row's first logit, the same in every lane without a round of shuffles; where that
-// overflows (a logit 69 above the first, a first one of -inf, one so large that c log2(e)
-// loses what is behind the point, NaN) the warp takes its rows again with their maxima.  The importances are summed less their even share, so
-// that what is left after M / E cancels keeps its bits, in runs of SUM_RUN rows a
+// at a time, with the next R rows' loads in flight.  exp(x - max) is taken with the row's
+// maximum, of R rows in one butterfly.  (Less the row's first logit, which needs no maximum,
+// the exponents of a row whose first expert is far below the others reach 100, where half
+// a step is 4e-6, and lse = c + log(sum) cancels.)  The importances are summed less their
+// even share, so that what is left after M / E cancels keeps its bits, in runs of SUM_RUN rows a
 // thread, then over the runs.
 #include <cooperative_groups.h>
 #include <math.h>
@@ -51,7 +51,7 @@ int lanes_of(int E) {
 }
 int rows_of(const Dims &p) { return BT / lanes_of(p.E) * R; }  // a CTA's rows at a time
 
-// CTAs that fill the card once: two an SM above 128 experts (112 to 128 registers), three
+// CTAs that fill the card once: two an SM above 128 experts (108 to 128 registers), three
 // below.
 int ctas_of(const Dims &p) { return 152 * (p.E > 128 ? 2 : 3); }
 
@@ -111,11 +111,31 @@ __device__ __forceinline__ void row_totals(float (&v)[Q]) {
         for (int i = 0; i < Q; ++i) v[i] = __shfl_sync(0xffffffffu, sum, i * (L / Q), L);
     }
 }
-template <int L>
-__device__ __forceinline__ float row_max(float v) {
+// The same for maxima (a NaN is passed over).
+template <int L, int Q>
+__device__ __forceinline__ void row_maxima(float (&v)[Q]) {
+    if constexpr (L < Q) {
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+        for (int o = L / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < Q; ++i) v[i] = fmaxf(v[i], __shfl_xor_sync(0xffffffffu, v[i], o));
+    } else {
+        const int lane = threadIdx.x % L;
+#pragma unroll
+        for (int h = Q / 2, o = L / 2; h > 0; h >>= 1, o >>= 1) {
+            const bool up = (lane & o) != 0;
+#pragma unroll
+            for (int i = 0; i < h; ++i) {
+                const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+                v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+            }
+        }
+#pragma unroll
+        for (int o = L / Q / 2; o > 0; o >>= 1) v[0] = fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], o));
+        const float top = v[0];
+#pragma unroll
+        for (int i = 0; i < Q; ++i) v[i] = __shfl_sync(0xffffffffu, top, i * (L / Q), L);
+    }
 }
 
 // Column of a lane's value i: runs of four, one after the other over the lanes.
@@ -147,17 +167,25 @@ __device__ __forceinline__ void load_row(const float *row, int E, int lane, bool
     }
 }
 
-// x[r] becomes exp(x[r] - c[r]); `row(r)` reads row r again.
-template <int L, int V, bool VEC, typename F>
-__device__ __forceinline__ void exp_rows(f32x2 (&x)[R][V / 2], float (&c)[R], float (&sum)[R], F row) {
+// x[r] becomes exp(x[r] - c[r]), c[r] the row's maximum (0 where that is -inf: nowhere to
+// go, a sum of 0; NaN and +inf make the sum NaN).
+template <int L, int V>
+__device__ __forceinline__ void exp_rows(f32x2 (&x)[R][V / 2], float (&c)[R], float (&sum)[R]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        c[r] = __shfl_sync(0xffffffffu, unpk2(x[r][0]).x, 0, L);
-        const f32x2 mc = pk2(-c[r] * LOG2E);
+        c[r] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) c[r] = fmaxf(c[r], fmaxf(unpk2(x[r][i]).x, unpk2(x[r][i]).y));
+    }
+    row_maxima<L, R>(c);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (c[r] == -INFINITY) c[r] = 0.0f;
+        const f32x2 mc = pk2(-c[r]);
         f32x2 s = 0;
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) {
-            const float2 a = unpk2(fma2(x[r][i], pk2(LOG2E), mc));
+            const float2 a = unpk2(mul2(add2(x[r][i], mc), pk2(LOG2E)));
             x[r][i] = pk2(ex2(a.x), ex2(a.y));
             s = add2(s, x[r][i]);
         }
@@ -165,37 +193,6 @@ __device__ __forceinline__ void exp_rows(f32x2 (&x)[R][V / 2], float (&c)[R], fl
         sum[r] = two.x + two.y;
     }
     row_totals<L, R>(sum);
-    bool again = false;
-#pragma unroll
-    for (int r = 0; r < R; ++r) again |= !(sum[r] > 0.5f && sum[r] < 1e30f);
-    if (!__any_sync(0xffffffffu, again)) return;
-#pragma unroll 1
-    for (int q = 0; q < R; ++q) {
-        f32x2 v[V / 2];
-        row(q, v);
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) m = fmaxf(m, fmaxf(unpk2(v[i]).x, unpk2(v[i]).y));
-        m = row_max<L>(m);
-        if (m == -INFINITY) m = 0.0f;  // nowhere to go: a sum of 0; NaN and +inf make it NaN
-        float s[1] = {0.0f};
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) {
-            const float2 a = unpk2(v[i]);
-            const float lo = ex2((a.x - m) * LOG2E), hi = ex2((a.y - m) * LOG2E);
-            v[i] = pk2(lo, hi);
-            s[0] += lo + hi;
-        }
-        row_totals<L, 1>(s);
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r == q) {
-#pragma unroll
-                for (int i = 0; i < V / 2; ++i) x[r][i] = v[i];
-                c[r] = m;
-                sum[r] = s[0];
-            }
-    }
 }
 
 // A CTA's sums.
@@ -328,10 +325,7 @@ balance_kernel(Dims p, const float *__restrict__ logits, const int32_t *__restri
                 for (int j = 0; j < V / 2; ++j) x[r][j] = next[r][j];
             if (n0 + STEP < end) fetch(n0 + STEP);
             float c[R], s[R];
-            const unsigned in = live;
-            exp_rows<L, V, VEC>(x, c, s, [&](int r, f32x2 (&v)[V / 2]) {
-                load_row<L, V, VEC>(lt + (long long)(n0 + group * R + r) * E, E, lane, (in >> r & 1) != 0, v);
-            });
+            exp_rows<L, V>(x, c, s);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if (s[r] == 0.0f) live &= ~(1u << r);
@@ -519,9 +513,7 @@ balance_bwd_kernel(Dims p, const float *logits, const uint8_t *__restrict__ mask
             for (int j = 0; j < V / 2; ++j) x[r][j] = next[r][j];
         if (n0 + STEP < end) fetch(n0 + STEP);
         float base[R], s[R], mean[R];
-        exp_rows<L, V, VEC>(x, base, s, [&](int r, f32x2 (&v)[V / 2]) {
-            load_row<L, V, VEC>(lt + (long long)(n0 + group * R + r) * E, E, lane, (in >> r & 1) != 0, v);
-        });
+        exp_rows<L, V>(x, base, s);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             f32x2 m = 0;
