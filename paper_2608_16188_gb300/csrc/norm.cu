@@ -319,7 +319,10 @@ struct JoinArgs {
         const float g = gate ? gate[at] : 1.0f, w = post_w ? post_w[at] : 1.0f, b = post_b ? post_b[at] : 0.0f;
         if (dpost_w) dpost_w[at] = g * s[0];
         if (dpost_b) dpost_b[at] = g * s[1];
-        if (dgate) dgate[at] = fmaf(w, s[0], b * s[1]);
+        if (dgate) {  // a weight or a bias of 0, or none, adds nothing, also where the other sum is infinite
+            const float bs = b == 0.0f && isinf(s[1]) ? 0.0f : b * s[1];
+            dgate[at] = w == 0.0f && isinf(s[0]) ? bs : fmaf(w, s[0], bs);
+        }
         if (dpre_w) dpre_w[at] = s[2];
         if (dpre_b) dpre_b[at] = s[3];
     }
