@@ -398,9 +398,9 @@ struct BwdRow {
     }
 };
 
-// ALL: every input is there and the branch has a norm, known to the compiler (49 us at 17 x
-// 1576 tokens of 768 channels, 55 without).
-template <typename T, int WC, int L, int MAXT, int MINB, int R, bool AHEAD, bool ALL>
+// POST: there is a branch and it has a norm.  ALL: and every input is there, known to the
+// compiler (49 us at 17 x 1576 tokens of 768 channels, 55 without).
+template <typename T, int WC, int L, int MAXT, int MINB, int R, bool AHEAD, bool POST, bool ALL>
 __global__ void __launch_bounds__(MAXT, MINB)
 norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     __shared__ float totals[2][32][16];
@@ -411,8 +411,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
     const int beg = (int)((long long)N * blockIdx.x / gridDim.x), end = (int)((long long)N * (blockIdx.x + 1) / gridDim.x);
     const bool have = c < d;
     const float share = 1.0f / (float)d, centre = a.rms ? 0.0f : share;
-    const bool has_u = ALL || a.du != nullptr, has_z = ALL || a.dz != nullptr, has_y = ALL || a.y != nullptr;
-    const bool post = ALL || a.post;
+    const bool has_u = ALL || a.du != nullptr, has_z = ALL || a.dz != nullptr, has_y = POST || a.y != nullptr;
     pdl_wait();
     f32x2 pw[4], aw[4];  // pre_w; gate . post_w
     float sum_aw;
@@ -463,7 +462,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             if (has_z) next[r].dz.load(dz0 + at);
             if (has_y) {
                 next[r].y.load(y0 + at);
-                if (post) next[r].py = py0[n];
+                if (POST) next[r].py = py0[n];
             }
         }
     };
@@ -496,9 +495,10 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
                 Pb[i] = add2(Pb[i], du[i]);
                 const f32x2 g = mul2(du[i], pw[i]);
                 e[r][i] = fma2(pk2(rz[r]), g, e[r][i]);
-                const f32x2 ea = mul2(e[r][i], aw[i]), za = mul2(zh[r][i], aw[i]);
                 s[0] = i ? add2(s[0], g) : g;
                 s[1] = i ? fma2(g, zh[r][i], s[1]) : mul2(g, zh[r][i]);
+                if (!POST) continue;  // the others are for the norm on the branch
+                const f32x2 ea = mul2(e[r][i], aw[i]), za = mul2(zh[r][i], aw[i]);
                 s[2] = i ? add2(s[2], ea) : ea;
                 s[3] = i ? fma2(ea, yh[r][i], s[3]) : mul2(ea, yh[r][i]);
                 s[4] = i ? add2(s[4], za) : za;
@@ -506,7 +506,7 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
                 s[6] = i ? fma2(za, yh[r][i], s[6]) : mul2(za, yh[r][i]);
             }
 #pragma unroll
-            for (int i = 0; i < 7; ++i) v[8 * r + i] = sum2(s[i]);
+            for (int i = 0; i < 7; ++i) v[8 * r + i] = POST || i < 2 ? sum2(s[i]) : 0.0f;
             v[8 * r + 7] = 0.0f;
         }
         if (AHEAD && n0 + groups * R < end) fetch(n0 + groups * R);
@@ -526,15 +526,16 @@ norm_bwd_kernel(Dims p, BwdArgs a, int warps, int groups) {
             for (int i = 0; i < 7; ++i) s[i] = L < 8 * R ? __shfl_sync(0xffffffffu, sum[r], i, L) : __shfl_sync(0xffffffffu, sum[0], 8 * r + i, L);
             const int n = n0 + group * R + r;
             const float z1 = has_u ? rz[r] : 0.0f, m1 = z1 * centre * s[0], m2 = z1 * share * s[1];
-            const float k1 = post ? centre * (s[2] - m1 * sum_aw - m2 * s[4]) : 0.0f;
-            const float k2 = post ? share * (s[3] - m1 * s[5] - m2 * s[6]) : 0.0f;
+            const float k1 = POST ? centre * (s[2] - m1 * sum_aw - m2 * s[4]) : 0.0f;
+            const float k2 = POST ? share * (s[3] - m1 * s[5] - m2 * s[6]) : 0.0f;
             f32x2 q[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 e[r][i] = fma2(pk2(-m2), zh[r][i], add2(e[r][i], pk2(-m1)));
                 A[i] = fma2(e[r][i], yh[r][i], A[i]);
                 B[i] = add2(B[i], e[r][i]);
-                q[i] = mul2(pk2(ry[r]), fma2(pk2(-k2), yh[r][i], fma2(e[r][i], aw[i], pk2(-k1))));
+                const f32x2 ea = mul2(e[r][i], aw[i]);  // dy without a norm, whatever y holds
+                q[i] = POST ? mul2(pk2(ry[r]), fma2(pk2(-k2), yh[r][i], fma2(e[r][i], aw[i], pk2(-k1)))) : ea;
                 if (has_y) e[r][i] = mul2(e[r][i], pk2(a.rho));
             }
             if (have && n < end) {
@@ -657,8 +658,9 @@ int launch_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
         if (a.parts) return launch_kernel(kern, grid, block, (size_t)(groups - 1) * 4 * p.d * sizeof(float), s, p, a, W, groups);
         return launch_cluster(kern, grid, block, (size_t)std::max(1, groups - 1) * 4 * p.d * sizeof(float), slices, s, p, a, W, groups);
     };
-    if (WC && a.du && a.dz && a.y && a.post) return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, WC != 0>);
-    return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, false>);
+    if (!a.y || !a.post) return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, false, false>);
+    if (WC && a.du && a.dz) return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, true, WC != 0>);
+    return go(norm_bwd_kernel<T, WC, L, MAXT, MINB, R, MAXT <= 512, true, false>);
 }
 template <typename T>
 int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {

@@ -1,10 +1,15 @@
-"""vmoe_block_norm_bwd with infinities, on a GB300: a sum of one infinity and numbers is that infinity."""
+"""vmoe_block_norm_bwd with infinities, on a GB300: a sum of one infinity and numbers is that infinity, and what
+does not depend on a value is a number whatever that value is.  Signs are exact; numbers within half a step of
+the type and 4e-6 of the value (three products in fp32)."""
 import pytest
 import torch
 
 import paper_2608_16188_gb300 as vm
 
 pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
 
 @pytest.fixture(scope="module", autouse=True)
 def _lib():
@@ -55,3 +60,18 @@ def test_an_infinite_gradient_reaches_the_gate(N, d, dtype, form):
     assert sign != 0 and float(got[1, 3]) == sign * float("inf"), got[1, 3]
     got[1, 3] = 0.0
     assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,d", SIZES)
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_without_a_norm_the_gradient_of_the_branch_does_not_depend_on_it(N, d, dtype, value):
+    """dy = gate dz and dx = dz, whatever y holds; dgate = sum dz y has it in its column alone."""
+    y, dz, gate = _data(dtype, N, d, seed=5)
+    y[0, N // 2, 5] = value
+    dx, dy, g = _run(dtype, N, d, False, y, dz, gate)
+    assert torch.equal(dx, dz)
+    ref = gate[:, None, :].double() * dz.double()
+    assert ((dy.double() - ref).abs() <= (HALF[dtype] + 4e-6) * ref.abs()).all()
+    bad = ~torch.isfinite(g["g"].cpu())
+    assert bad[0, 5] and int(bad.sum()) == 1
