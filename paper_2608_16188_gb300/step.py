@@ -57,8 +57,8 @@ class BalanceBuffers:
     """Outputs of the balance losses of problem ``p``, and the losses' weights.
 
     ``weights``: three numbers (balance, importance, router z-loss), the same for every
-    task, or a [T, 3] fp32 device tensor: the gradient of the whole loss by each task's
-    three, which the caller may change between steps."""
+    task, or a contiguous [T, 3] fp32 device tensor: the gradient of the whole loss by each
+    task's three.  The tensor is kept, not copied: the caller may change it between steps."""
 
     def __init__(self, p, weights, device="cuda"):
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
@@ -69,9 +69,10 @@ class BalanceBuffers:
         self.workspace = new(vmoe_balance_workspace_size(p), dtype=torch.uint8)
         if not isinstance(weights, torch.Tensor):
             weights = torch.tensor([[float(w) for w in weights]], device=device).repeat(p.T, 1)
-        if tuple(weights.shape) != (p.T, 3) or weights.dtype != torch.float32:
-            raise ValueError("balance weights: three numbers, or [T, 3] in fp32")
-        self.dloss = weights.contiguous()
+        # a copy of a strided tensor would not see what the caller writes into it
+        if tuple(weights.shape) != (p.T, 3) or weights.dtype != torch.float32 or not weights.is_contiguous():
+            raise ValueError("balance weights: three numbers, or a contiguous [T, 3] in fp32")
+        self.dloss = weights
 
 
 class StepRunner:
