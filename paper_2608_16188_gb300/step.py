@@ -145,7 +145,10 @@ class HostPipeline:
     activations, gradients) is shared, as the steps run in order on one compute
     stream.  The copies run on their own stream: step i+1's x and dY upload while
     step i computes, y of step i is read back while its backward runs, and dX as
-    soon as it is done.  ``weights`` holds w_router, bias, w1, w2 on the device.
+    soon as it is done.  ``weights`` holds w_router, bias, w1, w2 on the device, and
+    may hold token_mask, for steps that bring none of their own.
+    With ``balance`` (see StepRunner) a step's losses and counts are read back too if
+    its outputs ask for them; the BalanceBuffers hold those of the last step alone.
     """
 
     def __init__(self, p, weights, bufs: Buffers | None = None, device="cuda",
@@ -163,44 +166,75 @@ class HostPipeline:
             inp["x"] = torch.empty_like(base.y)
             inp["dy"] = torch.empty_like(base.y)
             self.slots.append(StepRunner(p, inp, b, router_grad=router_grad, balance=balance))
+        self.mask = weights.get("token_mask")
+        if balance is not None:  # each slot's: a step's mask, and its losses and counts until they are read back
+            self.masks = [torch.empty((p.T, p.N), dtype=torch.uint8, device=device) for _ in range(2)]
+            self.found = [(torch.empty_like(balance.loss), torch.empty_like(balance.count)) for _ in range(2)]
         self.copy_stream = torch.cuda.Stream(device)
         ev = lambda: [torch.cuda.Event() for _ in range(2)]  # noqa: E731
         self.h2d, self.fwd, self.done, self.d2h = ev(), ev(), ev(), ev()
 
-    def _upload(self, slot, x_host, dy_host):
+    def _upload(self, slot, x_host, dy_host, mask_host=None):
         r = self.slots[slot]
         with torch.cuda.stream(self.copy_stream):
             r.inp["x"].copy_(x_host, non_blocking=True)
             r.inp["dy"].copy_(dy_host, non_blocking=True)
+            if mask_host is not None:
+                self.masks[slot].copy_(mask_host, non_blocking=True)
         self.h2d[slot].record(self.copy_stream)
+        return self.mask if mask_host is None else self.masks[slot]
+
+    def _check(self, inputs, outputs):
+        have = self.slots[0].balance is not None
+        shape = (self.p.T, self.p.N)
+        for i, o in zip(inputs, outputs):
+            mask = i[2] if len(i) > 2 else None
+            if not have and (mask is not None or any(t is not None for t in o[2:])):
+                raise ValueError("token masks, losses and counts belong to the balance losses: give balance")
+            if mask is not None and (tuple(mask.shape) != shape or mask.dtype != torch.uint8):
+                raise ValueError("a step's token mask: [T, N] in uint8")
 
     def run(self, inputs, outputs, stream=None):
         """inputs[i] = (x, dY) and outputs[i] = (y, dX): pinned host tensors of
         step i.  Enqueues every step and returns; synchronise the copy stream (or
-        the device) before reading the outputs."""
+        the device) before reading the outputs.
+
+        With balance losses inputs[i] may have a third entry, the step's token_mask
+        [T,N] uint8 (None: the one in ``weights``, if any), and outputs[i] a third
+        and a fourth, its losses [T,3] fp32 and counts [T,E] int32 (either None)."""
         cs = stream if stream is not None else torch.cuda.current_stream()
         steps = len(inputs)
         if steps == 0:
             return
-        self._upload(0, *inputs[0])
+        self._check(inputs, outputs)
+        masks = [None, None]
+        masks[0] = self._upload(0, *inputs[0])
         for i in range(steps):
             s = i % 2
             r = self.slots[s]
+            r.inp["token_mask"] = masks[s]
             cs.wait_event(self.h2d[s])
             if i >= 2:  # this slot's y / dX of step i-2 have been read back
                 cs.wait_event(self.d2h[s])
             r.forward(cs)
+            more = [(h, n) for h, n in zip(outputs[i][2:], range(2)) if h is not None]
+            if more:  # the next step's losses take their place
+                with torch.cuda.stream(cs):
+                    for _, n in more:
+                        self.found[s][n].copy_((r.balance.loss, r.balance.count)[n])
             self.fwd[s].record(cs)
             r.backward(cs)
             self.done[s].record(cs)
             if i + 1 < steps:  # the other slot is free once step i-1 has finished
                 if i >= 1:
                     self.copy_stream.wait_event(self.done[s ^ 1])
-                self._upload(s ^ 1, *inputs[i + 1])
-            y_host, dx_host = outputs[i]
+                masks[s ^ 1] = self._upload(s ^ 1, *inputs[i + 1])
+            y_host, dx_host = outputs[i][:2]
             self.copy_stream.wait_event(self.fwd[s])
             with torch.cuda.stream(self.copy_stream):
                 y_host.copy_(r.b.y, non_blocking=True)
+                for host, n in more:
+                    host.copy_(self.found[s][n], non_blocking=True)
             self.copy_stream.wait_event(self.done[s])
             with torch.cuda.stream(self.copy_stream):
                 dx_host.copy_(r.b.dx, non_blocking=True)
