@@ -49,18 +49,15 @@ class AdamW:
         """One update from the gradients.  ``grad_scale``: a [1] fp32 device tensor that they are
         taken times; one that is infinite or NaN leaves everything as it was but for the step's
         number.  ``stream``: a torch.cuda.Stream, or None for the current one."""
-        self.steps += 1
         if self.step_dev is None:
-            vmoe_adamw(self.table, self.steps, self.lr, *self.betas, self.eps, self.seed, grad_scale=grad_scale,
+            vmoe_adamw(self.table, self.steps + 1, self.lr, *self.betas, self.eps, self.seed, grad_scale=grad_scale,
                        stream=_stream(stream))
-            return
-        if stream is not None:
+        else:  # counted behind the call: one that is refused leaves the number as it was
+            vmoe_adamw(self.table, 1, self.lr, *self.betas, self.eps, self.seed, self.step_dev, self.lr_factor, grad_scale,
+                       stream=_stream(stream))
             with torch.cuda.stream(stream):
                 self.step_dev.add_(1)
-        else:
-            self.step_dev.add_(1)
-        vmoe_adamw(self.table, 0, self.lr, *self.betas, self.eps, self.seed, self.step_dev, self.lr_factor, grad_scale,
-                   stream=_stream(stream))
+        self.steps += 1
 
     def moments(self, i):
         """(m, v) of tensor i as fp32 values."""
