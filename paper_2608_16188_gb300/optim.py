@@ -14,7 +14,8 @@ class AdamW:
     or weight_decay (this one instead of the common one).
     ``eight_bit``: moments of tensors of at least ``eight_bit_from`` elements in 8 bits.
     ``master``: an fp32 copy of bf16 parameters, which the updates work on; without it updates
-    below half a bf16 step are lost.
+    below half a bf16 step are lost.  The parameters are written from it: call
+    ``refresh_master`` after loading others into them.
     ``capturable``: the step number is counted on the device, so that ``step`` may be captured
     into a CUDA graph and replayed; ``lr_factor`` [1], a device tensor that the learning rate is
     taken times, is then the way to change it.
@@ -58,6 +59,42 @@ class AdamW:
             with torch.cuda.stream(stream):
                 self.step_dev.add_(1)
         self.steps += 1
+
+    def refresh_master(self, stream=None):
+        """Takes the master copies from the parameters again, after something else than ``step`` wrote them."""
+        with torch.cuda.stream(stream):
+            for t in self.tensors:
+                if t.get("master") is not None:
+                    t["master"].copy_(t["param"].detach())
+
+    STATE = ("m", "v", "m_scale", "v_scale", "master")
+
+    def state_dict(self):
+        """What a later run needs to go on, beside the parameters: the step's number, the seed of the 8-bit moments'
+        rounding, and each tensor's moments, scales and master copy (the arrays themselves, not copies)."""
+        out = dict(step=self.steps if self.step_dev is None else int(self.step_dev), seed=self.seed,
+                   tensors=[{k: t[k] for k in self.STATE if t.get(k) is not None} for t in self.tensors])
+        if self.lr_factor is not None:
+            out["lr_factor"] = float(self.lr_factor)
+        return out
+
+    def load_state_dict(self, state):
+        """Goes on from ``state``, of an AdamW over tensors of the same sizes in the same order, with the same kinds of
+        moments.  Written in place, so that captured graphs see it (their seed stays theirs)."""
+        theirs = state["tensors"]
+        if len(theirs) != len(self.tensors):
+            raise ValueError("a state of %d tensors for %d" % (len(theirs), len(self.tensors)))
+        for i, (t, s) in enumerate(zip(self.tensors, theirs)):
+            mine = {k: (tuple(t[k].shape), t[k].dtype) for k in self.STATE if t.get(k) is not None}
+            if mine != {k: (tuple(v.shape), v.dtype) for k, v in s.items()}:
+                raise ValueError("tensor %d: a state of other sizes, moments or master copies" % i)
+        for t, s in zip(self.tensors, theirs):
+            for k, v in s.items():
+                t[k].copy_(v)
+        self.steps, self.seed = int(state["step"]), state["seed"]
+        if self.step_dev is not None:
+            self.step_dev.fill_(self.steps)
+            self.lr_factor.fill_(state.get("lr_factor", 1.0))
 
     def moments(self, i):
         """(m, v) of tensor i as fp32 values."""

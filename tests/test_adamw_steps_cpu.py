@@ -36,3 +36,49 @@ def test_a_refused_step_is_not_counted(calls, capturable):
     o.step()
     assert seen == [1, 2] and o.steps == 2
     assert not capturable or int(o.step_dev) == 2
+
+
+def _opt(sizes, **kw):
+    return vm.AdamW([dict(param=torch.randn(n).to(torch.bfloat16), grad=torch.zeros(n, dtype=torch.bfloat16)) for n in sizes], **kw)
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+def test_a_state_is_taken_over_in_place(calls, capturable):
+    seen, _ = calls
+    a, b = (_opt((300, 5000), eight_bit=True, seed=s, capturable=c) for s, c in ((7, not capturable), (1, capturable)))
+    for _ in range(3):
+        a.step()
+    for t in a.tensors:
+        for k in a.STATE:
+            if t.get(k) is not None:
+                t[k].copy_(torch.rand(t[k].shape))
+    kept = [{k: t.get(k) for k in b.STATE} for t in b.tensors]
+    b.load_state_dict(a.state_dict())
+    assert b.seed == 7 and [sorted(s) for s in a.state_dict()["tensors"]] == [["m", "master", "v"], ["m", "m_scale", "master", "v", "v_scale"]]
+    for t, s, k in zip(a.tensors, b.tensors, kept):
+        for n in b.STATE:
+            assert s.get(n) is k[n]  # the addresses that the table holds
+            assert k[n] is None or torch.equal(k[n].view(torch.uint8), t[n].view(torch.uint8)), n
+    seen.clear()
+    b.step()
+    assert seen == [4] and b.state_dict()["step"] == 4
+
+
+def test_a_state_of_something_else_is_refused(calls):
+    o = _opt((300, 5000), eight_bit=True)
+    before = [t["m"].clone() for t in o.tensors]
+    for other in (_opt((300,), eight_bit=True), _opt((300, 5001), eight_bit=True), _opt((300, 5000)),
+                  _opt((300, 5000), eight_bit=True, master=False)):
+        for t in other.tensors:
+            t["m"].fill_(1.0)
+        with pytest.raises(ValueError):
+            o.load_state_dict(other.state_dict())
+    assert all(torch.equal(t["m"].view(torch.uint8), m.view(torch.uint8)) for t, m in zip(o.tensors, before)) and o.steps == 0
+
+
+def test_master_copies_follow_parameters_that_were_loaded(calls):
+    o = _opt((300, 20))
+    for t in o.tensors:
+        t["param"].fill_(2.5)
+    o.refresh_master()
+    assert all(torch.all(t["master"] == 2.5) for t in o.tensors)
