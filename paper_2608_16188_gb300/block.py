@@ -7,12 +7,19 @@ call.
 """
 from __future__ import annotations
 
+import bisect
+
 import torch
 
 from . import (VMOE_NORM_POST, _stream, norm_config, vmoe_block_norm, vmoe_block_norm_bwd, vmoe_block_norm_bwd_workspace_size)
 from .step import BalanceBuffers, Buffers, StepRunner
 
 NORM_PARAMS = ("pre_w", "pre_b", "post_w", "post_b", "gate")
+
+
+def _span(t):
+    """The bytes of a contiguous tensor, from and to."""
+    return t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
 
 
 class BlockStack:
@@ -26,8 +33,9 @@ class BlockStack:
 
     ``forward(x)`` returns z [T,N,d]; ``backward(dz)`` returns dx and leaves every parameter's
     gradient in ``grads[l][name]``.  Both run on the current stream, or on ``stream``, and write the
-    same buffers in every call: an ``x`` that is one of them (the z or dx of an earlier call) is refused,
-    since the backward reads x again; give a copy.
+    same buffers in every call: an ``x`` that lies in one of them (the z or dx of an earlier call, a
+    layer's y) is refused, since the backward reads x again; give a copy.  So is a ``dz`` in the last
+    layer's input gradient, which is written while dz is read; z and dx may be given.
     """
 
     def __init__(self, p, layers, norm=None, balance=None, token_mask=None, device="cuda"):
@@ -56,6 +64,11 @@ class BlockStack:
         self.dz = torch.empty_like(first)
         self.workspace = torch.empty(vmoe_block_norm_bwd_workspace_size(p), dtype=torch.uint8, device=device)
         self.x = None
+        own = [*self.z, self.dz, self.workspace, *self.pre_stat, *self.post_stat]
+        for r, g in zip(self.runners, self.grads):
+            own += [*vars(r.b).values(), r.inp["x"], r.inp["dy"], *g.values()]
+            own += [] if r.balance is None else [v for n, v in vars(r.balance).items() if n != "dloss"]
+        self._own = sorted({_span(t) for t in own if isinstance(t, torch.Tensor)})
 
     def _par(self, layer, name):
         return layer.get(name) if self.post or not name.startswith("post") else None
@@ -66,7 +79,9 @@ class BlockStack:
         return mine, [None] * 2 if after is None else [after.get("pre_w"), after.get("pre_b")]
 
     def forward(self, x, stream=None):
-        if any(x.data_ptr() == t.data_ptr() for t in (*self.z, self.dz)):
+        beg, end = _span(x)
+        last = bisect.bisect_left(self._own, (end, 0)) - 1  # the buffers do not overlap: the last that begins before x's end
+        if last >= 0 and self._own[last][1] > beg:
             raise ValueError("x is a buffer of the stack, which its own calls overwrite: give a copy")
         p, stream = self.p, _stream(stream)
         self.x = x
@@ -86,6 +101,11 @@ class BlockStack:
     def backward(self, dz, stream=None):
         if self.x is None:
             raise RuntimeError("backward before forward")
+        beg, end = _span(dz)
+        for t in (self.runners[-1].inp["dy"], self.dz):  # dx may be dz itself
+            b, e = _span(t)
+            if beg < e and b < end and not (t is self.dz and beg == b):
+                raise ValueError("dz lies in a buffer that is written while it is read: give a copy")
         p, stream = self.p, _stream(stream)
         du = None
         for i in reversed(range(len(self.runners))):
