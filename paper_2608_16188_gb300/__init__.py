@@ -201,6 +201,13 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _bytes(where, n):
+    """A count of bytes; a negative one would reach the library as a huge size_t and pass its checks."""
+    if n < 0:
+        raise VmoeError(VMOE_ERR_INVALID, "%s: %d bytes of workspace" % (where, n))
+    return int(n)
+
+
 def _check(st: int, where: str):
     if st != VMOE_OK:
         raise VmoeError(st, where)
@@ -257,7 +264,7 @@ def vmoe_expert_bwd(p, xe, h, a, w1, w2, dye, load, dxe, dw1, dw2, workspace, wo
         workspace_bytes = workspace.numel() * workspace.element_size()
     _check(library().vmoe_expert_bwd(ctypes.byref(p), _ptr(xe), _ptr(h), _ptr(a), _ptr(w1),
                                      _ptr(w2), _ptr(dye), _ptr(load), _ptr(dxe), _ptr(dw1),
-                                     _ptr(dw2), _ptr(workspace), int(workspace_bytes),
+                                     _ptr(dw2), _ptr(workspace), _bytes("vmoe_expert_bwd", workspace_bytes),
                                      _stream(stream)), "vmoe_expert_bwd")
 
 
@@ -295,7 +302,8 @@ def vmoe_attn_expert_bwd(p, heads, xe, qkv, o, lse, wqkv, wo, dye, load, dxe, dw
         workspace_bytes = workspace.numel() * workspace.element_size()
     _check(library().vmoe_attn_expert_bwd(
         ctypes.byref(p), int(heads), _ptr(xe), _ptr(qkv), _ptr(o), _ptr(lse), _ptr(wqkv), _ptr(wo),
-        _ptr(dye), _ptr(load), _ptr(dxe), _ptr(dwqkv), _ptr(dwo), _ptr(workspace), int(workspace_bytes),
+        _ptr(dye), _ptr(load), _ptr(dxe), _ptr(dwqkv), _ptr(dwo), _ptr(workspace),
+        _bytes("vmoe_attn_expert_bwd", workspace_bytes),
         _stream(stream)), "vmoe_attn_expert_bwd")
 
 
@@ -344,12 +352,12 @@ def _arrays(where, *args):
 
 def _workspace(where, t, nbytes):
     if t is None or isinstance(t, int):
-        return t, int(nbytes or 0)
+        return t, _bytes(where, nbytes or 0)
     have = t.numel() * t.element_size()
     at = t.get_device()
     if at < 0 or at != _device() or not t.is_contiguous() or (nbytes is not None and nbytes > have):
         raise VmoeError(VMOE_ERR_INVALID, "%s: the workspace" % where)
-    return t.data_ptr(), have if nbytes is None else int(nbytes)
+    return t.data_ptr(), have if nbytes is None else _bytes(where, nbytes)
 
 
 def vmoe_balance_workspace_size(p) -> int:
