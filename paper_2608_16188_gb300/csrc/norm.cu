@@ -119,6 +119,14 @@ int slices_of(const Dims &p, int R, int regs, int least) {
 // (one row and three to five CTAs 56 to 60, before other steps that took 3 off both); fp32
 // rows fill the registers of two CTAs: forward and backward of 3 x 1001 x 1000 26 us, 28 with
 // one row and three CTAs, 8 x 4096 x 1024 205 and 209.
+//
+// Above 1024 channels the compiler does not know the number of warps: up to 16 of 128
+// registers, with the next rows in flight, then 32 of 64 registers without (the backward
+// spills 400 to 650 bytes a thread).  8 x 1576 x 1024, bf16, both norms: 20.0 us forward and
+// 52.3 with the backward as above, 22.5 and 61.4 in the form for 16 warps; 4 x 1576 x 4096:
+// 50.9 and 125 in that, 77.9 and 209 in the one for 32.  There bf16 rows still go in twos
+// forward (29.0 us at 8 x 1576 x 1280, 42.7 one by one) and one by one backward (forward and
+// backward 77.7 us, 86.0 in twos and 255 registers; 114 and 111 at 2048 channels).
 constexpr int FR = 2, FB = 5, BR = 2, BB = 3, BB32 = 2;
 
 struct FwdArgs {
@@ -645,7 +653,6 @@ int run_fwd(const Dims &p, const FwdArgs &a, cudaStream_t s) {
         case 3: return go(norm_fwd_kernel<T, 3, 32, 96, FB * 4 / 3, R, true>, R, 512 / FB);
         case 4: return go(norm_fwd_kernel<T, 4, 32, 128, FB, R, true>, R, 512 / FB);
     }
-    if (W <= 8) return go(norm_fwd_kernel<T, 0, 32, 256, 2, R, true>, R, 128);
     if (W <= 16) return go(norm_fwd_kernel<T, 0, 32, 512, 1, R, true>, R, 128);
     return go(norm_fwd_kernel<T, 0, 32, 1024, 1, 1, false>, 1, 64);
 }
@@ -674,7 +681,6 @@ int run_bwd(const Dims &p, const BwdArgs &a, cudaStream_t s) {
         case 3: return launch_bwd<T, 3, 32, 96, B * 4 / 3, R>(p, a, s);
         case 4: return launch_bwd<T, 4, 32, 128, B, R>(p, a, s);
     }
-    if (W <= 8) return launch_bwd<T, 0, 32, 256, 2, 1>(p, a, s);
     if (W <= 16) return launch_bwd<T, 0, 32, 512, 1, 1>(p, a, s);
     return launch_bwd<T, 0, 32, 1024, 1, 1>(p, a, s);
 }
