@@ -418,8 +418,10 @@ def adamw_tensors(tensors):
 
     ``tensors``: dicts with param, grad, m, v (torch tensors; fp32 moments, or
     float8_e4m3fn ones with m_scale and v_scale), and optionally master, lr_scale and
-    weight_decay.  The table keeps the tensors alive.  One array in two places is refused:
-    its update would be a race."""
+    weight_decay.  The table keeps the tensors alive and is for the device that is current
+    now.  One array in two places is refused: its update would be a race.  It holds the
+    arrays' addresses, so gradients have to stay where they are; building it takes some 20 us
+    a tensor on the host, for every array is checked here and not in the calls."""
     tensors = [dict(t) for t in tensors]
     table = (VmoeAdamwTensor * max(1, len(tensors)))()
     kinds = _kinds()
@@ -453,12 +455,15 @@ def adamw_tensors(tensors):
             raise VmoeError(VMOE_ERR_INVALID, "adamw_tensors: two arrays overlap")
         end, last_write = max(end, e), max(last_write, e) if w else last_write
     table.tensors, table.count = tensors, len(tensors)
+    table.device = _device() if tensors else None  # where _arrays has found them all
     return table
 
 
 def vmoe_adamw(table, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, step_dev=None, lr_dev=None, grad_scale=None,
                stream=None):
     """One AdamW update of the tensors of ``table`` (adamw_tensors; see include/vmoe.h)."""
+    if table.device is not None and table.device != _device():
+        raise VmoeError(VMOE_ERR_INVALID, "vmoe_adamw: tensors on device %d, the current one is %d" % (table.device, _device()))
     a = _arrays("vmoe_adamw", (step_dev, "i32", 1), (lr_dev, "f32", 1), (grad_scale, "f32", 1))
     c = VmoeAdamwConfig(lr, beta1, beta2, eps, step, seed & 0xffffffff, *a)
     _check(library().vmoe_adamw(table.count, table, ctypes.byref(c), _stream(stream)), "vmoe_adamw")
