@@ -12,7 +12,7 @@ import bisect
 import torch
 
 from . import (VMOE_NORM_POST, _stream, norm_config, vmoe_block_norm, vmoe_block_norm_bwd, vmoe_block_norm_bwd_workspace_size)
-from .step import BalanceBuffers, Buffers, StepRunner
+from .step import BalanceBuffers, Buffers, StepRunner, _nothing_to_add_to
 
 NORM_PARAMS = ("pre_w", "pre_b", "post_w", "post_b", "gate")
 
@@ -41,6 +41,8 @@ class BlockStack:
     def __init__(self, p, layers, norm=None, balance=None, token_mask=None, device="cuda"):
         if not layers:
             raise ValueError("a stack has at least one block")
+        if _nothing_to_add_to(p, balance):
+            raise ValueError("VMOE_DLOGITS_ADD without balance: no step writes the gradients that it adds to")
         self.p, self.layers = p, layers
         self.norm = norm if norm is not None else norm_config()
         self.post = bool(self.norm.flags & VMOE_NORM_POST)

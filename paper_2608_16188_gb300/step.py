@@ -75,6 +75,11 @@ class BalanceBuffers:
         self.dloss = weights
 
 
+def _nothing_to_add_to(p, balance):
+    """Whether the router's gradient would be added to what an earlier step has left."""
+    return balance is None and bool(p.flags & VMOE_DLOGITS_ADD)
+
+
 class StepRunner:
     """Issues the library calls of one forward + backward step.
 
@@ -84,7 +89,9 @@ class StepRunner:
     (the losses' weights, see BalanceBuffers; needs ``router_grad``) the forward
     computes the balance losses and counts into ``self.balance`` and the router's
     gradient is that of <dY, y> plus the weighted losses; ``inputs`` may then hold
-    token_mask [T,N] uint8, 0 for padding that they leave out.
+    token_mask [T,N] uint8, 0 for padding that they leave out.  A problem with
+    VMOE_DLOGITS_ADD and no ``balance`` adds to what the caller writes into
+    ``b.dlogits`` before each backward.
     """
 
     def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False, balance=None):
@@ -153,6 +160,8 @@ class HostPipeline:
 
     def __init__(self, p, weights, bufs: Buffers | None = None, device="cuda",
                  router_grad: bool = False, balance=None):
+        if _nothing_to_add_to(p, balance):
+            raise ValueError("VMOE_DLOGITS_ADD without balance: no step writes the gradients that it adds to")
         self.p = p
         base = bufs if bufs is not None else Buffers(p, device)
         if balance is not None and not isinstance(balance, BalanceBuffers):
