@@ -469,14 +469,16 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
 
 // ---------------------------------------------------------------------------
 // Kernel 1b (VMOE_DLOGITS_ADD), bf16 problems: dX += dlogit W_r^T for dense rows, on
-// mma.sync tensor cores: K = E is short, and what bounds it is dX, read and written once.
+// mma.sync tensor cores: K = E is short, and what it has to move is dX, read and written once.
 // Both fp32 factors are taken as two bf16 parts each, hi hi + hi lo + lo hi: 2^-16 of the
 // products, against dX's own rounding of 2^-8.  A CTA holds 64 columns of W_r^T in shared
 // memory in the order of the fragments, one 16-byte read for a lane's k16 x n8 parts, and
 // its warps walk tiles of 16 tokens, whose dlogit rows come straight from global memory.
 // The columns are dealt so that a lane's results are 16 neighbouring ones of a row.
-// All of vmoe_router_bwd at 17 x 1576 tokens, 768 channels and 32 experts: 83 us, 134 us
-// with kernel 1's dense update; 8 x 1576, 1024, 64: 64 us against 2.7 ms.
+// 17 x 1576 tokens, 768 channels and 32 experts, L2 flushed before the call: 35 us, 12.9 us for
+// its bytes at the copy rate (DRAM at 18% of its peak, 22% of the warps active, first stall
+// the wait for dlogits and dX: latency); all of vmoe_router_bwd 88 us (76 without the flag, 133
+// with kernel 1's dense update).  8 x 1576, 1024, 64: 39 us of 73 (41 without the flag, 2.7 ms).
 constexpr int RX_COLS = 64, RX_TOKENS = 512, RX_THREADS = 256;
 
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
@@ -565,7 +567,9 @@ router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restri
 }
 
 // Kernel 1b, fp32 problems: the same on CUDA cores, 64 tokens x 128 columns a CTA, the
-// experts in chunks of 32 staged transposed; 4 tokens x 8 columns a thread.
+// experts in chunks of 32 staged transposed; 4 tokens x 8 columns a thread.  8 x 1576 tokens,
+// 768 channels, 32 experts: 41 us, 11.8 for its bytes; the call 124 us (108 without the flag, 143
+// with kernel 1's dense update).
 constexpr int RXF_N = 64, RXF_D = 128, RXF_E = 32;
 
 __global__ void __launch_bounds__(RX_THREADS)
