@@ -346,6 +346,68 @@ int vmoe_balance_bwd(const vmoe_problem *p, const float *logits, const uint8_t *
                      const int32_t *count, const int32_t *tokens, const float *excess,
                      const float *dloss, float *dlogits, void *cuda_stream);
 
+typedef enum {
+    VMOE_SCORE_SOFTMAX = 0, /* s_e: the softmax of a token's logits */
+    VMOE_SCORE_SIGMOID = 1  /* s_e = 1 / (1 + exp(-logit_e)) */
+} vmoe_score;
+
+/* How vmoe_gate chooses. */
+typedef struct {
+    int32_t score;       /* vmoe_score */
+    int32_t groups;      /* divides E: experts e with the same e / (E / groups) are a group; 1: none */
+    int32_t groups_kept; /* groups a token may choose from; groups_kept * (E / groups) >= k */
+    int32_t group_top;   /* 1 or 2, at most E / groups */
+    float scale;         /* > 0: what the gates are taken times */
+} vmoe_gating;
+
+/* Routing with scores, a bias for balance and groups of experts: vmoe_route's place
+ * in a step (Section 2.1; capacity limits of Challenge #1; sequential assignment of
+ * Section 3.3.1), for routers that are balanced by select_bias instead of by losses.
+ *   c_e = s_e + select_bias_e;  a group's value: the sum of its group_top largest c;
+ *   open: the groups_kept groups of the largest values; the choices: the k largest c
+ *   in open groups, descending;  gate_j = scale s_j / sum_i s_i over the choices,
+ *   scale s_j with VMOE_NO_RENORM.
+ * Equal values go to the lower index, and what is larger is decided in exact
+ * arithmetic (64 bits), not by fp32 roundings of s.  The bias acts on the choice
+ * alone.  An expert whose logit or bias is not finite (-inf, say) is switched off: never
+ * chosen, 0 in a softmax.  Where fewer than k experts can be chosen, the rest of the
+ * token's choices have expert_idx -1, gate 0 and slot -1 and take no capacity; the
+ * other entry points pass over them.  So it is for all choices of a token whose
+ * token_mask is 0, whose logits may hold anything.
+ *   x, w_router, logit_bias, logits, expert_idx, gate, slot, load as for vmoe_route;
+ *   select_bias [T,E] fp32 nullable; token_mask [T,N] uint8 nullable;
+ *   demand [T,E] int32 out, nullable: choices of each expert, dropped ones too;
+ *   workspace: caller-owned device scratch of vmoe_gate_workspace_size(p) bytes or
+ *   more (else VMOE_ERR_INVALID), 16-byte aligned, its contents clobbered.
+ * T*N < 2^31 and N*k < 2^31 (else VMOE_ERR_UNSUPPORTED). */
+int vmoe_gate(const vmoe_problem *p, const vmoe_gating *gating, const void *x, const float *w_router,
+              const float *logit_bias, const float *select_bias, const uint8_t *token_mask, float *logits,
+              int32_t *expert_idx, float *gate, int32_t *slot, int32_t *load, int32_t *demand, void *workspace,
+              size_t workspace_bytes, void *cuda_stream);
+
+/* Device bytes of scratch vmoe_gate needs for `p`, or 0 if `p` is invalid.  Host only. */
+size_t vmoe_gate_workspace_size(const vmoe_problem *p);
+
+/* vmoe_router_bwd for choices of vmoe_gate: the gradient of <dY, y> through the gates,
+ * choices and slots held fixed, with r_j = gate_j / scale, m = sum_i r_i dgate_i:
+ *   dgate_j = <dY[t,n], Ye[t, e_j, s_j]>, 0 where slot is -1
+ *   sigmoid: dlogit_{e_j} = gate_j (1 - s_j) (dgate_j - m), without m with VMOE_NO_RENORM
+ *   softmax: dlogit_{e_j} = gate_j (dgate_j - m); VMOE_NO_RENORM: dlogit_e =
+ *   scale s_e (dgate_e - m) for every e, dgate_e 0 unless chosen
+ *   dW_r = x^T dlogits, dbias = sum_n dlogits (of logit_bias), dX = dX_in + dlogits W_r^T
+ * Other dlogits, and those of a token without choices, are 0.  logits and select_bias
+ * have no other part in it.  VMOE_DLOGITS_ADD as for vmoe_router_bwd.
+ *   dx_in, dx [T,N,d] p->dtype, both or neither; dx_in may be dx.  The rest as for
+ *   vmoe_router_bwd (w_router is needed with dx, logits always). */
+int vmoe_gate_bwd(const vmoe_problem *p, const vmoe_gating *gating, const void *x, const float *w_router,
+                  const float *logits, const int32_t *expert_idx, const float *gate, const int32_t *slot, const void *dy,
+                  const void *ye, float *dgate, float *dlogits, float *dw_router, float *dbias, const void *dx_in, void *dx,
+                  void *cuda_stream);
+
+/* The balance of vmoe_gate's choices, after a step: select_bias[t,e] += rate where
+ * demand[t,e] is below the task's mean, -= rate where it is above it. */
+int vmoe_gate_bias(const vmoe_problem *p, const int32_t *demand, float rate, float *select_bias, void *cuda_stream);
+
 enum {
     VMOE_NORM_RMS = 1u << 0,  /* root-mean-square norms (no mean); default is the layer norm */
     VMOE_NORM_POST = 1u << 1  /* a norm on the branch y */

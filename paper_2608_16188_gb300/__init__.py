@@ -34,6 +34,9 @@ VMOE_NO_RENORM = 1 << 1
 VMOE_GELU_TANH = 1 << 2
 VMOE_DLOGITS_ADD = 1 << 3
 
+VMOE_SCORE_SOFTMAX = 0
+VMOE_SCORE_SIGMOID = 1
+
 VMOE_NORM_RMS = 1 << 0
 VMOE_NORM_POST = 1 << 1
 
@@ -48,6 +51,7 @@ EXPORTS = ("vmoe_version", "vmoe_status_string", "vmoe_problem_capacity", "vmoe_
            "vmoe_attn_expert_fwd", "vmoe_attn_expert_bwd", "vmoe_attn_expert_bwd_workspace_size",
            "vmoe_balance", "vmoe_balance_workspace_size", "vmoe_balance_bwd", "vmoe_block_norm", "vmoe_block_norm_bwd",
            "vmoe_block_norm_bwd_workspace_size", "vmoe_adamw",
+           "vmoe_gate", "vmoe_gate_workspace_size", "vmoe_gate_bwd", "vmoe_gate_bias",
            "vmoe_device_status", "vmoe_selftest_bounded_wait", "vmoe_trace_enable",
            "vmoe_trace_disable", "vmoe_trace_get")
 
@@ -69,6 +73,12 @@ class VmoeProblem(ctypes.Structure):
 class VmoeNorm(ctypes.Structure):
     """Mirror of ``vmoe_norm`` in include/vmoe.h."""
     _fields_ = [("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class VmoeGating(ctypes.Structure):
+    """Mirror of ``vmoe_gating`` in include/vmoe.h."""
+    _fields_ = [("score", ctypes.c_int32), ("groups", ctypes.c_int32), ("groups_kept", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class VmoeAdamwTensor(ctypes.Structure):
@@ -123,6 +133,10 @@ def library():
             "vmoe_block_norm": (ctypes.c_int, [PP, ctypes.POINTER(VmoeNorm)] + [_P] * 12),
             "vmoe_block_norm_bwd_workspace_size": (ctypes.c_size_t, [PP]),
             "vmoe_block_norm_bwd": (ctypes.c_int, [PP, ctypes.POINTER(VmoeNorm)] + [_P] * 18 + [ctypes.c_size_t, _P]),
+            "vmoe_gate_workspace_size": (ctypes.c_size_t, [PP]),
+            "vmoe_gate": (ctypes.c_int, [PP, ctypes.POINTER(VmoeGating)] + [_P] * 12 + [ctypes.c_size_t, _P]),
+            "vmoe_gate_bwd": (ctypes.c_int, [PP, ctypes.POINTER(VmoeGating)] + [_P] * 15),
+            "vmoe_gate_bias": (ctypes.c_int, [PP, _P, ctypes.c_float, _P, _P]),
             "vmoe_adamw": (ctypes.c_int, [ctypes.c_int, _P, ctypes.POINTER(VmoeAdamwConfig), _P]),
             "vmoe_plan_slices": (ctypes.c_int, [ctypes.c_int, _P, _P, ctypes.c_int64,
                                                 ctypes.c_double, ctypes.c_double, _P, _P]),
@@ -380,6 +394,47 @@ def vmoe_balance_bwd(p, logits, token_mask, count, tokens, excess, dloss, dlogit
     a = _arrays("vmoe_balance_bwd", (logits, "f32", tn * p.E), (token_mask, "u8", tn), (count, "i32", te),
                 (tokens, "i32", p.T), (excess, "f32", te), (dloss, "f32", 3 * p.T), (dlogits, "f32", tn * p.E))
     _check(library().vmoe_balance_bwd(ctypes.byref(p), *a, _stream(stream)), "vmoe_balance_bwd")
+
+
+def gating(score="softmax", groups=1, groups_kept=1, group_top=1, scale=1.0):
+    """Build a VmoeGating; ``score`` is "softmax", "sigmoid" or a VMOE_SCORE_* code."""
+    if isinstance(score, str):
+        score = {"softmax": VMOE_SCORE_SOFTMAX, "sigmoid": VMOE_SCORE_SIGMOID}[score]
+    return VmoeGating(int(score), int(groups), int(groups_kept), int(group_top), float(scale))
+
+
+def vmoe_gate_workspace_size(p) -> int:
+    return int(library().vmoe_gate_workspace_size(ctypes.byref(p)))
+
+
+def vmoe_gate(p, gating, x, w_router, logit_bias, select_bias, token_mask, logits, expert_idx, gate, slot, load, demand,
+              workspace, workspace_bytes=None, stream=None):
+    """Routing with scores, a bias for balance and groups of experts (see include/vmoe.h)."""
+    te, tn = p.T * p.E, p.T * p.N
+    a = _arrays("vmoe_gate", (x, p.dtype, tn * p.d_model), (w_router, "f32", te * p.d_model), (logit_bias, "f32", te),
+                (select_bias, "f32", te), (token_mask, "u8", tn), (logits, "f32", tn * p.E), (expert_idx, "i32", tn * p.k),
+                (gate, "f32", tn * p.k), (slot, "i32", tn * p.k), (load, "i32", te), (demand, "i32", te))
+    ws, nbytes = _workspace("vmoe_gate", workspace, workspace_bytes)
+    _check(library().vmoe_gate(ctypes.byref(p), ctypes.byref(gating), *a, ws, nbytes, _stream(stream)), "vmoe_gate")
+
+
+def vmoe_gate_bwd(p, gating, x, w_router, logits, expert_idx, gate, slot, dy, ye, dgate, dlogits, dw_router, dbias=None,
+                  dx_in=None, dx=None, stream=None):
+    """Router backward for choices of vmoe_gate (see include/vmoe.h); dx_in may be dx."""
+    te, tn = p.T * p.E, p.T * p.N
+    n = tn * p.d_model
+    a = _arrays("vmoe_gate_bwd", (x, p.dtype, n), (w_router, "f32", te * p.d_model), (logits, "f32", tn * p.E),
+                (expert_idx, "i32", tn * p.k), (gate, "f32", tn * p.k), (slot, "i32", tn * p.k), (dy, p.dtype, n),
+                (ye, p.dtype, te * vmoe_problem_capacity(p) * p.d_model), (dgate, "f32", tn * p.k), (dlogits, "f32", tn * p.E),
+                (dw_router, "f32", te * p.d_model), (dbias, "f32", te), (dx_in, p.dtype, n), (dx, p.dtype, n))
+    _check(library().vmoe_gate_bwd(ctypes.byref(p), ctypes.byref(gating), *a, _stream(stream)), "vmoe_gate_bwd")
+
+
+def vmoe_gate_bias(p, demand, rate, select_bias, stream=None):
+    """select_bias += rate for experts below the task's mean demand, -= rate above it."""
+    te = p.T * p.E
+    a = _arrays("vmoe_gate_bias", (demand, "i32", te), (select_bias, "f32", te))
+    _check(library().vmoe_gate_bias(ctypes.byref(p), a[0], rate, a[1], _stream(stream)), "vmoe_gate_bias")
 
 
 def norm_config(rms=False, post=True, eps=1e-6, residual_scale=1.0):

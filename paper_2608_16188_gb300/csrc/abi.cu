@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "around.cuh"
+#include "gate.cuh"
 
 namespace vmoe {
 
@@ -385,6 +386,68 @@ int vmoe_balance_bwd(const vmoe_problem *p, const float *logits, const uint8_t *
         !dev_ok(dloss) || !dev_ok(dlogits))
         return VMOE_ERR_INVALID;
     return launch_balance_bwd(d, logits, token_mask, count, tokens, excess, dloss, dlogits, (cudaStream_t)cuda_stream);
+}
+
+static int check_gating(const vmoe_problem *p, const vmoe_gating *g, Dims *d, Gating *out) {
+    int st = check_problem(p, d);
+    if (st != VMOE_OK) return st;
+    if (!g || (g->score != VMOE_SCORE_SOFTMAX && g->score != VMOE_SCORE_SIGMOID) || g->groups < 1 || d->E % g->groups != 0 ||
+        g->groups_kept < 1 || g->groups_kept > g->groups || g->group_top < 1 || g->group_top > 2 ||
+        g->group_top > d->E / g->groups || (long long)g->groups_kept * (d->E / g->groups) < d->k || !(g->scale > 0.0f) ||
+        !isfinite(g->scale))
+        return VMOE_ERR_INVALID;
+    if ((long long)d->T * d->N >= (1LL << 31) || (long long)d->N * d->k >= (1LL << 31)) return VMOE_ERR_UNSUPPORTED;
+    *out = Gating{g->score, g->groups, g->groups_kept, g->group_top, g->scale, !(p->flags & VMOE_NO_RENORM)};
+    return VMOE_OK;
+}
+
+size_t vmoe_gate_workspace_size(const vmoe_problem *p) {
+    Dims d;
+    return check_problem(p, &d) == VMOE_OK ? gate_workspace(d) : 0;
+}
+
+int vmoe_gate(const vmoe_problem *p, const vmoe_gating *gating, const void *x, const float *w_router,
+              const float *logit_bias, const float *select_bias, const uint8_t *token_mask, float *logits,
+              int32_t *expert_idx, float *gate, int32_t *slot, int32_t *load, int32_t *demand, void *workspace,
+              size_t workspace_bytes, void *cuda_stream) {
+    Dims d;
+    Gating g;
+    int st = check_gating(p, gating, &d, &g);
+    if (st != VMOE_OK) return st;
+    const bool given = (p->flags & VMOE_LOGITS_IN) != 0;
+    if (!given && (!dev_ok(x) || !dev_ok(w_router))) return VMOE_ERR_INVALID;
+    if (!opt_ok(logit_bias) || !opt_ok(select_bias) || !opt_ok(token_mask) || !dev_ok(logits) || !dev_ok(expert_idx) ||
+        !dev_ok(gate) || !dev_ok(slot) || !dev_ok(load) || !opt_ok(demand) || !dev_ok(workspace) ||
+        workspace_bytes < gate_workspace(d))
+        return VMOE_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (!given && (st = launch_router_logits(d, x, w_router, logit_bias, logits, s)) != VMOE_OK) return st;
+    return launch_gate(d, g, logits, select_bias, token_mask, expert_idx, gate, slot, load, demand, (int32_t *)workspace, s);
+}
+
+int vmoe_gate_bwd(const vmoe_problem *p, const vmoe_gating *gating, const void *x, const float *w_router,
+                  const float *logits, const int32_t *expert_idx, const float *gate, const int32_t *slot, const void *dy,
+                  const void *ye, float *dgate, float *dlogits, float *dw_router, float *dbias, const void *dx_in, void *dx,
+                  void *cuda_stream) {
+    Dims d;
+    Gating g;
+    int st = check_gating(p, gating, &d, &g);
+    if (st != VMOE_OK) return st;
+    if (!dev_ok(x) || !dev_ok(logits) || !dev_ok(expert_idx) || !dev_ok(gate) || !dev_ok(slot) || !dev_ok(dy) ||
+        !dev_ok(ye) || !dev_ok(dgate) || !dev_ok(dlogits) || !dev_ok(dw_router) || !opt_ok(dbias) || !opt_ok(dx_in) ||
+        !opt_ok(dx) || (dx_in != nullptr) != (dx != nullptr) || (dx ? !dev_ok(w_router) : !opt_ok(w_router)))
+        return VMOE_ERR_INVALID;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    if ((st = launch_gate_grad(d, g, logits, expert_idx, gate, slot, dy, ye, dgate, dlogits, s)) != VMOE_OK) return st;
+    return launch_router_grads(d, x, w_router, dlogits, dw_router, dbias, dx_in, dx, s);
+}
+
+int vmoe_gate_bias(const vmoe_problem *p, const int32_t *demand, float rate, float *select_bias, void *cuda_stream) {
+    Dims d;
+    int st = check_problem(p, &d);
+    if (st != VMOE_OK) return st;
+    if (!dev_ok(demand) || !dev_ok(select_bias) || !isfinite(rate)) return VMOE_ERR_INVALID;
+    return launch_gate_bias(d, demand, rate, select_bias, (cudaStream_t)cuda_stream);
 }
 
 // The problem and the norm's description; d <= 8192 (32 warps of 256 channels hold a row).

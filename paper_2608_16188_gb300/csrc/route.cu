@@ -20,7 +20,7 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
-#include "common.cuh"
+#include "gate.cuh"
 #include "topk.cuh"
 
 namespace cg = cooperative_groups;
@@ -625,13 +625,13 @@ int launch_scan(const Dims &p, const int32_t *idx, int32_t *slot, int32_t *load,
 
 }  // namespace
 
-int launch_route(const Dims &p, const void *x, const float *w_router, const float *bias,
-                 float *logits, int32_t *idx, float *gate, int32_t *slot, int32_t *load,
-                 cudaStream_t s) {
+// Logits, choices and gates: what precedes the capacity scan.
+static int launch_topk(const Dims &p, const void *x, const float *w_router, const float *bias, float *logits, int32_t *idx,
+                       float *gate, cudaStream_t s) {
     int st;
     if (p.bf16 && x != nullptr) {
         const __nv_bfloat16 *xb = (const __nv_bfloat16 *)x;
-        if (route_tc_enabled() && route_tc_width(p) > 0)
+        if (p.k > 0 && route_tc_enabled() && route_tc_width(p) > 0)
             st = launch_route_tc(p, xb, w_router, bias, logits, idx, gate, s);
         else
             st = p.E <= 32 ? launch_mma_router<4, 1>(p, xb, w_router, bias, logits, idx, gate, s)
@@ -652,6 +652,21 @@ int launch_route(const Dims &p, const void *x, const float *w_router, const floa
             st = p.E <= 32 ? launch_f32<32, 16, 128, 8>(p, xf, w_router, bias, logits, idx, gate, s)
                            : launch_f32<64, 16, 128, 4>(p, xf, w_router, bias, logits, idx, gate, s);
     }
+    return st;
+}
+
+// The kernels above with no choice to make: k = 0 passes over a row's logits and writes neither idx nor gate.
+int launch_router_logits(const Dims &p, const void *x, const float *w_router, const float *bias, float *logits,
+                         cudaStream_t s) {
+    Dims q = p;
+    q.k = 0;
+    return launch_topk(q, x, w_router, bias, logits, nullptr, nullptr, s);
+}
+
+int launch_route(const Dims &p, const void *x, const float *w_router, const float *bias,
+                 float *logits, int32_t *idx, float *gate, int32_t *slot, int32_t *load,
+                 cudaStream_t s) {
+    int st = launch_topk(p, x, w_router, bias, logits, idx, gate, s);
     if (st != VMOE_OK) return st;
     trace_before(s, "capacity_scan");
     st = p.E <= 128 ? launch_scan<1024>(p, idx, slot, load, s) : launch_scan<256>(p, idx, slot, load, s);

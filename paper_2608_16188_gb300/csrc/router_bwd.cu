@@ -34,7 +34,7 @@
 
 #include <algorithm>
 
-#include "common.cuh"
+#include "gate.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -495,7 +495,8 @@ __device__ __forceinline__ float2 two_of(const float *row, int k, int E) {
 
 template <bool EVEN>
 __global__ void __launch_bounds__(RX_THREADS)
-router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, __nv_bfloat16 *dx) {
+router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, const __nv_bfloat16 *dx_in,
+                     __nv_bfloat16 *dx) {
     extern __shared__ __align__(16) uint4 rx_w[];  // [k16 steps][8 column tiles][32 lanes]: hi k, hi k + 8, lo, lo
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int t = blockIdx.z, d = p.d, E = p.E, N = p.N, d0 = blockIdx.y * RX_COLS, steps = (E + 15) / 16;
@@ -520,13 +521,14 @@ router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restri
         const int na = n0 + g, nb = n0 + g + 8;
         const long long ra = (long long)t * N + min(na, N - 1), rb = (long long)t * N + min(nb, N - 1);
         __nv_bfloat16 *pa = dx + ra * d + c0, *pb = dx + rb * d + c0;
+        const __nv_bfloat16 *ia = dx_in + ra * d + c0, *ib = dx_in + rb * d + c0;  // may be pa, pb
         uint4 xa[2], xb[2];  // d and c0 are multiples of 8: a half's columns all are, or none
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             xa[h] = xb[h] = make_uint4(0, 0, 0, 0);
             if (c0 + 8 * h < d) {
-                if (na < N) xa[h] = *reinterpret_cast<const uint4 *>(pa + 8 * h);
-                if (nb < N) xb[h] = *reinterpret_cast<const uint4 *>(pb + 8 * h);
+                if (na < N) xa[h] = *reinterpret_cast<const uint4 *>(ia + 8 * h);
+                if (nb < N) xb[h] = *reinterpret_cast<const uint4 *>(ib + 8 * h);
             }
         }
         float acc[8][4] = {};
@@ -573,7 +575,7 @@ router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restri
 constexpr int RXF_N = 64, RXF_D = 128, RXF_E = 32;
 
 __global__ void __launch_bounds__(RX_THREADS)
-router_dx_simt_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, float *dx) {
+router_dx_simt_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, const float *dx_in, float *dx) {
     __shared__ __align__(16) float ds[RXF_E][RXF_N + 4];
     __shared__ __align__(16) float ws[RXF_E][RXF_D + 4];
     const int tid = threadIdx.x, tn = tid / 16, td = tid % 16;
@@ -621,15 +623,15 @@ router_dx_simt_kernel(Dims p, const float *__restrict__ dl, const float *__restr
         for (int h = 0; h < 2; ++h) {
             const int c = d0 + 64 * h + 4 * td;
             if (c >= d) continue;  // d is a multiple of 8, c of 4: all four or none
-            float4 *o = reinterpret_cast<float4 *>(dx + ((long long)t * N + n) * d + c);
+            const long long at = ((long long)t * N + n) * d + c;
             const float2 lo = unpk2(acc[r][2 * h]), hi = unpk2(acc[r][2 * h + 1]);
-            const float4 v = *o;
-            *o = make_float4(v.x + lo.x, v.y + lo.y, v.z + hi.x, v.w + hi.y);
+            const float4 v = *reinterpret_cast<const float4 *>(dx_in + at);
+            *reinterpret_cast<float4 *>(dx + at) = make_float4(v.x + lo.x, v.y + lo.y, v.z + hi.x, v.w + hi.y);
         }
     }
 }
 
-int launch_router_dx(const Dims &p, const float *dl, const float *wr, void *dx, cudaStream_t s) {
+int launch_router_dx(const Dims &p, const float *dl, const float *wr, const void *dx_in, void *dx, cudaStream_t s) {
     trace_before(s, "router_dx");
     int st;
     if (p.bf16) {
@@ -638,13 +640,14 @@ int launch_router_dx(const Dims &p, const float *dl, const float *wr, void *dx, 
         auto go = [&](auto kern, std::atomic<int>(&limit)[64]) {
             if (smem > 48 * 1024)
                 if (const int e = raise_smem_limit((const void *)kern, limit, (int)smem)) return e;
-            return launch_kernel(kern, grid, dim3(RX_THREADS), smem, s, p, dl, wr, (__nv_bfloat16 *)dx);
+            return launch_kernel(kern, grid, dim3(RX_THREADS), smem, s, p, dl, wr, (const __nv_bfloat16 *)dx_in,
+                                 (__nv_bfloat16 *)dx);
         };
         static std::atomic<int> even[64], odd[64];
         st = p.E % 2 == 0 ? go(router_dx_mma_kernel<true>, even) : go(router_dx_mma_kernel<false>, odd);
     } else {
         const dim3 grid((p.N + RXF_N - 1) / RXF_N, (p.d + RXF_D - 1) / RXF_D, p.T);
-        st = launch_kernel(router_dx_simt_kernel, grid, dim3(RX_THREADS), 0, s, p, dl, wr, (float *)dx);
+        st = launch_kernel(router_dx_simt_kernel, grid, dim3(RX_THREADS), 0, s, p, dl, wr, (const float *)dx_in, (float *)dx);
     }
     trace_after(s);
     return st;
@@ -1032,6 +1035,27 @@ int launch_router_dw_simt(const Dims &p, const float *x, const float *dl, float 
                : VMOE_ERR_CUDA;
 }
 
+int launch_router_dw(const Dims &p, const void *x, const float *dlogits, float *dw, float *dbias, cudaStream_t s) {
+    int st;
+    trace_before(s, "router_dw");
+    if (p.bf16 && (st = launch_router_dw_tc(p, (const __nv_bfloat16 *)x, dlogits, dw, dbias, s)) !=
+                      VMOE_ERR_UNSUPPORTED) {
+        trace_after(s);
+        return st;
+    }
+    if (p.bf16) {
+        dim3 grid(DW_SPLIT, (p.d + DW_BD - 1) / DW_BD, p.T * ((p.E + DW_BE - 1) / DW_BE));
+        router_dw_mma_kernel<<<grid, DW_THREADS, 0, s>>>(p, (const __nv_bfloat16 *)x, dlogits, dw,
+                                                         dbias);
+    } else {
+        st = launch_router_dw_simt(p, (const float *)x, dlogits, dw, dbias, s);
+        trace_after(s);
+        return st;
+    }
+    trace_after(s);
+    return launch_result();
+}
+
 // ---------------------------------------------------------------------------
 template <typename T, int KMAX, bool WSMEM>
 int launch_grad(const Dims &p, const float *wr, const float *logits, const int32_t *idx,
@@ -1161,24 +1185,8 @@ int run(const Dims &p, const void *x, const float *wr, const float *logits, cons
         st = launch_grad_k<T, 8>(p, wr, logits, idx, gate, slot, dyt, yet, dgate, dlogits, dxt, s);
     trace_after(s);
     if (st != VMOE_OK) return st;
-    if (dense_dx && (st = launch_router_dx(p, dlogits, wr, dense_dx, s)) != VMOE_OK) return st;
-    trace_before(s, "router_dw");
-    if (p.bf16 && (st = launch_router_dw_tc(p, (const __nv_bfloat16 *)x, dlogits, dw, dbias, s)) !=
-                      VMOE_ERR_UNSUPPORTED) {
-        trace_after(s);
-        return st;
-    }
-    if (p.bf16) {
-        dim3 grid(DW_SPLIT, (p.d + DW_BD - 1) / DW_BD, p.T * ((p.E + DW_BE - 1) / DW_BE));
-        router_dw_mma_kernel<<<grid, DW_THREADS, 0, s>>>(p, (const __nv_bfloat16 *)x, dlogits, dw,
-                                                         dbias);
-    } else {
-        st = launch_router_dw_simt(p, (const float *)x, dlogits, dw, dbias, s);
-        trace_after(s);
-        return st;
-    }
-    trace_after(s);
-    return launch_result();
+    if (dense_dx && (st = launch_router_dx(p, dlogits, wr, dense_dx, dense_dx, s)) != VMOE_OK) return st;
+    return launch_router_dw(p, x, dlogits, dw, dbias, s);
 }
 
 }  // namespace
@@ -1192,6 +1200,13 @@ int launch_router_bwd(const Dims &p, const void *x, const float *w_router, const
                                   dw_router, dbias, dx, s);
     return run<float>(p, x, w_router, logits, idx, gate, slot, dy, ye, dgate, dlogits, dw_router,
                       dbias, dx, s);
+}
+
+int launch_router_grads(const Dims &p, const void *x, const float *w_router, const float *dlogits, float *dw_router,
+                        float *dbias, const void *dx_in, void *dx, cudaStream_t s) {
+    if (dx)
+        if (const int st = launch_router_dx(p, dlogits, w_router, dx_in, dx, s)) return st;
+    return launch_router_dw(p, x, dlogits, dw_router, dbias, s);
 }
 
 }  // namespace vmoe
