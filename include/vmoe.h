@@ -409,6 +409,63 @@ int vmoe_gate_bwd(const vmoe_problem *p, const vmoe_gating *gating, const void *
 int vmoe_gate_bias(const vmoe_problem *p, const int32_t *demand, float rate, float *select_bias, void *cuda_stream);
 
 enum {
+    VMOE_HEAD_SHARED = 1u << 0 /* one head for all tasks: w, dw [V,d] instead of [T,V,d] */
+};
+
+/* A head over a vocabulary behind the blocks, and what it is trained against. */
+typedef struct {
+    int32_t V;         /* entries of the vocabulary */
+    int32_t teacher_k; /* K: entries of a teacher's list for each token, 0: no teacher; at most 128 */
+    float temperature; /* tau > 0 */
+    uint32_t flags;    /* VMOE_HEAD_SHARED */
+} vmoe_head;
+
+/* Losses of l[t,n,:] = w[t] z[t,n], the logits never written out (Section 3.1: the
+ * tasks adapt to labels and to what a larger model answers):
+ *   lse = log sum_v exp(l_v),  ce = lse - l_label           of tokens with a label;
+ *   tlse = log sum_v exp(l_v / tau),  logp_j = l_{i_j} / tau - tlse,
+ *   kl = sum_j q_j (log q_j - logp_j),  q the softmax of teacher_logit / tau over the
+ *   list's entries,                                          of tokens with a teacher.
+ * A label outside [0, V) is none.  Entries of a list whose index is outside [0, V) or whose
+ * logit is -inf are left out (logp 0); a list of such entries alone is no teacher.  An
+ * index may be there twice: each counts.  Where a token has no label, or no teacher,
+ * those outputs are 0; the z of a token that has neither is not read and costs nothing.
+ *   z [T,N,d], w [T,V,d] ([V,d] with VMOE_HEAD_SHARED) p->dtype, an entry a row as in
+ *   an embedding table; label [T,N] int32; teacher_idx [T,N,K] int32, teacher_logit [T,N,K]
+ *   fp32; ce, lse, kl, tlse [T,N], logp [T,N,K] fp32 out.  label, ce and lse are given
+ *   together or not at all; teacher_* and kl, tlse, logp exactly if teacher_k > 0; one
+ *   of both is there.
+ *   workspace: caller-owned device scratch, 16-byte aligned, its contents clobbered, of
+ *   vmoe_head_workspace_size(p, head) bytes for this call and the backward, or of any
+ *   size from vmoe_head_min_workspace_size(p, head) on (else VMOE_ERR_INVALID): the
+ *   backward then takes the vocabulary in more pieces.
+ * Sums in fp32; fp32 operands are taken as three bf16 parts each, six products of
+ * parts (2^-24).  T*N < 2^31 - 256 (else VMOE_ERR_UNSUPPORTED).  Of p only T, N,
+ * d_model, dtype and the checks matter. */
+int vmoe_head_loss(const vmoe_problem *p, const vmoe_head *head, const void *z, const void *w, const int32_t *label,
+                   const int32_t *teacher_idx, const float *teacher_logit, float *ce, float *lse, float *kl, float *tlse,
+                   float *logp, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Gradient of sum dce ce + dlse lse + dkl kl:
+ *   dl_v = (dce + dlse) exp(l_v - lse) - dce [v = label]
+ *        + dkl / tau (exp(l_v / tau - tlse) - sum_{j: i_j = v} q_j)
+ *   dz = dl w,  dw = dl^T z (of one head's tokens; all tokens with VMOE_HEAD_SHARED).
+ * The first arguments as given to vmoe_head_loss, ce to logp as it wrote them; dce,
+ * dlse, dkl [T,N] fp32, each nullable (zero; one at least is given; not looked at where
+ * a token has no label, or no teacher).  dz [T,N,d], dw as w, p->dtype out, every
+ * element written, either nullable.  dl is rounded to p->dtype.  No output may overlap an
+ * input.  Sums in fp32 and in fixed orders; no atomics. */
+int vmoe_head_loss_bwd(const vmoe_problem *p, const vmoe_head *head, const void *z, const void *w, const int32_t *label,
+                       const int32_t *teacher_idx, const float *teacher_logit, const float *ce, const float *lse,
+                       const float *tlse, const float *logp, const float *dce, const float *dlse, const float *dkl, void *dz,
+                       void *dw, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Device bytes of scratch for the two: what is recommended, and what will do; 0 if `p` or
+ * `head` is invalid or unsupported.  Host only. */
+size_t vmoe_head_workspace_size(const vmoe_problem *p, const vmoe_head *head);
+size_t vmoe_head_min_workspace_size(const vmoe_problem *p, const vmoe_head *head);
+
+enum {
     VMOE_NORM_RMS = 1u << 0,  /* root-mean-square norms (no mean); default is the layer norm */
     VMOE_NORM_POST = 1u << 1  /* a norm on the branch y */
 };

@@ -37,6 +37,8 @@ VMOE_DLOGITS_ADD = 1 << 3
 VMOE_SCORE_SOFTMAX = 0
 VMOE_SCORE_SIGMOID = 1
 
+VMOE_HEAD_SHARED = 1 << 0
+
 VMOE_NORM_RMS = 1 << 0
 VMOE_NORM_POST = 1 << 1
 
@@ -52,6 +54,7 @@ EXPORTS = ("vmoe_version", "vmoe_status_string", "vmoe_problem_capacity", "vmoe_
            "vmoe_balance", "vmoe_balance_workspace_size", "vmoe_balance_bwd", "vmoe_block_norm", "vmoe_block_norm_bwd",
            "vmoe_block_norm_bwd_workspace_size", "vmoe_adamw",
            "vmoe_gate", "vmoe_gate_workspace_size", "vmoe_gate_bwd", "vmoe_gate_bias",
+           "vmoe_head_loss", "vmoe_head_loss_bwd", "vmoe_head_workspace_size", "vmoe_head_min_workspace_size",
            "vmoe_device_status", "vmoe_selftest_bounded_wait", "vmoe_trace_enable",
            "vmoe_trace_disable", "vmoe_trace_get")
 
@@ -79,6 +82,12 @@ class VmoeGating(ctypes.Structure):
     """Mirror of ``vmoe_gating`` in include/vmoe.h."""
     _fields_ = [("score", ctypes.c_int32), ("groups", ctypes.c_int32), ("groups_kept", ctypes.c_int32),
                 ("group_top", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class VmoeHead(ctypes.Structure):
+    """Mirror of ``vmoe_head`` in include/vmoe.h."""
+    _fields_ = [("V", ctypes.c_int32), ("teacher_k", ctypes.c_int32), ("temperature", ctypes.c_float),
+                ("flags", ctypes.c_uint32)]
 
 
 class VmoeAdamwTensor(ctypes.Structure):
@@ -137,6 +146,10 @@ def library():
             "vmoe_gate": (ctypes.c_int, [PP, ctypes.POINTER(VmoeGating)] + [_P] * 12 + [ctypes.c_size_t, _P]),
             "vmoe_gate_bwd": (ctypes.c_int, [PP, ctypes.POINTER(VmoeGating)] + [_P] * 15),
             "vmoe_gate_bias": (ctypes.c_int, [PP, _P, ctypes.c_float, _P, _P]),
+            "vmoe_head_workspace_size": (ctypes.c_size_t, [PP, ctypes.POINTER(VmoeHead)]),
+            "vmoe_head_min_workspace_size": (ctypes.c_size_t, [PP, ctypes.POINTER(VmoeHead)]),
+            "vmoe_head_loss": (ctypes.c_int, [PP, ctypes.POINTER(VmoeHead)] + [_P] * 11 + [ctypes.c_size_t, _P]),
+            "vmoe_head_loss_bwd": (ctypes.c_int, [PP, ctypes.POINTER(VmoeHead)] + [_P] * 15 + [ctypes.c_size_t, _P]),
             "vmoe_adamw": (ctypes.c_int, [ctypes.c_int, _P, ctypes.POINTER(VmoeAdamwConfig), _P]),
             "vmoe_plan_slices": (ctypes.c_int, [ctypes.c_int, _P, _P, ctypes.c_int64,
                                                 ctypes.c_double, ctypes.c_double, _P, _P]),
@@ -435,6 +448,47 @@ def vmoe_gate_bias(p, demand, rate, select_bias, stream=None):
     te = p.T * p.E
     a = _arrays("vmoe_gate_bias", (demand, "i32", te), (select_bias, "f32", te))
     _check(library().vmoe_gate_bias(ctypes.byref(p), a[0], rate, a[1], _stream(stream)), "vmoe_gate_bias")
+
+
+def head_config(V, teacher_k=0, temperature=1.0, shared=False):
+    """Build a VmoeHead: a head over V entries, a teacher's teacher_k logits a token, one head for all tasks or not."""
+    return VmoeHead(int(V), int(teacher_k), float(temperature), VMOE_HEAD_SHARED if shared else 0)
+
+
+def vmoe_head_workspace_size(p, head) -> int:
+    return int(library().vmoe_head_workspace_size(ctypes.byref(p), ctypes.byref(head)))
+
+
+def vmoe_head_min_workspace_size(p, head) -> int:
+    return int(library().vmoe_head_min_workspace_size(ctypes.byref(p), ctypes.byref(head)))
+
+
+def _head_sizes(p, head):
+    tn = p.T * p.N
+    return tn, tn * p.d_model, (1 if head.flags & VMOE_HEAD_SHARED else p.T) * head.V * p.d_model, tn * head.teacher_k
+
+
+def vmoe_head_loss(p, head, z, w, label, teacher_idx, teacher_logit, ce, lse, kl, tlse, logp, workspace,
+                   workspace_bytes=None, stream=None):
+    """Cross entropy and distillation over a large vocabulary (see include/vmoe.h)."""
+    tn, nz, nw, nk = _head_sizes(p, head)
+    a = _arrays("vmoe_head_loss", (z, p.dtype, nz), (w, p.dtype, nw), (label, "i32", tn), (teacher_idx, "i32", nk),
+                (teacher_logit, "f32", nk), (ce, "f32", tn), (lse, "f32", tn), (kl, "f32", tn), (tlse, "f32", tn),
+                (logp, "f32", nk))
+    ws, nbytes = _workspace("vmoe_head_loss", workspace, workspace_bytes)
+    _check(library().vmoe_head_loss(ctypes.byref(p), ctypes.byref(head), *a, ws, nbytes, _stream(stream)), "vmoe_head_loss")
+
+
+def vmoe_head_loss_bwd(p, head, z, w, label, teacher_idx, teacher_logit, ce, lse, tlse, logp, dce, dlse, dkl, dz, dw,
+                       workspace, workspace_bytes=None, stream=None):
+    """Backward of vmoe_head_loss (see include/vmoe.h)."""
+    tn, nz, nw, nk = _head_sizes(p, head)
+    a = _arrays("vmoe_head_loss_bwd", (z, p.dtype, nz), (w, p.dtype, nw), (label, "i32", tn), (teacher_idx, "i32", nk),
+                (teacher_logit, "f32", nk), (ce, "f32", tn), (lse, "f32", tn), (tlse, "f32", tn), (logp, "f32", nk),
+                (dce, "f32", tn), (dlse, "f32", tn), (dkl, "f32", tn), (dz, p.dtype, nz), (dw, p.dtype, nw))
+    ws, nbytes = _workspace("vmoe_head_loss_bwd", workspace, workspace_bytes)
+    _check(library().vmoe_head_loss_bwd(ctypes.byref(p), ctypes.byref(head), *a, ws, nbytes, _stream(stream)),
+           "vmoe_head_loss_bwd")
 
 
 def norm_config(rms=False, post=True, eps=1e-6, residual_scale=1.0):

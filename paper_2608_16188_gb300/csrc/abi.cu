@@ -9,6 +9,7 @@
 
 #include "around.cuh"
 #include "gate.cuh"
+#include "head.cuh"
 
 namespace vmoe {
 
@@ -448,6 +449,73 @@ int vmoe_gate_bias(const vmoe_problem *p, const int32_t *demand, float rate, flo
     if (st != VMOE_OK) return st;
     if (!dev_ok(demand) || !dev_ok(select_bias) || !isfinite(rate)) return VMOE_ERR_INVALID;
     return launch_gate_bias(d, demand, rate, select_bias, (cudaStream_t)cuda_stream);
+}
+
+// The problem and the head; the products' tiles are counted in 32 bits.
+static int check_head(const vmoe_problem *p, const vmoe_head *h, Dims *d) {
+    int st = check_problem(p, d);
+    if (st != VMOE_OK) return st;
+    if (!h || h->V < 1 || h->teacher_k < 0 || !(h->temperature > 0.0f) || !isfinite(h->temperature) ||
+        !isfinite(1.0f / h->temperature) || (h->flags & ~(uint32_t)VMOE_HEAD_SHARED))
+        return VMOE_ERR_INVALID;
+    if (h->teacher_k > HEAD_K || (long long)d->T * d->N >= (1LL << 31) - HEAD_TILE) return VMOE_ERR_UNSUPPORTED;
+    const long long tiles = ((long long)d->T * d->N / HEAD_TILE + d->T) * (h->V / HEAD_TILE + 1LL);
+    if (tiles >= (1LL << 26) || (long long)d->T * (h->V / HEAD_TILE + 1LL) * (d->d / HEAD_TILE + 1LL) >= (1LL << 30))
+        return VMOE_ERR_UNSUPPORTED;
+    return VMOE_OK;
+}
+
+size_t vmoe_head_workspace_size(const vmoe_problem *p, const vmoe_head *head) {
+    Dims d;
+    HeadPlan h;
+    return check_head(p, head, &d) == VMOE_OK && head_plan(d, head, true, 0, &h) ? h.bytes : 0;
+}
+
+size_t vmoe_head_min_workspace_size(const vmoe_problem *p, const vmoe_head *head) {
+    Dims d;
+    return check_head(p, head, &d) == VMOE_OK ? head_min_workspace(d, head) : 0;
+}
+
+int vmoe_head_loss(const vmoe_problem *p, const vmoe_head *head, const void *z, const void *w, const int32_t *label,
+                   const int32_t *teacher_idx, const float *teacher_logit, float *ce, float *lse, float *kl, float *tlse,
+                   float *logp, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    Dims d;
+    int st = check_head(p, head, &d);
+    if (st != VMOE_OK) return st;
+    const bool teach = head->teacher_k > 0;
+    if (!dev_ok(z) || !dev_ok(w) || !opt_ok(label) || !opt_ok(teacher_idx) || !opt_ok(teacher_logit) || !opt_ok(ce) ||
+        !opt_ok(lse) || !opt_ok(kl) || !opt_ok(tlse) || !opt_ok(logp) || !dev_ok(workspace))
+        return VMOE_ERR_INVALID;
+    if ((!label && !teach) || (label != nullptr) != (ce != nullptr) || (label != nullptr) != (lse != nullptr) ||
+        teach != (teacher_idx != nullptr) || teach != (teacher_logit != nullptr) || teach != (kl != nullptr) ||
+        teach != (tlse != nullptr) || teach != (logp != nullptr))
+        return VMOE_ERR_INVALID;
+    HeadPlan h;
+    if (workspace_bytes == 0 || !head_plan(d, head, label != nullptr, workspace_bytes, &h)) return VMOE_ERR_INVALID;
+    return launch_head_loss(d, h, HeadIn{z, w, label, teacher_idx, teacher_logit}, ce, lse, kl, tlse, logp, workspace,
+                            (cudaStream_t)cuda_stream);
+}
+
+int vmoe_head_loss_bwd(const vmoe_problem *p, const vmoe_head *head, const void *z, const void *w, const int32_t *label,
+                       const int32_t *teacher_idx, const float *teacher_logit, const float *ce, const float *lse,
+                       const float *tlse, const float *logp, const float *dce, const float *dlse, const float *dkl, void *dz,
+                       void *dw, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    Dims d;
+    int st = check_head(p, head, &d);
+    if (st != VMOE_OK) return st;
+    const bool teach = head->teacher_k > 0;
+    if (!dev_ok(z) || !dev_ok(w) || !opt_ok(label) || !opt_ok(teacher_idx) || !opt_ok(teacher_logit) || !opt_ok(ce) ||
+        !opt_ok(lse) || !opt_ok(tlse) || !opt_ok(logp) || !opt_ok(dce) || !opt_ok(dlse) || !opt_ok(dkl) || !opt_ok(dz) ||
+        !opt_ok(dw) || !dev_ok(workspace))
+        return VMOE_ERR_INVALID;
+    if ((!label && !teach) || (label != nullptr) != (ce != nullptr) || (label != nullptr) != (lse != nullptr) ||
+        teach != (teacher_idx != nullptr) || teach != (teacher_logit != nullptr) || teach != (tlse != nullptr) ||
+        teach != (logp != nullptr) || (!label && (dce || dlse)) || (!teach && dkl) || (!dce && !dlse && !dkl) || (!dz && !dw))
+        return VMOE_ERR_INVALID;
+    HeadPlan h;
+    if (workspace_bytes == 0 || !head_plan(d, head, label != nullptr, workspace_bytes, &h)) return VMOE_ERR_INVALID;
+    return launch_head_loss_bwd(d, h, HeadIn{z, w, label, teacher_idx, teacher_logit}, ce, lse, tlse, logp, dce, dlse, dkl, dz,
+                                dw, workspace, (cudaStream_t)cuda_stream);
 }
 
 // The problem and the norm's description; d <= 8192 (32 warps of 256 channels hold a row).

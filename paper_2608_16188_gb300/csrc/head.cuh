@@ -1,0 +1,66 @@
+// head.cuh -- a head over a large vocabulary: shared declarations of its matrix products (head_tc.cu) and of what is
+// around them (head.cu) (internal).
+#pragma once
+
+#include "common.cuh"
+
+namespace vmoe {
+
+constexpr int HEAD_K = 128;     // entries of a teacher's list at most
+constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
+
+// Sizes of a call, and where its scratch lies in the workspace (byte offsets).
+struct HeadPlan {
+    int T, N, d, V, K;   // heads, tokens of a head (all tasks' with a shared one), width, vocabulary, teacher's entries
+    int Np;              // N in whole tiles: row pitch of what holds tokens
+    int parts;           // bf16 parts of a value: 1, or 3 (fp32)
+    int stats;           // sums of a row: 1, or 2 (labels and a teacher at another temperature)
+    int piece;           // backward: columns of a piece of the vocabulary, whole tiles
+    int splits;          // backward: parts of the sum over the vocabulary in dz
+    float tau;           // the temperature
+    float c1, c2;        // log2(e), log2(e) / temperature
+    size_t rows, pos, map, label, z, w;     // both ways
+    size_t part, part2, picked;             // forward
+    size_t coef, at_label, dl, dzp;         // backward
+    size_t bytes;
+};
+
+// One product of the head's, for launch_head_gemm.
+enum { HEAD_STATS = 0, HEAD_DLOGITS = 1, HEAD_DZ = 2, HEAD_DW = 3 };
+struct HeadGemm {
+    int T, Np, V, d, parts, np;   // np: products of parts
+    int stats;                    // 1 or 2 sums, or coefficients, a row
+    const int *rows;              // [T] tokens that take part
+    int v0, vn;                   // the piece: first column, columns
+    int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows
+    int splits, first;            // HEAD_DZ: parts of the sum; whether this is the first piece
+    float c1, c2;
+    const int *label;             // [T][Np] of compact rows, -1: none
+    float2 *part;                 // HEAD_STATS out: [T][2 tiles_n][Np] largest logit times c1, sum
+    float2 *part2;                // the same at c2
+    float *picked;                // [T][Np] the label's logit
+    const float4 *coef;           // HEAD_DLOGITS: a, lse times log2(e), b, tlse times log2(e) of a row
+    const float *at_label;        // the first sum's share of the gradient there
+    float *out;                   // HEAD_DZ: [splits][T][Np][d]; HEAD_DW, fp32: [T][V][d]
+    int *status;
+};
+
+// a, b: the operands; dw: HEAD_DW's bf16 output; dl: HEAD_DLOGITS' output, [parts][T][Np][piece].
+int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat16 *z, const __nv_bfloat16 *w,
+                     __nv_bfloat16 *dl, __nv_bfloat16 *dw, cudaStream_t s);
+
+struct HeadIn {
+    const void *z, *w;
+    const int32_t *label, *tidx;
+    const float *tlogit;
+};
+// The plan for a workspace of `bytes` (0: the one that is recommended); false if they do not do.
+bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, HeadPlan *out);
+size_t head_min_workspace(const Dims &p, const vmoe_head *head);
+int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *ce, float *lse, float *kl, float *tlse,
+                     float *logp, void *workspace, cudaStream_t s);
+int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, const float *ce, const float *lse,
+                         const float *tlse, const float *logp, const float *dce, const float *dlse, const float *dkl,
+                         void *dz, void *dw, void *workspace, cudaStream_t s);
+
+}  // namespace vmoe
