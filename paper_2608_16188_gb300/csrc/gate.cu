@@ -11,8 +11,8 @@
 // a bound on its error, and where a choice's runner-up is within it, those experts alone are compared in 64 bits (a
 // row in a thousand at 256 experts).  Without a bias the order is that of the logits, which needs neither.
 //
-// gate_rows: a warp a row, lane l holding experts l, l + 32, ...; a CTA's tile of rows also counts its choices by
-// (choice, expert).  gate_slots: the tile's first place for every (choice, expert) is the sum of the counts of all
+// gate_fast: a row on a few lanes, in fp32; gate_rows: a warp a row, for groups of odd sizes.  A CTA's tile of rows also
+// counts its choices by (choice, expert).  gate_slots: the tile's first place for every (choice, expert) is the sum of the counts of all
 // tiles' earlier choices and of the earlier tiles' same choice; a warp then ranks a choice of the tile 32 rows at a
 // time.  Slots are those of vmoe_route: choice by choice, in token order.  No floating-point sum depends on an order of
 // arrival, and the integer atomics' order does not show.
@@ -47,259 +47,289 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// M experts a lane: E <= 32 M.
+// A row's choices: lane j has the j-th expert and its logit, -1 and -inf where there is none.  mx, sum: the softmax's
+// largest logit and sum of exponentials.
+struct Choice {
+    int e;
+    float x, mx, sum;
+};
+
+// One row by a whole warp, whatever the groups' size, M experts a lane (E <= 32 M), with the comparisons in 64 bits where
+// fp32 leaves them open.  cd [32 M], cf [32 M], gs [32 M]: this warp's scratch.
 template <int M>
-__global__ void __launch_bounds__(GT_THREADS)
+__device__ __noinline__ Choice choose_row(const Dims &p, const Gating &g, int t, long long tn, const float *__restrict__ logits,
+                                          const float *__restrict__ sbias, double *cd, float *cf, float *gs) {
+    const int E = p.E, k = p.k, lane = threadIdx.x & 31, gsize = E / g.groups;
+    const bool softmax = g.score == VMOE_SCORE_SOFTMAX, grouped = g.groups > 1;
+    const bool by_logit = sbias == nullptr;  // the order of c is that of the logits
+    const bool group_by_logit = by_logit && g.top == 1;
+    float x[M], s[M], c[M], b[M], mx = -INFINITY;
+    bool on[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        const int e = lane + 32 * i;
+        x[i] = e < E ? __ldg(logits + tn * E + e) : -INFINITY;
+        b[i] = sbias && e < E ? __ldg(sbias + (long long)t * E + e) : 0.0f;
+        if (!(fabsf(x[i]) < INFINITY)) x[i] = -INFINITY;
+        on[i] = x[i] > -INFINITY && fabsf(b[i]) < INFINITY;  // what is not finite is off
+        mx = fmaxf(mx, x[i]);
+    }
+    mx = softmax ? warp_max(mx) : 0.0f;
+    float sum = 1.0f;
+    if (softmax) {
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            s[i] = x[i] > -INFINITY ? expf(x[i] - mx) : 0.0f;
+            sum += s[i];
+        }
+        sum = warp_sum(sum);
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        s[i] = softmax ? s[i] / sum : 1.0f / (1.0f + expf(-x[i]));
+        c[i] = on[i] ? (by_logit ? x[i] : s[i] + b[i]) : -INFINITY;
+    }
+    double top64 = mx, inv64 = 0.0;
+    auto row64 = [&]() {  // the row's sum in 64 bits, once it is needed
+        if (!softmax || inv64 != 0.0) return;
+        double v = 0.0;
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+            if (x[i] > -INFINITY) v += exp((double)x[i] - top64);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+        inv64 = 1.0 / v;
+    };
+    if (grouped) {
+        // a lane a group: the sum of its `top` largest values, its rank among the groups
+        float err = 0.0f;
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const int e = lane + 32 * i;
+            if (e >= E) continue;
+            const float v = !on[i] ? -INFINITY : group_by_logit ? x[i] : s[i] + b[i];
+            cf[e] = v;
+            if (on[i] && !group_by_logit) err = fmaxf(err, near_of(s[i], v));
+        }
+        err = 2.0f * g.top * warp_max(err);
+        __syncwarp();
+        for (int q = lane; q < g.groups; q += 32) {
+            float a = -INFINITY, a2 = -INFINITY;
+            for (int i = 0; i < gsize; ++i) {
+                const float v = cf[q * gsize + i];
+                a2 = fmaxf(a2, fminf(a, v));
+                a = fmaxf(a, v);
+            }
+            gs[q] = g.top == 2 ? a + a2 : a;
+        }
+        __syncwarp();
+        // the groups before q in the order: a larger score, or the same and a lower index
+        auto rank_of = [&](int q, auto *score) {
+            int r = 0;
+            for (int o = 0; o < g.groups; ++o) r += score[o] > score[q] || (score[o] == score[q] && o < q);
+            return r;
+        };
+        float in = INFINITY, out = -INFINITY;
+        unsigned open = 0;  // bit q / 32: group q of this lane
+        for (int q = lane; q < g.groups; q += 32) {
+            const bool kept = rank_of(q, gs) < g.kept;
+            open |= (unsigned)kept << (q >> 5);
+            if (kept) in = fminf(in, gs[q]);
+            else out = fmaxf(out, gs[q]);
+        }
+        in = -warp_max(-in);
+        out = warp_max(out);
+        if (!group_by_logit && out > -INFINITY && !(in - out > err)) {
+            // all of the same logit and bias: the fp32 values are equal where the exact ones are
+            float lo = INFINITY, hi = -INFINITY, blo = INFINITY, bhi = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (on[i]) {
+                    lo = fminf(lo, x[i]);
+                    hi = fmaxf(hi, x[i]);
+                    blo = fminf(blo, b[i]);
+                    bhi = fmaxf(bhi, b[i]);
+                }
+            if (warp_max(-lo) != -warp_max(hi) || warp_max(-blo) != -warp_max(bhi)) {
+                row64();
+#pragma unroll
+                for (int i = 0; i < M; ++i)
+                    if (lane + 32 * i < E)
+                        cd[lane + 32 * i] = on[i] ? exact_value(x[i], b[i], softmax, top64, inv64) : -INFINITY;
+                __syncwarp();
+                double mine[M];
+                int m = 0;
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    mine[i] = -INFINITY;
+                    const int q = lane + 32 * i;
+                    if (q >= g.groups) continue;
+                    double a = -INFINITY, a2 = -INFINITY;
+                    for (int o = 0; o < gsize; ++o) {
+                        const double v = cd[q * gsize + o];
+                        a2 = fmax(a2, fmin(a, v));
+                        a = fmax(a, v);
+                    }
+                    mine[i] = g.top == 2 ? a + a2 : a;
+                    m = i + 1;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < M; ++i)
+                    if (i < m) cd[lane + 32 * i] = mine[i];
+                __syncwarp();
+                open = 0;
+                for (int q = lane; q < g.groups; q += 32) open |= (unsigned)(rank_of(q, cd) < g.kept) << (q >> 5);
+                __syncwarp();
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+            const int q = min(lane + 32 * i, E - 1) / gsize;
+            const unsigned word = __shfl_sync(FULL, open, q & 31);
+            if (!((word >> (q >> 5)) & 1u)) c[i] = -INFINITY;
+        }
+        __syncwarp();
+    }
+    // the k largest c in turn
+    Choice r;
+    r.x = -INFINITY;
+    r.e = -1;
+    r.mx = mx;
+    r.sum = sum;
+    for (int j = 0; j < k; ++j) {
+        float m = c[0];
+        int at = 0;
+#pragma unroll
+        for (int i = 1; i < M; ++i)
+            if (c[i] > m) {
+                m = c[i];
+                at = i;
+            }
+        const float best = warp_max(m);
+        if (!(best > -INFINITY)) break;
+        float low = best;  // by_logit: equal ones alone
+        if (!by_logit) {
+            float sb = 0.0f;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (i == at && m == best) sb = s[i];
+            low -= near_of(warp_max(sb), best);
+        }
+        auto may_be = [&](int i) { return c[i] > -INFINITY && (by_logit ? c[i] == low : c[i] + near_of(s[i], c[i]) >= low); };
+        // whoever may be the largest: one, as a rule
+        int mine = 0, e = E;
+#pragma unroll
+        for (int i = M - 1; i >= 0; --i)
+            if (may_be(i)) {
+                ++mine;
+                e = lane + 32 * i;
+            }
+        if (!by_logit && __reduce_add_sync(FULL, mine) > 1) {
+            // the first of them, and whether all have its logit and bias
+            const int first = __reduce_min_sync(FULL, e);
+            float fx = 0.0f, fb = 0.0f;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (lane + 32 * i == first) {
+                    fx = x[i];
+                    fb = b[i];
+                }
+            fx = __shfl_sync(FULL, fx, first & 31);
+            fb = __shfl_sync(FULL, fb, first & 31);
+            bool same = true;
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+                if (may_be(i)) same &= x[i] == fx && b[i] == fb;
+            if (!__all_sync(FULL, same)) {
+                row64();
+                double v = -INFINITY;
+                e = E;
+#pragma unroll
+                for (int i = 0; i < M; ++i)
+                    if (may_be(i)) {
+                        const double w = exact_value(x[i], b[i], softmax, top64, inv64);
+                        if (w > v || e == E) {
+                            v = w;
+                            e = lane + 32 * i;
+                        }
+                    }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const double ov = __shfl_xor_sync(FULL, v, o);
+                    const int oe = __shfl_xor_sync(FULL, e, o);
+                    if (oe < E && (e == E || ov > v || (ov == v && oe < e))) {
+                        v = ov;
+                        e = oe;
+                    }
+                }
+            }
+        }
+        const int chosen = __reduce_min_sync(FULL, e);
+        float cx = 0.0f;
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+            if (lane + 32 * i == chosen) {
+                cx = x[i];
+                c[i] = -INFINITY;
+            }
+        cx = __shfl_sync(FULL, cx, chosen & 31);
+        if (lane == j) {
+            r.x = cx;
+            r.e = chosen;
+        }
+    }
+    return r;
+}
+
+// Gate of lane j's choice; `size` lanes of the warp hold a row's.
+__device__ __forceinline__ float gate_of(const Gating &g, const Choice &r, int size) {
+    float xmax = r.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < size) xmax = fmaxf(xmax, __shfl_xor_sync(FULL, xmax, o));
+    const bool softmax = g.score == VMOE_SCORE_SOFTMAX;
+    float w = 0.0f;
+    if (r.e >= 0) {
+        // exp(x - xmax) is a softmax's ratio, and a sigmoid's where all are so far out that it is exp(x)
+        if (softmax && !g.renorm) w = expf(r.x - r.mx) / r.sum;
+        else if (softmax || (g.renorm && xmax < -60.0f)) w = expf(r.x - xmax);
+        else w = 1.0f / (1.0f + expf(-r.x));
+    }
+    float mass = w;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < size) mass += __shfl_xor_sync(FULL, mass, o);
+    return r.e < 0 ? 0.0f : g.renorm ? g.scale * (w / mass) : g.scale * w;
+}
+
+constexpr size_t row_scratch(int M) { return (size_t)GT_WARPS * 32 * M * 16; }
+
+// Groups that are neither a power of two nor at least four experts.
+template <int M>
+__global__ void __launch_bounds__(GT_THREADS, 3)
 gate_rows_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, const float *__restrict__ sbias,
                  const uint8_t *__restrict__ mask, int32_t *__restrict__ out_idx, float *__restrict__ out_gate,
                  int32_t *__restrict__ hist) {
     extern __shared__ __align__(16) uint8_t gt_smem[];
     const int E = p.E, k = p.k, N = p.N, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    double *cd = reinterpret_cast<double *>(gt_smem) + warp * 32 * M;                // [32 M] a warp: c in 64 bits
-    float *cf = reinterpret_cast<float *>(gt_smem + GT_WARPS * 32 * M * 8) + warp * 64 * M;  // [32 M] c, [32 M] the groups' scores
-    float *gs = cf + 32 * M;
-    int *count = reinterpret_cast<int *>(gt_smem + GT_WARPS * 32 * M * 16);          // [k][E]
-    const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows), gsize = E / g.groups;
-    const bool softmax = g.score == VMOE_SCORE_SOFTMAX, grouped = g.groups > 1;
-    const bool by_logit = sbias == nullptr;                      // the order of c is that of the logits
-    const bool group_by_logit = by_logit && g.top == 1;
+    double *cd = reinterpret_cast<double *>(gt_smem) + warp * 64 * M;
+    float *cf = reinterpret_cast<float *>(cd + 32 * M), *gs = cf + 32 * M;
+    int *count = reinterpret_cast<int *>(gt_smem + row_scratch(M));  // [k][E]
+    const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows);
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) count[i] = 0;
     pdl_wait();
-    float b[M];
-#pragma unroll
-    for (int i = 0; i < M; ++i) b[i] = sbias && lane + 32 * i < E ? sbias[(long long)t * E + lane + 32 * i] : 0.0f;
     __syncthreads();
     for (int n = n0 + warp; n < n1; n += GT_WARPS) {
         const long long tn = (long long)t * N + n;
-        const bool takes = mask == nullptr || mask[tn] != 0;
-        float x[M], s[M], c[M], mx = -INFINITY;
-        bool on[M];
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
-            const int e = lane + 32 * i;
-            x[i] = takes && e < E ? __ldg(logits + tn * E + e) : -INFINITY;
-            if (!(fabsf(x[i]) < INFINITY)) x[i] = -INFINITY;
-            on[i] = x[i] > -INFINITY && fabsf(b[i]) < INFINITY;  // what is not finite is off
-            mx = fmaxf(mx, x[i]);
-        }
-        mx = softmax ? warp_max(mx) : 0.0f;
-        float sum = 1.0f;
-        if (softmax) {
-            sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                s[i] = x[i] > -INFINITY ? expf(x[i] - mx) : 0.0f;
-                sum += s[i];
-            }
-            sum = warp_sum(sum);
-        }
-#pragma unroll
-        for (int i = 0; i < M; ++i) {
-            s[i] = softmax ? s[i] / sum : 1.0f / (1.0f + expf(-x[i]));
-            c[i] = on[i] ? (by_logit ? x[i] : s[i] + b[i]) : -INFINITY;
-        }
-        double top64 = mx, inv64 = 0.0;
-        auto row64 = [&]() {  // the row's sum in 64 bits, once it is needed
-            if (!softmax || inv64 != 0.0) return;
-            double v = 0.0;
-#pragma unroll
-            for (int i = 0; i < M; ++i)
-                if (x[i] > -INFINITY) v += exp((double)x[i] - top64);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-            inv64 = 1.0 / v;
-        };
-        if (grouped) {
-            // a lane a group: the sum of its `top` largest values, its rank among the groups
-            float err = 0.0f;
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                const int e = lane + 32 * i;
-                if (e >= E) continue;
-                const float v = !on[i] ? -INFINITY : group_by_logit ? x[i] : s[i] + b[i];
-                cf[e] = v;
-                if (on[i] && !group_by_logit) err = fmaxf(err, near_of(s[i], v));
-            }
-            err = 2.0f * g.top * warp_max(err);
-            __syncwarp();
-            for (int q = lane; q < g.groups; q += 32) {
-                float a = -INFINITY, a2 = -INFINITY;
-                for (int i = 0; i < gsize; ++i) {
-                    const float v = cf[q * gsize + i];
-                    a2 = fmaxf(a2, fminf(a, v));
-                    a = fmaxf(a, v);
-                }
-                gs[q] = g.top == 2 ? a + a2 : a;
-            }
-            __syncwarp();
-            // the groups before q in the order: a larger score, or the same and a lower index
-            auto rank_of = [&](int q, auto *score) {
-                int r = 0;
-                for (int o = 0; o < g.groups; ++o) r += score[o] > score[q] || (score[o] == score[q] && o < q);
-                return r;
-            };
-            float in = INFINITY, out = -INFINITY;
-            unsigned open = 0;  // bit q / 32: group q of this lane
-            for (int q = lane; q < g.groups; q += 32) {
-                const bool kept = rank_of(q, gs) < g.kept;
-                open |= (unsigned)kept << (q >> 5);
-                if (kept) in = fminf(in, gs[q]);
-                else out = fmaxf(out, gs[q]);
-            }
-            in = -warp_max(-in);
-            out = warp_max(out);
-            if (!group_by_logit && out > -INFINITY && !(in - out > err)) {
-                // all of the same logit and bias: the fp32 values are equal where the exact ones are
-                float lo = INFINITY, hi = -INFINITY, blo = INFINITY, bhi = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < M; ++i)
-                    if (on[i]) {
-                        lo = fminf(lo, x[i]);
-                        hi = fmaxf(hi, x[i]);
-                        blo = fminf(blo, b[i]);
-                        bhi = fmaxf(bhi, b[i]);
-                    }
-                if (warp_max(-lo) != -warp_max(hi) || warp_max(-blo) != -warp_max(bhi)) {
-                    row64();
-#pragma unroll
-                    for (int i = 0; i < M; ++i)
-                        if (lane + 32 * i < E)
-                            cd[lane + 32 * i] = on[i] ? exact_value(x[i], b[i], softmax, top64, inv64) : -INFINITY;
-                    __syncwarp();
-                    double mine[M];
-                    int m = 0;
-#pragma unroll
-                    for (int i = 0; i < M; ++i) {
-                        mine[i] = -INFINITY;
-                        const int q = lane + 32 * i;
-                        if (q >= g.groups) continue;
-                        double a = -INFINITY, a2 = -INFINITY;
-                        for (int o = 0; o < gsize; ++o) {
-                            const double v = cd[q * gsize + o];
-                            a2 = fmax(a2, fmin(a, v));
-                            a = fmax(a, v);
-                        }
-                        mine[i] = g.top == 2 ? a + a2 : a;
-                        m = i + 1;
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < M; ++i)
-                        if (i < m) cd[lane + 32 * i] = mine[i];
-                    __syncwarp();
-                    open = 0;
-                    for (int q = lane; q < g.groups; q += 32) open |= (unsigned)(rank_of(q, cd) < g.kept) << (q >> 5);
-                    __syncwarp();
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < M; ++i) {
-                const int q = min(lane + 32 * i, E - 1) / gsize;
-                const unsigned word = __shfl_sync(FULL, open, q & 31);
-                if (!((word >> (q >> 5)) & 1u)) c[i] = -INFINITY;
-            }
-            __syncwarp();
-        }
-        // the k largest c in turn
-        float my_x = -INFINITY;
-        int my_e = -1;
-        for (int j = 0; j < k; ++j) {
-            float m = c[0];
-            int at = 0;
-#pragma unroll
-            for (int i = 1; i < M; ++i)
-                if (c[i] > m) {
-                    m = c[i];
-                    at = i;
-                }
-            const float best = warp_max(m);
-            if (!(best > -INFINITY)) break;
-            float low = best;  // by_logit: equal ones alone
-            if (!by_logit) {
-                float sb = 0.0f;
-#pragma unroll
-                for (int i = 0; i < M; ++i)
-                    if (i == at && m == best) sb = s[i];
-                low -= near_of(warp_max(sb), best);
-            }
-            auto may_be = [&](int i) { return c[i] > -INFINITY && (by_logit ? c[i] == low : c[i] + near_of(s[i], c[i]) >= low); };
-            // whoever may be the largest: one, as a rule
-            int mine = 0, e = E;
-#pragma unroll
-            for (int i = M - 1; i >= 0; --i)
-                if (may_be(i)) {
-                    ++mine;
-                    e = lane + 32 * i;
-                }
-            if (!by_logit && __reduce_add_sync(FULL, mine) > 1) {
-                // the first of them, and whether all have its logit and bias
-                const int first = __reduce_min_sync(FULL, e);
-                float fx = 0.0f, fb = 0.0f;
-#pragma unroll
-                for (int i = 0; i < M; ++i)
-                    if (lane + 32 * i == first) {
-                        fx = x[i];
-                        fb = b[i];
-                    }
-                fx = __shfl_sync(FULL, fx, first & 31);
-                fb = __shfl_sync(FULL, fb, first & 31);
-                bool same = true;
-#pragma unroll
-                for (int i = 0; i < M; ++i)
-                    if (may_be(i)) same &= x[i] == fx && b[i] == fb;
-                if (!__all_sync(FULL, same)) {
-                    row64();
-                    double v = -INFINITY;
-                    e = E;
-#pragma unroll
-                    for (int i = 0; i < M; ++i)
-                        if (may_be(i)) {
-                            const double w = exact_value(x[i], b[i], softmax, top64, inv64);
-                            if (w > v || e == E) {
-                                v = w;
-                                e = lane + 32 * i;
-                            }
-                        }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) {
-                        const double ov = __shfl_xor_sync(FULL, v, o);
-                        const int oe = __shfl_xor_sync(FULL, e, o);
-                        if (oe < E && (e == E || ov > v || (ov == v && oe < e))) {
-                            v = ov;
-                            e = oe;
-                        }
-                    }
-                }
-            }
-            const int chosen = __reduce_min_sync(FULL, e);
-            float cx = 0.0f;
-#pragma unroll
-            for (int i = 0; i < M; ++i)
-                if (lane + 32 * i == chosen) {
-                    cx = x[i];
-                    c[i] = -INFINITY;
-                }
-            cx = __shfl_sync(FULL, cx, chosen & 31);
-            if (lane == j) {
-                my_x = cx;
-                my_e = chosen;
-            }
-        }
-        // the gates: lanes 0 to k - 1
-        const float xmax = warp_max(my_x);
-        float w = 0.0f;
-        if (my_e >= 0) {
-            // exp(x - xmax) is a softmax's ratio, and a sigmoid's where all are so far out that it is exp(x)
-            if (softmax && g.renorm) w = expf(my_x - xmax);
-            else if (softmax) w = expf(my_x - mx) / sum;
-            else if (g.renorm && xmax < -60.0f) w = expf(my_x - xmax);
-            else w = 1.0f / (1.0f + expf(-my_x));
-        }
-        const float mass = warp_sum(w);
+        Choice r = {-1, -INFINITY, 0.0f, 1.0f};
+        if (mask == nullptr || mask[tn] != 0) r = choose_row<M>(p, g, t, tn, logits, sbias, cd, cf, gs);
+        const float gate = gate_of(g, r, 32);
         if (lane < k) {
-            out_idx[tn * k + lane] = my_e;
-            out_gate[tn * k + lane] = my_e < 0 ? 0.0f : g.renorm ? g.scale * (w / mass) : g.scale * w;
-            if (my_e >= 0) atomicAdd(count + lane * E + my_e, 1);
+            out_idx[tn * k + lane] = r.e;
+            out_gate[tn * k + lane] = gate;
+            if (r.e >= 0) atomicAdd(count + lane * E + r.e, 1);
         }
     }
     __syncthreads();
@@ -307,15 +337,260 @@ gate_rows_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) h[i] = count[i];
 }
 
+__device__ __forceinline__ float ex2(float v) {
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(v));
+    return v;
+}
+__device__ __forceinline__ float rcp(float v) {
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(v));
+    return v;
+}
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// A row on L lanes, V experts in a row each (L V >= E), 32 / L rows a warp, the next ones' logits in flight; no group, or
+// groups of a power of two of experts, at least V of them.  c is formed with the approximate exponential and
+// reciprocal; a row with two of the first k + 1 values, or two groups, closer than their error is done again by choose_row:
+//   sigmoid: the exponential is off by 2^-22 + |x| 2^-23.5 relative, which e / (1 + e)^2 <= 1 / 4 and |x| e / (1 + e)^2 <=
+//   0.23 take to 8e-8 of 1 in s, the reciprocal and the sum add 1.8e-7 s; softmax: 1e-6 s for |x - max| <= 10, and s
+//   |x - max| 6e-8 <= s 2e-6 up to 30, below which s is nothing beside the bias' rounding; c's rounding 6e-8 |c|.
+template <int L, int V>
+__global__ void __launch_bounds__(GT_THREADS, V == 8 ? 3 : 4)
+gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, const float *__restrict__ sbias,
+                 const uint8_t *__restrict__ mask, int32_t *__restrict__ out_idx, float *__restrict__ out_gate,
+                 int32_t *__restrict__ hist) {
+    constexpr int RW = 32 / L, M = L * V / 32 > 0 ? L * V / 32 : 1;
+    constexpr float LOG2E = 1.4426950408889634f;
+    extern __shared__ __align__(16) uint8_t gt_smem[];
+    const int E = p.E, k = p.k, N = p.N, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    double *cd = reinterpret_cast<double *>(gt_smem) + warp * 64 * M;
+    float *cf = reinterpret_cast<float *>(cd + 32 * M), *gs = cf + 32 * M;
+    int *count = reinterpret_cast<int *>(gt_smem + row_scratch(M));  // [k][E]
+    const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows), gsize = E / g.groups;
+    const int sub = lane / L, sl = lane % L, e0 = sl * V, mine = e0 / gsize, glanes = gsize / V;
+    const bool softmax = g.score == VMOE_SCORE_SOFTMAX, by_logit = sbias == nullptr, group_by_logit = by_logit && g.top == 1;
+    const bool scored = !by_logit || (g.groups > 1 && !group_by_logit);  // s is needed for the choice
+    for (int i = threadIdx.x; i < k * E; i += GT_THREADS) count[i] = 0;
+    pdl_wait();
+    float b[V], bmax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        b[i] = sbias && e0 + i < E ? __ldg(sbias + (long long)t * E + e0 + i) : 0.0f;
+        if (fabsf(b[i]) < INFINITY) bmax = fmaxf(bmax, fabsf(b[i]));
+    }
+    bmax = warp_max(bmax);
+    __syncthreads();
+    float next[V];
+    bool next_in = false;
+    auto load = [&](int n) {
+        const long long tn = (long long)t * N + n;
+        next_in = n < n1 && (mask == nullptr || mask[tn] != 0);
+        const float *src = logits + tn * E + e0;
+        if (V % 4 == 0 && E % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (n < n1 && e0 + i < E) v = __ldg(reinterpret_cast<const float4 *>(src + i));
+                next[i] = v.x, next[i + 1] = v.y, next[i + 2] = v.z, next[i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) next[i] = n < n1 && e0 + i < E ? __ldg(src + i) : -INFINITY;
+        }
+    };
+    load(n0 + warp * RW + sub);
+    for (int base = n0 + warp * RW; base < n1; base += GT_WARPS * RW) {
+        const int n = base + sub;
+        const bool in = next_in;
+        float x[V], c[V], mx = 0.0f, sum = 1.0f, smax = 1.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = in && fabsf(next[i]) < INFINITY ? next[i] : -INFINITY;
+        load(n + GT_WARPS * RW);
+        if (softmax && (scored || !g.renorm)) {
+            mx = x[0];
+#pragma unroll
+            for (int i = 1; i < V; ++i) mx = fmaxf(mx, x[i]);
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, o));
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                c[i] = x[i] > -INFINITY ? (scored ? ex2((x[i] - mx) * LOG2E) : expf(x[i] - mx)) : 0.0f;
+                sum += c[i];
+            }
+#pragma unroll
+            for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
+            if (scored) {
+                smax = rcp(sum);
+#pragma unroll
+                for (int i = 0; i < V; ++i) c[i] *= smax;
+                if (!g.renorm) {  // the gates' sum, of exponentials to the last place
+                    sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum += x[i] > -INFINITY ? expf(x[i] - mx) : 0.0f;
+#pragma unroll
+                    for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
+                }
+            }
+        } else if (scored) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) c[i] = rcp(1.0f + ex2(-x[i] * LOG2E));
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (!scored) c[i] = x[i];
+            else c[i] = x[i] > -INFINITY && fabsf(b[i]) < INFINITY ? c[i] + b[i] : -INFINITY;
+        }
+        const float rel = softmax ? 2e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
+        auto tol = [&](float v) { return fmaf(rel, fminf(smax, v + bmax), fmaf(1.2e-7f, fabsf(v), abs1)); };
+        bool open = false;  // whether two values are too close for fp32
+        if (g.groups > 1) {
+            float a = -INFINITY, a2 = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                a2 = fmaxf(a2, fminf(a, c[i]));
+                a = fmaxf(a, c[i]);
+            }
+            for (int o = 1; o < glanes; o <<= 1) {
+                const float oa = __shfl_xor_sync(FULL, a, o), oa2 = __shfl_xor_sync(FULL, a2, o);
+                a2 = fmaxf(fminf(a, oa), fmaxf(a2, oa2));
+                a = fmaxf(a, oa);
+            }
+            const float score = g.top == 2 ? a + a2 : a;
+            const float err = (float)g.top * tol(a);
+            int rank = 0;
+            for (int q = 0; q < g.groups; ++q) {
+                const float other = __shfl_sync(FULL, score, q * glanes, L);
+                rank += other > score || (other == score && q < mine);
+                open |= q != mine && fabsf(other - score) <= err + (float)g.top * tol(fabsf(other) + bmax);
+            }
+            open &= !group_by_logit && a > -INFINITY && e0 < E;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (by_logit && scored && c[i] > -INFINITY) c[i] = x[i];  // the choice's own order
+                if (rank >= g.kept) c[i] = -INFINITY;
+            }
+        }
+        Choice r = {-1, -INFINITY, mx, sum};
+        float value = -INFINITY, last = -INFINITY;  // c of this lane's choice; of the best that was not chosen
+        for (int j = 0; j <= k; ++j) {
+            float m = c[0];
+#pragma unroll
+            for (int i = 1; i < V; ++i) m = fmaxf(m, c[i]);
+            int e = 0;
+            if (L == 32) {
+                const float best = redux_max(m);
+                const int first = __ffs(__ballot_sync(FULL, m == best)) - 1;
+                m = best;
+                e = first;
+            } else {
+                e = sl;
+#pragma unroll
+                for (int o = L / 2; o > 0; o >>= 1) {
+                    const float om = __shfl_xor_sync(FULL, m, o);
+                    const int oe = __shfl_xor_sync(FULL, e, o);
+                    if (om > m || (om == m && oe < e)) {
+                        m = om;
+                        e = oe;
+                    }
+                }
+            }
+            if (j == k) {
+                last = m;
+                break;
+            }
+            // e: the lane that has it; its first expert of that value
+            float ex = 0.0f;
+            int at = 0;
+#pragma unroll
+            for (int i = V - 1; i >= 0; --i)
+                if (c[i] == m) {
+                    at = i;
+                    ex = x[i];
+                }
+            const int chosen = e * V + __shfl_sync(FULL, at, e, L);
+            ex = __shfl_sync(FULL, ex, e, L);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (e0 + i == chosen) c[i] = -INFINITY;
+            if (sl == j && m > -INFINITY) {
+                r.e = chosen;
+                r.x = ex;
+                value = m;
+            }
+        }
+        if (!by_logit) {
+            float after = __shfl_down_sync(FULL, value, 1, L);
+            if (sl >= k - 1) after = last;
+            open |= sl < k && after > -INFINITY && !(value - after > tol(value) + tol(after));
+        }
+        unsigned again = __ballot_sync(FULL, open && n < n1);
+        while (again) {  // rows of their own, by the whole warp
+            const int who = (__ffs(again) - 1) / L;
+            again &= ~((L == 32 ? FULL : (1u << (L & 31)) - 1u) << (who * L));
+            const Choice s = choose_row<M>(p, g, t, (long long)t * N + base + who, logits, sbias, cd, cf, gs);
+            const int e = __shfl_sync(FULL, s.e, sl);
+            const float sx = __shfl_sync(FULL, s.x, sl);
+            if (sub == who) {
+                r.e = e;
+                r.x = sx;
+            }
+        }
+        const float gate = gate_of(g, r, L);
+        if (sl < k && n < n1) {
+            const long long at = ((long long)t * N + n) * k + sl;
+            out_idx[at] = r.e;
+            out_gate[at] = gate;
+            if (r.e >= 0) atomicAdd(count + sl * E + r.e, 1);
+        }
+    }
+    __syncthreads();
+    int32_t *h = hist + ((long long)t * gridDim.x + blockIdx.x) * k * E;
+    for (int i = threadIdx.x; i < k * E; i += GT_THREADS) h[i] = count[i];
+}
+
+// Counts of the tiles before each, in place, and of all of them: hist [T][tiles][k][E], all [T][k][E].
+__global__ void __launch_bounds__(GT_THREADS)
+gate_scan_kernel(int kE, int tiles, int32_t *__restrict__ hist, int32_t *__restrict__ all) {
+    const int t = blockIdx.y, i = blockIdx.x * GT_THREADS + threadIdx.x;
+    pdl_wait();
+    if (i >= kE) return;
+    int32_t *h = hist + (long long)t * tiles * kE + i;
+    int run = 0;
+    for (int q = 0; q < tiles; q += 16) {
+        int v[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = q + u < tiles ? h[(long long)(q + u) * kE] : 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+            if (q + u < tiles) {
+                h[(long long)(q + u) * kE] = run;
+                run += v[u];
+            }
+    }
+    all[(long long)t * kE + i] = run;
+}
+
+// SCANNED: behind gate_scan, for many tiles.
+template <bool SCANNED>
 __global__ void __launch_bounds__(GT_THREADS)
 gate_slots_kernel(Dims p, int rows, const int32_t *__restrict__ idx, const int32_t *__restrict__ hist,
-                  int32_t *__restrict__ slot, int32_t *__restrict__ load, int32_t *__restrict__ demand) {
+                  const int32_t *__restrict__ sums, int32_t *__restrict__ slot, int32_t *__restrict__ load,
+                  int32_t *__restrict__ demand) {
     extern __shared__ int gt_base[];  // [k][E]: the next place of each (choice, expert); then [k][E] whole counts
     const int E = p.E, k = p.k, N = p.N, t = blockIdx.y, tiles = gridDim.x, tile = blockIdx.x;
     int *all = gt_base + k * E;
     pdl_wait();
     const int32_t *h = hist + (long long)t * tiles * k * E;
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) {
+        if (SCANNED) {
+            gt_base[i] = h[(long long)tile * k * E + i];
+            all[i] = sums[(long long)t * k * E + i];
+            continue;
+        }
         int before = 0, total = 0;
 #pragma unroll 8
         for (int q = 0; q < tiles; ++q) {
@@ -494,34 +769,69 @@ int tile_rows(int N) {
     return rows;
 }
 
-template <int M>
-int launch_rows(const Dims &p, const Gating &g, int rows, const float *logits, const float *sbias, const uint8_t *mask,
-                int32_t *idx, float *gate, int32_t *hist, cudaStream_t s) {
-    const size_t smem = (size_t)GT_WARPS * 32 * M * 16 + (size_t)p.k * p.E * 4;  // at most 40 KB
-    return launch_kernel(gate_rows_kernel<M>, dim3((p.N + rows - 1) / rows, p.T), dim3(GT_THREADS), smem, s, p, g, rows,
-                         logits, sbias, mask, idx, gate, hist);
+// Launch arguments of gate_rows and gate_fast.
+struct RowArgs {
+    Dims p;
+    Gating g;
+    int rows;
+    const float *logits, *sbias;
+    const uint8_t *mask;
+    int32_t *idx;
+    float *gate;
+    int32_t *hist;
+};
+template <typename Kern>
+int launch_rows(Kern kern, int M, const RowArgs &a, cudaStream_t s) {
+    const size_t smem = row_scratch(M) + (size_t)a.p.k * a.p.E * 4;  // at most 40 KB
+    return launch_kernel(kern, dim3((a.p.N + a.rows - 1) / a.rows, a.p.T), dim3(GT_THREADS), smem, s, a.p, a.g, a.rows, a.logits,
+                         a.sbias, a.mask, a.idx, a.gate, a.hist);
+}
+int choose_rows(const RowArgs &a, cudaStream_t s) {
+    const int E = a.p.E, gsize = E / a.g.groups;
+    const int V = E > 128 ? 8 : 4;
+    const bool aligned = a.g.groups == 1 || (gsize >= V && (gsize & (gsize - 1)) == 0);
+    if (!aligned) {
+        if (E <= 32) return launch_rows(gate_rows_kernel<1>, 1, a, s);
+        if (E <= 64) return launch_rows(gate_rows_kernel<2>, 2, a, s);
+        if (E <= 128) return launch_rows(gate_rows_kernel<4>, 4, a, s);
+        return launch_rows(gate_rows_kernel<8>, 8, a, s);
+    }
+    int L = 1;  // lanes for the experts and for the choices
+    while (L * V < E || L < a.p.k) L *= 2;
+    if (V == 8) return launch_rows(gate_fast_kernel<32, 8>, 8, a, s);
+    if (L <= 2) return launch_rows(gate_fast_kernel<2, 4>, 1, a, s);
+    if (L <= 4) return launch_rows(gate_fast_kernel<4, 4>, 1, a, s);
+    if (L <= 8) return launch_rows(gate_fast_kernel<8, 4>, 1, a, s);
+    if (L <= 16) return launch_rows(gate_fast_kernel<16, 4>, 2, a, s);
+    return launch_rows(gate_fast_kernel<32, 4>, 4, a, s);
 }
 
 }  // namespace
 
 size_t gate_workspace(const Dims &p) {
     const int rows = tile_rows(p.N);
-    return (size_t)p.T * ((p.N + rows - 1) / rows) * p.k * p.E * 4;
+    return (size_t)p.T * ((p.N + rows - 1) / rows + 1) * p.k * p.E * 4;
 }
 
 int launch_gate(const Dims &p, const Gating &g, const float *logits, const float *sbias, const uint8_t *mask, int32_t *idx,
                 float *gate, int32_t *slot, int32_t *load, int32_t *demand, int32_t *hist, cudaStream_t s) {
-    const int rows = tile_rows(p.N);
+    const int rows = tile_rows(p.N), tiles = (p.N + rows - 1) / rows, kE = p.k * p.E;
     trace_before(s, "gate_rows");
-    int st = p.E <= 32    ? launch_rows<1>(p, g, rows, logits, sbias, mask, idx, gate, hist, s)
-             : p.E <= 64  ? launch_rows<2>(p, g, rows, logits, sbias, mask, idx, gate, hist, s)
-             : p.E <= 128 ? launch_rows<4>(p, g, rows, logits, sbias, mask, idx, gate, hist, s)
-                          : launch_rows<8>(p, g, rows, logits, sbias, mask, idx, gate, hist, s);
+    int st = choose_rows(RowArgs{p, g, rows, logits, sbias, mask, idx, gate, hist}, s);
     trace_after(s);
     if (st != VMOE_OK) return st;
+    int32_t *all = hist + (long long)p.T * tiles * kE;
+    const bool scan = tiles > 32;
+    if (scan) {
+        trace_before(s, "gate_scan");
+        st = launch_kernel(gate_scan_kernel, dim3((kE + GT_THREADS - 1) / GT_THREADS, p.T), dim3(GT_THREADS), 0, s, kE, tiles,
+                           hist, all);
+        trace_after(s);
+        if (st != VMOE_OK) return st;
+    }
     trace_before(s, "gate_slots");
-    st = launch_kernel(gate_slots_kernel, dim3((p.N + rows - 1) / rows, p.T), dim3(GT_THREADS), (size_t)p.k * p.E * 8, s, p,
-                       rows, idx, hist, slot, load, demand);
+    st = launch_kernel(scan ? gate_slots_kernel<true> : gate_slots_kernel<false>, dim3(tiles, p.T), dim3(GT_THREADS),
+                       (size_t)kE * 8, s, p, rows, idx, hist, all, slot, load, demand);
     trace_after(s);
     return st;
 }
