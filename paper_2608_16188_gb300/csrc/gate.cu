@@ -351,9 +351,39 @@ __device__ __forceinline__ float redux_max(float v) {
     return r;
 }
 
+// V values of a lane, the largest first; at: where each came from, 4 bits apiece (a network of compare-exchanges).
+template <int V>
+__device__ __forceinline__ unsigned sort_lane(float (&h)[V]) {
+    int at[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) at[i] = i;
+    auto order = [&](int i, int j) {
+        const bool swap = h[j] > h[i];
+        const float hi = swap ? h[j] : h[i], lo = swap ? h[i] : h[j];
+        const int ai = swap ? at[j] : at[i], aj = swap ? at[i] : at[j];
+        h[i] = hi, h[j] = lo, at[i] = ai, at[j] = aj;
+    };
+    auto merge4 = [&](int i) {
+        order(i, i + 1), order(i + 2, i + 3), order(i, i + 2), order(i + 1, i + 3), order(i + 1, i + 2);
+    };
+    merge4(0);
+    if constexpr (V == 8) {
+        merge4(4);
+        order(0, 4), order(1, 5), order(2, 6), order(3, 7);
+        order(2, 4), order(3, 5);
+        order(1, 2), order(3, 4), order(5, 6);
+    }
+    unsigned r = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r |= (unsigned)at[i] << (4 * i);
+    return r;
+}
+
 // A row on L lanes, V experts in a row each (L V >= E), 32 / L rows a warp, the next ones' logits in flight; no group, or
-// groups of a power of two of experts, at least V of them.  c is formed with the approximate exponential and
-// reciprocal; a row with two of the first k + 1 values, or two groups, closer than their error is done again by choose_row:
+// groups of a power of two of experts, at least V of them.  A lane sorts its values once; a choice is then the largest of
+// the lanes' first values, and its lane moves up.  c is formed with the approximate exponential and reciprocal; a row
+// with two of the first k + 1 values, or an open and a shut group, closer than their error (or equal) is done again by
+// choose_row behind the loop:
 //   sigmoid: the exponential is off by 2^-22 + |x| 2^-23.5 relative, which e / (1 + e)^2 <= 1 / 4 and |x| e / (1 + e)^2 <=
 //   0.23 take to 8e-8 of 1 in s, the reciprocal and the sum add 1.8e-7 s; softmax: 1e-6 s for |x - max| <= 10, and s
 //   |x - max| 6e-8 <= s 2e-6 up to 30, below which s is nothing beside the bias' rounding; c's rounding 6e-8 |c|.
@@ -366,29 +396,29 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     constexpr float LOG2E = 1.4426950408889634f;
     extern __shared__ __align__(16) uint8_t gt_smem[];
     const int E = p.E, k = p.k, N = p.N, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    double *cd = reinterpret_cast<double *>(gt_smem) + warp * 64 * M;
-    float *cf = reinterpret_cast<float *>(cd + 32 * M), *gs = cf + 32 * M;
     int *count = reinterpret_cast<int *>(gt_smem + row_scratch(M));  // [k][E]
+    unsigned *again = reinterpret_cast<unsigned *>(count + k * E);   // a bit a row of the tile
     const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows), gsize = E / g.groups;
     const int sub = lane / L, sl = lane % L, e0 = sl * V, mine = e0 / gsize, glanes = gsize / V;
     const bool softmax = g.score == VMOE_SCORE_SOFTMAX, by_logit = sbias == nullptr, group_by_logit = by_logit && g.top == 1;
     const bool scored = !by_logit || (g.groups > 1 && !group_by_logit);  // s is needed for the choice
-    for (int i = threadIdx.x; i < k * E; i += GT_THREADS) count[i] = 0;
+    const float *row = logits + (long long)t * N * E;
+    for (int i = threadIdx.x; i < k * E + (rows + 31) / 32; i += GT_THREADS) count[i] = 0;
     pdl_wait();
-    float b[V], bmax = 0.0f;
+    float b[V], bmax = 0.0f;  // -inf: off
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         b[i] = sbias && e0 + i < E ? __ldg(sbias + (long long)t * E + e0 + i) : 0.0f;
         if (fabsf(b[i]) < INFINITY) bmax = fmaxf(bmax, fabsf(b[i]));
+        else b[i] = -INFINITY;
     }
     bmax = warp_max(bmax);
     __syncthreads();
     float next[V];
     bool next_in = false;
     auto load = [&](int n) {
-        const long long tn = (long long)t * N + n;
-        next_in = n < n1 && (mask == nullptr || mask[tn] != 0);
-        const float *src = logits + tn * E + e0;
+        next_in = n < n1 && (mask == nullptr || mask[(long long)t * N + n] != 0);
+        const float *src = row + (long long)n * E + e0;
         if (V % 4 == 0 && E % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
@@ -402,92 +432,83 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
         }
     };
     load(n0 + warp * RW + sub);
+    const float rel = softmax ? 2e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
     for (int base = n0 + warp * RW; base < n1; base += GT_WARPS * RW) {
         const int n = base + sub;
-        const bool in = next_in;
-        float x[V], c[V], mx = 0.0f, sum = 1.0f, smax = 1.0f;
+        float c[V], mx = 0.0f, sum = 1.0f, smax = 1.0f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = in && fabsf(next[i]) < INFINITY ? next[i] : -INFINITY;
+        for (int i = 0; i < V; ++i) c[i] = next_in && fabsf(next[i]) < INFINITY ? next[i] : -INFINITY;
         load(n + GT_WARPS * RW);
         if (softmax && (scored || !g.renorm)) {
-            mx = x[0];
+            mx = c[0];
 #pragma unroll
-            for (int i = 1; i < V; ++i) mx = fmaxf(mx, x[i]);
+            for (int i = 1; i < V; ++i) mx = fmaxf(mx, c[i]);
 #pragma unroll
             for (int o = L / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, o));
+            mx = fmaxf(mx, -3.4028235e38f);  // a row of nothing: exponentials of -inf, not of a NaN
             sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                c[i] = x[i] > -INFINITY ? (scored ? ex2((x[i] - mx) * LOG2E) : expf(x[i] - mx)) : 0.0f;
-                sum += c[i];
-            }
+            for (int i = 0; i < V; ++i) sum += g.renorm ? ex2((c[i] - mx) * LOG2E) : expf(c[i] - mx);
 #pragma unroll
             for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
-            if (scored) {
-                smax = rcp(sum);
-#pragma unroll
-                for (int i = 0; i < V; ++i) c[i] *= smax;
-                if (!g.renorm) {  // the gates' sum, of exponentials to the last place
-                    sum = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) sum += x[i] > -INFINITY ? expf(x[i] - mx) : 0.0f;
-#pragma unroll
-                    for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
-                }
-            }
-        } else if (scored) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) c[i] = rcp(1.0f + ex2(-x[i] * LOG2E));
+            smax = rcp(sum);
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (!scored) c[i] = x[i];
-            else c[i] = x[i] > -INFINITY && fabsf(b[i]) < INFINITY ? c[i] + b[i] : -INFINITY;
-        }
-        const float rel = softmax ? 2e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
-        auto tol = [&](float v) { return fmaf(rel, fminf(smax, v + bmax), fmaf(1.2e-7f, fabsf(v), abs1)); };
-        bool open = false;  // whether two values are too close for fp32
-        if (g.groups > 1) {
-            float a = -INFINITY, a2 = -INFINITY;
+        const float before = softmax && (scored || !g.renorm) ? mx : 0.0f;
+        if (scored) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                a2 = fmaxf(a2, fminf(a, c[i]));
-                a = fmaxf(a, c[i]);
+                const float s = softmax ? ex2((c[i] - before) * LOG2E) * smax : rcp(1.0f + ex2(-c[i] * LOG2E));
+                c[i] = c[i] > -INFINITY ? s + b[i] : -INFINITY;
             }
+        }
+        // the error of a value, from s <= smax, c + bmax
+        auto tol = [&](float v) { return fmaf(rel, fminf(smax, v + bmax), fmaf(1.2e-7f, fabsf(v), abs1)); };
+        bool open = false;  // whether two values are too close for fp32
+        unsigned at = sort_lane<V>(c);
+        if (g.groups > 1) {
+            float a = c[0], a2 = c[1];
             for (int o = 1; o < glanes; o <<= 1) {
                 const float oa = __shfl_xor_sync(FULL, a, o), oa2 = __shfl_xor_sync(FULL, a2, o);
                 a2 = fmaxf(fminf(a, oa), fmaxf(a2, oa2));
                 a = fmaxf(a, oa);
             }
             const float score = g.top == 2 ? a + a2 : a;
-            const float err = (float)g.top * tol(a);
             int rank = 0;
             for (int q = 0; q < g.groups; ++q) {
                 const float other = __shfl_sync(FULL, score, q * glanes, L);
                 rank += other > score || (other == score && q < mine);
-                open |= q != mine && fabsf(other - score) <= err + (float)g.top * tol(fabsf(other) + bmax);
             }
-            open &= !group_by_logit && a > -INFINITY && e0 < E;
+            const bool kept = rank < g.kept;
+            float in = kept ? score : INFINITY, out = kept || mine >= g.groups ? -INFINITY : score;
+            for (int o = glanes; o < L; o <<= 1) {
+                in = fminf(in, __shfl_xor_sync(FULL, in, o));
+                out = fmaxf(out, __shfl_xor_sync(FULL, out, o));
+            }
+            // values at the border are at most |score| + bmax each
+            open = !group_by_logit && out > -INFINITY &&
+                   !(in - out > (float)g.top * (tol(fabsf(in) + bmax) + tol(fabsf(out) + bmax)));
+            if (by_logit && scored) {  // the choice has the logits' order: the lane's values again, as they came
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (by_logit && scored && c[i] > -INFINITY) c[i] = x[i];  // the choice's own order
-                if (rank >= g.kept) c[i] = -INFINITY;
+                for (int i = 0; i < V; ++i) {
+                    const float l = n < n1 && e0 + i < E ? __ldg(row + (long long)n * E + e0 + i) : -INFINITY;
+                    c[i] = a > -INFINITY && fabsf(l) < INFINITY ? l : -INFINITY;
+                }
+                at = sort_lane<V>(c);
+            }
+            if (!kept) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) c[i] = -INFINITY;
             }
         }
-        Choice r = {-1, -INFINITY, mx, sum};
+        int my_e = -1;
         float value = -INFINITY, last = -INFINITY;  // c of this lane's choice; of the best that was not chosen
         for (int j = 0; j <= k; ++j) {
             float m = c[0];
-#pragma unroll
-            for (int i = 1; i < V; ++i) m = fmaxf(m, c[i]);
-            int e = 0;
+            int e = sl;  // the lane that has the largest, the first of equals
             if (L == 32) {
-                const float best = redux_max(m);
-                const int first = __ffs(__ballot_sync(FULL, m == best)) - 1;
-                m = best;
-                e = first;
+                m = redux_max(m);
+                e = __ffs(__ballot_sync(FULL, c[0] == m)) - 1;
             } else {
-                e = sl;
 #pragma unroll
                 for (int o = L / 2; o > 0; o >>= 1) {
                     const float om = __shfl_xor_sync(FULL, m, o);
@@ -502,49 +523,52 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
                 last = m;
                 break;
             }
-            // e: the lane that has it; its first expert of that value
-            float ex = 0.0f;
-            int at = 0;
+            const int chosen = e * V + (int)(__shfl_sync(FULL, at, e, L) & 15u);
+            if (sl == e) {
 #pragma unroll
-            for (int i = V - 1; i >= 0; --i)
-                if (c[i] == m) {
-                    at = i;
-                    ex = x[i];
-                }
-            const int chosen = e * V + __shfl_sync(FULL, at, e, L);
-            ex = __shfl_sync(FULL, ex, e, L);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (e0 + i == chosen) c[i] = -INFINITY;
+                for (int i = 0; i + 1 < V; ++i) c[i] = c[i + 1];
+                c[V - 1] = -INFINITY;
+                at >>= 4;
+            }
             if (sl == j && m > -INFINITY) {
-                r.e = chosen;
-                r.x = ex;
+                my_e = chosen;
                 value = m;
             }
         }
-        if (!by_logit) {
+        {
             float after = __shfl_down_sync(FULL, value, 1, L);
             if (sl >= k - 1) after = last;
-            open |= sl < k && after > -INFINITY && !(value - after > tol(value) + tol(after));
+            const float err = by_logit ? 0.0f : tol(value) + tol(after);
+            open |= sl < k && after > -INFINITY && !(value - after > err);
         }
-        unsigned again = __ballot_sync(FULL, open && n < n1);
-        while (again) {  // rows of their own, by the whole warp
-            const int who = (__ffs(again) - 1) / L;
-            again &= ~((L == 32 ? FULL : (1u << (L & 31)) - 1u) << (who * L));
-            const Choice s = choose_row<M>(p, g, t, (long long)t * N + base + who, logits, sbias, cd, cf, gs);
-            const int e = __shfl_sync(FULL, s.e, sl);
-            const float sx = __shfl_sync(FULL, s.x, sl);
-            if (sub == who) {
-                r.e = e;
-                r.x = sx;
-            }
+        const unsigned redo = __ballot_sync(FULL, open && n < n1) >> (sub * L) & (L == 32 ? FULL : (1u << (L & 31)) - 1u);
+        Choice r;
+        r.e = my_e;
+        r.x = my_e >= 0 ? __ldg(row + (long long)n * E + my_e) : -INFINITY;
+        r.mx = mx;
+        r.sum = sum;
+        const float gate = gate_of(g, r, L < 8 ? L : 8);
+        if (redo) {
+            if (sl == 0) atomicOr(again + ((n - n0) >> 5), 1u << ((n - n0) & 31));
+        } else if (sl < k && n < n1) {
+            const long long o = ((long long)t * N + n) * k + sl;
+            out_idx[o] = my_e;
+            out_gate[o] = gate;
+            if (my_e >= 0) atomicAdd(count + sl * E + my_e, 1);
         }
-        const float gate = gate_of(g, r, L);
-        if (sl < k && n < n1) {
-            const long long at = ((long long)t * N + n) * k + sl;
-            out_idx[at] = r.e;
-            out_gate[at] = gate;
-            if (r.e >= 0) atomicAdd(count + sl * E + r.e, 1);
+    }
+    __syncthreads();
+    double *cd = reinterpret_cast<double *>(gt_smem) + warp * 64 * M;
+    float *cf = reinterpret_cast<float *>(cd + 32 * M);
+    for (int i = warp; i < n1 - n0; i += GT_WARPS) {  // a warp a row
+        if (!(again[i >> 5] >> (i & 31) & 1u)) continue;
+        const long long tn = (long long)t * N + n0 + i;
+        const Choice r = choose_row<M>(p, g, t, tn, logits, sbias, cd, cf, cf + 32 * M);
+        const float gate = gate_of(g, r, 32);
+        if (lane < k) {
+            out_idx[tn * k + lane] = r.e;
+            out_gate[tn * k + lane] = gate;
+            if (r.e >= 0) atomicAdd(count + lane * E + r.e, 1);
         }
     }
     __syncthreads();
@@ -765,7 +789,7 @@ int launch_grad_k(const Dims &p, const Gating &g, const float *logits, const int
 // Rows of a tile: 64, more where a task would have over 128 tiles.
 int tile_rows(int N) {
     int rows = 64;
-    while ((N + rows - 1) / rows > 128) rows *= 2;
+    while (rows < 32768 && (N + rows - 1) / rows > 128) rows *= 2;  // their bits: 4 KB of shared memory
     return rows;
 }
 
@@ -782,7 +806,7 @@ struct RowArgs {
 };
 template <typename Kern>
 int launch_rows(Kern kern, int M, const RowArgs &a, cudaStream_t s) {
-    const size_t smem = row_scratch(M) + (size_t)a.p.k * a.p.E * 4;  // at most 40 KB
+    const size_t smem = row_scratch(M) + ((size_t)a.p.k * a.p.E + (a.rows + 31) / 32) * 4;
     return launch_kernel(kern, dim3((a.p.N + a.rows - 1) / a.rows, a.p.T), dim3(GT_THREADS), smem, s, a.p, a.g, a.rows, a.logits,
                          a.sbias, a.mask, a.idx, a.gate, a.hist);
 }
