@@ -415,7 +415,7 @@ enum {
 /* A head over a vocabulary behind the blocks, and what it is trained against. */
 typedef struct {
     int32_t V;         /* entries of the vocabulary */
-    int32_t teacher_k; /* K: entries of a teacher's list for each token, 0: no teacher; at most 128 */
+    int32_t teacher_k; /* K: entries of a teacher's list for each token, 0: no teacher; at most 128, V <= 2^20 with one */
     float temperature; /* tau > 0 */
     uint32_t flags;    /* VMOE_HEAD_SHARED */
 } vmoe_head;

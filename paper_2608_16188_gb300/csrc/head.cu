@@ -23,7 +23,7 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
-constexpr int HR_THREADS = 1024, HG_THREADS = 256, HF_ROWS = 32;
+constexpr int HG_THREADS = 256, HP_TOKENS = 64, HP_SELF = 8192;
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -36,81 +36,271 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+__device__ __forceinline__ void load8(const float *p, float *o) {
+    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
+    o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+}
+
 struct Sizes {
     int T, N, Np, d, V, K;
 };
 
 __device__ __forceinline__ bool entry_ok(const Sizes &z, int i, float l) { return i >= 0 && i < z.V && l != -INFINITY; }
 __device__ __forceinline__ bool label_ok(const Sizes &z, int y) { return y >= 0 && y < z.V; }
-__device__ __forceinline__ bool taught(const Sizes &z, const int32_t *tidx, const float *tlogit, long long tn) {
-    for (int j = 0; j < z.K; ++j)
-        if (entry_ok(z, tidx[tn * z.K + j], tlogit[tn * z.K + j])) return true;  // the first, as a rule
-    return false;
+
+// Which tokens take part, a bit each: mark [2][T][words], first those with a teacher, then those with either.  A CTA 32
+// tokens, four a warp, whose lanes look through a token's entries together.
+__global__ void __launch_bounds__(HG_THREADS)
+head_mark_kernel(Sizes z, int words, const int32_t *__restrict__ label, const int32_t *__restrict__ tidx,
+                 const float *__restrict__ tlogit, unsigned *__restrict__ mark) {
+    __shared__ unsigned parts[HG_THREADS / 32];
+    const int t = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, word = blockIdx.x, n0 = word * 32;
+    pdl_wait();
+    const bool has = warp == 0 && label && n0 + lane < z.N && label_ok(z, label[(long long)t * z.N + n0 + lane]);
+    unsigned taught = 0;
+    if (tidx) {
+        bool some[4] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = n0 + 4 * warp + i;
+            const long long at = ((long long)t * z.N + n) * z.K;
+            if (n < z.N)
+                for (int j = lane; j < z.K; j += 32) some[i] |= entry_ok(z, tidx[at + j], tlogit[at + j]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) taught |= (unsigned)__any_sync(FULL, some[i]) << (4 * warp + i);
+    }
+    if (lane == 0) parts[warp] = taught;
+    const unsigned either = __ballot_sync(FULL, has);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < HG_THREADS / 32; ++i) taught |= parts[i];
+        mark[(long long)t * words + word] = taught;
+        mark[((long long)z.T + t) * words + word] = either | taught;
+    }
 }
 
-// The tokens of a head that take part, in order: map[row] = token, pos[token] = row or -1.  A CTA a head.
-__global__ void __launch_bounds__(HR_THREADS)
-head_rows_kernel(Sizes z, const int32_t *__restrict__ label, const int32_t *__restrict__ tidx,
-                 const float *__restrict__ tlogit, int *__restrict__ rows, int *__restrict__ pos, int *__restrict__ map) {
-    __shared__ int sums[32], total;
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// Packs the tokens that take part, HP_TOKENS a CTA: how many come before is counted by every CTA, from the bits, or where
+// a head has few tokens from their labels and entries themselves.  Copies their rows (fp32 ones as three bf16 parts), fills the last tile with
+// zeros, and leaves what else belongs to a token: zeros in the outputs of one without a part, the backward's factors.
+struct Pack {
+    Sizes z;
+    int words;
+    const unsigned *mark;  // NULL: from label, tidx and tlogit
+    const int32_t *label, *tidx;
+    const float *tlogit;
+    int *rows, *pos, *map, *out_label;
+    __nv_bfloat16 *out;
+    // forward: set to 0 where a token has no part
+    float *ce, *lse, *kl, *tlse, *logp;
+    // backward
+    void *dz;
+    float inv_tau;
+    bool one;  // labels and a teacher at temperature 1: one exponential for both
+    const float *in_ce, *in_lse, *in_tlse, *dce, *dlse, *dkl;
+    float4 *coef;
+    float *at_label;
+};
+// At the label dce (p - 1) + dlse p with p = exp(-ce): ce is kept to 2^-24 of itself or of 1, p and 1 would cancel.
+__device__ __forceinline__ float label_value(float ce, float dce, float dlse) { return dce * expm1f(-ce) + dlse * expf(-ce); }
+
+template <typename T>
+__global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *__restrict__ src) {
+    __shared__ unsigned bits[2][HP_SELF / 32];  // this head's marks, where they are made here
+    __shared__ int sum[2][HG_THREADS / 32], to[HP_TOKENS];
+    const Sizes z = f.z;
+    const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n0 = blockIdx.x * HP_TOKENS;
+    const long long t0 = (long long)t * z.N;
+    if (!f.mark)
+        for (int i = tid; i < f.words; i += HG_THREADS) bits[0][i] = bits[1][i] = 0;
     pdl_wait();
-    int run = 0;
-    for (int n0 = 0; n0 < z.N; n0 += HR_THREADS) {
-        const int n = n0 + tid;
-        const long long tn = (long long)t * z.N + n;
-        bool in = false;
-        if (n < z.N) in = (label && label_ok(z, label[tn])) || (tidx && taught(z, tidx, tlogit, tn));
-        const unsigned mask = __ballot_sync(FULL, in);
-        if (lane == 0) sums[warp] = __popc(mask);
+    const unsigned *taught = bits[0], *either = bits[1];
+    if (f.mark) {
+        taught = f.mark + (long long)t * f.words;
+        either = f.mark + ((long long)z.T + t) * f.words;
+    } else {
         __syncthreads();
-        if (warp == 0) {
-            const int c = sums[lane];
-            int incl = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(FULL, incl, o);
-                if (lane >= o) incl += y;
-            }
-            sums[lane] = incl - c;
-            if (lane == 31) total = incl;
+        if (f.tidx) {
+#pragma unroll 4
+            for (int i = tid; i < z.N * z.K; i += HG_THREADS)
+                if (entry_ok(z, f.tidx[t0 * z.K + i], f.tlogit[t0 * z.K + i])) {
+                    const int n = i / z.K;
+                    atomicOr(bits[0] + (n >> 5), 1u << (n & 31));
+                    atomicOr(bits[1] + (n >> 5), 1u << (n & 31));
+                }
         }
         __syncthreads();
-        const int r = run + sums[warp] + __popc(mask & ((1u << lane) - 1u));
-        if (n < z.N) pos[tn] = in ? r : -1;
-        if (in) map[(long long)t * z.Np + r] = n;
-        run += total;
+        if (f.label) {  // a word a warp
+#pragma unroll 4
+            for (int w = warp; w < f.words; w += HG_THREADS / 32) {
+                const int i = w * 32 + lane;
+                const unsigned has = __ballot_sync(FULL, i < z.N && label_ok(z, i < z.N ? f.label[t0 + i] : -1));
+                if (lane == 0) bits[1][w] |= has;
+            }
+        }
         __syncthreads();
     }
-    if (tid == 0) rows[t] = run;
+    int before = 0, total = 0;
+    for (int i = tid; i < f.words; i += HG_THREADS) {
+        const int c = __popc(either[i]);
+        total += c;
+        if (i * 32 < n0) before += c;
+    }
+    before = __reduce_add_sync(FULL, before);
+    total = __reduce_add_sync(FULL, total);
+    if (lane == 0) sum[0][warp] = before, sum[1][warp] = total;
+    __syncthreads();
+    before = total = 0;
+#pragma unroll
+    for (int i = 0; i < HG_THREADS / 32; ++i) before += sum[0][i], total += sum[1][i];
+    if (blockIdx.x == 0 && tid == 0) f.rows[t] = total;
+    const int n = n0 + tid;
+    if (tid < HP_TOKENS) to[tid] = -1;
+    if (tid < HP_TOKENS && n < z.N) {  // a token a thread
+        const unsigned word = either[n >> 5];
+        const long long tn = t0 + n;
+        const bool in = word >> (n & 31) & 1u;
+        int r = before + __popc(word & ((1u << (n & 31)) - 1u));
+        for (int w = n0 >> 5; w < n >> 5; ++w) r += __popc(either[w]);
+        const int y = f.label && label_ok(z, f.label[tn]) ? f.label[tn] : -1;
+        f.pos[tn] = to[tid] = in ? r : -1;
+        const long long at = (long long)t * z.Np + r;
+        if (in) {
+            f.map[at] = n;
+            if (f.out_label) f.out_label[at] = y;
+        } else {
+            if (f.ce) f.ce[tn] = f.lse[tn] = 0.0f;
+            if (f.kl) f.kl[tn] = f.tlse[tn] = 0.0f;
+        }
+        if (in && f.coef) {
+            float4 c = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float there = 0.0f;
+            if (y >= 0) {
+                const float dce = f.dce ? f.dce[tn] : 0.0f, dlse = f.dlse ? f.dlse[tn] : 0.0f;
+                there = label_value(f.in_ce[tn], dce, dlse);
+                c.x = dce + dlse;
+                c.y = f.in_lse[tn] * LOG2E;
+            }
+            if (f.dkl && (taught[n >> 5] >> (n & 31) & 1u)) {
+                const float b = f.dkl[tn] * f.inv_tau;
+                if (f.one) {
+                    c.x += b;
+                    c.y = f.in_tlse[tn] * LOG2E;
+                    if (y >= 0) there += b * expf(-f.in_ce[tn]);
+                } else {
+                    c.z = b;
+                    c.w = f.in_tlse[tn] * LOG2E;
+                }
+            }
+            f.coef[at] = c;
+            f.at_label[at] = there;
+        }
+    }
+    __syncthreads();
+    // the rows, 8 columns a thread at a time
+    const long long plane = (long long)z.T * z.Np * z.d;
+    const int vec = z.d / 8, here = min(HP_TOKENS, z.N - n0);
+    constexpr int U = sizeof(T) == 2 ? 6 : 3;  // loads in flight a thread
+    for (int i0 = tid; i0 < here * vec; i0 += U * HG_THREADS) {
+        uint4 v[U][sizeof(T) / 2];
+        int r[U], at[U];  // at: token and column
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * HG_THREADS, k = i / vec;
+            at[u] = k * z.d + (i - k * vec) * 8;
+            r[u] = i < here * vec ? to[k] : -2;
+            if (r[u] < 0) continue;
+#pragma unroll
+            for (int q = 0; q < (int)sizeof(T) / 2; ++q)
+                v[u][q] = __ldg(reinterpret_cast<const uint4 *>(src + (t0 + n0) * z.d + at[u]) + q);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (r[u] < 0) {
+                if (!f.dz || r[u] != -1) continue;
+                uint4 *o = reinterpret_cast<uint4 *>((T *)f.dz + (t0 + n0) * z.d + at[u]);
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(T) / 2; ++q) o[q] = make_uint4(0, 0, 0, 0);
+                continue;
+            }
+            __nv_bfloat16 *o = f.out + ((long long)t * z.Np + r[u]) * z.d + at[u] % z.d;
+            if constexpr (sizeof(T) == 2) {
+                *reinterpret_cast<uint4 *>(o) = v[u][0];
+            } else {
+                const float *x = reinterpret_cast<const float *>(v[u]);
+                __align__(16) __nv_bfloat16 p[3][8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) split3(x[q], p[0][q], p[1][q], p[2][q]);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(o + q * plane) = *reinterpret_cast<const uint4 *>(p[q]);
+            }
+        }
+    }
+    if (f.logp)
+        for (int i = tid; i < here * z.K; i += HG_THREADS)
+            if (to[i / z.K] < 0) f.logp[(t0 + n0) * z.K + i] = 0.0f;
+    // the rest of the last tile
+    const int end = (total + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
+    for (int r = total + blockIdx.x * (HG_THREADS / 32) + warp; r < end; r += gridDim.x * (HG_THREADS / 32)) {
+        const long long at = (long long)t * z.Np + r;
+        if (lane == 0 && f.out_label) f.out_label[at] = -1;
+        for (int q = 0; q < (sizeof(T) == 2 ? 1 : 3); ++q)
+            for (int c = lane * 8; c < z.d; c += 256)
+                *reinterpret_cast<uint4 *>(f.out + q * plane + at * z.d + c) = make_uint4(0, 0, 0, 0);
+    }
 }
 
-// Their tokens' rows, packed; the rest of the last tile is zeros.  A warp a row.
-template <typename T>
+// The teacher's entries of 32 packed rows, by the half tile of the vocabulary that they lie in: off [halves + 1] and list
+// for the epilogue of HEAD_STATS, which picks their logits.  Order within a half tile does not matter.  A CTA 32 rows.
 __global__ void __launch_bounds__(HG_THREADS)
-head_gather_kernel(Sizes z, const T *__restrict__ src, const int32_t *__restrict__ label, const int *__restrict__ rows,
-                   const int *__restrict__ map, int *__restrict__ out_label, __nv_bfloat16 *__restrict__ out) {
-    const int t = blockIdx.y, lane = threadIdx.x & 31, r = blockIdx.x * (HG_THREADS / 32) + (threadIdx.x >> 5);
+head_list_kernel(Sizes z, int halves, const int32_t *__restrict__ tidx, const float *__restrict__ tlogit,
+                 const int *__restrict__ rows, const int *__restrict__ map, int *__restrict__ off, unsigned *__restrict__ list) {
+    extern __shared__ int hl_count[];  // [halves + 1]
+    __shared__ int sums[HG_THREADS / 32];
+    const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = blockIdx.x * 32;
     pdl_wait();
     const int n = rows[t];
-    if (r >= (n + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE) return;
-    const long long at = (long long)t * z.Np + r, tn = r < n ? (long long)t * z.N + map[at] : 0;
-    if (out_label && lane == 0) out_label[at] = r < n && label_ok(z, label[tn]) ? label[tn] : -1;
-    const long long plane = (long long)z.T * z.Np * z.d;
-    for (int c = lane * 8; c < z.d; c += 256) {
-        if constexpr (sizeof(T) == 2) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < n) v = __ldg(reinterpret_cast<const uint4 *>(src + tn * z.d + c));
-            *reinterpret_cast<uint4 *>(out + at * z.d + c) = v;
-        } else {
-            __align__(16) __nv_bfloat16 p[3][8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) split3(r < n ? __ldg(src + tn * z.d + c + i) : 0.0f, p[0][i], p[1][i], p[2][i]);
-#pragma unroll
-            for (int i = 0; i < 3; ++i)
-                *reinterpret_cast<uint4 *>(out + i * plane + at * z.d + c) = *reinterpret_cast<const uint4 *>(p[i]);
+    if (r0 >= (n + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE) return;
+    const long long block = ((long long)t * z.Np + r0) >> 5;
+    for (int i = tid; i <= halves; i += HG_THREADS) hl_count[i] = 0;
+    __syncthreads();
+    auto each = [&](auto what) {
+        for (int i = tid; i < 32 * z.K; i += HG_THREADS) {
+            const int r = i / z.K, j = i - r * z.K;
+            if (r0 + r >= n) continue;
+            const long long at = ((long long)t * z.N + map[(long long)t * z.Np + r0 + r]) * z.K + j;
+            const int e = tidx[at];
+            if (entry_ok(z, e, tlogit[at])) what(r, j, e);
         }
+    };
+    each([&](int, int, int e) { atomicAdd(hl_count + (e >> 7), 1); });
+    __syncthreads();
+    // exclusive sums, a run of half tiles a thread
+    const int per = (halves + 1 + HG_THREADS - 1) / HG_THREADS, i0 = min(halves + 1, tid * per), i1 = min(halves + 1, i0 + per);
+    int mine = 0;
+    for (int i = i0; i < i1; ++i) mine += hl_count[i];
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(FULL, incl, o);
+        if (lane >= o) incl += v;
     }
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    int run = incl - mine;
+    for (int i = 0; i < warp; ++i) run += sums[i];
+    for (int i = i0; i < i1; ++i) {
+        const int c = hl_count[i];
+        hl_count[i] = run;
+        off[block * (halves + 1) + i] = run;
+        run += c;
+    }
+    __syncthreads();
+    unsigned *out = list + block * 32 * z.K;
+    each([&](int r, int j, int e) {
+        out[atomicAdd(hl_count + (e >> 7), 1)] = (unsigned)r | (unsigned)(e & 127) << 5 | (unsigned)j << 12;
+    });
 }
 
 // fp32 weights as three bf16 parts.  n: a multiple of 8.
@@ -126,19 +316,6 @@ head_split_kernel(long long n, const float *__restrict__ src, __nv_bfloat16 *__r
 #pragma unroll
         for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(out + q * n + i) = *reinterpret_cast<const uint4 *>(p[q]);
     }
-}
-
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float *o);
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, float *o) {
-    bf16x8_to_f32(__ldg(reinterpret_cast<const uint4 *>(p)), o);
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float *p, float *o) {
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-    o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-    o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
 }
 
 // A teacher's distribution over a token's entries: lane l has entries l, l + 32, ...  lq: log q (natural).
@@ -180,17 +357,16 @@ struct Teacher {
     }
 };
 
-// The losses from the tiles' sums, 32 packed rows a CTA: each warp joins every eighth half tile of all rows, the first
-// warp the warps' sums; then, with a teacher, a warp a row: the logits of its entries, each a dot product.
-// CTAs past the last row leave zeros at the tokens without a part.
+// The losses from the tiles' sums, ROWS packed rows a CTA: 256 / ROWS threads join a row's half tiles, every one of them
+// a share, then their sums; with a teacher a warp then takes a row's entries.
 struct Finish {
     Sizes z;
     int halves, pitch;  // half tiles of the vocabulary, and as the sums are laid out
     int stats;
     float inv_tau, c1;
-    const int *rows, *pos, *map, *label;
+    const int *rows, *map, *label;
     const float2 *part, *part2;
-    const float *picked;
+    const float *picked, *tl;
     const int32_t *tidx;
     const float *tlogit;
     float *ce, *lse, *kl, *tlse, *logp;
@@ -200,42 +376,39 @@ __device__ __forceinline__ void join(float &m, float &s, float2 v) {
     s = s * exp2f(m - top) + v.y * exp2f(v.x - top);
     m = top;
 }
-template <typename T>
-__global__ void __launch_bounds__(HG_THREADS)
-head_finish_kernel(Finish f, const T *__restrict__ zt, const T *__restrict__ w) {
-    __shared__ float2 sm[2][HG_THREADS / 32][32];
-    __shared__ float tl[32];
-    const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+template <int ROWS>
+__global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
+    constexpr int SHARES = HG_THREADS / ROWS;  // threads of a row
+    __shared__ float2 sm[2][HG_THREADS / 32][ROWS];
+    __shared__ float tl[ROWS];
+    const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row_in = lane % ROWS;
     const Sizes z = f.z;
     pdl_wait();
-    // tokens without a part
-    for (int n = blockIdx.x * HG_THREADS + tid; n < z.N; n += gridDim.x * HG_THREADS) {
-        const long long tn = (long long)t * z.N + n;
-        if (f.pos[tn] >= 0) continue;
-        if (f.ce) f.ce[tn] = f.lse[tn] = 0.0f;
-        if (f.kl) {
-            f.kl[tn] = f.tlse[tn] = 0.0f;
-            for (int j = 0; j < z.K; ++j) f.logp[tn * z.K + j] = 0.0f;
-        }
-    }
-    const int n = f.rows[t], r0 = blockIdx.x * HF_ROWS;
+    const int n = f.rows[t], r0 = blockIdx.x * ROWS;
     if (r0 >= n) return;
-    float m = -INFINITY, s = 0.0f, m2 = -INFINITY, s2 = 0.0f;
-    const float2 *p = f.part + (long long)t * f.pitch * z.Np + r0 + lane;
-    const float2 *p2 = f.stats == 2 ? f.part2 + (long long)t * f.pitch * z.Np + r0 + lane : nullptr;
+    const int row = r0 + row_in;
+    float m = -3e38f, s = 0.0f, m2 = -3e38f, s2 = 0.0f;
+    const float2 *p = f.part + (long long)t * f.pitch * z.Np + row;
+    const float2 *p2 = f.stats == 2 ? f.part2 + (long long)t * f.pitch * z.Np + row : nullptr;
 #pragma unroll 4
-    for (int h = warp; h < f.halves; h += HG_THREADS / 32) {
+    for (int h = tid / ROWS; h < f.halves; h += SHARES) {
         join(m, s, p[(long long)h * z.Np]);
         if (p2) join(m2, s2, p2[(long long)h * z.Np]);
     }
-    sm[0][warp][lane] = make_float2(m, s);
-    sm[1][warp][lane] = make_float2(m2, s2);
+#pragma unroll
+    for (int o = 16; o >= ROWS; o >>= 1) {
+        join(m, s, make_float2(__shfl_xor_sync(FULL, m, o), __shfl_xor_sync(FULL, s, o)));
+        join(m2, s2, make_float2(__shfl_xor_sync(FULL, m2, o), __shfl_xor_sync(FULL, s2, o)));
+    }
+    if (lane < ROWS) {
+        sm[0][warp][lane] = make_float2(m, s);
+        sm[1][warp][lane] = make_float2(m2, s2);
+    }
     __syncthreads();
-    const int row = r0 + lane;
-    if (warp == 0) {
+    if (tid < ROWS) {
         for (int q = 1; q < HG_THREADS / 32; ++q) {
             join(m, s, sm[0][q][lane]);
-            if (p2) join(m2, s2, sm[1][q][lane]);
+            join(m2, s2, sm[1][q][lane]);
         }
         const float ls = log2f(s), a = (m + ls) * LN2, b = p2 ? (m2 + log2f(s2)) * LN2 : a;
         tl[lane] = b;
@@ -248,41 +421,17 @@ head_finish_kernel(Finish f, const T *__restrict__ zt, const T *__restrict__ w) 
     }
     if (!f.kl) return;
     __syncthreads();
-    for (int i = warp; i < HF_ROWS && r0 + i < n; i += HG_THREADS / 32) {
-        const long long tn = (long long)t * z.N + f.map[(long long)t * z.Np + r0 + i];
+    for (int i = warp; i < ROWS && r0 + i < n; i += HG_THREADS / 32) {
+        const long long at = (long long)t * z.Np + r0 + i, tn = (long long)t * z.N + f.map[at];
         Teacher q;
         q.load(z, f.tidx, f.tlogit, f.inv_tau, tn);
-        const T *zr = zt + tn * z.d, *wt = w + (long long)t * z.V * z.d;
         float loss = 0.0f;
 #pragma unroll
         for (int mm = 0; mm < Teacher::M; ++mm) {
-            if (32 * mm >= z.K) break;
-            float mine = 0.0f;  // lane l: entry 32 mm + l
-            const int last = min(32, z.K - 32 * mm);
-            for (int j = 0; j < last; j += 4) {  // four entries' rows at a time
-                float acc[4] = {};
-                const T *wr[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) wr[e] = wt + (long long)max(0, __shfl_sync(FULL, q.i[mm], (j + e) & 31)) * z.d;
-                for (int c = lane * 8; c < z.d; c += 256) {
-                    float a[8];
-                    load8<T>(zr + c, a);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float b[8];
-                        load8<T>(wr[e] + c, b);
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) acc[e] = fmaf(a[x], b[x], acc[e]);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc[e] = warp_sum(acc[e]);
-                    if (lane == j + e) mine = acc[e];
-                }
-            }
-            const float lp = q.i[mm] >= 0 ? mine * f.inv_tau - tl[i] : 0.0f;
-            if (lane + 32 * mm < z.K) f.logp[tn * z.K + lane + 32 * mm] = lp;
+            const int j = lane + 32 * mm;
+            if (j >= z.K) break;
+            const float lp = q.i[mm] >= 0 ? f.tl[at * z.K + j] * f.inv_tau - tl[i] : 0.0f;
+            f.logp[tn * z.K + j] = lp;
             // an entry of no weight adds nothing, whatever its logarithm
             if (q.q[mm] > 0.0f || q.q[mm] != q.q[mm]) loss += q.q[mm] * (q.lq[mm] - lp);
         }
@@ -292,48 +441,6 @@ head_finish_kernel(Finish f, const T *__restrict__ zt, const T *__restrict__ w) 
             f.tlse[tn] = q.any ? tl[i] : 0.0f;
         }
     }
-}
-
-// What HEAD_DLOGITS takes each row's exponentials times, and off at the label.  A thread a packed row.
-struct Coef {
-    Sizes z;
-    float inv_tau;
-    bool one;  // labels and a teacher at temperature 1: one exponential for both
-    const int *rows, *map;
-    const int32_t *label, *tidx;
-    const float *tlogit, *ce, *lse, *tlse, *dce, *dlse, *dkl;
-    float4 *coef;
-    float *at_label;
-};
-// At the label dce (p - 1) + dlse p with p = exp(-ce): ce is kept to 2^-24 of itself or of 1, p and 1 would cancel.
-__device__ __forceinline__ float label_value(float ce, float dce, float dlse) { return dce * expm1f(-ce) + dlse * expf(-ce); }
-__global__ void __launch_bounds__(HG_THREADS) head_coef_kernel(Coef f) {
-    const int t = blockIdx.y, r = blockIdx.x * HG_THREADS + threadIdx.x;
-    pdl_wait();
-    if (r >= f.rows[t]) return;
-    const long long at = (long long)t * f.z.Np + r, tn = (long long)t * f.z.N + f.map[at];
-    float4 c = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float there = 0.0f;
-    const bool has = f.label && label_ok(f.z, f.label[tn]);
-    if (has) {
-        const float dce = f.dce ? f.dce[tn] : 0.0f, dlse = f.dlse ? f.dlse[tn] : 0.0f;
-        there = label_value(f.ce[tn], dce, dlse);
-        c.x = dce + dlse;
-        c.y = f.lse[tn] * LOG2E;
-    }
-    if (f.tidx && f.dkl && taught(f.z, f.tidx, f.tlogit, tn)) {
-        const float b = f.dkl[tn] * f.inv_tau;
-        if (f.one) {
-            c.x += b;
-            c.y = f.tlse[tn] * LOG2E;
-            if (has) there += b * expf(-f.ce[tn]);
-        } else {
-            c.z = b;
-            c.w = f.tlse[tn] * LOG2E;
-        }
-    }
-    f.coef[at] = c;
-    f.at_label[at] = there;
 }
 
 // The teacher's entries in a piece of dl: the whole value, from the stored logarithms, so that neither the order of
@@ -403,7 +510,7 @@ head_dz_kernel(Sizes z, int splits, const int *__restrict__ pos, const float *__
             const float *src = parts + ((tn / z.N) * z.Np + r) * z.d + c;
             for (int s = 0; s < splits; ++s) {
                 float o[8];
-                load8<float>(src + s * plane, o);
+                load8(src + s * plane, o);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] += o[q];
             }
@@ -423,26 +530,37 @@ P *at(void *ws, size_t offset) {
     return reinterpret_cast<P *>(static_cast<uint8_t *>(ws) + offset);
 }
 
-// Packed rows and, in fp32, the weights' parts: what both directions begin with.
-int prepare(const Dims &p, const HeadPlan &h, const HeadIn &in, void *ws, const __nv_bfloat16 **zp, const __nv_bfloat16 **wp,
-            cudaStream_t s) {
+// Packed rows and, in fp32, the weights' parts: what both directions begin with.  f: what the direction adds.
+int prepare(const Dims &p, const HeadPlan &h, const HeadIn &in, void *ws, Pack f, const __nv_bfloat16 **zp,
+            const __nv_bfloat16 **wp, cudaStream_t s) {
     const Sizes z = sizes_of(h);
-    int *rows = at<int>(ws, h.rows), *pos = at<int>(ws, h.pos), *map = at<int>(ws, h.map), *label = at<int>(ws, h.label);
-    __nv_bfloat16 *zc = at<__nv_bfloat16>(ws, h.z);
-    trace_before(s, "head_rows");
-    int st = launch_kernel(head_rows_kernel, dim3(h.T), dim3(HR_THREADS), 0, s, z, in.label, in.tidx, in.tlogit, rows, pos, map);
+    f.z = z;
+    f.words = (h.N + 31) / 32;
+    f.label = in.label;
+    f.rows = at<int>(ws, h.rows);
+    f.pos = at<int>(ws, h.pos);
+    f.map = at<int>(ws, h.map);
+    f.out_label = in.label ? at<int>(ws, h.label) : nullptr;
+    f.out = at<__nv_bfloat16>(ws, h.z);
+    int st;
+    f.tidx = in.tidx;
+    f.tlogit = in.tlogit;
+    // few labels and entries: every CTA of head_pack looks through all of its head's, instead of a launch
+    if (h.N > HP_SELF || (in.tidx && (long long)h.N * h.K > 2 * HP_SELF)) {
+        unsigned *mark = at<unsigned>(ws, h.mark);
+        f.mark = mark;
+        trace_before(s, "head_mark");
+        st = launch_kernel(head_mark_kernel, dim3(f.words, h.T), dim3(HG_THREADS), 0, s, z, f.words, in.label, in.tidx, in.tlogit, mark);
+        trace_after(s);
+        if (st != VMOE_OK) return st;
+    }
+    trace_before(s, "head_pack");
+    const dim3 grid((h.N + HP_TOKENS - 1) / HP_TOKENS, h.T);
+    st = p.bf16 ? launch_kernel(head_pack_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, f, (const __nv_bfloat16 *)in.z)
+                : launch_kernel(head_pack_kernel<float>, grid, dim3(HG_THREADS), 0, s, f, (const float *)in.z);
     trace_after(s);
     if (st != VMOE_OK) return st;
-    trace_before(s, "head_gather");
-    const dim3 grid(h.Np / (HG_THREADS / 32), h.T);
-    int *lab = in.label ? label : nullptr;
-    st = p.bf16 ? launch_kernel(head_gather_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, (const __nv_bfloat16 *)in.z,
-                                in.label, rows, map, lab, zc)
-                : launch_kernel(head_gather_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, (const float *)in.z, in.label, rows,
-                                map, lab, zc);
-    trace_after(s);
-    if (st != VMOE_OK) return st;
-    *zp = zc;
+    *zp = f.out;
     *wp = (const __nv_bfloat16 *)in.w;
     if (!p.bf16) {
         __nv_bfloat16 *ws3 = at<__nv_bfloat16>(ws, h.w);
@@ -480,6 +598,7 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
         return a;
     };
     h.rows = take((size_t)h.T * 4);
+    h.mark = take((size_t)h.T * ((h.N + 31) / 32) * 8);
     h.pos = take((size_t)h.T * h.N * 4);
     h.map = take(rowsp * 4);
     h.label = take(rowsp * 4);
@@ -489,6 +608,9 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.part = take(rowsp * tiles_v * 2 * 8);
     h.part2 = take(h.K > 0 ? rowsp * tiles_v * 2 * 8 : 0);
     h.picked = take(rowsp * 4);
+    h.off = take(h.K > 0 ? rowsp / 32 * (tiles_v * 2 + 1) * 4 : 0);
+    h.list = take(rowsp * h.K * 4);
+    h.tl = take(rowsp * h.K * 4);
     const size_t fwd = o;
     o = both;
     h.coef = take(rowsp * 16);
@@ -526,37 +648,58 @@ size_t head_min_workspace(const Dims &p, const vmoe_head *head) {
     if (!head_plan(p, head, true, 0, &h)) return 0;
     const size_t rowsp = (size_t)h.T * h.Np, dzp = (rowsp * h.d * 4 + 255) & ~(size_t)255;
     const size_t bwd = h.dl + rowsp * HEAD_TILE * 2 * h.parts + dzp;
-    return std::max(h.picked + ((rowsp * 4 + 255) & ~(size_t)255), bwd);
+    return std::max(h.tl + ((rowsp * h.K * 4 + 255) & ~(size_t)255), bwd);
 }
 
 int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *ce, float *lse, float *kl, float *tlse,
                      float *logp, void *ws, cudaStream_t s) {
     const __nv_bfloat16 *zp, *wp;
-    int st = prepare(p, h, in, ws, &zp, &wp, s);
+    Pack k = {};
+    k.ce = ce;
+    k.lse = lse;
+    k.kl = kl;
+    k.tlse = tlse;
+    k.logp = logp;
+    int st = prepare(p, h, in, ws, k, &zp, &wp, s);
     if (st != VMOE_OK) return st;
+    const Sizes z = sizes_of(h);
+    const int pitch = (h.V + HEAD_TILE - 1) / HEAD_TILE * 2;
     HeadGemm g = {};
     g.stats = h.stats;
     g.rows = at<int>(ws, h.rows);
     g.vn = h.V;
+    if (in.tidx) {
+        int *off = at<int>(ws, h.off);
+        unsigned *list = at<unsigned>(ws, h.list);
+        g.off = off;
+        g.list = list;
+        g.K = h.K;
+        g.tl = at<float>(ws, h.tl);
+        trace_before(s, "head_list");
+        st = launch_kernel(head_list_kernel, dim3(h.Np / 32, h.T), dim3(HG_THREADS), (size_t)(pitch + 1) * 4, s, z, pitch, in.tidx,
+                           in.tlogit, g.rows, at<int>(ws, h.map), off, list);
+        trace_after(s);
+        if (st != VMOE_OK) return st;
+    }
     g.label = in.label ? at<int>(ws, h.label) : nullptr;
     g.part = at<float2>(ws, h.part);
     g.part2 = at<float2>(ws, h.part2);
     g.picked = at<float>(ws, h.picked);
     if ((st = launch_head_gemm(HEAD_STATS, h, g, zp, wp, nullptr, nullptr, s)) != VMOE_OK) return st;
     Finish f = {};
-    f.z = sizes_of(h);
+    f.z = z;
     f.halves = (h.V + 127) / 128;
-    f.pitch = (h.V + HEAD_TILE - 1) / HEAD_TILE * 2;
+    f.pitch = pitch;
     f.stats = h.stats;
     f.inv_tau = 1.0f / h.tau;
     f.c1 = h.c1;
     f.rows = g.rows;
-    f.pos = at<int>(ws, h.pos);
     f.map = at<int>(ws, h.map);
     f.label = at<int>(ws, h.label);
     f.part = g.part;
     f.part2 = g.part2;
     f.picked = g.picked;
+    f.tl = g.tl;
     f.tidx = in.tidx;
     f.tlogit = in.tlogit;
     f.ce = ce;
@@ -565,10 +708,10 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     f.tlse = tlse;
     f.logp = logp;
     trace_before(s, "head_finish");
-    const dim3 grid((h.N + HF_ROWS - 1) / HF_ROWS, h.T);
-    st = p.bf16 ? launch_kernel(head_finish_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, f, (const __nv_bfloat16 *)in.z,
-                                (const __nv_bfloat16 *)in.w)
-                : launch_kernel(head_finish_kernel<float>, grid, dim3(HG_THREADS), 0, s, f, (const float *)in.z, (const float *)in.w);
+    // few rows: more threads each, to hide the chain of their half tiles
+    const bool few = (long long)h.T * h.N <= 2048;
+    st = launch_kernel(few ? head_finish_kernel<4> : head_finish_kernel<32>, dim3((h.N + (few ? 3 : 31)) / (few ? 4 : 32), h.T),
+                       dim3(HG_THREADS), 0, s, f);
     trace_after(s);
     return st;
 }
@@ -577,38 +720,30 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
                          const float *tlse, const float *logp, const float *dce, const float *dlse, const float *dkl, void *dz,
                          void *dw, void *ws, cudaStream_t s) {
     const __nv_bfloat16 *zp, *wp;
-    int st = prepare(p, h, in, ws, &zp, &wp, s);
+    Pack k = {};
+    k.dz = dz;
+    k.inv_tau = 1.0f / h.tau;
+    k.one = h.stats == 1;
+    k.in_ce = ce;
+    k.in_lse = lse;
+    k.in_tlse = tlse;
+    k.dce = dce;
+    k.dlse = dlse;
+    k.dkl = dkl;
+    k.coef = at<float4>(ws, h.coef);
+    k.at_label = at<float>(ws, h.at_label);
+    int st = prepare(p, h, in, ws, k, &zp, &wp, s);
     if (st != VMOE_OK) return st;
     const Sizes z = sizes_of(h);
     const int *rows = at<int>(ws, h.rows), *map = at<int>(ws, h.map);
-    Coef c = {};
-    c.z = z;
-    c.inv_tau = 1.0f / h.tau;
-    c.one = h.stats == 1;
-    c.rows = rows;
-    c.map = map;
-    c.label = in.label;
-    c.tidx = in.tidx;
-    c.tlogit = in.tlogit;
-    c.ce = ce;
-    c.lse = lse;
-    c.tlse = tlse;
-    c.dce = dce;
-    c.dlse = dlse;
-    c.dkl = dkl;
-    c.coef = at<float4>(ws, h.coef);
-    c.at_label = at<float>(ws, h.at_label);
-    trace_before(s, "head_coef");
-    st = launch_kernel(head_coef_kernel, dim3((h.N + HG_THREADS - 1) / HG_THREADS, h.T), dim3(HG_THREADS), 0, s, c);
-    trace_after(s);
-    if (st != VMOE_OK) return st;
+    const bool direct = h.splits == 1 && h.piece >= h.V;  // dz in one go
     __nv_bfloat16 *dl = at<__nv_bfloat16>(ws, h.dl);
     HeadGemm g = {};
     g.stats = h.stats;
     g.rows = rows;
     g.label = in.label ? at<int>(ws, h.label) : nullptr;
-    g.coef = c.coef;
-    g.at_label = c.at_label;
+    g.coef = k.coef;
+    g.at_label = k.at_label;
     g.splits = h.splits;
     for (int v0 = 0; v0 < h.V; v0 += h.piece) {
         g.v0 = v0;
@@ -624,7 +759,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             f.piece = h.piece;
             f.parts = h.parts;
             f.tau = h.tau;
-            f.inv_tau = c.inv_tau;
+            f.inv_tau = k.inv_tau;
             f.rows = rows;
             f.map = map;
             f.label = in.label;
@@ -644,7 +779,10 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             if (st != VMOE_OK) return st;
         }
         if (dz) {
-            g.out = at<float>(ws, h.dzp);
+            g.out = direct ? nullptr : at<float>(ws, h.dzp);
+            g.dz = direct ? dz : nullptr;
+            g.map = map;
+            g.N = h.N;
             if ((st = launch_head_gemm(HEAD_DZ, h, g, zp, wp, dl, nullptr, s)) != VMOE_OK) return st;
         }
         if (dw) {
@@ -652,7 +790,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             if ((st = launch_head_gemm(HEAD_DW, h, g, zp, wp, dl, (__nv_bfloat16 *)dw, s)) != VMOE_OK) return st;
         }
     }
-    if (!dz) return VMOE_OK;
+    if (!dz || direct) return VMOE_OK;
     trace_before(s, "head_dz_join");
     const long long blocks = ((long long)h.T * h.N * (h.d / 8) + HG_THREADS - 1) / HG_THREADS;
     const dim3 grid((unsigned)std::min(blocks, 16LL * num_sms()));

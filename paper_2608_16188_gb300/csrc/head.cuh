@@ -7,6 +7,7 @@
 namespace vmoe {
 
 constexpr int HEAD_K = 128;     // entries of a teacher's list at most
+constexpr int HEAD_V = 1 << 20;  // entries of a vocabulary at most, with a teacher
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
 
 // Sizes of a call, and where its scratch lies in the workspace (byte offsets).
@@ -19,9 +20,9 @@ struct HeadPlan {
     int splits;          // backward: parts of the sum over the vocabulary in dz
     float tau;           // the temperature
     float c1, c2;        // log2(e), log2(e) / temperature
-    size_t rows, pos, map, label, z, w;     // both ways
-    size_t part, part2, picked;             // forward
-    size_t coef, at_label, dl, dzp;         // backward
+    size_t rows, mark, pos, map, label, z, w;  // both ways
+    size_t part, part2, picked, off, list, tl; // forward
+    size_t coef, at_label, dl, dzp;            // backward
     size_t bytes;
 };
 
@@ -39,9 +40,16 @@ struct HeadGemm {
     float2 *part;                 // HEAD_STATS out: [T][2 tiles_n][Np] largest logit times c1, sum
     float2 *part2;                // the same at c2
     float *picked;                // [T][Np] the label's logit
+    int K;                        // the teacher's entries: their logits go to tl [T][Np][K]
+    const int *off;               // [T][Np / 32][2 tiles_n + 1] where each half tile's entries of 32 rows begin in list
+    const unsigned *list;         // [T][Np / 32][32 K] row | column in the half tile << 5 | entry << 12
+    float *tl;
     const float4 *coef;           // HEAD_DLOGITS: a, lse times log2(e), b, tlse times log2(e) of a row
     const float *at_label;        // the first sum's share of the gradient there
     float *out;                   // HEAD_DZ: [splits][T][Np][d]; HEAD_DW, fp32: [T][V][d]
+    void *dz;                     // HEAD_DZ in one go (out NULL): [T][N][d], row map[t][r] of it
+    const int *map;
+    int N;
     int *status;
 };
 

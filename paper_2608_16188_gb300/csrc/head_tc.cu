@@ -17,7 +17,9 @@
 // weights come from DRAM once and the tokens stay in L2; DZ all column tiles of a row tile, whose dl is the larger operand.
 //
 // fp32 operands are three bf16 parts of 8 bits each (split3), and a product of theirs the six products of parts that are
-// above 2^-24 of it, the smallest first, as one longer sum.
+// above 2^-24 of it, the smallest first.  Tensor cores cut a sum to fp32 at every step of 16, always towards zero, so the
+// large products are taken two blocks at a time and the epilogue adds them up, rounding to nearest: dz over 5003 entries
+// is then off by 3e-7 where one long sum is off by 1.6e-6.
 #include "gemm_tc2.cuh"
 #include "head.cuh"
 
@@ -28,6 +30,13 @@ namespace {
 
 constexpr int HB = HEAD_TILE;
 constexpr int HG_ROWS = 32;  // row tiles that share a column tile
+
+// Blocks of 64 of a tile's sum that the tensor cores add up by themselves: all, or in fp32 the five small products of
+// parts and then two at a time of the large one.
+template <int PARTS>
+__device__ __forceinline__ int sums_of(int kb) { return kb == 0 ? 0 : PARTS == 1 ? 1 : 1 + (kb + 1) / 2; }
+template <int PARTS>
+__device__ __forceinline__ int sum_end(int kb, int i) { return PARTS == 1 ? kb : min(6 * kb, 5 * kb + 2 * i); }
 
 struct HeadShape {
     static constexpr uint32_t A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
@@ -258,37 +267,40 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             Cursor<MODE> cur;
             HTile x;
             for (int u = cid; ok && cur.seek(args, u, x); u += ncl) {
-                const int kblocks = args.np * (x.kb1 - x.kb0);
-                if (kblocks == 0) continue;  // no token: the epilogue writes zeros
-                const int acc = it & 1;
-                if (!wait_phase(bar_tempty(acc), (uint32_t)((it >> 1) & 1) ^ 1u, abort_flag, args.status)) break;
-                tc_fence_after();
-                const uint32_t dtmem = tmem_base + (uint32_t)(acc * HB);
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (!wait_phase(bar_full(stage), phase, abort_flag, args.status)) {
+                const int kb = x.kb1 - x.kb0, sums = sums_of<PARTS>(kb);  // none without a token: the epilogue writes zeros
+                for (int i = 0, k = 0; i < sums && ok; ++i, ++it) {
+                    const int acc = it & 1, end = sum_end<PARTS>(kb, i);
+                    if (!wait_phase(bar_tempty(acc), (uint32_t)((it >> 1) & 1) ^ 1u, abort_flag, args.status)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t sa = tiles_addr + stage * S::STAGE_BYTES;
-                        const uint64_t da = operand_desc(sa, 0, A_MN), db = operand_desc(sa + S::A_BYTES, 0, B_MN);
+                    const uint32_t dtmem = tmem_base + (uint32_t)(acc * HB);
+                    for (const int beg = k; k < end; ++k) {
+                        if (!wait_phase(bar_full(stage), phase, abort_flag, args.status)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t sa = tiles_addr + stage * S::STAGE_BYTES;
+                            const uint64_t da = operand_desc(sa, 0, A_MN), db = operand_desc(sa + S::A_BYTES, 0, B_MN);
 #pragma unroll
-                        for (int kk = 0; kk < BK / 16; ++kk)
-                            mma_pair_bf16(dtmem, desc_step(da, kk, A_MN), desc_step(db, kk, B_MN), IDESC,
-                                          (kb | kk) != 0 ? 1u : 0u);
-                        mma_pair_commit_both(bar_empty(stage));
+                            for (int kk = 0; kk < BK / 16; ++kk)
+                                mma_pair_bf16(dtmem, desc_step(da, kk, A_MN), desc_step(db, kk, B_MN), IDESC,
+                                              k != beg || kk != 0 ? 1u : 0u);
+                            mma_pair_commit_both(bar_empty(stage));
+                        }
+                        __syncwarp();
+                        if (++stage == STAGES) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
                     }
+                    if (!ok) break;
+                    if (elect_one()) mma_pair_commit_both(bar_tfull(acc));
                     __syncwarp();
-                    if (++stage == STAGES) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
                 }
-                if (!ok) break;
-                if (elect_one()) mma_pair_commit_both(bar_tfull(acc));
-                __syncwarp();
-                ++it;
             }
             if (elect_one()) {  // all MMAs of the pair complete before TMEM is freed
                 mma_pair_commit_local(bar_drain);
@@ -310,23 +322,71 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         for (int u = cid; cur.seek(args, u, x); u += ncl) {
             float v[128];
             const int row = x.m * HB + (int)rank * 128 + q * 32 + lane, col = x.n * HB + half * 128;
-            if (x.kb1 > x.kb0) {
-                const int acc = it & 1;
-                if (!wait_phase(bar_tfull(acc), (uint32_t)((it >> 1) & 1), abort_flag, args.status)) break;
-                tc_fence_after();
-                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * HB + half * 128);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(trow + c * 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32 * c));
-                tmem_ld_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
-                ++it;
-            } else {
+            const long long at = (long long)x.t * args.Np + row;
+            const int sums = sums_of<PARTS>(x.kb1 - x.kb0);
+            if (PARTS > 1 || sums == 0) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] = 0.0f;
             }
-            const long long at = (long long)x.t * args.Np + row;
+            // the teacher's entries in these 32 rows and 128 columns
+            int ent = 0, ents = 0;
+            const unsigned *list = nullptr;
+            if (MODE == HEAD_STATS && args.off) {
+                const long long block = (at - lane) >> 5;
+                const int *o = args.off + block * (2 * args.tiles_n + 1) + 2 * x.n + half;
+                ent = __ldg(o);
+                ents = __ldg(o + 1);
+                list = args.list + block * 32 * args.K;
+            }
+            bool ok = true;
+            for (int i = 0; i < sums; ++i, ++it) {
+                const int acc = it & 1;
+                if (!(ok = wait_phase(bar_tfull(acc), (uint32_t)((it >> 1) & 1), abort_flag, args.status))) break;
+                tc_fence_after();
+                const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * HB + half * 128);
+                if (PARTS == 1) {
+                    if (MODE == HEAD_STATS) {
+                        for (; ent < ents; ent += 32) {  // their columns, by the column
+                            const unsigned mine = ent + lane < ents ? __ldg(list + ent + lane) : 0u;
+                            for (int e = 0; e < min(32, ents - ent); ++e) {
+                                const unsigned what = __shfl_sync(0xffffffffu, mine, e);
+                                uint32_t l;
+                                asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(l) : "r"(trow + ((what >> 5) & 127u)));
+                                tmem_ld_wait();
+                                if (lane == (int)(what & 31u)) args.tl[at * args.K + (what >> 12)] = __uint_as_float(l);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(trow + c * 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32 * c));
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t r[32];
+                        tmem_ld32(trow + c * 32, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[32 * c + j] += __uint_as_float(r[j]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
+            }
+            if (!ok) break;
+            if (MODE == HEAD_STATS && PARTS > 1) {
+                for (; ent < ents; ++ent) {
+                    const unsigned what = __ldg(list + ent);
+                    if (lane != (int)(what & 31u)) continue;
+                    const int c = (int)((what >> 5) & 127u);
+                    float l = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i == c) l = v[i];
+                    args.tl[at * args.K + (what >> 12)] = l;
+                }
+            }
             if (MODE == HEAD_STATS) {
                 if (col >= args.V) continue;  // the other half's columns are the last
                 const int lab = args.label ? __ldg(args.label + at) - col : -1;
@@ -401,6 +461,22 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 for (int part = 0; part < PARTS; ++part) {
                     store64<(PARTS > 1)>(&tmD, v, stg, col, r0, x.t + args.T * part);
                     store64<(PARTS > 1)>(&tmD, v + 64, stg, col + 64, r0, x.t + args.T * part);
+                }
+            } else if (MODE == HEAD_DZ && args.dz) {
+                // straight into the tokens' rows
+                if (row < x.rows) {
+                    const long long o = ((long long)x.t * args.N + __ldg(args.map + at)) * args.d + col;
+#pragma unroll
+                    for (int i = 0; i < 128; i += 8) {
+                        if (col + i >= args.d) break;
+                        if (PARTS == 1) {
+                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(args.dz) + o + i) = f32_to_bf16x8(v + i);
+                        } else {
+                            float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(args.dz) + o + i);
+                            p[0] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                            p[1] = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
+                        }
+                    }
                 }
             } else if (MODE == HEAD_DZ || PARTS > 1) {
                 // fp32: 32 bytes at a time, d and the columns being multiples of 8

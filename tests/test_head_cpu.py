@@ -42,7 +42,7 @@ def test_head_refusals():
                   vm.head_config(100, 8, float("inf")), vm.head_config(100, 8, float("nan")), vm.head_config(100, 8, 1e-42),
                   vm.VmoeHead(100, 8, 1.0, 2)):
             assert call(h) == INVALID
-        assert call(vm.head_config(100, 129)) == UNSUPPORTED
+        assert call(vm.head_config(100, 129)) == UNSUPPORTED and call(vm.head_config((1 << 20) + 1, 8)) == UNSUPPORTED
         assert call(vm.head_config(100)) == INVALID  # a teacher's arrays without a teacher
         assert call(p=_p(T=1, N=(1 << 25), d=8), h=vm.head_config(1 << 30, 8)) == UNSUPPORTED
         least = vm.vmoe_head_min_workspace_size(_p(), head)
