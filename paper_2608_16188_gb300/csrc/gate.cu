@@ -320,6 +320,7 @@ gate_rows_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows);
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) count[i] = 0;
     pdl_wait();
+    pdl_launch_dependents();
     __syncthreads();
     for (int n = n0 + warp; n < n1; n += GT_WARPS) {
         const long long tn = (long long)t * N + n;
@@ -405,6 +406,7 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     const float *row = logits + (long long)t * N * E;
     for (int i = threadIdx.x; i < k * E + (rows + 31) / 32; i += GT_THREADS) count[i] = 0;
     pdl_wait();
+    pdl_launch_dependents();
     float b[V], bmax = 0.0f;  // -inf: off
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -581,6 +583,7 @@ __global__ void __launch_bounds__(GT_THREADS)
 gate_scan_kernel(int kE, int tiles, int32_t *__restrict__ hist, int32_t *__restrict__ all) {
     const int t = blockIdx.y, i = blockIdx.x * GT_THREADS + threadIdx.x;
     pdl_wait();
+    pdl_launch_dependents();
     if (i >= kE) return;
     int32_t *h = hist + (long long)t * tiles * kE + i;
     int run = 0;
@@ -608,6 +611,7 @@ gate_slots_kernel(Dims p, int rows, const int32_t *__restrict__ idx, const int32
     const int E = p.E, k = p.k, N = p.N, t = blockIdx.y, tiles = gridDim.x, tile = blockIdx.x;
     int *all = gt_base + k * E;
     pdl_wait();
+    pdl_launch_dependents();
     const int32_t *h = hist + (long long)t * tiles * k * E;
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) {
         if (SCANNED) {
@@ -658,6 +662,7 @@ gate_slots_kernel(Dims p, int rows, const int32_t *__restrict__ idx, const int32
 // b_e += rate sign(mean - count_e): E count_e against the sum, both whole.
 __global__ void gate_bias_kernel(int E, const int32_t *__restrict__ demand, float rate, float *__restrict__ bias) {
     pdl_wait();
+    pdl_launch_dependents();
     const int t = blockIdx.x, lane = threadIdx.x;
     const int32_t *c = demand + (long long)t * E;
     long long sum = 0;
@@ -696,6 +701,7 @@ gate_grad_kernel(Dims p, Gating g, const float *__restrict__ logits, const int32
     const int lane = threadIdx.x & 31, d = p.d, E = p.E, k = p.k;
     const long long tn = (long long)blockIdx.x * GT_WARPS + (threadIdx.x >> 5);
     pdl_wait();
+    pdl_launch_dependents();
     if (tn >= (long long)p.T * p.N) return;
     const int t = (int)(tn / p.N);
     int ei[KMAX], sl[KMAX];

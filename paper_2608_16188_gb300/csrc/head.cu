@@ -57,6 +57,7 @@ head_mark_kernel(Sizes z, int words, const int32_t *__restrict__ label, const in
     __shared__ unsigned parts[HG_THREADS / 32];
     const int t = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, word = blockIdx.x, n0 = word * 32;
     pdl_wait();
+    pdl_launch_dependents();
     const bool has = warp == 0 && label && n0 + lane < z.N && label_ok(z, label[(long long)t * z.N + n0 + lane]);
     unsigned taught = 0;
     if (tidx) {
@@ -115,6 +116,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
     if (!f.mark)
         for (int i = tid; i < f.words; i += HG_THREADS) bits[0][i] = bits[1][i] = 0;
     pdl_wait();
+    pdl_launch_dependents();
     const unsigned *taught = bits[0], *either = bits[1];
     if (f.mark) {
         taught = f.mark + (long long)t * f.words;
@@ -260,6 +262,7 @@ head_list_kernel(Sizes z, int halves, const int32_t *__restrict__ tidx, const fl
     __shared__ int sums[HG_THREADS / 32];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r0 = blockIdx.x * 32;
     pdl_wait();
+    pdl_launch_dependents();
     const int n = rows[t];
     if (r0 >= (n + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE) return;
     const long long block = ((long long)t * z.Np + r0) >> 5;
@@ -307,6 +310,7 @@ head_list_kernel(Sizes z, int halves, const int32_t *__restrict__ tidx, const fl
 __global__ void __launch_bounds__(HG_THREADS)
 head_split_kernel(long long n, const float *__restrict__ src, __nv_bfloat16 *__restrict__ out) {
     pdl_wait();
+    pdl_launch_dependents();
     for (long long i = ((long long)blockIdx.x * HG_THREADS + threadIdx.x) * 8; i < n; i += (long long)gridDim.x * HG_THREADS * 8) {
         const float4 a = __ldg(reinterpret_cast<const float4 *>(src + i)), b = __ldg(reinterpret_cast<const float4 *>(src + i) + 1);
         const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -384,6 +388,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row_in = lane % ROWS;
     const Sizes z = f.z;
     pdl_wait();
+    pdl_launch_dependents();
     const int n = f.rows[t], r0 = blockIdx.x * ROWS;
     if (r0 >= n) return;
     const int row = r0 + row_in;
@@ -458,6 +463,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_patch_kernel(Patch f) {
     const int t = blockIdx.y, lane = threadIdx.x & 31, r = blockIdx.x * (HG_THREADS / 32) + (threadIdx.x >> 5);
     const Sizes z = f.z;
     pdl_wait();
+    pdl_launch_dependents();
     if (r >= f.rows[t]) return;
     const long long at = (long long)t * z.Np + r, tn = (long long)t * z.N + f.map[at];
     Teacher q;
@@ -500,6 +506,7 @@ template <typename T>
 __global__ void __launch_bounds__(HG_THREADS)
 head_dz_kernel(Sizes z, int splits, const int *__restrict__ pos, const float *__restrict__ parts, T *__restrict__ dz) {
     pdl_wait();
+    pdl_launch_dependents();
     const int vec = z.d / 8;
     const long long total = (long long)z.T * z.N * vec, plane = (long long)z.T * z.Np * z.d;
     for (long long i = (long long)blockIdx.x * HG_THREADS + threadIdx.x; i < total; i += (long long)gridDim.x * HG_THREADS) {
