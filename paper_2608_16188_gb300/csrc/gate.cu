@@ -399,6 +399,8 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     const int E = p.E, k = p.k, N = p.N, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int *count = reinterpret_cast<int *>(gt_smem + row_scratch(M));  // [k][E]
     unsigned *again = reinterpret_cast<unsigned *>(count + k * E);   // a bit a row of the tile
+    int4 *wait_of = reinterpret_cast<int4 *>(gt_smem + (size_t)warp * 512 * M);  // a warp's scratch, which choose_row has behind the loop
+    int2 *mine_of = reinterpret_cast<int2 *>(wait_of + 32);
     const int t = blockIdx.y, n0 = blockIdx.x * rows, n1 = min(N, n0 + rows), gsize = E / g.groups;
     const int sub = lane / L, sl = lane % L, e0 = sl * V, mine = e0 / gsize, glanes = gsize / V;
     const bool softmax = g.score == VMOE_SCORE_SOFTMAX, by_logit = sbias == nullptr, group_by_logit = by_logit && g.top == 1;
@@ -433,6 +435,22 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
             for (int i = 0; i < V; ++i) next[i] = n < n1 && e0 + i < E ? __ldg(src + i) : -INFINITY;
         }
     };
+    // choice j of token n (-1: none; -2: not now): its gate, out and counted
+    auto finish = [&](int e, int n, float mx, float sum, int j) {
+        Choice r;
+        r.e = e;
+        r.x = e >= 0 ? __ldg(row + (long long)n * E + e) : -INFINITY;
+        r.mx = mx;
+        r.sum = sum;
+        const float gate = gate_of(g, r, L < 8 ? L : 8);
+        if (j < k && e != -2) {
+            const long long o = ((long long)t * N + n) * k + j;
+            out_idx[o] = e;
+            out_gate[o] = gate;
+            if (e >= 0) atomicAdd(count + j * E + e, 1);
+        }
+    };
+    int batch = 0;
     load(n0 + warp * RW + sub);
     const float rel = softmax ? 2e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
     for (int base = n0 + warp * RW; base < n1; base += GT_WARPS * RW) {
@@ -466,51 +484,109 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
         // the error of a value, from s <= smax, c + bmax
         auto tol = [&](float v) { return fmaf(rel, fminf(smax, v + bmax), fmaf(1.2e-7f, fabsf(v), abs1)); };
         bool open = false;  // whether two values are too close for fp32
-        unsigned at = sort_lane<V>(c);
         if (g.groups > 1) {
-            float a = c[0], a2 = c[1];
+            float a = c[0], a2 = -INFINITY;
+#pragma unroll
+            for (int i = 1; i < V; ++i) {
+                a2 = fmaxf(a2, fminf(a, c[i]));
+                a = fmaxf(a, c[i]);
+            }
             for (int o = 1; o < glanes; o <<= 1) {
                 const float oa = __shfl_xor_sync(FULL, a, o), oa2 = __shfl_xor_sync(FULL, a2, o);
                 a2 = fmaxf(fminf(a, oa), fmaxf(a2, oa2));
                 a = fmaxf(a, oa);
             }
             const float score = g.top == 2 ? a + a2 : a;
-            int rank = 0;
-            for (int q = 0; q < g.groups; ++q) {
-                const float other = __shfl_sync(FULL, score, q * glanes, L);
-                rank += other > score || (other == score && q < mine);
+            // the smallest of the `kept` largest scores, and the largest of the others; equal ones fall together and
+            // leave the row open
+            auto largest = [&](float v) {
+                if constexpr (L == 32) v = redux_max(v);
+                else
+                    for (int o = glanes; o < L; o <<= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+                return v;
+            };
+            float left = mine < g.groups ? score : -INFINITY, in = INFINITY;
+            bool tie = false;
+            for (int q = 0; q < g.kept; ++q) {
+                in = largest(left);
+                const unsigned has = __ballot_sync(FULL, left == in) >> (sub * L) & (L == 32 ? FULL : (1u << (L & 31)) - 1u);
+                tie |= in > -INFINITY && __popc(has) != glanes;
+                if (left == in) left = -INFINITY;
             }
-            const bool kept = rank < g.kept;
-            float in = kept ? score : INFINITY, out = kept || mine >= g.groups ? -INFINITY : score;
-            for (int o = glanes; o < L; o <<= 1) {
-                in = fminf(in, __shfl_xor_sync(FULL, in, o));
-                out = fmaxf(out, __shfl_xor_sync(FULL, out, o));
-            }
+            const float out = largest(left);
+            const bool kept = score >= in;
+            // fewer whole groups than may be open: the others, with an expert or none, go by their index
+            tie |= in == -INFINITY && a > -INFINITY && score == -INFINITY;
             // values at the border are at most |score| + bmax each
-            open = !group_by_logit && out > -INFINITY &&
-                   !(in - out > (float)g.top * (tol(fabsf(in) + bmax) + tol(fabsf(out) + bmax)));
+            open = tie || (!group_by_logit && out > -INFINITY &&
+                           !(in - out > (float)g.top * (tol(fabsf(in) + bmax) + tol(fabsf(out) + bmax))));
             if (by_logit && scored) {  // the choice has the logits' order: the lane's values again, as they came
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float l = n < n1 && e0 + i < E ? __ldg(row + (long long)n * E + e0 + i) : -INFINITY;
                     c[i] = a > -INFINITY && fabsf(l) < INFINITY ? l : -INFINITY;
                 }
-                at = sort_lane<V>(c);
             }
             if (!kept) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) c[i] = -INFINITY;
             }
         }
-        int my_e = -1;
-        float value = -INFINITY, last = -INFINITY;  // c of this lane's choice; of the best that was not chosen
-        for (int j = 0; j <= k; ++j) {
+        int my_e = -1;  // lane j: the j-th choice
+        bool few = false;
+        if (L == 32) {
+            // The k-th largest of the lanes' largest values is not above the k-th largest value: what is not below it, a
+            // dozen values, goes to shared memory, a value a lane, and each counts how many are above it.
             float m = c[0];
-            int e = sl;  // the lane that has the largest, the first of equals
-            if (L == 32) {
-                m = redux_max(m);
-                e = __ffs(__ballot_sync(FULL, c[0] == m)) - 1;
-            } else {
+#pragma unroll
+            for (int i = 1; i < V; ++i) m = fmaxf(m, c[i]);
+            float left = m, least = INFINITY;
+            for (int j = 0; j < k; ++j) {
+                least = redux_max(left);
+                if (left == least) left = -INFINITY;
+            }
+            if (!by_logit && least > -INFINITY) least -= 2.0f * tol(least);  // and the next one, if it is near
+            least = fmaxf(least, -3.4028235e38f);                            // nothing that is off
+            int found = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const bool take = c[i] >= least;
+                const unsigned who = __ballot_sync(FULL, take);
+                const int to = found + __popc(who & ((1u << lane) - 1u));
+                if (take && to < 32) mine_of[to] = make_int2(__float_as_int(c[i]), e0 + i);
+                found += __popc(who);
+            }
+            few = found <= 32;
+            if (few) {
+                __syncwarp();
+                const int2 own = mine_of[lane];
+                const float v = lane < found ? __int_as_float(own.x) : -INFINITY;
+                int above = 0;
+                float gap = INFINITY;  // to the nearest one above
+                bool equal = false;
+                for (int q = 0; q < found; ++q) {
+                    const float other = __shfl_sync(FULL, v, q);
+                    above += other > v;
+                    equal |= other == v && q != lane;
+                    if (other > v) gap = fminf(gap, other - v);
+                }
+                // of k + 1 values in a row none may be near the next (which adds 3e-6 of the gap to the error)
+                const float err = by_logit ? 0.0f : 2.00001f * tol(v);
+                open |= lane < found && above <= k && (equal || !(gap > err));
+                const unsigned at_rank = lane < found && above < k ? 1u << above : 0u;
+                my_e = -1;
+                if (at_rank) mine_of[32 + above].y = own.y;
+                __syncwarp();
+                if (lane < min(k, found)) my_e = mine_of[32 + lane].y;
+                __syncwarp();
+            }
+        }
+        if (!few) {
+            float value = -INFINITY, last = -INFINITY;  // c of this lane's choice; of the best that was not chosen
+            unsigned at = sort_lane<V>(c);
+            for (int j = 0; j <= k; ++j) {
+                float m = c[0];
+                int e = sl;  // the lane that has the largest, the first of equals
 #pragma unroll
                 for (int o = L / 2; o > 0; o >>= 1) {
                     const float om = __shfl_xor_sync(FULL, m, o);
@@ -520,43 +596,43 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
                         e = oe;
                     }
                 }
-            }
-            if (j == k) {
-                last = m;
-                break;
-            }
-            const int chosen = e * V + (int)(__shfl_sync(FULL, at, e, L) & 15u);
-            if (sl == e) {
+                if (j == k) {
+                    last = m;
+                    break;
+                }
+                const int chosen = e * V + (int)(__shfl_sync(FULL, at, e, L) & 15u);
+                if (sl == e) {
 #pragma unroll
-                for (int i = 0; i + 1 < V; ++i) c[i] = c[i + 1];
-                c[V - 1] = -INFINITY;
-                at >>= 4;
+                    for (int i = 0; i + 1 < V; ++i) c[i] = c[i + 1];
+                    c[V - 1] = -INFINITY;
+                    at >>= 4;
+                }
+                if (sl == j && m > -INFINITY) {
+                    my_e = chosen;
+                    value = m;
+                }
             }
-            if (sl == j && m > -INFINITY) {
-                my_e = chosen;
-                value = m;
-            }
-        }
-        {
             float after = __shfl_down_sync(FULL, value, 1, L);
             if (sl >= k - 1) after = last;
             const float err = by_logit ? 0.0f : tol(value) + tol(after);
             open |= sl < k && after > -INFINITY && !(value - after > err);
         }
         const unsigned redo = __ballot_sync(FULL, open && n < n1) >> (sub * L) & (L == 32 ? FULL : (1u << (L & 31)) - 1u);
-        Choice r;
-        r.e = my_e;
-        r.x = my_e >= 0 ? __ldg(row + (long long)n * E + my_e) : -INFINITY;
-        r.mx = mx;
-        r.sum = sum;
-        const float gate = gate_of(g, r, L < 8 ? L : 8);
-        if (redo) {
-            if (sl == 0) atomicOr(again + ((n - n0) >> 5), 1u << ((n - n0) & 31));
-        } else if (sl < k && n < n1) {
-            const long long o = ((long long)t * N + n) * k + sl;
-            out_idx[o] = my_e;
-            out_gate[o] = gate;
-            if (my_e >= 0) atomicAdd(count + sl * E + my_e, 1);
+        if (redo && sl == 0) atomicOr(again + ((n - n0) >> 5), 1u << ((n - n0) & 31));
+        // the gates of four rows of eight lanes at a time
+        if (L > 8) {
+            if (sl < 8) {
+                const int slot = (batch * RW + sub) * 8 + sl;
+                wait_of[slot] = make_int4(redo || n >= n1 ? -2 : my_e, n, __float_as_int(mx), __float_as_int(sum));
+            }
+            if (++batch < L / 8 && base + GT_WARPS * RW < n1) continue;
+            __syncwarp();
+            const int4 w = lane < batch * RW * 8 ? wait_of[lane] : make_int4(-2, 0, 0, 0);
+            batch = 0;
+            finish(w.x, w.y, __int_as_float(w.z), __int_as_float(w.w), lane & 7);
+            __syncwarp();
+        } else {
+            finish(redo || n >= n1 ? -2 : my_e, n, mx, sum, sl);
         }
     }
     __syncthreads();
