@@ -389,7 +389,7 @@ __device__ __forceinline__ unsigned sort_lane(float (&h)[V]) {
 //   0.23 take to 8e-8 of 1 in s, the reciprocal and the sum add 1.8e-7 s; softmax: 1e-6 s for |x - max| <= 10, and s
 //   |x - max| 6e-8 <= s 2e-6 up to 30, below which s is nothing beside the bias' rounding; c's rounding 6e-8 |c|.
 template <int L, int V>
-__global__ void __launch_bounds__(GT_THREADS, V == 8 ? 3 : 4)
+__global__ void __launch_bounds__(GT_THREADS, 4)
 gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, const float *__restrict__ sbias,
                  const uint8_t *__restrict__ mask, int32_t *__restrict__ out_idx, float *__restrict__ out_gate,
                  int32_t *__restrict__ hist) {
@@ -654,27 +654,37 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     for (int i = threadIdx.x; i < k * E; i += GT_THREADS) h[i] = count[i];
 }
 
-// Counts of the tiles before each, in place, and of all of them: hist [T][tiles][k][E], all [T][k][E].
+// Counts of the tiles before each, in place, and of all of them: hist [T][tiles][k][E], all [T][k][E].  A CTA 32 columns, a
+// warp an eighth of the tiles, twice: their sum, then each one's place.
 __global__ void __launch_bounds__(GT_THREADS)
 gate_scan_kernel(int kE, int tiles, int32_t *__restrict__ hist, int32_t *__restrict__ all) {
-    const int t = blockIdx.y, i = blockIdx.x * GT_THREADS + threadIdx.x;
+    __shared__ int sum[GT_WARPS][32];
+    const int t = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     pdl_wait();
     pdl_launch_dependents();
-    if (i >= kE) return;
     int32_t *h = hist + (long long)t * tiles * kE + i;
+    const int per = (tiles + GT_WARPS - 1) / GT_WARPS, q0 = warp * per, q1 = min(tiles, q0 + per);
     int run = 0;
-    for (int q = 0; q < tiles; q += 16) {
+    if (i < kE)
+#pragma unroll 16
+        for (int q = q0; q < q1; ++q) run += h[(long long)q * kE];
+    sum[warp][lane] = run;
+    __syncthreads();
+    run = 0;
+    for (int w = 0; w < warp; ++w) run += sum[w][lane];
+    if (i >= kE) return;
+    for (int q = q0; q < q1; q += 16) {
         int v[16];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) v[u] = q + u < tiles ? h[(long long)(q + u) * kE] : 0;
+        for (int u = 0; u < 16; ++u) v[u] = q + u < q1 ? h[(long long)(q + u) * kE] : 0;
 #pragma unroll
         for (int u = 0; u < 16; ++u)
-            if (q + u < tiles) {
+            if (q + u < q1) {
                 h[(long long)(q + u) * kE] = run;
                 run += v[u];
             }
     }
-    all[(long long)t * kE + i] = run;
+    if (warp == GT_WARPS - 1) all[(long long)t * kE + i] = run;
 }
 
 // SCANNED: behind gate_scan, for many tiles.
@@ -868,10 +878,11 @@ int launch_grad_k(const Dims &p, const Gating &g, const float *logits, const int
     return launch_grad<T, 8>(p, g, logits, idx, gate, slot, dy, ye, dgate, dlogits, s);
 }
 
-// Rows of a tile: 64, more where a task would have over 128 tiles.
+// Rows of a tile: 64, more where a task would have over 256 tiles (65536 x 4 rows of 256 experts: gate_fast 324 us with
+// 128 tiles, 1.1 waves; 268 with 256; 260 with 512, and as much longer for their counts).
 int tile_rows(int N) {
     int rows = 64;
-    while (rows < 32768 && (N + rows - 1) / rows > 128) rows *= 2;  // their bits: 4 KB of shared memory
+    while (rows < 32768 && (N + rows - 1) / rows > 256) rows *= 2;  // their bits: 4 KB of shared memory
     return rows;
 }
 
@@ -930,7 +941,7 @@ int launch_gate(const Dims &p, const Gating &g, const float *logits, const float
     const bool scan = tiles > 32;
     if (scan) {
         trace_before(s, "gate_scan");
-        st = launch_kernel(gate_scan_kernel, dim3((kE + GT_THREADS - 1) / GT_THREADS, p.T), dim3(GT_THREADS), 0, s, kE, tiles,
+        st = launch_kernel(gate_scan_kernel, dim3((kE + 31) / 32, p.T), dim3(GT_THREADS), 0, s, kE, tiles,
                            hist, all);
         trace_after(s);
         if (st != VMOE_OK) return st;
