@@ -42,6 +42,12 @@ __device__ __forceinline__ void load8(const float *p, float *o) {
     o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
 }
 
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *v) { *reinterpret_cast<uint4 *>(p) = f32_to_bf16x8(v); }
+__device__ __forceinline__ void store8(float *p, const float *v) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
 struct Sizes {
     int T, N, Np, d, V, K;
 };
@@ -501,34 +507,59 @@ __global__ void __launch_bounds__(HG_THREADS) head_patch_kernel(Patch f) {
     }
 }
 
-// dz from the parts of the sum; 0 for a token without a part.  Eight columns a thread.
+// dz from its sums over the pieces of the vocabulary; 0 for a token without a part.  Eight columns a thread.
 template <typename T>
 __global__ void __launch_bounds__(HG_THREADS)
-head_dz_kernel(Sizes z, int splits, const int *__restrict__ pos, const float *__restrict__ parts, T *__restrict__ dz) {
+head_dz_kernel(Sizes z, const int *__restrict__ pos, const float *__restrict__ sums, T *__restrict__ dz) {
     pdl_wait();
     pdl_launch_dependents();
     const int vec = z.d / 8;
-    const long long total = (long long)z.T * z.N * vec, plane = (long long)z.T * z.Np * z.d;
+    const long long total = (long long)z.T * z.N * vec;
     for (long long i = (long long)blockIdx.x * HG_THREADS + threadIdx.x; i < total; i += (long long)gridDim.x * HG_THREADS) {
         const long long tn = i / vec;
         const int c = (int)(i - tn * vec) * 8, r = pos[tn];
         float v[8] = {};
-        if (r >= 0) {
-            const float *src = parts + ((tn / z.N) * z.Np + r) * z.d + c;
-            for (int s = 0; s < splits; ++s) {
-                float o[8];
-                load8(src + s * plane, o);
+        if (r >= 0) load8(sums + ((tn / z.N) * z.Np + r) * z.d + c, v);
+        store8(dz + tn * z.d + c, v);
+    }
+}
+
+// The tiles of dz whose sums were cut (DzShares), from their parts in order.  A CTA 16 rows of a tile.
+template <typename T>
+__global__ void __launch_bounds__(HG_THREADS)
+head_dz_join_kernel(Sizes z, int pairs, int kb, int tiles_n, const int *__restrict__ rows, const int *__restrict__ map,
+                    const float *__restrict__ parts, T *__restrict__ dz) {
+    pdl_wait();
+    pdl_launch_dependents();
+    int tiles = 0;
+    for (int t = 0; t < z.T; ++t) tiles += (rows[t] + HEAD_TILE - 1) / HEAD_TILE * tiles_n;
+    const DzShares s(tiles, pairs, kb);
+    const int tile = blockIdx.x;
+    if (tile >= s.left || s.cuts == 1) return;
+    int local = s.full + tile, t = 0, n = 0;
+    for (;; ++t) {
+        n = rows[t];
+        const int c = (n + HEAD_TILE - 1) / HEAD_TILE * tiles_n;
+        if (local < c) break;
+        local -= c;
+    }
+    const int in = blockIdx.y * 16 + (threadIdx.x >> 4), r = local / tiles_n * HEAD_TILE + in;
+    const int c0 = (threadIdx.x & 15) * 16, col = local % tiles_n * HEAD_TILE + c0;
+    if (r >= n || col >= z.d) return;
+    float v[16] = {};
+    for (int cut = 0; cut < s.cuts; ++cut) {
+        const float *p = parts + ((long long)(cut * s.left + tile) * HEAD_TILE + in) * HEAD_TILE + c0;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] += o[q];
-            }
-        }
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4 *>(dz + tn * z.d + c) = f32_to_bf16x8(v);
-        } else {
-            reinterpret_cast<float4 *>(dz + tn * z.d + c)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4 *>(dz + tn * z.d + c)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        for (int h = 0; h < 16; h += 8) {
+            float o[8];
+            load8(p + h, o);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[h + q] += o[q];
         }
     }
+    T *o = dz + ((long long)t * z.N + map[(long long)t * z.Np + r]) * z.d + col;
+    store8(o, v);
+    if (col + 8 < z.d) store8(o + 8, v + 8);
 }
 
 Sizes sizes_of(const HeadPlan &h) { return Sizes{h.T, h.N, h.Np, h.d, h.V, h.K}; }
@@ -622,29 +653,23 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     o = both;
     h.coef = take(rowsp * 16);
     h.at_label = take(rowsp * 4);
-    // parts of dz's sum: while its tiles do not fill the SM pairs twice and each keeps 16 blocks of 64
-    const size_t tiles_dz = (rowsp / HEAD_TILE) * ((h.d + HEAD_TILE - 1) / HEAD_TILE), pairs = num_sms() / 2;
-    size_t splits = 1;
-    while (splits < 16 && tiles_dz * splits * 2 <= pairs * 2 && tiles_v * 4 >= splits * 2 * 16) splits *= 2;
     const size_t fixed = o, column = rowsp * HEAD_TILE * 2 * h.parts;  // a tile of columns of dl
+    // the whole vocabulary at once where there is room: dz is then shared out to the SM pairs
+    const size_t tiles_d = rowsp / HEAD_TILE * ((h.d + HEAD_TILE - 1) / HEAD_TILE), blocks = ((size_t)h.V + 63) / 64;
+    const size_t pairs = std::min<size_t>(std::max(1, num_sms() / 2), std::max(tiles_d, tiles_d * blocks / 8));
+    const size_t whole = pairs * HEAD_TILE * HEAD_TILE * 4, sums = (rowsp * h.d * 4 + 255) & ~(size_t)255;
+    if (bytes && bytes < fwd) return false;
     size_t cols = tiles_v;
-    const size_t want = (size_t)2 << 30;
-    if (bytes == 0) {
-        if (cols * column > want) cols = std::max<size_t>(1, want / column);
+    const size_t have = bytes ? bytes : fixed + std::max(whole, sums) + std::max(column, (size_t)2 << 30);
+    if (have >= fixed + whole + tiles_v * column) {
+        h.pairs = (int)pairs;
     } else {
-        if (bytes < fwd) return false;
-        auto rest = [&](size_t sp) {
-            const size_t dzp = (sp * rowsp * h.d * 4 + 255) & ~(size_t)255;
-            return bytes < fixed + dzp ? 0 : (bytes - fixed - dzp) / column;
-        };
-        while (splits > 1 && rest(splits) < 1) splits /= 2;
-        cols = std::min(cols, rest(splits));
-        if (cols < 1) return false;
+        if (have < fixed + sums + column) return false;
+        cols = std::min(tiles_v, (have - fixed - sums) / column);
     }
-    h.splits = (int)splits;
     h.piece = (int)(cols * HEAD_TILE);
     h.dl = take(cols * column);
-    h.dzp = take(splits * rowsp * h.d * 4);
+    h.dzp = take(h.pairs ? whole : sums);
     h.bytes = std::max(o, fwd);
     *out = h;
     return true;
@@ -743,7 +768,9 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
     if (st != VMOE_OK) return st;
     const Sizes z = sizes_of(h);
     const int *rows = at<int>(ws, h.rows), *map = at<int>(ws, h.map);
-    const bool direct = h.splits == 1 && h.piece >= h.V;  // dz in one go
+    const bool direct = h.pairs > 0;  // dz in one go
+    const int pairs = direct && dz ? std::min(h.pairs, head_dz_pairs(h.parts)) : 0;
+    if (direct && dz && pairs == 0) return VMOE_ERR_CUDA;
     __nv_bfloat16 *dl = at<__nv_bfloat16>(ws, h.dl);
     HeadGemm g = {};
     g.stats = h.stats;
@@ -751,7 +778,6 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
     g.label = in.label ? at<int>(ws, h.label) : nullptr;
     g.coef = k.coef;
     g.at_label = k.at_label;
-    g.splits = h.splits;
     for (int v0 = 0; v0 < h.V; v0 += h.piece) {
         g.v0 = v0;
         g.vn = std::min(h.piece, h.V - v0);
@@ -786,25 +812,36 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             if (st != VMOE_OK) return st;
         }
         if (dz) {
-            g.out = direct ? nullptr : at<float>(ws, h.dzp);
+            g.out = at<float>(ws, h.dzp);
             g.dz = direct ? dz : nullptr;
+            g.pairs = pairs;
             g.map = map;
             g.N = h.N;
             if ((st = launch_head_gemm(HEAD_DZ, h, g, zp, wp, dl, nullptr, s)) != VMOE_OK) return st;
+            g.pairs = 0;
         }
         if (dw) {
             g.out = (float *)dw;
             if ((st = launch_head_gemm(HEAD_DW, h, g, zp, wp, dl, (__nv_bfloat16 *)dw, s)) != VMOE_OK) return st;
         }
     }
-    if (!dz || direct) return VMOE_OK;
+    if (!dz) return VMOE_OK;
     trace_before(s, "head_dz_join");
-    const long long blocks = ((long long)h.T * h.N * (h.d / 8) + HG_THREADS - 1) / HG_THREADS;
-    const dim3 grid((unsigned)std::min(blocks, 16LL * num_sms()));
     const int *pos = at<int>(ws, h.pos);
     const float *parts = at<float>(ws, h.dzp);
-    st = p.bf16 ? launch_kernel(head_dz_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, h.splits, pos, parts, (__nv_bfloat16 *)dz)
-                : launch_kernel(head_dz_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, h.splits, pos, parts, (float *)dz);
+    if (direct) {
+        const int kb = (h.V + 63) / 64, tiles_n = (h.d + HEAD_TILE - 1) / HEAD_TILE;
+        const dim3 grid(pairs, HEAD_TILE / 16);
+        st = p.bf16 ? launch_kernel(head_dz_join_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, tiles_n, rows,
+                                    map, parts, (__nv_bfloat16 *)dz)
+                    : launch_kernel(head_dz_join_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, tiles_n, rows, map,
+                                    parts, (float *)dz);
+    } else {
+        const long long blocks = ((long long)h.T * h.N * (h.d / 8) + HG_THREADS - 1) / HG_THREADS;
+        const dim3 grid((unsigned)std::min(blocks, 16LL * num_sms()));
+        st = p.bf16 ? launch_kernel(head_dz_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, pos, parts, (__nv_bfloat16 *)dz)
+                    : launch_kernel(head_dz_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, pos, parts, (float *)dz);
+    }
     trace_after(s);
     return st;
 }

@@ -17,7 +17,7 @@ struct HeadPlan {
     int parts;           // bf16 parts of a value: 1, or 3 (fp32)
     int stats;           // sums of a row: 1, or 2 (labels and a teacher at another temperature)
     int piece;           // backward: columns of a piece of the vocabulary, whole tiles
-    int splits;          // backward: parts of the sum over the vocabulary in dz
+    int pairs;           // backward: SM pairs, at most, that dz is shared out to; 0: in pieces of the vocabulary
     float tau;           // the temperature
     float c1, c2;        // log2(e), log2(e) / temperature
     size_t rows, mark, pos, map, label, z, w;  // both ways
@@ -34,7 +34,7 @@ struct HeadGemm {
     const int *rows;              // [T] tokens that take part
     int v0, vn;                   // the piece: first column, columns
     int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows
-    int splits, first;            // HEAD_DZ: parts of the sum; whether this is the first piece
+    int pairs, first;             // HEAD_DZ: SM pairs; whether this is the first piece
     float c1, c2;
     const int *label;             // [T][Np] of compact rows, -1: none
     float2 *part;                 // HEAD_STATS out: [T][2 tiles_n][Np] largest logit times c1, sum
@@ -46,13 +46,32 @@ struct HeadGemm {
     float *tl;
     const float4 *coef;           // HEAD_DLOGITS: a, lse times log2(e), b, tlse times log2(e) of a row
     const float *at_label;        // the first sum's share of the gradient there
-    float *out;                   // HEAD_DZ: [splits][T][Np][d]; HEAD_DW, fp32: [T][V][d]
-    void *dz;                     // HEAD_DZ in one go (out NULL): [T][N][d], row map[t][r] of it
+    float *out;                   // HEAD_DZ: in pieces [T][Np][d], else [pairs][256][256] parts of tiles; HEAD_DW, fp32: [T][V][d]
+    void *dz;                     // HEAD_DZ in one go: [T][N][d], row map[t][r] of it
     const int *map;
     int N;
     int *status;
 };
 
+// HEAD_DZ in one go has tiles for all SM pairs at once for a while, and then `left` more: their sums, of kb blocks each, are
+// cut into `cuts` equal parts while there are pairs for them and a part keeps eight blocks.  Pair c takes part c / left of
+// tile c % left, so that neighbours go through the same weights and rows together, and leaves it in out[c].  (Equal shares
+// of all the blocks left over, with cuts anywhere, fill the pairs better and lose that: a frozen head of 50304 entries, 64
+// tiles over 76 pairs, 225 -> 342 us; 17 tasks of 32000, 53 tiles left, 815 -> 925.)
+struct DzShares {
+    int full, left, kb, cuts;
+    __host__ __device__ DzShares(int tiles, int pairs, int kb_) {
+        kb = kb_;
+        left = tiles % pairs;
+        full = tiles - left;
+        cuts = left ? pairs / left : 1;
+        if (cuts > kb / 8) cuts = kb / 8;
+        if (cuts < 1) cuts = 1;
+    }
+    __host__ __device__ int beg(int cut) const { return (int)((long long)kb * cut / cuts); }
+};
+
+int head_dz_pairs(int parts);  // SM pairs that run HEAD_DZ at once, 0: the query fails
 // a, b: the operands; dw: HEAD_DW's bf16 output; dl: HEAD_DLOGITS' output, [parts][T][Np][piece].
 int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat16 *z, const __nv_bfloat16 *w,
                      __nv_bfloat16 *dl, __nv_bfloat16 *dw, cudaStream_t s);

@@ -15,6 +15,7 @@
 // Tokens that take part lie packed, and their number is known on the device alone: a role walks the tiles with a cursor
 // over the heads.  Order: STATS and DLOGITS take all row tiles of a group of 32 under one column tile, so that the
 // weights come from DRAM once and the tokens stay in L2; DZ all column tiles of a row tile, whose dl is the larger operand.
+// DZ's tiles are few and long (a sum over the vocabulary): what does not fill all pairs is cut along the sum (DzShares).
 //
 // fp32 operands are three bf16 parts of 8 bits each (split3), and a product of theirs the six products of parts that are
 // above 2^-24 of it, the smallest first.  Tensor cores cut a sum to fp32 at every step of 16, always towards zero, so the
@@ -52,51 +53,63 @@ __device__ __forceinline__ int part_a(int np, int i) { return np == 1 ? 0 : i ==
 __device__ __forceinline__ int part_b(int np, int i) { return np == 1 ? 0 : i == 1 ? 2 : i == 2 || i == 4 ? 1 : 0; }
 
 struct HTile {
-    int t, m, n, split, rows, kb0, kb1;  // k-blocks of one product of parts
+    int t, m, n, rows, kb0, kb1;  // k-blocks of one product of parts
+    int part;                     // HEAD_DZ: where a part of a tile goes, -1: a whole one
 };
 
-// A role's place among the tiles of all heads.
+// A role's way through the tiles of all heads: every `step`-th one, then a part of HEAD_DZ's last ones.
 template <int MODE>
 struct Cursor {
-    int t = -1, base = 0, cnt = 0, rows = 0;
-    __device__ bool seek(const HeadGemm &g, int u, HTile &x) {
-        while (u - base >= cnt) {
+    int t = -1, base = 0, cnt = 0, rows = 0, u, step;
+    int full = 0x7fffffff, left = 0;
+    __device__ Cursor(const HeadGemm &g, int first, int stride) : u(first), step(stride) {
+        if (MODE != HEAD_DZ || !g.dz) return;
+        int tiles = 0;
+        for (int i = 0; i < g.T; ++i) tiles += (__ldg(g.rows + i) + HB - 1) / HB * g.tiles_n;
+        left = tiles % g.pairs;
+        full = tiles - left;
+    }
+    __device__ bool seek(const HeadGemm &g, int at, HTile &x) {
+        while (at - base >= cnt) {
             base += cnt;
             if (++t >= g.T) return false;
             rows = __ldg(g.rows + t);
-            const int tm = (rows + HB - 1) / HB;
-            cnt = MODE == HEAD_DW ? g.tiles_m * g.tiles_n : tm * g.tiles_n * (MODE == HEAD_DZ ? g.splits : 1);
+            cnt = MODE == HEAD_DW ? g.tiles_m * g.tiles_n : (rows + HB - 1) / HB * g.tiles_n;
         }
-        int local = u - base;
+        int local = at - base;
         x.t = t;
         x.rows = rows;
-        x.split = 0;
+        x.part = -1;
+        x.kb0 = 0;
         if (MODE == HEAD_STATS || MODE == HEAD_DLOGITS) {
             const int tm = (rows + HB - 1) / HB, g0 = local / (HG_ROWS * g.tiles_n);
             local -= g0 * HG_ROWS * g.tiles_n;
             const int gm = min(HG_ROWS, tm - g0 * HG_ROWS);
             x.n = local / gm;
             x.m = g0 * HG_ROWS + local - x.n * gm;
+            x.kb1 = (g.d + BK - 1) / BK;
         } else {
             x.n = local % g.tiles_n;
-            local /= g.tiles_n;
-            if (MODE == HEAD_DZ) {
-                x.split = local % g.splits;
-                local /= g.splits;
-            }
-            x.m = local;
+            x.m = local / g.tiles_n;
+            x.kb1 = MODE == HEAD_DZ ? (g.vn + BK - 1) / BK : (rows + BK - 1) / BK;
         }
-        if (MODE == HEAD_STATS || MODE == HEAD_DLOGITS) {
-            x.kb0 = 0;
-            x.kb1 = (g.d + BK - 1) / BK;
-        } else if (MODE == HEAD_DZ) {
-            const int kb = (g.vn + BK - 1) / BK;
-            x.kb0 = (int)((long long)kb * x.split / g.splits);
-            x.kb1 = (int)((long long)kb * (x.split + 1) / g.splits);
-        } else {
-            x.kb0 = 0;
-            x.kb1 = (rows + BK - 1) / BK;
+        return true;
+    }
+    __device__ bool next(const HeadGemm &g, HTile &x) {
+        if (MODE != HEAD_DZ || u < full) {
+            const bool ok = seek(g, u, x);
+            u += step;
+            return ok;
         }
+        // this pair's part of a tile that is left, once
+        const int c = (int)(blockIdx.x >> 1);
+        const DzShares s(left, g.pairs, (g.vn + BK - 1) / BK);
+        if (u == 0x7fffffff || left == 0 || c >= left * s.cuts) return false;
+        u = 0x7fffffff;
+        if (!seek(g, full + c % left, x)) return false;
+        x.kb0 = s.beg(c / left);
+        x.kb1 = s.beg(c / left + 1);
+        if (s.cuts > 1) x.part = c;
         return true;
     }
 };
@@ -208,9 +221,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             int stage = 0, issued = 0;
             uint32_t phase = 0;
             bool ok = true;
-            Cursor<MODE> cur;
+            Cursor<MODE> cur(args, cid, ncl);
             HTile x;
-            for (int u = cid; ok && cur.seek(args, u, x); u += ncl) {
+            while (ok && cur.next(args, x)) {
                 const int a0 = x.m * HB + (int)rank * 128, b0 = x.n * HB + (int)rank * 128;
                 for (int i = 0; i < args.np && ok; ++i) {
                     const int ta = x.t + args.T * part_a(args.np, i), tb = x.t + args.T * part_b(args.np, i);
@@ -264,9 +277,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             int stage = 0, it = 0;
             uint32_t phase = 0;
             bool ok = true;
-            Cursor<MODE> cur;
+            Cursor<MODE> cur(args, cid, ncl);
             HTile x;
-            for (int u = cid; ok && cur.seek(args, u, x); u += ncl) {
+            while (ok && cur.next(args, x)) {
                 const int kb = x.kb1 - x.kb0, sums = sums_of<PARTS>(kb);  // none without a token: the epilogue writes zeros
                 for (int i = 0, k = 0; i < sums && ok; ++i, ++it) {
                     const int acc = it & 1, end = sum_end<PARTS>(kb, i);
@@ -317,9 +330,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         const int q = warp & 3, half = (warp - 2) >> 2;
         uint8_t *stg = epi_base + (warp - 2) * 4096;
         int it = 0;
-        Cursor<MODE> cur;
+        Cursor<MODE> cur(args, cid, ncl);
         HTile x;
-        for (int u = cid; cur.seek(args, u, x); u += ncl) {
+        while (cur.next(args, x)) {
             float v[128];
             const int row = x.m * HB + (int)rank * 128 + q * 32 + lane, col = x.n * HB + half * 128;
             const long long at = (long long)x.t * args.Np + row;
@@ -462,7 +475,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     store64<(PARTS > 1)>(&tmD, v, stg, col, r0, x.t + args.T * part);
                     store64<(PARTS > 1)>(&tmD, v + 64, stg, col + 64, r0, x.t + args.T * part);
                 }
-            } else if (MODE == HEAD_DZ && args.dz) {
+            } else if (MODE == HEAD_DZ && args.dz && x.part < 0) {
                 // straight into the tokens' rows
                 if (row < x.rows) {
                     const long long o = ((long long)x.t * args.N + __ldg(args.map + at)) * args.d + col;
@@ -481,16 +494,16 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             } else if (MODE == HEAD_DZ || PARTS > 1) {
                 // fp32: 32 bytes at a time, d and the columns being multiples of 8
                 const bool live = MODE == HEAD_DZ ? row < x.rows : row < args.vn;
-                float *o = MODE == HEAD_DZ
-                               ? args.out + (((long long)x.split * args.T + x.t) * args.Np + row) * args.d + col
-                               : args.out + ((long long)x.t * args.V + args.v0 + row) * args.d + col;
+                float *o = MODE == HEAD_DW ? args.out + ((long long)x.t * args.V + args.v0 + row) * args.d + col
+                           : x.part < 0    ? args.out + at * args.d + col
+                                           : args.out + ((long long)x.part * HB + row - x.m * HB) * HB + half * 128;
                 if (live) {
 #pragma unroll
                     for (int i = 0; i < 128; i += 4) {
                         if (col + i >= args.d) break;
                         float4 r = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                         float4 *p = reinterpret_cast<float4 *>(o + i);
-                        if (MODE == HEAD_DZ && !args.first) {
+                        if (MODE == HEAD_DZ && !args.dz && !args.first) {
                             const float4 b = *p;
                             r = make_float4(r.x + b.x, r.y + b.y, r.z + b.z, r.w + b.w);
                         }
@@ -516,37 +529,47 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     if (warp == 0) tmem_dealloc_pair(tmem_base, 2 * HB);
 }
 
+// SM pairs that run the kernel at once on the current device, its shared memory granted first; 0: the query fails.
 template <int MODE, bool STATS2, int PARTS>
-int launch(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &md, const HeadGemm &g, long long tiles,
-           cudaStream_t s, const char *name) {
+int pairs_of(cudaLaunchConfig_t *cfg, cudaLaunchAttribute (&attr)[2]) {
     auto kern = head_gemm_kernel<MODE, STATS2, PARTS>;
-    static std::atomic<int> smem_limit[64], pairs[64];
-    if (const int st = raise_smem_limit((const void *)kern, smem_limit, (int)HeadShape::SMEM_BYTES)) return st;
+    static std::atomic<int> smem_limit[64], fits[64];
+    if (raise_smem_limit((const void *)kern, smem_limit, (int)HeadShape::SMEM_BYTES) != VMOE_OK) return 0;
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VMOE_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * (unsigned)num_sms());
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = HeadShape::SMEM_BYTES;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    *cfg = {};
+    cfg->gridDim = dim3(2 * (unsigned)num_sms());
+    cfg->blockDim = dim3(THREADS);
+    cfg->dynamicSmemBytes = HeadShape::SMEM_BYTES;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int ncl = pairs[dev].load(std::memory_order_relaxed);
-    if (!ncl) {
-        if (cudaOccupancyMaxActiveClusters(&ncl, kern, &cfg) != cudaSuccess || ncl <= 0) return VMOE_ERR_CUDA;
-        pairs[dev].store(ncl, std::memory_order_relaxed);
+    cfg->attrs = attr;
+    cfg->numAttrs = 1;
+    int n = fits[dev].load(std::memory_order_relaxed);
+    if (!n) {
+        if (cudaOccupancyMaxActiveClusters(&n, kern, cfg) != cudaSuccess || n <= 0) return 0;
+        fits[dev].store(n, std::memory_order_relaxed);
     }
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < ncl ? tiles : ncl)));
+    return n;
+}
+
+template <int MODE, bool STATS2, int PARTS>
+int launch(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &md, const HeadGemm &g, long long tiles,
+           cudaStream_t s, const char *name) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    const int fits = pairs_of<MODE, STATS2, PARTS>(&cfg, attr);
+    if (!fits) return VMOE_ERR_CUDA;
+    const int pairs = g.pairs ? g.pairs : (int)(tiles < fits ? tiles : fits);
+    cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(2 * pairs));
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
     trace_before(s, name);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, md, g);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, STATS2, PARTS>, ma, mb, md, g);
     trace_after(s);
     return e == cudaSuccess ? VMOE_OK : VMOE_ERR_CUDA;
 }
@@ -555,6 +578,12 @@ int launch(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &md, 
 }  // namespace tc
 
 using namespace tc;
+
+int head_dz_pairs(int parts) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    return parts > 1 ? pairs_of<HEAD_DZ, false, 3>(&cfg, attr) : pairs_of<HEAD_DZ, false, 1>(&cfg, attr);
+}
 
 int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat16 *z, const __nv_bfloat16 *w,
                      __nv_bfloat16 *dl, __nv_bfloat16 *dw, cudaStream_t s) {
@@ -589,8 +618,8 @@ int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat1
     g.tiles_n = tn_d;
     if (mode == HEAD_DZ) {
         if (!make_map(&ma, dl, h.piece, h.Np, batches, 128) || !make_map(&mb, w, h.d, h.V, batches, 64)) return VMOE_ERR_CUDA;
-        return f32 ? launch<HEAD_DZ, false, 3>(ma, mb, ma, g, tm * tn_d * g.splits, s, "head_dz")
-                   : launch<HEAD_DZ, false, 1>(ma, mb, ma, g, tm * tn_d * g.splits, s, "head_dz");
+        return f32 ? launch<HEAD_DZ, false, 3>(ma, mb, ma, g, tm * tn_d, s, "head_dz")
+                   : launch<HEAD_DZ, false, 1>(ma, mb, ma, g, tm * tn_d, s, "head_dz");
     }
     g.tiles_m = tn_v;
     const long long tiles = (long long)h.T * tn_v * tn_d;
