@@ -7,8 +7,8 @@ or CPU fallback, and importing a function whose library is missing raises.
 The functions carry the C names (``vmoe_route``, ``vmoe_dispatch``,
 ``vmoe_expert_fwd``, ``vmoe_expert_bwd``, ``vmoe_combine``) and take torch tensors
 (device memory, any dtype matching the problem) or raw integer device pointers;
-those around the layer (``vmoe_balance``, ``vmoe_block_norm``, ``vmoe_adamw`` and their
-backwards) check a tensor's dtype, size, strides and device first;
+those around the layer (``vmoe_balance``, ``vmoe_block_norm``, ``vmoe_adamw``, ``vmoe_gate``,
+``vmoe_head_loss`` and their backwards) check a tensor's dtype, size, strides and device first;
 ``stream`` is a ``torch.cuda.Stream``, a raw ``cudaStream_t`` integer, or None for
 the current torch stream.  A non-zero status raises ``VmoeError``.
 """
@@ -633,6 +633,7 @@ def vmoe_trace_get(i: int):
     return name.value.decode(), ms.value
 
 
-from .step import BalanceBuffers, Buffers, HostPipeline, StepRunner  # noqa: E402  (needs the names above)
+from .step import BalanceBuffers, Buffers, GateBuffers, HostPipeline, StepRunner  # noqa: E402  (needs the names above)
 from .block import BlockStack  # noqa: E402
+from .head import Head  # noqa: E402
 from .optim import AdamW  # noqa: E402

@@ -12,7 +12,7 @@ import bisect
 import torch
 
 from . import (VMOE_NORM_POST, _stream, norm_config, vmoe_block_norm, vmoe_block_norm_bwd, vmoe_block_norm_bwd_workspace_size)
-from .step import BalanceBuffers, Buffers, StepRunner, _nothing_to_add_to
+from .step import BalanceBuffers, Buffers, GateBuffers, StepRunner, _nothing_to_add_to
 
 NORM_PARAMS = ("pre_w", "pre_b", "post_w", "post_b", "gate")
 
@@ -29,7 +29,9 @@ class BlockStack:
     StepRunner, and of its norms' fp32 [T,d] parameters pre_w, pre_b, post_w, post_b, gate, each
     optional.  ``norm``: norm_config(...); post_* are used only if it has a norm on the branch.
     ``balance``: the balance losses' weights, see BalanceBuffers; each block computes its own.
-    ``token_mask`` [T,N] uint8: 0 for padding that the losses leave out.
+    ``token_mask`` [T,N] uint8: 0 for padding that the losses leave out.  ``gating``: a VmoeGating
+    (gating(...)) for experts that are chosen by vmoe_gate, each block with a bias of its own, in
+    ``gates``, which ``update_gates(rate)`` moves; token_mask's padding then goes nowhere.
 
     ``forward(x)`` returns z [T,N,d]; ``backward(dz)`` returns dx and leaves every parameter's
     gradient in ``grads[l][name]``.  Both run on the current stream, or on ``stream``, and write the
@@ -38,7 +40,7 @@ class BlockStack:
     layer's input gradient, which is written while dz is read; z and dx may be given.
     """
 
-    def __init__(self, p, layers, norm=None, balance=None, token_mask=None, device="cuda"):
+    def __init__(self, p, layers, norm=None, balance=None, token_mask=None, device="cuda", gating=None):
         if not layers:
             raise ValueError("a stack has at least one block")
         if _nothing_to_add_to(p, balance):
@@ -54,11 +56,13 @@ class BlockStack:
             inp = dict(x=torch.empty_like(b.y), dy=torch.empty_like(b.y), w_router=w["w_router"], bias=w.get("bias"),
                        w1=w["w1"], w2=w["w2"], token_mask=token_mask)
             r = StepRunner(p, inp, b, router_grad=True,
-                           balance=None if balance is None else BalanceBuffers(p, balance, device))
+                           balance=None if balance is None else BalanceBuffers(p, balance, device),
+                           gating=None if gating is None else GateBuffers(p, gating, device=device))
             self.runners.append(r)
             g = {n: like(self._par(w, n)) for n in NORM_PARAMS}
             g.update(w_router=b.dw_router, bias=None if w.get("bias") is None else b.dbias, w1=b.dw1, w2=b.dw2)
             self.grads.append(g)
+        self.gates = [r.gating for r in self.runners]
         first = self.runners[0].b.y
         self.z = [torch.empty_like(first) for _ in layers]  # behind each block
         self.pre_stat = [stat() for _ in layers]
@@ -70,6 +74,7 @@ class BlockStack:
         for r, g in zip(self.runners, self.grads):
             own += [*vars(r.b).values(), r.inp["x"], r.inp["dy"], *g.values()]
             own += [] if r.balance is None else [v for n, v in vars(r.balance).items() if n != "dloss"]
+            own += [] if r.gating is None else [r.gating.select_bias, r.gating.demand, r.gating.workspace]
         self._own = sorted({_span(t) for t in own if isinstance(t, torch.Tensor)})
 
     def _par(self, layer, name):
@@ -129,6 +134,13 @@ class BlockStack:
     def balance_losses(self):
         """[T,3] losses of each block's last forward (see vmoe_balance), or None without them."""
         return [None if r.balance is None else r.balance.loss for r in self.runners]
+
+    def update_gates(self, rate, stream=None):
+        """Moves every block's selection bias towards an even demand, by ``rate`` (see vmoe_gate_bias)."""
+        stream = _stream(stream)
+        for gate in self.gates:
+            if gate is not None:
+                gate.update(rate, stream)
 
     def parameters(self):
         """A dict for each adapted tensor: name, param, grad, and decay: False for biases, norms and

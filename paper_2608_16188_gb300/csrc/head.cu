@@ -377,6 +377,7 @@ struct Finish {
     const int *rows, *map, *label;
     const float2 *part, *part2;
     const float *picked, *tl;
+    const __nv_bfloat16 *few_z, *few_w;  // few tokens: the entries' logits are formed here
     const int32_t *tidx;
     const float *tlogit;
     float *ce, *lse, *kl, *tlse, *logp;
@@ -386,6 +387,34 @@ __device__ __forceinline__ void join(float &m, float &s, float2 v) {
     s = s * exp2f(m - top) + v.y * exp2f(v.x - top);
     m = top;
 }
+// Lane l: the logit of entry i of lane l, for the first `n` lanes; -1 gives 0.  Four entries' rows at a time.
+__device__ float entries_logits(const Sizes &z, const __nv_bfloat16 *zr, const __nv_bfloat16 *w, int i, int n) {
+    const int lane = threadIdx.x & 31;
+    float mine = 0.0f;
+    for (int j = 0; j < min(n, 32); j += 4) {
+        float acc[4] = {};
+        const __nv_bfloat16 *row[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) row[e] = w + (long long)max(0, __shfl_sync(FULL, i, j + e)) * z.d;
+        for (int c = lane * 8; c < z.d; c += 256) {
+            float a[8], b[8];
+            bf16x8_to_f32(*reinterpret_cast<const uint4 *>(zr + c), a);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                bf16x8_to_f32(__ldg(reinterpret_cast<const uint4 *>(row[e] + c)), b);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) acc[e] = fmaf(a[x], b[x], acc[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            acc[e] = warp_sum(acc[e]);
+            if (lane == j + e) mine = acc[e];
+        }
+    }
+    return i >= 0 ? mine : 0.0f;
+}
+
 template <int ROWS>
 __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
     constexpr int SHARES = HG_THREADS / ROWS;  // threads of a row
@@ -439,9 +468,12 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
         float loss = 0.0f;
 #pragma unroll
         for (int mm = 0; mm < Teacher::M; ++mm) {
+            if (32 * mm >= z.K) break;
             const int j = lane + 32 * mm;
-            if (j >= z.K) break;
-            const float lp = q.i[mm] >= 0 ? f.tl[at * z.K + j] * f.inv_tau - tl[i] : 0.0f;
+            const float l = f.few_z ? entries_logits(z, f.few_z + at * z.d, f.few_w + (long long)t * z.V * z.d, q.i[mm], z.K - 32 * mm)
+                            : j < z.K && q.i[mm] >= 0 ? f.tl[at * z.K + j] : 0.0f;
+            if (j >= z.K) continue;
+            const float lp = q.i[mm] >= 0 ? l * f.inv_tau - tl[i] : 0.0f;
             f.logp[tn * z.K + j] = lp;
             // an entry of no weight adds nothing, whatever its logarithm
             if (q.q[mm] > 0.0f || q.q[mm] != q.q[mm]) loss += q.q[mm] * (q.lq[mm] - lp);
@@ -527,13 +559,13 @@ head_dz_kernel(Sizes z, const int *__restrict__ pos, const float *__restrict__ s
 // The tiles of dz whose sums were cut (DzShares), from their parts in order.  A CTA 16 rows of a tile.
 template <typename T>
 __global__ void __launch_bounds__(HG_THREADS)
-head_dz_join_kernel(Sizes z, int pairs, int kb, int tiles_n, const int *__restrict__ rows, const int *__restrict__ map,
+head_dz_join_kernel(Sizes z, int pairs, int kb, int least, int tiles_n, const int *__restrict__ rows, const int *__restrict__ map,
                     const float *__restrict__ parts, T *__restrict__ dz) {
     pdl_wait();
     pdl_launch_dependents();
     int tiles = 0;
     for (int t = 0; t < z.T; ++t) tiles += (rows[t] + HEAD_TILE - 1) / HEAD_TILE * tiles_n;
-    const DzShares s(tiles, pairs, kb);
+    const DzShares s(tiles, pairs, kb, least);
     const int tile = blockIdx.x;
     if (tile >= s.left || s.cuts == 1) return;
     int local = s.full + tile, t = 0, n = 0;
@@ -624,6 +656,9 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.K = head->teacher_k;
     h.Np = (h.N + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
     h.parts = p.bf16 ? 1 : 3;
+    // a warp 32 entries at a time, two CTAs of eight warps an SM
+    if (p.bf16 && h.N <= HEAD_FEW && h.d <= 2048)
+        h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));
     h.tau = head->temperature;
     h.stats = label && h.K > 0 && head->temperature != 1.0f ? 2 : 1;
     h.c2 = (float)(1.4426950408889634 / (double)head->temperature);
@@ -656,7 +691,7 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     const size_t fixed = o, column = rowsp * HEAD_TILE * 2 * h.parts;  // a tile of columns of dl
     // the whole vocabulary at once where there is room: dz is then shared out to the SM pairs
     const size_t tiles_d = rowsp / HEAD_TILE * ((h.d + HEAD_TILE - 1) / HEAD_TILE), blocks = ((size_t)h.V + 63) / 64;
-    const size_t pairs = std::min<size_t>(std::max(1, num_sms() / 2), std::max(tiles_d, tiles_d * blocks / 8));
+    const size_t pairs = std::min<size_t>(std::max(1, num_sms() / 2), std::max(tiles_d, tiles_d * blocks / dz_least(h.parts)));
     const size_t whole = pairs * HEAD_TILE * HEAD_TILE * 4, sums = (rowsp * h.d * 4 + 255) & ~(size_t)255;
     if (bytes && bytes < fwd) return false;
     size_t cols = tiles_v;
@@ -700,7 +735,7 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     g.stats = h.stats;
     g.rows = at<int>(ws, h.rows);
     g.vn = h.V;
-    if (in.tidx) {
+    if (in.tidx && !h.few) {
         int *off = at<int>(ws, h.off);
         unsigned *list = at<unsigned>(ws, h.list);
         g.off = off;
@@ -717,11 +752,12 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     g.part = at<float2>(ws, h.part);
     g.part2 = at<float2>(ws, h.part2);
     g.picked = at<float>(ws, h.picked);
-    if ((st = launch_head_gemm(HEAD_STATS, h, g, zp, wp, nullptr, nullptr, s)) != VMOE_OK) return st;
+    st = h.few ? launch_head_few(h, g, zp, wp, s) : launch_head_gemm(HEAD_STATS, h, g, zp, wp, nullptr, nullptr, s);
+    if (st != VMOE_OK) return st;
     Finish f = {};
     f.z = z;
-    f.halves = (h.V + 127) / 128;
-    f.pitch = pitch;
+    f.halves = h.few ? h.few : (h.V + 127) / 128;
+    f.pitch = h.few ? h.few : pitch;
     f.stats = h.stats;
     f.inv_tau = 1.0f / h.tau;
     f.c1 = h.c1;
@@ -732,6 +768,8 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     f.part2 = g.part2;
     f.picked = g.picked;
     f.tl = g.tl;
+    f.few_z = h.few ? zp : nullptr;
+    f.few_w = wp;
     f.tidx = in.tidx;
     f.tlogit = in.tlogit;
     f.ce = ce;
@@ -825,16 +863,16 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             if ((st = launch_head_gemm(HEAD_DW, h, g, zp, wp, dl, (__nv_bfloat16 *)dw, s)) != VMOE_OK) return st;
         }
     }
-    if (!dz) return VMOE_OK;
+    if (!dz || (direct && (h.V + 63) / 64 < 2 * dz_least(h.parts))) return VMOE_OK;  // no tile was cut
     trace_before(s, "head_dz_join");
     const int *pos = at<int>(ws, h.pos);
     const float *parts = at<float>(ws, h.dzp);
     if (direct) {
-        const int kb = (h.V + 63) / 64, tiles_n = (h.d + HEAD_TILE - 1) / HEAD_TILE;
+        const int kb = (h.V + 63) / 64, least = dz_least(h.parts), tiles_n = (h.d + HEAD_TILE - 1) / HEAD_TILE;
         const dim3 grid(pairs, HEAD_TILE / 16);
-        st = p.bf16 ? launch_kernel(head_dz_join_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, tiles_n, rows,
+        st = p.bf16 ? launch_kernel(head_dz_join_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, least, tiles_n, rows,
                                     map, parts, (__nv_bfloat16 *)dz)
-                    : launch_kernel(head_dz_join_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, tiles_n, rows, map,
+                    : launch_kernel(head_dz_join_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, least, tiles_n, rows, map,
                                     parts, (float *)dz);
     } else {
         const long long blocks = ((long long)h.T * h.N * (h.d / 8) + HG_THREADS - 1) / HG_THREADS;

@@ -8,6 +8,7 @@ namespace vmoe {
 
 constexpr int HEAD_K = 128;     // entries of a teacher's list at most
 constexpr int HEAD_V = 1 << 20;  // entries of a vocabulary at most, with a teacher
+constexpr int HEAD_FEW = 16;    // tokens of a head at most for head_few
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
 
 // Sizes of a call, and where its scratch lies in the workspace (byte offsets).
@@ -18,6 +19,7 @@ struct HeadPlan {
     int stats;           // sums of a row: 1, or 2 (labels and a teacher at another temperature)
     int piece;           // backward: columns of a piece of the vocabulary, whole tiles
     int pairs;           // backward: SM pairs, at most, that dz is shared out to; 0: in pieces of the vocabulary
+    int few;             // forward: CTAs a head of head_few, 0: HEAD_STATS
     float tau;           // the temperature
     float c1, c2;        // log2(e), log2(e) / temperature
     size_t rows, mark, pos, map, label, z, w;  // both ways
@@ -54,18 +56,19 @@ struct HeadGemm {
 };
 
 // HEAD_DZ in one go has tiles for all SM pairs at once for a while, and then `left` more: their sums, of kb blocks each, are
-// cut into `cuts` equal parts while there are pairs for them and a part keeps eight blocks.  Pair c takes part c / left of
+// cut into `cuts` equal parts while there are pairs for them and a part keeps `least` blocks.  Pair c takes part c / left of
 // tile c % left, so that neighbours go through the same weights and rows together, and leaves it in out[c].  (Equal shares
 // of all the blocks left over, with cuts anywhere, fill the pairs better and lose that: a frozen head of 50304 entries, 64
 // tiles over 76 pairs, 225 -> 342 us; 17 tasks of 32000, 53 tiles left, 815 -> 925.)
+constexpr int dz_least(int parts) { return parts == 1 ? 16 : 8; }
 struct DzShares {
     int full, left, kb, cuts;
-    __host__ __device__ DzShares(int tiles, int pairs, int kb_) {
+    __host__ __device__ DzShares(int tiles, int pairs, int kb_, int least) {
         kb = kb_;
         left = tiles % pairs;
         full = tiles - left;
         cuts = left ? pairs / left : 1;
-        if (cuts > kb / 8) cuts = kb / 8;
+        if (cuts > kb / least) cuts = kb / least;
         if (cuts < 1) cuts = 1;
     }
     __host__ __device__ int beg(int cut) const { return (int)((long long)kb * cut / cuts); }
@@ -75,6 +78,9 @@ int head_dz_pairs(int parts);  // SM pairs that run HEAD_DZ at once, 0: the quer
 // a, b: the operands; dw: HEAD_DW's bf16 output; dl: HEAD_DLOGITS' output, [parts][T][Np][piece].
 int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat16 *z, const __nv_bfloat16 *w,
                      __nv_bfloat16 *dl, __nv_bfloat16 *dw, cudaStream_t s);
+
+// The sums of HEAD_STATS for at most HEAD_FEW bf16 tokens a head (head_few.cu): one entry of part a CTA, `few` CTAs a head.
+int launch_head_few(const HeadPlan &h, const HeadGemm &g, const __nv_bfloat16 *z, const __nv_bfloat16 *w, cudaStream_t s);
 
 struct HeadIn {
     const void *z, *w;

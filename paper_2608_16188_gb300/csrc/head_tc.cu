@@ -103,7 +103,7 @@ struct Cursor {
         }
         // this pair's part of a tile that is left, once
         const int c = (int)(blockIdx.x >> 1);
-        const DzShares s(left, g.pairs, (g.vn + BK - 1) / BK);
+        const DzShares s(left, g.pairs, (g.vn + BK - 1) / BK, dz_least(g.parts));
         if (u == 0x7fffffff || left == 0 || c >= left * s.cuts) return false;
         u = 0x7fffffff;
         if (!seek(g, full + c % left, x)) return false;

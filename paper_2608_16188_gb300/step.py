@@ -3,8 +3,9 @@
 Plumbing only: torch allocates the caller-owned device buffers the C ABI writes
 into, and ``StepRunner`` issues the seven library calls of one step in order on
 one stream -- eight with the router backward (``router_grad=True``), which adds
-the gradient of the gating network, ten with the balance losses.  No arithmetic of
-the method happens here.
+the gradient of the gating network, ten with the balance losses.  With ``gating``
+the experts are chosen by vmoe_gate instead of vmoe_route.  No arithmetic of the
+method happens here.
 """
 from __future__ import annotations
 
@@ -14,8 +15,8 @@ import torch
 
 from . import (VMOE_BF16, VMOE_DLOGITS_ADD, VmoeProblem, _stream, vmoe_balance, vmoe_balance_bwd,
                vmoe_balance_workspace_size, vmoe_combine, vmoe_dispatch, vmoe_expert_bwd,
-               vmoe_expert_bwd_workspace_size, vmoe_expert_fwd, vmoe_problem_capacity, vmoe_route,
-               vmoe_router_bwd)
+               vmoe_expert_bwd_workspace_size, vmoe_expert_fwd, vmoe_gate, vmoe_gate_bias, vmoe_gate_bwd,
+               vmoe_gate_workspace_size, vmoe_problem_capacity, vmoe_route, vmoe_router_bwd)
 
 
 class Buffers:
@@ -75,6 +76,27 @@ class BalanceBuffers:
         self.dloss = weights
 
 
+class GateBuffers:
+    """What choosing experts by vmoe_gate needs beside a step's buffers, for problem ``p``.
+
+    ``config``: gating(...).  ``select_bias``: a contiguous [T, E] fp32 device tensor, kept, not
+    copied; zeros if none is given.  ``demand`` has every expert's choices of the last forward, and
+    ``update(rate)`` moves the bias towards an even demand."""
+
+    def __init__(self, p, config, select_bias=None, device="cuda"):
+        if select_bias is None:
+            select_bias = torch.zeros((p.T, p.E), device=device)
+        if tuple(select_bias.shape) != (p.T, p.E) or select_bias.dtype != torch.float32 or not select_bias.is_contiguous():
+            raise ValueError("a selection bias: a contiguous [T, E] in fp32")
+        self.p, self.config, self.select_bias = p, config, select_bias
+        self.demand = torch.empty((p.T, p.E), dtype=torch.int32, device=device)
+        self.workspace = torch.empty(vmoe_gate_workspace_size(p), dtype=torch.uint8, device=device)
+
+    def update(self, rate, stream=None):
+        """Adds ``rate`` to the bias of experts below their task's mean demand, takes it from those above."""
+        vmoe_gate_bias(self.p, self.demand, rate, self.select_bias, stream)
+
+
 def _nothing_to_add_to(p, balance):
     """Whether the router's gradient would be added to what an earlier step has left."""
     return balance is None and bool(p.flags & VMOE_DLOGITS_ADD)
@@ -91,15 +113,21 @@ class StepRunner:
     gradient is that of <dY, y> plus the weighted losses; ``inputs`` may then hold
     token_mask [T,N] uint8, 0 for padding that they leave out.  A problem with
     VMOE_DLOGITS_ADD and no ``balance`` adds to what the caller writes into
-    ``b.dlogits`` before each backward.
+    ``b.dlogits`` before each backward.  With ``gating`` (a VmoeGating, or
+    GateBuffers with a bias of the caller's) the experts are chosen by vmoe_gate, in
+    ``self.gating``; a token whose token_mask is 0 then goes nowhere and takes no
+    capacity.
     """
 
-    def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False, balance=None):
+    def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False, balance=None, gating=None):
         self.p = p
         self.inp = inputs
         self.router_grad = router_grad
         self.b = bufs if bufs is not None else Buffers(p, inputs["x"].device)
         self.balance = balance
+        self.gating = gating
+        if gating is not None and not isinstance(gating, GateBuffers):
+            self.gating = GateBuffers(p, gating, device=inputs["x"].device)
         if balance is not None:
             if not router_grad:
                 raise ValueError("the balance losses act on the router: router_grad=True")
@@ -110,8 +138,13 @@ class StepRunner:
 
     def forward(self, stream=None):
         p, i, b, stream = self.p, self.inp, self.b, _stream(stream)
-        vmoe_route(p, i["x"], i["w_router"], i.get("bias"), b.logits, b.idx, b.gate, b.slot,
-                   b.load, stream)
+        if self.gating is None:
+            vmoe_route(p, i["x"], i["w_router"], i.get("bias"), b.logits, b.idx, b.gate, b.slot,
+                       b.load, stream)
+        else:
+            o = self.gating
+            vmoe_gate(p, o.config, i["x"], i["w_router"], i.get("bias"), o.select_bias, i.get("token_mask"), b.logits,
+                      b.idx, b.gate, b.slot, b.load, o.demand, o.workspace, stream=stream)
         if self.balance is not None:
             o = self.balance
             vmoe_balance(p, b.logits, b.idx, i.get("token_mask"), o.count, o.tokens, o.excess, o.loss, o.workspace,
@@ -135,8 +168,12 @@ class StepRunner:
             o, p = self.balance, self.p_add
             vmoe_balance_bwd(p, b.logits, i.get("token_mask"), o.count, o.tokens, o.excess, o.dloss, b.dlogits,
                              stream=stream)
-        vmoe_router_bwd(p, i["x"], i["w_router"], b.logits, b.idx, b.gate, b.slot, i["dy"], b.ye,
-                        b.dgate, b.dlogits, b.dw_router, b.dbias, b.dx, stream)
+        if self.gating is None:
+            vmoe_router_bwd(p, i["x"], i["w_router"], b.logits, b.idx, b.gate, b.slot, i["dy"], b.ye,
+                            b.dgate, b.dlogits, b.dw_router, b.dbias, b.dx, stream)
+        else:
+            vmoe_gate_bwd(p, self.gating.config, i["x"], i["w_router"], b.logits, b.idx, b.gate, b.slot, i["dy"], b.ye,
+                          b.dgate, b.dlogits, b.dw_router, b.dbias, b.dx, b.dx, stream)
 
     def step(self, stream=None):
         stream = _stream(stream)
@@ -156,16 +193,21 @@ class HostPipeline:
     may hold token_mask, for steps that bring none of their own.
     With ``balance`` (see StepRunner) a step's losses and counts are read back too if
     its outputs ask for them; the BalanceBuffers hold those of the last step alone.
+    With ``gating`` (see StepRunner) the experts are chosen by vmoe_gate, all steps with
+    one bias.
     """
 
     def __init__(self, p, weights, bufs: Buffers | None = None, device="cuda",
-                 router_grad: bool = False, balance=None):
+                 router_grad: bool = False, balance=None, gating=None):
         if _nothing_to_add_to(p, balance):
             raise ValueError("VMOE_DLOGITS_ADD without balance: no step writes the gradients that it adds to")
         self.p = p
         base = bufs if bufs is not None else Buffers(p, device)
         if balance is not None and not isinstance(balance, BalanceBuffers):
             balance = BalanceBuffers(p, balance, device)
+        if gating is not None and not isinstance(gating, GateBuffers):
+            gating = GateBuffers(p, gating, device=device)
+        self.gating = gating
         self.slots = []
         for _ in range(2):
             b = copy.copy(base)
@@ -174,10 +216,11 @@ class HostPipeline:
             inp = dict(weights)
             inp["x"] = torch.empty_like(base.y)
             inp["dy"] = torch.empty_like(base.y)
-            self.slots.append(StepRunner(p, inp, b, router_grad=router_grad, balance=balance))
+            self.slots.append(StepRunner(p, inp, b, router_grad=router_grad, balance=balance, gating=gating))
         self.mask = weights.get("token_mask")
-        if balance is not None:  # each slot's: a step's mask, and its losses and counts until they are read back
+        if balance is not None or gating is not None:  # each slot's: a step's mask
             self.masks = [torch.empty((p.T, p.N), dtype=torch.uint8, device=device) for _ in range(2)]
+        if balance is not None:  # and its losses and counts until they are read back
             self.found = [(torch.empty_like(balance.loss), torch.empty_like(balance.count)) for _ in range(2)]
         self.copy_stream = torch.cuda.Stream(device)
         ev = lambda: [torch.cuda.Event() for _ in range(2)]  # noqa: E731
@@ -198,7 +241,7 @@ class HostPipeline:
         shape = (self.p.T, self.p.N)
         for i, o in zip(inputs, outputs):
             mask = i[2] if len(i) > 2 else None
-            if not have and (mask is not None or any(t is not None for t in o[2:])):
+            if not have and ((mask is not None and self.gating is None) or any(t is not None for t in o[2:])):
                 raise ValueError("token masks, losses and counts belong to the balance losses: give balance")
             if mask is not None and (tuple(mask.shape) != shape or mask.dtype != torch.uint8):
                 raise ValueError("a step's token mask: [T, N] in uint8")
@@ -210,7 +253,8 @@ class HostPipeline:
 
         With balance losses inputs[i] may have a third entry, the step's token_mask
         [T,N] uint8 (None: the one in ``weights``, if any), and outputs[i] a third
-        and a fourth, its losses [T,3] fp32 and counts [T,E] int32 (either None)."""
+        and a fourth, its losses [T,3] fp32 and counts [T,E] int32 (either None).  With
+        gating inputs[i] may have the token_mask too."""
         cs = stream if stream is not None else torch.cuda.current_stream()
         steps = len(inputs)
         if steps == 0:

@@ -124,7 +124,7 @@ def _check(o, z, w, s, tau, dtype):
 
 # (T, N, V, d): one token, one entry, ends inside and at a tile, odd sizes, widths from 8 on, more row tiles than a group
 SIZES = [(1, 1, 1, 8), (1, 1, 1000, 384), (2, 3, 2, 64), (1, 256, 256, 64), (3, 257, 255, 72), (1, 197, 1000, 384),
-         (2, 300, 2057, 200), (17, 20, 300, 128), (1, 700, 129, 768)]
+         (2, 300, 2057, 200), (17, 20, 300, 128), (1, 700, 129, 768), (3, 16, 700, 72), (2, 17, 131, 64)]
 MODES = {"ce": (True, 0, 1.0), "kd": (False, 9, 2.0), "both": (True, 33, 4.0), "both_tau1": (True, 5, 1.0), "kd_cold": (False, 128, 0.5)}
 
 

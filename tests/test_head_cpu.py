@@ -72,3 +72,18 @@ def test_binding_refuses_other_tensors():
         with pytest.raises(vm.VmoeError) as e:
             vm.vmoe_head_loss(p, head, z, P, P, None, None, P, P, None, None, None, P, 1 << 40)
         assert e.value.status == INVALID
+
+
+def test_head_and_gate_buffers_refuse_what_does_not_fit():
+    p = _p()
+    w = torch.zeros(2, 100, 64, dtype=torch.bfloat16)
+    for kw in (dict(labels=False), dict(w=torch.zeros(100, dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            vm.Head(p, **dict(dict(w=w, device="cpu"), **kw))
+    head = vm.Head(p, w, device="cpu")
+    with pytest.raises(RuntimeError):
+        head.backward(torch.zeros(2, 64))
+    assert not head.shared and vm.Head(p, w[0], device="cpu", train=False).parameters() == []
+    for bias in (torch.zeros(2, 7), torch.zeros(2, 8, dtype=torch.float64), torch.zeros(8, 2).t()):
+        with pytest.raises(ValueError):
+            vm.GateBuffers(vm.problem(2, 64, 64, 8, 8, 2, 1.0), vm.gating(), bias, device="cpu")
