@@ -21,9 +21,12 @@
  *                  dW1 = Xe^T dH, dW2 = A^T dYe
  *   vmoe_combine   dX  = sum_j dXe[e_j, s_j]
  *   vmoe_router_bwd dgate, dlogits, dW_r, dbias; dX += dlogits W_r^T
+ * vmoe_gate and vmoe_gate_bwd stand in the places of vmoe_route and vmoe_router_bwd for
+ * routers with scores, groups of experts and a bias for balance (vmoe_gate_bias).
  * Around it, in training: vmoe_balance and vmoe_balance_bwd (the routers' balance
  * losses), vmoe_block_norm and vmoe_block_norm_bwd (a block's norms, gate and
- * residual), vmoe_adamw (the update).
+ * residual), vmoe_head_loss and vmoe_head_loss_bwd (a head over a vocabulary, cross
+ * entropy and distillation), vmoe_adamw (the update).
  *
  * Conventions for every entry point:
  *  - Ownership: every array argument is caller-owned DEVICE memory (except
@@ -47,7 +50,8 @@
  *    calls share one device array (see there).
  *  - Dtypes: x, dY, weights and all activations use p->dtype (fp32 or bf16);
  *    W_r, bias, logits and gates are always fp32.  bf16 contractions
- *    accumulate in fp32 on the tcgen05 tensor cores; fp32 runs on CUDA cores.
+ *    accumulate in fp32 on the tcgen05 tensor cores; fp32 runs on CUDA cores, but for
+ *    the head's products (three bf16 parts of each value).
  *
  * Shapes (t < T tasks, n < N tokens per task, e < E experts per task,
  * j < k choices, s < C capacity slots, g = t*E + e):
