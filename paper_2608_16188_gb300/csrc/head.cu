@@ -855,11 +855,13 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             g.pairs = pairs;
             g.map = map;
             g.N = h.N;
+            g.overlap = dw != nullptr && pdl_enabled();
             if ((st = launch_head_gemm(HEAD_DZ, h, g, zp, wp, dl, nullptr, s)) != VMOE_OK) return st;
             g.pairs = 0;
         }
         if (dw) {
             g.out = (float *)dw;
+            g.overlap = dz != nullptr && pdl_enabled();
             if ((st = launch_head_gemm(HEAD_DW, h, g, zp, wp, dl, (__nv_bfloat16 *)dw, s)) != VMOE_OK) return st;
         }
     }

@@ -37,6 +37,7 @@ struct HeadGemm {
     int v0, vn;                   // the piece: first column, columns
     int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows
     int pairs, first;             // HEAD_DZ: SM pairs; whether this is the first piece
+    int overlap;                  // HEAD_DZ: HEAD_DW follows and may run beside it; HEAD_DW: behind such a one
     float c1, c2;
     const int *label;             // [T][Np] of compact rows, -1: none
     float2 *part;                 // HEAD_STATS out: [T][2 tiles_n][Np] largest logit times c1, sum

@@ -65,7 +65,7 @@ struct Cursor {
     __device__ Cursor(const HeadGemm &g, int first, int stride) : u(first), step(stride) {
         if (MODE != HEAD_DZ || !g.dz) return;
         int tiles = 0;
-        for (int i = 0; i < g.T; ++i) tiles += (__ldg(g.rows + i) + HB - 1) / HB * g.tiles_n;
+        for (int i = 0; i < g.T; ++i) tiles += (__ldcg(g.rows + i) + HB - 1) / HB * g.tiles_n;
         left = tiles % g.pairs;
         full = tiles - left;
     }
@@ -73,7 +73,7 @@ struct Cursor {
         while (at - base >= cnt) {
             base += cnt;
             if (++t >= g.T) return false;
-            rows = __ldg(g.rows + t);
+            rows = __ldcg(g.rows + t);  // not the read-only path: see `overlap`
             cnt = MODE == HEAD_DW ? g.tiles_m * g.tiles_n : (rows + HB - 1) / HB * g.tiles_n;
         }
         int local = at - base;
@@ -208,7 +208,16 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     tc_fence_before();
     cluster_sync_all();  // barriers initialised and TMEM allocated in both CTAs
     tc_fence_after();
-    pdl_wait();
+    if (MODE == HEAD_DW && args.overlap) {
+        // HEAD_DZ ahead may still run: it writes nothing that is read here and reads nothing that is written, and whatever
+        // came before it had completed when it let this kernel start.  That is made visible as in wait_for_predecessor
+        // (gemm_tc.cuh); its completion is waited for at the end, for whoever waits for this kernel.
+        __threadfence();
+        asm volatile("fence.proxy.async;" ::: "memory");
+    } else {
+        pdl_wait();
+        if (MODE == HEAD_DZ && args.overlap) pdl_launch_dependents();
+    }
     const uint32_t tmem_base = (uint32_t)misc[0];
     const int cid = blockIdx.x >> 1, ncl = gridDim.x >> 1;
     auto give_up = [&]() {
@@ -260,7 +269,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     }
                 }
             }
-            pdl_launch_dependents();
+            if (MODE != HEAD_DZ || !args.overlap) pdl_launch_dependents();
             if (*abort_flag && leader) {  // copies in flight (both CTAs') land before the pair exits
                 const unsigned long long t0 = global_ns();
                 for (int s = 0; s < STAGES && s < issued; ++s)
@@ -523,6 +532,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         give_up();
     }
 
+    if (MODE == HEAD_DW && args.overlap) pdl_wait();
     tc_fence_before();
     cluster_sync_all();  // no MMA, copy or remote arrive of either CTA is still in flight
     tc_fence_after();
