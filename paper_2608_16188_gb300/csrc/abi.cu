@@ -439,7 +439,11 @@ int vmoe_gate_bwd(const vmoe_problem *p, const vmoe_gating *gating, const void *
         !opt_ok(dx) || (dx_in != nullptr) != (dx != nullptr) || (dx ? !dev_ok(w_router) : !opt_ok(w_router)))
         return VMOE_ERR_INVALID;
     cudaStream_t s = (cudaStream_t)cuda_stream;
-    if ((st = launch_gate_grad(d, g, logits, expert_idx, gate, slot, dy, ye, dgate, dlogits, s)) != VMOE_OK) return st;
+    st = launch_gate_grad_dx(d, g, w_router, logits, expert_idx, gate, slot, dy, ye, dgate, dlogits, dx_in, dx, s);
+    if (st == VMOE_OK) dx = nullptr;  // done
+    else if (st == VMOE_ERR_UNSUPPORTED)
+        st = launch_gate_grad(d, g, logits, expert_idx, gate, slot, dy, ye, dgate, dlogits, s);
+    if (st != VMOE_OK) return st;
     return launch_router_grads(d, x, w_router, dlogits, dw_router, dbias, dx_in, dx, s);
 }
 
@@ -458,7 +462,7 @@ static int check_head(const vmoe_problem *p, const vmoe_head *h, Dims *d) {
     if (!h || h->V < 1 || h->teacher_k < 0 || !(h->temperature > 0.0f) || !isfinite(h->temperature) ||
         !isfinite(1.0f / h->temperature) || (h->flags & ~(uint32_t)VMOE_HEAD_SHARED))
         return VMOE_ERR_INVALID;
-    if (h->teacher_k > HEAD_K || (h->teacher_k > 0 && h->V > HEAD_V) || (long long)d->T * d->N >= (1LL << 31) - HEAD_TILE) return VMOE_ERR_UNSUPPORTED;
+    if (h->V > (1 << 30) || h->teacher_k > HEAD_K || (h->teacher_k > 0 && h->V > HEAD_V) || (long long)d->T * d->N >= (1LL << 31) - HEAD_TILE) return VMOE_ERR_UNSUPPORTED;
     const long long tiles = ((long long)d->T * d->N / HEAD_TILE + d->T) * (h->V / HEAD_TILE + 1LL);
     if (tiles >= (1LL << 26) || (long long)d->T * (h->V / HEAD_TILE + 1LL) * (d->d / HEAD_TILE + 1LL) >= (1LL << 30))
         return VMOE_ERR_UNSUPPORTED;

@@ -26,9 +26,9 @@ namespace {
 constexpr int GT_THREADS = 256, GT_WARPS = GT_THREADS / 32;
 constexpr unsigned FULL = 0xffffffffu;
 
-// The largest c is within this of another: the two may be in either order.  s: expf and the division are off by
-// 2^-21 of it in all, the sum of a softmax's row by as much; c: its rounding.
-__device__ __forceinline__ float near_of(float s, float c) { return 2e-6f * s + 1.3e-7f * fabsf(c); }
+// The largest c is within this of another: the two may be in either order.  s: expf, the sum and the division are off by
+// 1e-6 of it in all, x - max's rounding by 6e-8 |x - max|, at most 87 of them before s is 0; c: its rounding.
+__device__ __forceinline__ float near_of(float s, float c) { return 8e-6f * s + 1.3e-7f * fabsf(c); }
 
 // c in 64 bits; softmax: top the row's largest logit, inv 1 / its sum
 __device__ __noinline__ double exact_value(float x, float b, int softmax, double top, double inv) {
@@ -386,8 +386,8 @@ __device__ __forceinline__ unsigned sort_lane(float (&h)[V]) {
 // with two of the first k + 1 values, or an open and a shut group, closer than their error (or equal) is done again by
 // choose_row behind the loop:
 //   sigmoid: the exponential is off by 2^-22 + |x| 2^-23.5 relative, which e / (1 + e)^2 <= 1 / 4 and |x| e / (1 + e)^2 <=
-//   0.23 take to 8e-8 of 1 in s, the reciprocal and the sum add 1.8e-7 s; softmax: 1e-6 s for |x - max| <= 10, and s
-//   |x - max| 6e-8 <= s 2e-6 up to 30, below which s is nothing beside the bias' rounding; c's rounding 6e-8 |c|.
+//   0.23 take to 8e-8 of 1 in s, the reciprocal and the sum add 1.8e-7 s; softmax: exponential, sum and reciprocal 1e-6 s
+//   and 6e-8 |x - max| s, at most 87 of them before s is 0: 8e-6 s; c's rounding 6e-8 |c|.
 template <int L, int V>
 __global__ void __launch_bounds__(GT_THREADS, 4)
 gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, const float *__restrict__ sbias,
@@ -452,7 +452,7 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
     };
     int batch = 0;
     load(n0 + warp * RW + sub);
-    const float rel = softmax ? 2e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
+    const float rel = softmax ? 8e-6f : 3e-7f, abs1 = softmax ? 0.0f : 1e-7f;
     for (int base = n0 + warp * RW; base < n1; base += GT_WARPS * RW) {
         const int n = base + sub;
         float c[V], mx = 0.0f, sum = 1.0f, smax = 1.0f;

@@ -17,6 +17,9 @@ int launch_gate(const Dims &p, const Gating &g, const float *logits, const float
                 float *gate, int32_t *slot, int32_t *load, int32_t *demand, int32_t *hist, cudaStream_t s);
 int launch_gate_grad(const Dims &p, const Gating &g, const float *logits, const int32_t *idx, const float *gate,
                      const int32_t *slot, const void *dy, const void *ye, float *dgate, float *dlogits, cudaStream_t s);
+int launch_gate_grad_dx(const Dims &p, const Gating &g, const float *wr, const float *logits, const int32_t *idx,
+                        const float *gate, const int32_t *slot, const void *dy, const void *ye, float *dgate, float *dlogits,
+                        const void *dx_in, void *dx, cudaStream_t s);
 int launch_gate_bias(const Dims &p, const int32_t *demand, float rate, float *bias, cudaStream_t s);
 
 // The router's logits alone.

@@ -23,7 +23,7 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
-constexpr int HG_THREADS = 256, HP_TOKENS = 64, HP_SELF = 8192;
+constexpr int HG_THREADS = 256, HP_TOKENS = 64, HP_SELF = 8192, HF_DOTS = 16384;
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -377,7 +377,8 @@ struct Finish {
     const int *rows, *map, *label;
     const float2 *part, *part2;
     const float *picked, *tl;
-    const __nv_bfloat16 *few_z, *few_w;  // few tokens: the entries' logits are formed here
+    const void *dot_z, *dot_w;  // few entries: their logits are formed here, from the tokens and weights
+    bool bf16;
     const int32_t *tidx;
     const float *tlogit;
     float *ce, *lse, *kl, *tlse, *logp;
@@ -387,21 +388,25 @@ __device__ __forceinline__ void join(float &m, float &s, float2 v) {
     s = s * exp2f(m - top) + v.y * exp2f(v.x - top);
     m = top;
 }
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *o) { bf16x8_to_f32(__ldg(reinterpret_cast<const uint4 *>(p)), o); }
+
 // Lane l: the logit of entry i of lane l, for the first `n` lanes; -1 gives 0.  Four entries' rows at a time.
-__device__ float entries_logits(const Sizes &z, const __nv_bfloat16 *zr, const __nv_bfloat16 *w, int i, int n) {
+template <typename T>
+__device__ __noinline__ float entries_logits(int d, const T *zr, const T *w, int i, int n) {
     const int lane = threadIdx.x & 31;
     float mine = 0.0f;
     for (int j = 0; j < min(n, 32); j += 4) {
         float acc[4] = {};
-        const __nv_bfloat16 *row[4];
+        const T *row[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) row[e] = w + (long long)max(0, __shfl_sync(FULL, i, j + e)) * z.d;
-        for (int c = lane * 8; c < z.d; c += 256) {
+        for (int e = 0; e < 4; ++e) row[e] = w + (long long)max(0, __shfl_sync(FULL, i, j + e)) * d;
+#pragma unroll 2
+        for (int c = lane * 8; c < d; c += 256) {
             float a[8], b[8];
-            bf16x8_to_f32(*reinterpret_cast<const uint4 *>(zr + c), a);
+            load8(zr + c, a);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                bf16x8_to_f32(__ldg(reinterpret_cast<const uint4 *>(row[e] + c)), b);
+                load8(row[e] + c, b);
 #pragma unroll
                 for (int x = 0; x < 8; ++x) acc[e] = fmaf(a[x], b[x], acc[e]);
             }
@@ -470,8 +475,11 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
         for (int mm = 0; mm < Teacher::M; ++mm) {
             if (32 * mm >= z.K) break;
             const int j = lane + 32 * mm;
-            const float l = f.few_z ? entries_logits(z, f.few_z + at * z.d, f.few_w + (long long)t * z.V * z.d, q.i[mm], z.K - 32 * mm)
-                            : j < z.K && q.i[mm] >= 0 ? f.tl[at * z.K + j] : 0.0f;
+            const long long head = (long long)t * z.V * z.d;
+            float l;
+            if (!f.dot_z) l = j < z.K && q.i[mm] >= 0 ? f.tl[at * z.K + j] : 0.0f;
+            else if (f.bf16) l = entries_logits(z.d, (const __nv_bfloat16 *)f.dot_z + tn * z.d, (const __nv_bfloat16 *)f.dot_w + head, q.i[mm], z.K - 32 * mm);
+            else l = entries_logits(z.d, (const float *)f.dot_z + tn * z.d, (const float *)f.dot_w + head, q.i[mm], z.K - 32 * mm);
             if (j >= z.K) continue;
             const float lp = q.i[mm] >= 0 ? l * f.inv_tau - tl[i] : 0.0f;
             f.logp[tn * z.K + j] = lp;
@@ -735,7 +743,9 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     g.stats = h.stats;
     g.rows = at<int>(ws, h.rows);
     g.vn = h.V;
-    if (in.tidx && !h.few) {
+    // few entries: a dot product each in head_finish, instead of a launch for their list
+    const bool dots = in.tidx && (h.few || (long long)h.T * h.N * h.K <= HF_DOTS);
+    if (in.tidx && !dots) {
         int *off = at<int>(ws, h.off);
         unsigned *list = at<unsigned>(ws, h.list);
         g.off = off;
@@ -768,8 +778,9 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     f.part2 = g.part2;
     f.picked = g.picked;
     f.tl = g.tl;
-    f.few_z = h.few ? zp : nullptr;
-    f.few_w = wp;
+    f.dot_z = dots ? in.z : nullptr;
+    f.dot_w = in.w;
+    f.bf16 = p.bf16;
     f.tidx = in.tidx;
     f.tlogit = in.tlogit;
     f.ce = ce;

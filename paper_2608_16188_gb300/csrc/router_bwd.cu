@@ -220,6 +220,41 @@ __device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, bool 
     return true;
 }
 
+// gate_backward for choices of vmoe_gate (gate.cu has the formulas) but for a softmax's unrenormalised gates, whose rows
+// are dense: choices may be missing (e_j = -1).
+template <int KMAX>
+__device__ __forceinline__ bool gate_backward_scored(const Gating &g, int k, int E, int lane, long long tn, float (&dg)[KMAX],
+                                                     const float (&gt)[KMAX], const int (&ei)[KMAX], const float *logits,
+                                                     float *dgate, float *dlogits, float (&c)[KMAX]) {
+    float m = 0.0f, mine = 0.0f;
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j) {
+        c[j] = 0.0f;
+        if (j >= k) continue;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) dg[j] += __shfl_xor_sync(0xffffffffu, dg[j], o);
+        if (j == lane) mine = dg[j];
+        if (ei[j] >= 0) m = fmaf(gt[j] / g.scale, dg[j], m);
+    }
+    if (lane < k) dgate[tn * k + lane] = mine;
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < KMAX; ++j) {
+        if (j >= k || ei[j] < 0) continue;
+        c[j] = gt[j] * (g.renorm ? dg[j] - m : dg[j]);
+        if (g.score == VMOE_SCORE_SIGMOID) c[j] *= 1.0f / (1.0f + expf(__ldg(logits + tn * E + ei[j])));
+        any |= c[j] != 0.0f;
+    }
+    for (int e = lane; e < E; e += 32) {
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < KMAX; ++j)
+            if (ei[j] == e) v = c[j];
+        dlogits[tn * E + e] = v;
+    }
+    return any;
+}
+
 // dx_terms: r[0..7] = sum over the dX terms of dlogit_e * W_r[v + q][e] for the
 // 8 columns v..v+7: the k chosen experts (renormalised gates) or all E.
 template <int KMAX, bool WSMEM>
@@ -342,18 +377,19 @@ router_grad_kernel(Dims p, const T *__restrict__ dy, const T *__restrict__ ye,
 // registers a thread, so every load of a token -- the dY row, its k expert-output
 // rows and its dX row -- is in flight at once (one memory round trip per token),
 // and the next token's routing is fetched while this one is reduced.
-template <int NCH, int KMAX, bool WSMEM>
+// SCORED: for vmoe_gate_bwd, whose dX may come from another array.
+template <int NCH, int KMAX, bool WSMEM, bool SCORED = false>
 __global__ void __launch_bounds__(RG_THREADS, 1)
 router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
                         const __nv_bfloat16 *__restrict__ ye, const float *__restrict__ logits,
                         const int32_t *__restrict__ idx, const float *__restrict__ gate,
                         const int32_t *__restrict__ slot, const float *__restrict__ wr,
                         float *__restrict__ dgate, float *__restrict__ dlogits,
-                        __nv_bfloat16 *dx) {
+                        __nv_bfloat16 *dx, const __nv_bfloat16 *dx_in, Gating sg) {
     extern __shared__ __align__(16) float rg_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int d = p.d, E = p.E, k = p.k, N = p.N;
-    const bool norenorm = (p.flags & VMOE_NO_RENORM) != 0, add = (p.flags & VMOE_DLOGITS_ADD) != 0;
+    const bool norenorm = !SCORED && (p.flags & VMOE_NO_RENORM) != 0, add = (p.flags & VMOE_DLOGITS_ADD) != 0;
     const int dp = wt_pitch(d);
     float *dlrow = rg_smem + warp * E;
     float *WT = rg_smem + (norenorm ? RG_WARPS * E : 0);
@@ -405,7 +441,7 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
 #pragma unroll
                 for (int ch = 0; ch < NCH; ++ch) {
                     const int v = lane * 8 + 256 * ch;
-                    if (v < d) xo[ch] = *reinterpret_cast<const uint4 *>(dx + tn * d + v);
+                    if (v < d) xo[ch] = *reinterpret_cast<const uint4 *>((SCORED ? dx_in : dx) + tn * d + v);
                 }
             }
             // the next token's routing
@@ -439,8 +475,14 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
                 }
             }
             float c[KMAX];
-            const bool any = gate_backward<KMAX>(k, E, norenorm, add, lane, tn, dg, gt, ei, logits,
-                                                 dgate, dlogits, dlrow, c);
+            bool any;
+            if constexpr (SCORED) {
+                any = gate_backward_scored<KMAX>(sg, k, E, lane, tn, dg, gt, ei, logits, dgate, dlogits, c) || dx != dx_in;
+#pragma unroll
+                for (int j = 0; j < KMAX; ++j) ei[j] = max(ei[j], 0);
+            } else {
+                any = gate_backward<KMAX>(k, E, norenorm, add, lane, tn, dg, gt, ei, logits, dgate, dlogits, dlrow, c);
+            }
             if (dx != nullptr && any) {
                 const int ne = norenorm ? E : k;
 #pragma unroll
@@ -1086,12 +1128,12 @@ int launch_grad(const Dims &p, const float *wr, const float *logits, const int32
     return launch_result();
 }
 
-template <int NCH, int KMAX, bool WSMEM>
+template <int NCH, int KMAX, bool WSMEM, bool SCORED = false>
 int launch_grad_fast(const Dims &p, const float *wr, const float *logits, const int32_t *idx,
                      const float *gate, const int32_t *slot, const __nv_bfloat16 *dy,
                      const __nv_bfloat16 *ye, float *dgate, float *dlogits, __nv_bfloat16 *dx,
-                     size_t smem, cudaStream_t s) {
-    auto kern = router_grad_fast_kernel<NCH, KMAX, WSMEM>;
+                     size_t smem, cudaStream_t s, const __nv_bfloat16 *dx_in = nullptr, const Gating &sg = Gating()) {
+    auto kern = router_grad_fast_kernel<NCH, KMAX, WSMEM, SCORED>;
     static std::atomic<int> smem_limit[64];
     static std::atomic<uint64_t> occupancy[64];  // per device: (smem << 32) | CTAs per SM
     int dev = 0;
@@ -1111,7 +1153,7 @@ int launch_grad_fast(const Dims &p, const float *wr, const float *logits, const 
     long long grid = (long long)per_sm * num_sms();
     grid = std::min(grid, (tokens + RG_WARPS - 1) / RG_WARPS);
     kern<<<(unsigned)grid, RG_THREADS, smem, s>>>(p, dy, ye, logits, idx, gate, slot, wr, dgate,
-                                                  dlogits, dx);
+                                                  dlogits, dx, dx_in, sg);
     return launch_result();
 }
 
@@ -1200,6 +1242,33 @@ int launch_router_bwd(const Dims &p, const void *x, const float *w_router, const
                                   dw_router, dbias, dx, s);
     return run<float>(p, x, w_router, logits, idx, gate, slot, dy, ye, dgate, dlogits, dw_router,
                       dbias, dx, s);
+}
+
+// dgate, dlogits and dX = dX_in + dlogits W_r^T of vmoe_gate's choices in one launch, where the rows of dlogits hold one or two
+// values; VMOE_ERR_UNSUPPORTED where they do not, or W_r does not fit into shared memory.
+int launch_gate_grad_dx(const Dims &p, const Gating &g, const float *wr, const float *logits, const int32_t *idx,
+                        const float *gate, const int32_t *slot, const void *dy, const void *ye, float *dgate, float *dlogits,
+                        const void *dx_in, void *dx, cudaStream_t s) {
+    const size_t smem = rg_smem_w(p);
+    if (!p.bf16 || p.k > 2 || p.d > 1024 || dx == nullptr || (g.score == VMOE_SCORE_SOFTMAX && !g.renorm) ||
+        (p.flags & VMOE_DLOGITS_ADD) || smem > RG_SMEM_CAP)
+        return VMOE_ERR_UNSUPPORTED;
+    trace_before(s, "gate_grad_dx");
+    auto go = [&](auto nch, auto kmax) {
+        return launch_grad_fast<decltype(nch)::value, decltype(kmax)::value, true, true>(
+            p, wr, logits, idx, gate, slot, (const __nv_bfloat16 *)dy, (const __nv_bfloat16 *)ye, dgate, dlogits,
+            (__nv_bfloat16 *)dx, smem, s, (const __nv_bfloat16 *)dx_in, g);
+    };
+    auto pick = [&](auto nch) {
+        return p.k <= 1 ? go(nch, std::integral_constant<int, 1>()) : go(nch, std::integral_constant<int, 2>());
+    };
+    const int n = (p.d + 255) / 256;
+    const int st = n <= 1   ? pick(std::integral_constant<int, 1>())
+                   : n <= 2 ? pick(std::integral_constant<int, 2>())
+                   : n <= 3 ? pick(std::integral_constant<int, 3>())
+                            : pick(std::integral_constant<int, 4>());
+    trace_after(s);
+    return st;
 }
 
 int launch_router_grads(const Dims &p, const void *x, const float *w_router, const float *dlogits, float *dw_router,

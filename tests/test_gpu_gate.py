@@ -118,7 +118,8 @@ def _bwd(p, cfg, o, x, wr, dy, ye, dx_in, stream=None):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("score,renorm", [("sigmoid", True), ("softmax", True), ("sigmoid", False), ("softmax", False)])
-@pytest.mark.parametrize("shape", [(1, 1, 8, 1, 1), (2, 65, 64, 8, 2), (2, 130, 136, 32, 4), (1, 197, 384, 60, 8), (3, 40, 1032, 31, 2)],
+@pytest.mark.parametrize("shape", [(1, 1, 8, 1, 1), (2, 65, 64, 8, 2), (2, 130, 136, 32, 4), (1, 197, 384, 60, 8), (3, 40, 1032, 31, 2),
+                                   (3, 700, 264, 33, 1), (2, 150, 768, 32, 2), (2, 90, 1024, 64, 2)],
                          ids=str)
 def test_gate_bwd_parity(shape, score, renorm, dtype):
     T, N, d, E, k = shape
