@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "head.cuh"
 
@@ -23,7 +24,7 @@ namespace {
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
-constexpr int HG_THREADS = 256, HP_TOKENS = 64, HP_SELF = 8192, HF_DOTS = 16384;
+constexpr int HG_THREADS = 256, HP_TOKENS = 32, HP_SELF = 2048, HF_DOTS = 16384;
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -378,7 +379,6 @@ struct Finish {
     const float2 *part, *part2;
     const float *picked, *tl;
     const void *dot_z, *dot_w;  // few entries: their logits are formed here, from the tokens and weights
-    bool bf16;
     const int32_t *tidx;
     const float *tlogit;
     float *ce, *lse, *kl, *tlse, *logp;
@@ -392,7 +392,7 @@ __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *o) { bf16x8
 
 // Lane l: the logit of entry i of lane l, for the first `n` lanes; -1 gives 0.  Four entries' rows at a time.
 template <typename T>
-__device__ __noinline__ float entries_logits(int d, const T *zr, const T *w, int i, int n) {
+__device__ __forceinline__ float entries_logits(int d, const T *zr, const T *w, int i, int n) {
     const int lane = threadIdx.x & 31;
     float mine = 0.0f;
     for (int j = 0; j < min(n, 32); j += 4) {
@@ -420,7 +420,8 @@ __device__ __noinline__ float entries_logits(int d, const T *zr, const T *w, int
     return i >= 0 ? mine : 0.0f;
 }
 
-template <int ROWS>
+// DOTS: void, or the type of z and w where the entries' logits are formed here.
+template <int ROWS, typename DOTS>
 __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
     constexpr int SHARES = HG_THREADS / ROWS;  // threads of a row
     __shared__ float2 sm[2][HG_THREADS / 32][ROWS];
@@ -475,11 +476,13 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
         for (int mm = 0; mm < Teacher::M; ++mm) {
             if (32 * mm >= z.K) break;
             const int j = lane + 32 * mm;
-            const long long head = (long long)t * z.V * z.d;
-            float l;
-            if (!f.dot_z) l = j < z.K && q.i[mm] >= 0 ? f.tl[at * z.K + j] : 0.0f;
-            else if (f.bf16) l = entries_logits(z.d, (const __nv_bfloat16 *)f.dot_z + tn * z.d, (const __nv_bfloat16 *)f.dot_w + head, q.i[mm], z.K - 32 * mm);
-            else l = entries_logits(z.d, (const float *)f.dot_z + tn * z.d, (const float *)f.dot_w + head, q.i[mm], z.K - 32 * mm);
+            float l = 0.0f;
+            if constexpr (std::is_void<DOTS>::value) {
+                if (j < z.K && q.i[mm] >= 0) l = f.tl[at * z.K + j];
+            } else {
+                l = entries_logits(z.d, (const DOTS *)f.dot_z + tn * z.d, (const DOTS *)f.dot_w + (long long)t * z.V * z.d, q.i[mm],
+                                   z.K - 32 * mm);
+            }
             if (j >= z.K) continue;
             const float lp = q.i[mm] >= 0 ? l * f.inv_tau - tl[i] : 0.0f;
             f.logp[tn * z.K + j] = lp;
@@ -623,8 +626,9 @@ int prepare(const Dims &p, const HeadPlan &h, const HeadIn &in, void *ws, Pack f
     int st;
     f.tidx = in.tidx;
     f.tlogit = in.tlogit;
-    // few labels and entries: every CTA of head_pack looks through all of its head's, instead of a launch
-    if (h.N > HP_SELF || (in.tidx && (long long)h.N * h.K > 2 * HP_SELF)) {
+    // few labels and entries: every CTA of head_pack looks through all of its head's, instead of a launch (8192 tokens: 24 us
+    // so, 21 with the marks)
+    if (h.N > HP_SELF || (in.tidx && (long long)h.N * h.K > HF_DOTS)) {
         unsigned *mark = at<unsigned>(ws, h.mark);
         f.mark = mark;
         trace_before(s, "head_mark");
@@ -778,9 +782,8 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     f.part2 = g.part2;
     f.picked = g.picked;
     f.tl = g.tl;
-    f.dot_z = dots ? in.z : nullptr;
+    f.dot_z = in.z;
     f.dot_w = in.w;
-    f.bf16 = p.bf16;
     f.tidx = in.tidx;
     f.tlogit = in.tlogit;
     f.ce = ce;
@@ -791,8 +794,10 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     trace_before(s, "head_finish");
     // few rows: more threads each, to hide the chain of their half tiles
     const bool few = (long long)h.T * h.N <= 2048;
-    st = launch_kernel(few ? head_finish_kernel<4> : head_finish_kernel<32>, dim3((h.N + (few ? 3 : 31)) / (few ? 4 : 32), h.T),
-                       dim3(HG_THREADS), 0, s, f);
+    auto kern = !dots    ? (few ? head_finish_kernel<4, void> : head_finish_kernel<32, void>)
+                : p.bf16 ? (few ? head_finish_kernel<4, __nv_bfloat16> : head_finish_kernel<32, __nv_bfloat16>)
+                         : (few ? head_finish_kernel<4, float> : head_finish_kernel<32, float>);
+    st = launch_kernel(kern, dim3((h.N + (few ? 3 : 31)) / (few ? 4 : 32), h.T), dim3(HG_THREADS), 0, s, f);
     trace_after(s);
     return st;
 }
