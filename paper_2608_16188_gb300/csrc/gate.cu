@@ -541,7 +541,9 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
 #pragma unroll
             for (int i = 1; i < V; ++i) m = fmaxf(m, c[i]);
             float left = m, least = INFINITY;
-            for (int j = 0; j < k; ++j) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j == k) break;
                 least = redux_max(left);
                 if (left == least) left = -INFINITY;
             }
@@ -561,18 +563,18 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
                 __syncwarp();
                 const int2 own = mine_of[lane];
                 const float v = lane < found ? __int_as_float(own.x) : -INFINITY;
-                int above = 0;
-                float gap = INFINITY;  // to the nearest one above
-                bool equal = false;
-                for (int q = 0; q < found; ++q) {
-                    const float other = __shfl_sync(FULL, v, q);
-                    above += other > v;
-                    equal |= other == v && q != lane;
-                    if (other > v) gap = fminf(gap, other - v);
-                }
-                // of k + 1 values in a row none may be near the next (which adds 3e-6 of the gap to the error)
+                // of k + 1 values in a row none may be near the next (the larger one's error is the smaller's and 3e-6 of the gap)
                 const float err = by_logit ? 0.0f : 2.00001f * tol(v);
-                open |= lane < found && above <= k && (equal || !(gap > err));
+                int above = 0, near = 0;  // itself among the near ones
+                for (int q = 0; q < found; q += 4) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {  // past the last one: -inf
+                        const float gap = __shfl_sync(FULL, v, q + u) - v;
+                        above += gap > 0.0f;
+                        near += fabsf(gap) <= err;
+                    }
+                }
+                open |= lane < found && above <= k && near > 1;
                 const unsigned at_rank = lane < found && above < k ? 1u << above : 0u;
                 my_e = -1;
                 if (at_rank) mine_of[32 + above].y = own.y;
