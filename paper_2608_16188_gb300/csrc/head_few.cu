@@ -62,7 +62,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
         const __nv_bfloat16 *row[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) row[n] = wt + (long long)min(V - 1, v0 + 8 * n + g) * d + 8 * q;
-        float acc[4][4] = {};
+        float sum[4][4] = {};
         constexpr int U = 4;  // steps of 32 k in flight: 8 KB a warp
         for (int k0 = 0; k0 < d; k0 += 32 * U) {
             uint4 x[U][4];
@@ -73,6 +73,8 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
                     x[u][n] = make_uint4(0, 0, 0, 0);
                     if (k0 + 32 * u + 8 * q < d) x[u][n] = __ldcs(reinterpret_cast<const uint4 *>(row[n] + k0 + 32 * u));
                 }
+            // 128 k at a time: the products cut every step of their sums towards zero (all 1024 in one: ce off by 1.1e-6; so 1e-7)
+            float acc[4][4] = {};
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (k0 + 32 * u >= d) break;
@@ -83,6 +85,10 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
                     mma_bf16_16816(acc[n], a.z, c.z, a.w, c.w, x[u][n].z, x[u][n].w);
                 }
             }
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[n][i] += acc[n][i];
         }
         // columns v0 + 8 n + 2 q, + 1 of tokens g (0, 1) and g + 8 (2, 3)
 #pragma unroll
@@ -91,7 +97,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int col = v0 + 8 * (i >> 1) + 2 * q + (i & 1);
-                l[i] = acc[i >> 1][2 * h + (i & 1)];
+                l[i] = sum[i >> 1][2 * h + (i & 1)];
                 if (col == lab[h]) args.picked[at + 8 * h] = l[i];
                 if (col >= V) l[i] = -INFINITY;
                 top = fmaxf(top, l[i]);
