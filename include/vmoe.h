@@ -444,8 +444,8 @@ typedef struct {
  *   size from vmoe_head_min_workspace_size(p, head) on (else VMOE_ERR_INVALID): the
  *   backward then takes the vocabulary in more pieces.
  * Sums in fp32; fp32 operands are taken as three bf16 parts each, six products of
- * parts (2^-24).  T*N < 2^31 - 256, V <= 2^30 (else VMOE_ERR_UNSUPPORTED).  Of p only T, N,
- * d_model, dtype and the checks matter. */
+ * parts (2^-24).  T*N < 2^31 - 256, V <= 2^30, d_model <= 65536 (else
+ * VMOE_ERR_UNSUPPORTED).  Of p only T, N, d_model, dtype and the checks matter. */
 int vmoe_head_loss(const vmoe_problem *p, const vmoe_head *head, const void *z, const void *w, const int32_t *label,
                    const int32_t *teacher_idx, const float *teacher_logit, float *ce, float *lse, float *kl, float *tlse,
                    float *logp, void *workspace, size_t workspace_bytes, void *cuda_stream);

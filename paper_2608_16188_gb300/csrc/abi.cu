@@ -462,7 +462,10 @@ static int check_head(const vmoe_problem *p, const vmoe_head *h, Dims *d) {
     if (!h || h->V < 1 || h->teacher_k < 0 || !(h->temperature > 0.0f) || !isfinite(h->temperature) ||
         !isfinite(1.0f / h->temperature) || (h->flags & ~(uint32_t)VMOE_HEAD_SHARED))
         return VMOE_ERR_INVALID;
-    if (h->V > (1 << 30) || h->teacher_k > HEAD_K || (h->teacher_k > 0 && h->V > HEAD_V) || (long long)d->T * d->N >= (1LL << 31) - HEAD_TILE) return VMOE_ERR_UNSUPPORTED;
+    // offsets within a CTA's tokens (32 rows of d, of several tasks with a shared head) and token numbers are 32 bits
+    if (d->d > (1 << 16) || h->V > (1 << 30) || h->teacher_k > HEAD_K || (h->teacher_k > 0 && h->V > HEAD_V) ||
+        (long long)d->T * d->N >= (1LL << 31) - HEAD_TILE)
+        return VMOE_ERR_UNSUPPORTED;
     const long long tiles = ((long long)d->T * d->N / HEAD_TILE + d->T) * (h->V / HEAD_TILE + 1LL);
     if (tiles >= (1LL << 26) || (long long)d->T * (h->V / HEAD_TILE + 1LL) * (d->d / HEAD_TILE + 1LL) >= (1LL << 30))
         return VMOE_ERR_UNSUPPORTED;

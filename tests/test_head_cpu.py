@@ -43,6 +43,7 @@ def test_head_refusals():
                   vm.VmoeHead(100, 8, 1.0, 2)):
             assert call(h) == INVALID
         assert call(vm.head_config(100, 129)) == UNSUPPORTED and call(vm.head_config((1 << 20) + 1, 8)) == UNSUPPORTED
+        assert call(p=_p(d=65544)) == UNSUPPORTED and call(vm.head_config((1 << 30) + 1)) == UNSUPPORTED
         assert call(vm.head_config(100)) == INVALID  # a teacher's arrays without a teacher
         assert call(p=_p(T=1, N=(1 << 25), d=8), h=vm.head_config(1 << 30, 8)) == UNSUPPORTED
         least = vm.vmoe_head_min_workspace_size(_p(), head)
