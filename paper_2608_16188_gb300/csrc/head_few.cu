@@ -102,7 +102,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
                 if (col >= V) l[i] = -INFINITY;
                 top = fmaxf(top, l[i]);
             }
-            if (top == -INFINITY) continue;  // past the vocabulary's end
+            if (v0 + 2 * q >= V) continue;  // past the vocabulary's end; NaNs alone leave no top, but a sum
             auto add = [&](Sum &s, float c) {
                 const float m = fmaxf(s.m, top * c);
                 float v = s.s * ex2(s.m - m);

@@ -431,14 +431,15 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 #pragma unroll
                     for (int i = 1; i < 32; ++i) m[j] = fmaxf(m[j], v[4 * i + j]);
                 }
-                const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = top * args.c1;
+                // finite where every logit here is -inf (their sum is then 0) or NaN
+                const float top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), ref = fmaxf(top * args.c1, -3e38f);
                 float s[4] = {};
 #pragma unroll
                 for (int i = 0; i < 128; ++i) s[i & 3] += ex2(fmaf(v[i], args.c1, -ref));
                 const long long o = ((long long)x.t * 2 * args.tiles_n + 2 * x.n + half) * args.Np + row;
                 args.part[o] = make_float2(ref, (s[0] + s[1]) + (s[2] + s[3]));
                 if (STATS2) {
-                    const float ref2 = top * args.c2;
+                    const float ref2 = fmaxf(top * args.c2, -3e38f);
                     float s2[4] = {};
 #pragma unroll
                     for (int i = 0; i < 128; ++i) s2[i & 3] += ex2(fmaf(v[i], args.c2, -ref2));

@@ -229,3 +229,49 @@ def test_stream_graph_and_two_at_once():
         torch.cuda.synchronize()
         for n in names:
             assert torch.equal(o[n], want[k][n]) and torch.equal(other[n], want[1 - k][n]), n
+
+
+def _forward(p, head, z, w, s):
+    T, N, K = p.T, p.N, head.teacher_k
+    new = lambda *sh: torch.empty(sh, device="cuda")  # noqa: E731
+    o = dict(ce=new(T, N), lse=new(T, N), kl=new(T, N) if K else None, tlse=new(T, N) if K else None,
+             logp=new(T, N, K) if K else None)
+    ws = torch.full((vm.vmoe_head_workspace_size(p, head),), 255, dtype=torch.uint8, device="cuda")
+    vm.vmoe_head_loss(p, head, z.cuda(), w.cuda(), _dev(s["label"]), _dev(s["tidx"]), _dev(s["tlogit"]), o["ce"], o["lse"], o["kl"],
+                      o["tlse"], o["logp"], ws)
+    return o
+
+
+@pytest.mark.parametrize("tau", (1.0, 2.0))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("N", (5, 40))
+def test_nan_token(N, dtype, tau):
+    """A token of NaN that takes part: its losses are NaN, whichever kernel sums its logits; the others' stay."""
+    p, head, T, V, d, K = vm.problem(2, N, 64, 8, 1, 1, 1.0, dtype), vm.head_config(300, 4, tau), 2, 300, 64, 4
+    z, w, s = _inputs(T, N, V, d, K, dtype, False, True, False, seed=4)
+    z[1, 3] = float("nan")
+    o = _forward(p, head, z, w, s)
+    bad = torch.zeros(T, N, dtype=torch.bool)
+    bad[1, 3] = True
+    for n in ("ce", "lse", "kl", "tlse"):
+        assert torch.equal(torch.isnan(o[n]).cpu(), bad), n
+
+
+@pytest.mark.parametrize("N", (5, 40))
+def test_entries_out_of_reach(N):
+    """Weights of -inf against tokens of positive values: logits of -inf, whole half tiles of them, add nothing."""
+    T, V, d = 2, 600, 64
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, "bf16"), vm.head_config(V)
+    z, w, s = _inputs(T, N, V, d, 0, "bf16", False, True, False, seed=5)
+    z = z.abs() + 1
+    s["label"] = s["label"] % 100
+    cut = torch.zeros(V, dtype=torch.bool)
+    cut[128:256] = cut[500:] = True
+    lost = w.clone()
+    lost[:, cut] = float("-inf")
+    o = _forward(p, head, z, lost, s)
+    few = w[:, ~cut].contiguous()
+    r = ref.loss(z, few, s["label"], None, None, 1.0)  # labels lie before what is cut out
+    D = (d / 16 + 4) * 2.0 ** -23 * np.einsum("tnd,tvd->tnv", np64(z), np.abs(np64(few))).max(axis=2)
+    assert np.all(np.abs(np64(o["lse"]) - r["lse"]) <= D + 1e-6 + 2.0 ** -23 * np.abs(r["lse"]))
+    assert np.all(np.abs(np64(o["ce"]) - r["ce"]) <= 2 * D + 2e-6 + 2.0 ** -22 * np.abs(r["ce"]))
