@@ -8,13 +8,13 @@
 //
 // The choices are whole numbers that everything behind them follows, and two experts' c may be closer than the
 // rounding of fp32.  They are defined by exact arithmetic, equal ones to the lower index: c is computed in fp32 with
-// a bound on its error, and where a choice's runner-up is within it, those experts alone are compared in 64 bits (a
-// row in a thousand at 256 experts).  Without a bias the order is that of the logits, which needs neither.
+// a bound on its error, and where a choice's runner-up is within it, those experts alone are compared in 64 bits (four
+// rows in ten thousand at 256 experts).  Without a bias the order is that of the logits, which needs neither.
 //
 // gate_fast: a row on a few lanes, in fp32; gate_rows: a warp a row, for groups of odd sizes.  A CTA's tile of rows also
-// counts its choices by (choice, expert).  gate_slots: the tile's first place for every (choice, expert) is the sum of the counts of all
-// tiles' earlier choices and of the earlier tiles' same choice; a warp then ranks a choice of the tile 32 rows at a
-// time.  Slots are those of vmoe_route: choice by choice, in token order.  No floating-point sum depends on an order of
+// counts its choices by (choice, expert).  gate_slots: the tile's first place for every (choice, expert) is the sum of
+// the counts of all tiles' earlier choices and of the earlier tiles' same choice; a warp then ranks a choice of the tile
+// 32 rows at a time.  Slots are those of vmoe_route: choice by choice, in token order.  No floating-point sum depends on an order of
 // arrival, and the integer atomics' order does not show.
 #include <math.h>
 
@@ -306,7 +306,7 @@ __device__ __forceinline__ float gate_of(const Gating &g, const Choice &r, int s
 
 constexpr size_t row_scratch(int M) { return (size_t)GT_WARPS * 32 * M * 16; }
 
-// Groups that are neither a power of two nor at least four experts.
+// Groups of a number of experts that is no power of two or below a lane's in gate_fast.
 template <int M>
 __global__ void __launch_bounds__(GT_THREADS, 3)
 gate_rows_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, const float *__restrict__ sbias,

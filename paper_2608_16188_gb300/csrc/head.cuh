@@ -32,7 +32,6 @@ struct HeadPlan {
 enum { HEAD_STATS = 0, HEAD_DLOGITS = 1, HEAD_DZ = 2, HEAD_DW = 3 };
 struct HeadGemm {
     int T, Np, V, d, parts, np;   // np: products of parts
-    int stats;                    // 1 or 2 sums, or coefficients, a row
     const int *rows;              // [T] tokens that take part
     int v0, vn;                   // the piece: first column, columns
     int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows
