@@ -4,17 +4,19 @@
 //
 // What bounds it is the weights' way from DRAM, read once: V d 2 bytes.  A warp streams 32 rows of w at a time, whole rows
 // that lie together, straight into the B fragments of mma.sync m16n8k16: a lane's 16 bytes are eight neighbouring
-// k of one row, which the products take in an order of their own (two of four k each: any order of the sum will do, if A has the
-// same); the tokens, 16 rows, are A, from shared memory.  A lane keeps the running maximum and sum of its two tokens, a CTA leaves
-// one of each.
-// 4 tokens, 128000 entries, d 1024 (262 MB, 38.6 us at the copy rate): 47 us; as 256 x 256 tiles of head_tc.cu 57, whose
-// 128-byte pieces of 19000 rows at a time lose DRAM's pages.
+// k of one row, which the products take in an order of their own (two of four k each: any order of the sum will do, if A
+// has the same); the tokens, 16 rows, are A, from shared memory.  A lane keeps the running maximum and sum of its two
+// tokens, a CTA leaves one of each.
+// 4 tokens, 128000 entries, d 1024 (262 MB, 38.6 us at the copy rate): 51 us, and 52 for the whole pass, whose packing runs
+// under the first rows' way from DRAM; as 256 x 256 tiles of head_tc.cu, whose 128-byte pieces of 19000 rows at a time lose
+// DRAM's pages, 57.
 #include "head.cuh"
 
 namespace vmoe {
 namespace {
 
 constexpr int FW_THREADS = 256, FW_WARPS = FW_THREADS / 32, FW_ROWS = 32;
+constexpr int FW_AHEAD = 1536;  // bytes of a row of w that are fetched ahead
 constexpr unsigned FULL = 0xffffffffu;
 
 __device__ __forceinline__ float ex2(float v) {
@@ -42,6 +44,15 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
     __shared__ float2 joined[2][FW_WARPS][HEAD_FEW];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
     const int d = args.d, V = args.V, pitch = fw_pitch(d);
+    const __nv_bfloat16 *wt = w + (long long)t * V * d;
+    // The warp's first rows, a lane each, on their way into L2 while head_pack runs: at most 120 MB of its 129 (2432 warps).
+    // A pass of 4 tokens, 128000 entries, d 1024: 60.7 us without, 58.9 with 256 bytes a row, 57.4 with 512, 54.4 with 1024,
+    // 52.2 with 1536 or 1792.  Fetched ahead all the way, a block's rows under the products of the last: 62.
+    const int first = (blockIdx.x * FW_WARPS + warp) * FW_ROWS + lane;
+    if (first < V)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global(wt + (long long)first * d)),
+                     "r"(min(d * 2, FW_AHEAD))
+                     : "memory");
     pdl_wait();
     pdl_launch_dependents();
     for (int i = tid; i < HEAD_FEW * (pitch / 8); i += FW_THREADS) {
@@ -54,7 +65,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
     __syncthreads();
     const long long at = (long long)t * args.Np + g;
     const int lab[2] = {args.label ? __ldg(args.label + at) : -1, args.label ? __ldg(args.label + at + 8) : -1};
-    const __nv_bfloat16 *za = fw_z + g * pitch + 8 * q, *zb = za + 8 * pitch, *wt = w + (long long)t * V * d;
+    const __nv_bfloat16 *za = fw_z + g * pitch + 8 * q, *zb = za + 8 * pitch;
     Sum one[2], two[2];
     const int blocks = (V + FW_ROWS - 1) / FW_ROWS;
     for (int b = blockIdx.x * FW_WARPS + warp; b < blocks; b += gridDim.x * FW_WARPS) {
