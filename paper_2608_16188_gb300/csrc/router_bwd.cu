@@ -221,10 +221,10 @@ __device__ __forceinline__ bool gate_backward(int k, int E, bool norenorm, bool 
 }
 
 // gate_backward for choices of vmoe_gate (gate.cu has the formulas) but for a softmax's unrenormalised gates, whose rows
-// are dense: choices may be missing (e_j = -1).
+// are dense: choices may be missing (e_j = -1).  le: the choices' logits, for sigmoid scores.
 template <int KMAX>
 __device__ __forceinline__ bool gate_backward_scored(const Gating &g, int k, int E, int lane, long long tn, float (&dg)[KMAX],
-                                                     const float (&gt)[KMAX], const int (&ei)[KMAX], const float *logits,
+                                                     const float (&gt)[KMAX], const int (&ei)[KMAX], const float (&le)[KMAX],
                                                      float *dgate, float *dlogits, float (&c)[KMAX]) {
     float m = 0.0f, mine = 0.0f;
 #pragma unroll
@@ -242,7 +242,7 @@ __device__ __forceinline__ bool gate_backward_scored(const Gating &g, int k, int
     for (int j = 0; j < KMAX; ++j) {
         if (j >= k || ei[j] < 0) continue;
         c[j] = gt[j] * (g.renorm ? dg[j] - m : dg[j]);
-        if (g.score == VMOE_SCORE_SIGMOID) c[j] *= 1.0f / (1.0f + expf(__ldg(logits + tn * E + ei[j])));
+        if (g.score == VMOE_SCORE_SIGMOID) c[j] *= 1.0f / (1.0f + expf(le[j]));
         any |= c[j] != 0.0f;
     }
     for (int e = lane; e < E; e += 32) {
@@ -444,6 +444,12 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
                     if (v < d) xo[ch] = *reinterpret_cast<const uint4 *>((SCORED ? dx_in : dx) + tn * d + v);
                 }
             }
+            float le[KMAX] = {};  // behind the reduction this load is 6 of 59 us
+            if constexpr (SCORED) {
+#pragma unroll
+                for (int j = 0; j < KMAX; ++j)
+                    if (sg.score == VMOE_SCORE_SIGMOID && ei[j] >= 0) le[j] = __ldg(logits + tn * E + ei[j]);
+            }
             // the next token's routing
             const long long tn2 = tn + RG_WARPS;
             int ei2[KMAX], sl2[KMAX];
@@ -477,7 +483,7 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
             float c[KMAX];
             bool any;
             if constexpr (SCORED) {
-                any = gate_backward_scored<KMAX>(sg, k, E, lane, tn, dg, gt, ei, logits, dgate, dlogits, c) || dx != dx_in;
+                any = gate_backward_scored<KMAX>(sg, k, E, lane, tn, dg, gt, ei, le, dgate, dlogits, c) || dx != dx_in;
 #pragma unroll
                 for (int j = 0; j < KMAX; ++j) ei[j] = max(ei[j], 0);
             } else {
@@ -517,11 +523,13 @@ router_grad_fast_kernel(Dims p, const __nv_bfloat16 *__restrict__ dy,
 // memory in the order of the fragments, one 16-byte read for a lane's k16 x n8 parts, and
 // its warps walk tiles of 16 tokens, whose dlogit rows come straight from global memory.
 // The columns are dealt so that a lane's results are 16 neighbouring ones of a row.
-// 17 x 1576 tokens, 768 channels and 32 experts, L2 flushed before the call: 35 us, 12.9 us for
-// its bytes at the copy rate (DRAM at 18% of its peak, 22% of the warps active, first stall
-// the wait for dlogits and dX: latency); all of vmoe_router_bwd 88 us (76 without the flag, 133
-// with kernel 1's dense update).  8 x 1576, 1024, 64: 39 us of 73 (41 without the flag, 2.7 ms).
-constexpr int RX_COLS = 64, RX_TOKENS = 512, RX_THREADS = 256;
+// 17 x 1576 tokens, 768 channels and 32 experts, L2 flushed before the call: 32 us, 12.9 us for
+// its bytes at the copy rate (DRAM at 18% of its peak, 22% of the warps active, L1 at 60%: dlogits
+// and dX are read 8 rows a load); all of vmoe_router_bwd 86 us (76 without the flag, 133
+// with kernel 1's dense update).  8 x 1576, 1024, 64: 32 us of 67 (41 without the flag, 2.7 ms).
+// 256 tokens a CTA, three CTAs an SM: with 512 and two, 34 and 38 us, the last of few waves being
+// part full; with 128 tokens 34 and 36, the weights' parts being formed once more for each.
+constexpr int RX_COLS = 64, RX_TOKENS = 256, RX_THREADS = 256;
 
 __device__ __forceinline__ void split2(float a, float b, uint32_t &hi, uint32_t &lo) {
     hi = pack_bf16x2(a, b);
@@ -536,13 +544,14 @@ __device__ __forceinline__ float2 two_of(const float *row, int k, int E) {
 }
 
 template <bool EVEN>
-__global__ void __launch_bounds__(RX_THREADS)
+__global__ void __launch_bounds__(RX_THREADS, 3)
 router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restrict__ wr, const __nv_bfloat16 *dx_in,
                      __nv_bfloat16 *dx) {
     extern __shared__ __align__(16) uint4 rx_w[];  // [k16 steps][8 column tiles][32 lanes]: hi k, hi k + 8, lo, lo
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int t = blockIdx.z, d = p.d, E = p.E, N = p.N, d0 = blockIdx.y * RX_COLS, steps = (E + 15) / 16;
-    pdl_wait();
+    // before the wait: what came before the kernel ahead, which is always one of this call's, had completed when it let this
+    // one start
     // column c of tile j, c = 2 q + b as a lane's result has it, is column 16 q + 2 j + b
     for (int i = warp; i < steps * 8; i += RX_THREADS / 32) {
         const int c = d0 + 16 * (g >> 1) + 2 * (i & 7) + (g & 1), k = 16 * (i >> 3) + 2 * q;
@@ -557,6 +566,7 @@ router_dx_mma_kernel(Dims p, const float *__restrict__ dl, const float *__restri
         split2(w1.x, w1.y, v.y, v.w);
         rx_w[i * 32 + lane] = v;
     }
+    pdl_wait();
     __syncthreads();
     const int c0 = d0 + 16 * q, stop = min(N, (int)(blockIdx.x + 1) * RX_TOKENS);
     for (int n0 = blockIdx.x * RX_TOKENS + warp * 16; n0 < stop; n0 += RX_THREADS / 2) {
