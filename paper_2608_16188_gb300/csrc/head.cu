@@ -96,7 +96,7 @@ head_mark_kernel(Sizes z, int words, const int32_t *__restrict__ label, const in
 
 // Packs the tokens that take part, HP_TOKENS a CTA: how many come before is counted by every CTA, from the bits, or where
 // a head has few tokens from their labels and entries themselves.  Copies their rows (fp32 ones as three bf16 parts),
-// fills the last tile with zeros, and leaves what else belongs to a token: zeros in the outputs of one without a part,
+// fills the last block with zeros, and leaves what else belongs to a token: zeros in the outputs of one without a part,
 // the backward's factors.
 struct Pack {
     Sizes z;
@@ -110,6 +110,7 @@ struct Pack {
     float *ce, *lse, *kl, *tlse, *logp;
     // backward
     void *dz;
+    bool fill;
     float inv_tau;
     bool one;  // labels and a teacher at temperature 1: one exponential for both
     const float *in_ce, *in_lse, *in_tlse, *dce, *dlse, *dkl;
@@ -254,11 +255,12 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
     if (f.logp)
         for (int i = tid; i < here * z.K; i += HG_THREADS)
             if (to[i / z.K] < 0) f.logp[(t0 + n0) * z.K + i] = 0.0f;
-    // the rest of the last tile
-    const int end = (total + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
+    // the rest of HEAD_DW's last block of tokens, whose sum has zeros times these; elsewhere a row reaches nothing but what is
+    // its own, and nobody reads that.  (Whole tiles for everybody: a head of 8 tokens, d 1024, fp32, 30 us a call.)
+    if (!f.fill) return;
+    const int end = (total + HEAD_BLOCK - 1) / HEAD_BLOCK * HEAD_BLOCK;
     for (int r = total + blockIdx.x * (HG_THREADS / 32) + warp; r < end; r += gridDim.x * (HG_THREADS / 32)) {
         const long long at = (long long)t * z.Np + r;
-        if (lane == 0 && f.out_label) f.out_label[at] = -1;
         for (int q = 0; q < (sizeof(T) == 2 ? 1 : 3); ++q)
             for (int c = lane * 8; c < z.d; c += 256)
                 *reinterpret_cast<uint4 *>(f.out + q * plane + at * z.d + c) = make_uint4(0, 0, 0, 0);
@@ -574,7 +576,7 @@ head_dz_kernel(Sizes z, const int *__restrict__ pos, const float *__restrict__ s
     }
 }
 
-// The tiles of dz whose sums were cut (DzShares), from their parts in order.  A CTA 16 rows of a tile.
+// The tiles of dz whose sums were cut (DzShares), from their parts in order.  A CTA eight rows of a tile.
 template <typename T>
 __global__ void __launch_bounds__(HG_THREADS)
 head_dz_join_kernel(Sizes z, int pairs, int kb, int least, int tiles_n, const int *__restrict__ rows, const int *__restrict__ map,
@@ -593,23 +595,25 @@ head_dz_join_kernel(Sizes z, int pairs, int kb, int least, int tiles_n, const in
         if (local < c) break;
         local -= c;
     }
-    const int in = blockIdx.y * 16 + (threadIdx.x >> 4), r = local / tiles_n * HEAD_TILE + in;
-    const int c0 = (threadIdx.x & 15) * 16, col = local % tiles_n * HEAD_TILE + c0;
+    const int in = blockIdx.y * 8 + (threadIdx.x >> 5), r = local / tiles_n * HEAD_TILE + in;
+    const int c0 = (threadIdx.x & 31) * 8, col = local % tiles_n * HEAD_TILE + c0;
     if (r >= n || col >= z.d) return;
-    float v[16] = {};
-    for (int cut = 0; cut < s.cuts; ++cut) {
-        const float *p = parts + ((long long)(cut * s.left + tile) * HEAD_TILE + in) * HEAD_TILE + c0;
-#pragma unroll
-        for (int h = 0; h < 16; h += 8) {
-            float o[8];
-            load8(p + h, o);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[h + q] += o[q];
-        }
-    }
     T *o = dz + ((long long)t * z.N + map[(long long)t * z.Np + r]) * z.d + col;
+    const float *p = parts + ((long long)tile * HEAD_TILE + in) * HEAD_TILE + c0;
+    const long long step = (long long)s.left * HEAD_TILE * HEAD_TILE;
+    float v[8] = {};
+    constexpr int U = 8;  // parts in flight
+    for (int cut = 0; cut < s.cuts; cut += U) {
+        float b[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load8(p + min(cut + u, s.cuts - 1) * step, b[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (cut + u < s.cuts)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] += b[u][q];
+    }
     store8(o, v);
-    if (col + 8 < z.d) store8(o + 8, v + 8);
 }
 
 Sizes sizes_of(const HeadPlan &h) { return Sizes{h.T, h.N, h.Np, h.d, h.V, h.K}; }
@@ -814,6 +818,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
     const __nv_bfloat16 *zp, *wp;
     Pack k = {};
     k.dz = dz;
+    k.fill = dw != nullptr;
     k.inv_tau = 1.0f / h.tau;
     k.one = h.stats == 1;
     k.in_ce = ce;
@@ -892,7 +897,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
     const float *parts = at<float>(ws, h.dzp);
     if (direct) {
         const int kb = (h.V + 63) / 64, least = dz_least(h.parts), tiles_n = (h.d + HEAD_TILE - 1) / HEAD_TILE;
-        const dim3 grid(pairs, HEAD_TILE / 16);
+        const dim3 grid(pairs, HEAD_TILE / 8);
         st = p.bf16 ? launch_kernel(head_dz_join_kernel<__nv_bfloat16>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, least, tiles_n, rows,
                                     map, parts, (__nv_bfloat16 *)dz)
                     : launch_kernel(head_dz_join_kernel<float>, grid, dim3(HG_THREADS), 0, s, z, pairs, kb, least, tiles_n, rows, map,

@@ -10,6 +10,7 @@ constexpr int HEAD_K = 128;     // entries of a teacher's list at most
 constexpr int HEAD_V = 1 << 20;  // entries of a vocabulary at most, with a teacher
 constexpr int HEAD_FEW = 16;    // tokens of a head at most for head_few
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
+constexpr int HEAD_BLOCK = 64;  // of its sum that are loaded at a time
 
 // Sizes of a call, and where its scratch lies in the workspace (byte offsets).
 struct HeadPlan {

@@ -30,6 +30,7 @@ namespace tc {
 namespace {
 
 constexpr int HB = HEAD_TILE;
+static_assert(BK == HEAD_BLOCK, "HEAD_DW's last block of tokens");
 constexpr int HG_ROWS = 32;  // row tiles that share a column tile
 
 // Blocks of 64 of a tile's sum that the tensor cores add up by themselves: all, or in fp32 the five small products of
