@@ -714,7 +714,8 @@ constexpr int DW_BD = 128;          // rows of d per CTA
 constexpr int DW_BE = 32;           // experts per CTA
 constexpr int DW_KC = 32;           // tokens per stage
 constexpr int DW_STAGES = 3;
-constexpr int DW_SPLIT = 4;         // cluster size: the token range is split 4 ways
+constexpr int DW_SPLIT = 4;         // cluster size: the token range is split 4 ways, or up to
+constexpr int DW_SPLIT_MAX = 16;    // so many
 constexpr int DW_XP = DW_BD + 8;    // x row pitch (bf16): 272 B, conflict-free ldmatrix
 constexpr int DW_PP = DW_KC + 8;    // dlogit-part row pitch (bf16): 80 B, conflict-free
 constexpr int DW_RP = DW_BE + 1;    // fp32 partial-tile row pitch
@@ -755,11 +756,12 @@ __device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], const void *smem) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
 }
 
-// grid (DW_SPLIT, ceil(d / DW_BD), T * ceil(E / DW_BE)), cluster (DW_SPLIT, 1, 1).
+// grid (SPLIT, ceil(d / DW_BD), T * ceil(E / DW_BE)), cluster (SPLIT, 1, 1).
 // Warp w owns rows [32 w, 32 w + 32) of the CTA's d-slice (two m16 tiles, so
 // each dlogit fragment read from shared memory feeds two products) and all 32
 // experts.
-__global__ void __cluster_dims__(DW_SPLIT, 1, 1) __launch_bounds__(DW_THREADS)
+template <int SPLIT>
+__global__ void __launch_bounds__(DW_THREADS)
 router_dw_mma_kernel(Dims p, const __nv_bfloat16 *__restrict__ x,
                      const float *__restrict__ dlg, float *__restrict__ dw,
                      float *__restrict__ dbias) {
@@ -772,8 +774,8 @@ router_dw_mma_kernel(Dims p, const __nv_bfloat16 *__restrict__ x,
     const int t = blockIdx.z / etiles;
     const int e0 = (blockIdx.z - t * etiles) * DW_BE;
     const int d0 = blockIdx.y * DW_BD;
-    const int n_beg = (int)((long long)N * rank / DW_SPLIT);
-    const int n_end = (int)((long long)N * (rank + 1) / DW_SPLIT);
+    const int n_beg = (int)((long long)N * rank / SPLIT);
+    const int n_end = (int)((long long)N * (rank + 1) / SPLIT);
     const int nchunks = (n_end - n_beg + DW_KC - 1) / DW_KC;
     const __nv_bfloat16 *xt = x + (long long)t * N * d;
     const float *dlt = dlg + (long long)t * N * E;
@@ -938,18 +940,18 @@ router_dw_mma_kernel(Dims p, const __nv_bfloat16 *__restrict__ x,
     cluster.sync();
     // rank r writes rows [32 r, 32 r + 32) of the tile, summing ranks 0..3 in order
     float *dwt = dw + (long long)t * d * E;
-    constexpr int ROWS = DW_BD / DW_SPLIT;
+    constexpr int ROWS = DW_BD / SPLIT;
     for (int v = tid; v < ROWS * DW_BE; v += DW_THREADS) {
         const int m = rank * ROWS + v / DW_BE, n = v % DW_BE;
         float sum = 0.0f;
 #pragma unroll
-        for (int q = 0; q < DW_SPLIT; ++q) sum += cluster.map_shared_rank(red, q)[m * DW_RP + n];
+        for (int q = 0; q < SPLIT; ++q) sum += cluster.map_shared_rank(red, q)[m * DW_RP + n];
         if (d0 + m < d && e0 + n < E) dwt[(long long)(d0 + m) * E + e0 + n] = sum;
     }
     if (do_bias && rank == 0 && tid < DW_BE && e0 + tid < E) {
         float b = 0.0f;
 #pragma unroll
-        for (int q = 0; q < DW_SPLIT; ++q) b += cluster.map_shared_rank(sm.bias_sum, q)[tid];
+        for (int q = 0; q < SPLIT; ++q) b += cluster.map_shared_rank(sm.bias_sum, q)[tid];
         dbias[(long long)t * E + e0 + tid] = b;
     }
     cluster.sync();  // every rank's shared memory stays alive until the remote reads are done
@@ -1087,7 +1089,34 @@ int launch_router_dw_simt(const Dims &p, const float *x, const float *dl, float 
                : VMOE_ERR_CUDA;
 }
 
-int launch_router_dw(const Dims &p, const void *x, const float *dlogits, float *dw, float *dbias, cudaStream_t s) {
+template <int SPLIT>
+int launch_dw_mma(const Dims &p, const __nv_bfloat16 *x, const float *dl, float *dw, float *dbias, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(SPLIT, (p.d + DW_BD - 1) / DW_BD, p.T * ((p.E + DW_BE - 1) / DW_BE));
+    cfg.blockDim = dim3(DW_THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = SPLIT;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (SPLIT > 8) {  // above the portable size
+        static std::atomic<int> allowed[64];
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VMOE_ERR_CUDA;
+        if (!allowed[dev].load(std::memory_order_relaxed)) {
+            if (cudaFuncSetAttribute(router_dw_mma_kernel<SPLIT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+                return VMOE_ERR_CUDA;
+            allowed[dev].store(1, std::memory_order_relaxed);
+        }
+    }
+    return cudaLaunchKernelEx(&cfg, router_dw_mma_kernel<SPLIT>, p, x, dl, dw, dbias) == cudaSuccess ? VMOE_OK : VMOE_ERR_CUDA;
+}
+
+// splits: ways that the tokens of a tile may be split.
+int launch_router_dw(const Dims &p, const void *x, const float *dlogits, float *dw, float *dbias, int splits, cudaStream_t s) {
     int st;
     trace_before(s, "router_dw");
     if (p.bf16 && (st = launch_router_dw_tc(p, (const __nv_bfloat16 *)x, dlogits, dw, dbias, s)) !=
@@ -1096,16 +1125,20 @@ int launch_router_dw(const Dims &p, const void *x, const float *dlogits, float *
         return st;
     }
     if (p.bf16) {
-        dim3 grid(DW_SPLIT, (p.d + DW_BD - 1) / DW_BD, p.T * ((p.E + DW_BE - 1) / DW_BE));
-        router_dw_mma_kernel<<<grid, DW_THREADS, 0, s>>>(p, (const __nv_bfloat16 *)x, dlogits, dw,
-                                                         dbias);
+        // more CTAs a tile while SMs are idle and each keeps 16 chunks: 4 tasks of 20000 tokens, d 256, 30 experts, 133 us as
+        // 32 CTAs and 50 as 128
+        const long long tiles = (long long)((p.d + DW_BD - 1) / DW_BD) * p.T * ((p.E + DW_BE - 1) / DW_BE);
+        int split = DW_SPLIT;
+        while (split < splits && tiles * split < 2LL * num_sms() && p.N >= split * 16 * DW_KC) split *= 2;
+        const __nv_bfloat16 *xb = (const __nv_bfloat16 *)x;
+        st = split <= 4   ? launch_dw_mma<4>(p, xb, dlogits, dw, dbias, s)
+             : split <= 8 ? launch_dw_mma<8>(p, xb, dlogits, dw, dbias, s)
+                          : launch_dw_mma<16>(p, xb, dlogits, dw, dbias, s);
     } else {
         st = launch_router_dw_simt(p, (const float *)x, dlogits, dw, dbias, s);
-        trace_after(s);
-        return st;
     }
     trace_after(s);
-    return launch_result();
+    return st;
 }
 
 // ---------------------------------------------------------------------------
@@ -1238,7 +1271,7 @@ int run(const Dims &p, const void *x, const float *wr, const float *logits, cons
     trace_after(s);
     if (st != VMOE_OK) return st;
     if (dense_dx && (st = launch_router_dx(p, dlogits, wr, dense_dx, dense_dx, s)) != VMOE_OK) return st;
-    return launch_router_dw(p, x, dlogits, dw, dbias, s);
+    return launch_router_dw(p, x, dlogits, dw, dbias, DW_SPLIT, s);
 }
 
 }  // namespace
@@ -1285,7 +1318,7 @@ int launch_router_grads(const Dims &p, const void *x, const float *w_router, con
                         float *dbias, const void *dx_in, void *dx, cudaStream_t s) {
     if (dx)
         if (const int st = launch_router_dx(p, dlogits, w_router, dx_in, dx, s)) return st;
-    return launch_router_dw(p, x, dlogits, dw_router, dbias, s);
+    return launch_router_dw(p, x, dlogits, dw_router, dbias, DW_SPLIT_MAX, s);
 }
 
 }  // namespace vmoe
