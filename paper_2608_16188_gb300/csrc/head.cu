@@ -398,34 +398,32 @@ __device__ __forceinline__ void join(float &m, float &s, float2 v) {
 }
 __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *o) { bf16x8_to_f32(__ldg(reinterpret_cast<const uint4 *>(p)), o); }
 
-// Lane l: the logit of entry i of lane l, for the first `n` lanes; -1 gives 0.  Four entries' rows at a time.
+// Lane l < 8: the logit of entry i of lane l; all eight rows at a time.
 template <typename T>
-__device__ __forceinline__ float entries_logits(int d, const T *zr, const T *w, int i, int n) {
+__device__ __forceinline__ float entries_logits(int d, const T *zr, const T *w, int i) {
+    constexpr int U = 8;
     const int lane = threadIdx.x & 31;
-    float mine = 0.0f;
-    for (int j = 0; j < min(n, 32); j += 4) {
-        float acc[4] = {};
-        const T *row[4];
+    float acc[U] = {}, mine = 0.0f;
+    const T *row[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) row[e] = w + (long long)max(0, __shfl_sync(FULL, i, j + e)) * d;
+    for (int e = 0; e < U; ++e) row[e] = w + (long long)max(0, __shfl_sync(FULL, i, e)) * d;
 #pragma unroll 2
-        for (int c = lane * 8; c < d; c += 256) {
-            float a[8], b[8];
-            load8(zr + c, a);
+    for (int c = lane * 8; c < d; c += 256) {
+        float a[8], b[U][8];
+        load8(zr + c, a);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                load8(row[e] + c, b);
+        for (int e = 0; e < U; ++e) load8(row[e] + c, b[e]);
 #pragma unroll
-                for (int x = 0; x < 8; ++x) acc[e] = fmaf(a[x], b[x], acc[e]);
-            }
-        }
+        for (int e = 0; e < U; ++e)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            acc[e] = warp_sum(acc[e]);
-            if (lane == j + e) mine = acc[e];
-        }
+            for (int x = 0; x < 8; ++x) acc[e] = fmaf(a[x], b[e][x], acc[e]);
     }
-    return i >= 0 ? mine : 0.0f;
+#pragma unroll
+    for (int e = 0; e < U; ++e) {
+        acc[e] = warp_sum(acc[e]);
+        if (lane == e) mine = acc[e];
+    }
+    return mine;
 }
 
 // DOTS: void, or the type of z and w where the entries' logits are formed here.
@@ -434,6 +432,8 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
     constexpr int SHARES = HG_THREADS / ROWS;  // threads of a row
     __shared__ float2 sm[2][HG_THREADS / 32][ROWS];
     __shared__ float tl[ROWS];
+    constexpr bool DOT = !std::is_void<DOTS>::value;
+    __shared__ float dots[DOT ? ROWS : 1][DOT ? HEAD_K : 1];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row_in = lane % ROWS;
     const Sizes z = f.z;
     pdl_wait();
@@ -474,6 +474,20 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
         }
     }
     if (!f.kl) return;
+    if constexpr (DOT) {  // eight entries of a row a warp
+        const int each = (z.K + 7) / 8;
+        for (int b = warp; b < min(ROWS, n - r0) * each; b += HG_THREADS / 32) {
+            const int i = b / each, j = (b - i * each) * 8 + lane;
+            const long long tn = (long long)t * z.N + f.map[(long long)t * z.Np + r0 + i];
+            int e = -1;
+            if (lane < 8 && j < z.K) {
+                e = f.tidx[tn * z.K + j];
+                if (!entry_ok(z, e, f.tlogit[tn * z.K + j])) e = -1;
+            }
+            const float l = entries_logits(z.d, (const DOTS *)f.dot_z + tn * z.d, (const DOTS *)f.dot_w + (long long)t * z.V * z.d, e);
+            if (e >= 0) dots[i][j] = l;
+        }
+    }
     __syncthreads();
     for (int i = warp; i < ROWS && r0 + i < n; i += HG_THREADS / 32) {
         const long long at = (long long)t * z.Np + r0 + i, tn = (long long)t * z.N + f.map[at];
@@ -485,12 +499,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
             if (32 * mm >= z.K) break;
             const int j = lane + 32 * mm;
             float l = 0.0f;
-            if constexpr (std::is_void<DOTS>::value) {
-                if (j < z.K && q.i[mm] >= 0) l = f.tl[at * z.K + j];
-            } else {
-                l = entries_logits(z.d, (const DOTS *)f.dot_z + tn * z.d, (const DOTS *)f.dot_w + (long long)t * z.V * z.d, q.i[mm],
-                                   z.K - 32 * mm);
-            }
+            if (j < z.K && q.i[mm] >= 0) l = DOT ? dots[DOT ? i : 0][DOT ? j : 0] : f.tl[at * z.K + j];
             if (j >= z.K) continue;
             const float lp = q.i[mm] >= 0 ? l * f.inv_tau - tl[i] : 0.0f;
             f.logp[tn * z.K + j] = lp;
@@ -804,10 +813,15 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     trace_before(s, "head_finish");
     // few rows: more threads each, to hide the chain of their half tiles
     const bool few = (long long)h.T * h.N <= 2048;
+    const int rows = !few ? 32 : dots && h.K > 32 ? 1 : 4;  // a row's entries keep its warps busy
     auto kern = !dots    ? (few ? head_finish_kernel<4, void> : head_finish_kernel<32, void>)
-                : p.bf16 ? (few ? head_finish_kernel<4, __nv_bfloat16> : head_finish_kernel<32, __nv_bfloat16>)
-                         : (few ? head_finish_kernel<4, float> : head_finish_kernel<32, float>);
-    st = launch_kernel(kern, dim3((h.N + (few ? 3 : 31)) / (few ? 4 : 32), h.T), dim3(HG_THREADS), 0, s, f);
+                : p.bf16 ? (rows == 1   ? head_finish_kernel<1, __nv_bfloat16>
+                            : rows == 4 ? head_finish_kernel<4, __nv_bfloat16>
+                                        : head_finish_kernel<32, __nv_bfloat16>)
+                         : (rows == 1   ? head_finish_kernel<1, float>
+                            : rows == 4 ? head_finish_kernel<4, float>
+                                        : head_finish_kernel<32, float>);
+    st = launch_kernel(kern, dim3((h.N + rows - 1) / rows, h.T), dim3(HG_THREADS), 0, s, f);
     trace_after(s);
     return st;
 }
