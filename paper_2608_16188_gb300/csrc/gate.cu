@@ -353,6 +353,13 @@ __device__ __forceinline__ float redux_max(float v) {
     asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
+// The largest of this lane's half of the warp, for two rows a warp: 8 x 60000 of 64 experts, k 8, 8 groups, 350 -> 316 us
+// against four exchanges with their comparisons.
+__device__ __forceinline__ float redux_max_half(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "r"((threadIdx.x & 16) ? 0xffff0000u : 0x0000ffffu));
+    return r;
+}
 
 // V values of a lane, the largest first; at: where each came from, 4 bits apiece (a network of compare-exchanges).
 template <int V>
@@ -503,6 +510,7 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
             // leave the row open
             auto largest = [&](float v) {
                 if constexpr (L == 32) v = redux_max(v);
+                else if constexpr (L == 16) v = redux_max_half(v);
                 else
                     for (int o = glanes; o < L; o <<= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
                 return v;
@@ -591,13 +599,18 @@ gate_fast_kernel(Dims p, Gating g, int rows, const float *__restrict__ logits, c
             for (int j = 0; j <= k; ++j) {
                 float m = c[0];
                 int e = sl;  // the lane that has the largest, the first of equals
+                if constexpr (L >= 16) {
+                    m = L == 32 ? redux_max(m) : redux_max_half(m);
+                    e = __ffs(__ballot_sync(FULL, c[0] == m) >> (L == 32 ? 0 : sub * L)) - 1;
+                } else {
 #pragma unroll
-                for (int o = L / 2; o > 0; o >>= 1) {
-                    const float om = __shfl_xor_sync(FULL, m, o);
-                    const int oe = __shfl_xor_sync(FULL, e, o);
-                    if (om > m || (om == m && oe < e)) {
-                        m = om;
-                        e = oe;
+                    for (int o = L / 2; o > 0; o >>= 1) {
+                        const float om = __shfl_xor_sync(FULL, m, o);
+                        const int oe = __shfl_xor_sync(FULL, e, o);
+                        if (om > m || (om == m && oe < e)) {
+                            m = om;
+                            e = oe;
+                        }
                     }
                 }
                 if (j == k) {
