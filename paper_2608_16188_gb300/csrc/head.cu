@@ -633,7 +633,7 @@ P *at(void *ws, size_t offset) {
 
 // Packed rows and, in fp32, the weights' parts: what both directions begin with.  f: what the direction adds.
 int prepare(const Dims &p, const HeadPlan &h, const HeadIn &in, void *ws, Pack f, const __nv_bfloat16 **zp,
-            const __nv_bfloat16 **wp, cudaStream_t s) {
+            const __nv_bfloat16 **wp, bool split, cudaStream_t s) {
     const Sizes z = sizes_of(h);
     f.z = z;
     f.words = (h.N + 31) / 32;
@@ -664,7 +664,7 @@ int prepare(const Dims &p, const HeadPlan &h, const HeadIn &in, void *ws, Pack f
     if (st != VMOE_OK) return st;
     *zp = f.out;
     *wp = (const __nv_bfloat16 *)in.w;
-    if (!p.bf16) {
+    if (split) {
         __nv_bfloat16 *ws3 = at<__nv_bfloat16>(ws, h.w);
         const long long n = (long long)h.T * h.V * h.d, blocks = (n / 8 + HG_THREADS - 1) / HG_THREADS;
         trace_before(s, "head_split");
@@ -688,8 +688,8 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.K = head->teacher_k;
     h.Np = (h.N + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
     h.parts = p.bf16 ? 1 : 3;
-    // a warp 32 entries at a time, two CTAs of eight warps an SM
-    if (p.bf16 && h.N <= HEAD_FEW && h.d <= 2048)
+    // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM
+    if (h.N <= HEAD_FEW && h.d <= (p.bf16 ? 2048 : 1024))
         h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));
     h.tau = head->temperature;
     h.stats = label && h.K > 0 && head->temperature != 1.0f ? 2 : 1;
@@ -759,7 +759,7 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     k.kl = kl;
     k.tlse = tlse;
     k.logp = logp;
-    int st = prepare(p, h, in, ws, k, &zp, &wp, s);
+    int st = prepare(p, h, in, ws, k, &zp, &wp, !p.bf16 && !h.few, s);
     if (st != VMOE_OK) return st;
     const Sizes z = sizes_of(h);
     const int pitch = (h.V + HEAD_TILE - 1) / HEAD_TILE * 2;
@@ -785,7 +785,7 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     g.part = at<float2>(ws, h.part);
     g.part2 = at<float2>(ws, h.part2);
     g.picked = at<float>(ws, h.picked);
-    st = h.few ? launch_head_few(h, g, zp, wp, s) : launch_head_gemm(HEAD_STATS, h, g, zp, wp, nullptr, nullptr, s);
+    st = h.few ? launch_head_few(h, g, zp, in.w, s) : launch_head_gemm(HEAD_STATS, h, g, zp, wp, nullptr, nullptr, s);
     if (st != VMOE_OK) return st;
     Finish f = {};
     f.z = z;
@@ -843,7 +843,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
     k.dkl = dkl;
     k.coef = at<float4>(ws, h.coef);
     k.at_label = at<float>(ws, h.at_label);
-    int st = prepare(p, h, in, ws, k, &zp, &wp, s);
+    int st = prepare(p, h, in, ws, k, &zp, &wp, !p.bf16, s);
     if (st != VMOE_OK) return st;
     const Sizes z = sizes_of(h);
     const int *rows = at<int>(ws, h.rows), *map = at<int>(ws, h.map);

@@ -80,8 +80,9 @@ int head_dz_pairs(int parts);  // SM pairs that run HEAD_DZ at once, 0: the quer
 int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat16 *z, const __nv_bfloat16 *w,
                      __nv_bfloat16 *dl, __nv_bfloat16 *dw, cudaStream_t s);
 
-// The sums of HEAD_STATS for at most HEAD_FEW bf16 tokens a head (head_few.cu): one entry of part a CTA, `few` CTAs a head.
-int launch_head_few(const HeadPlan &h, const HeadGemm &g, const __nv_bfloat16 *z, const __nv_bfloat16 *w, cudaStream_t s);
+// The sums of HEAD_STATS for at most HEAD_FEW tokens a head (head_few.cu): one entry of part a CTA, `few` CTAs a head.  z: the
+// packed parts; w: the weights as they are given.
+int launch_head_few(const HeadPlan &h, const HeadGemm &g, const __nv_bfloat16 *z, const void *w, cudaStream_t s);
 
 struct HeadIn {
     const void *z, *w;

@@ -10,13 +10,17 @@
 // 4 tokens, 128000 entries, d 1024 (262 MB, 38.6 us at the copy rate): 51 us, and 52 for the whole pass, whose packing runs
 // under the first rows' way from DRAM; as 256 x 256 tiles of head_tc.cu, whose 128-byte pieces of 19000 rows at a time lose
 // DRAM's pages, 57.
+// fp32: a lane's eight values are split into three bf16 parts on their way, 16 rows at a time, for six products each; nothing
+// but the weights themselves is read.  8 tokens, 50000 entries, d 1024 (205 MB, 30 us): 85 us the pass, bound by the splits'
+// and products' issue; with the weights' parts written first and head_tc.cu 191.
 #include "head.cuh"
 
 namespace vmoe {
 namespace {
 
-constexpr int FW_THREADS = 256, FW_WARPS = FW_THREADS / 32, FW_ROWS = 32;
-constexpr int FW_AHEAD = 1536;  // bytes of a row of w that are fetched ahead
+constexpr int FW_THREADS = 256, FW_WARPS = FW_THREADS / 32;
+constexpr int fw_tiles(int parts) { return parts == 1 ? 4 : 2; }              // of 8 rows of w, a warp at a time
+constexpr int fw_ahead(int parts) { return 1536 * 4 / fw_tiles(parts); }      // bytes of a row of w that are fetched ahead
 constexpr unsigned FULL = 0xffffffffu;
 
 __device__ __forceinline__ float ex2(float v) {
@@ -37,28 +41,68 @@ struct Sum {
 // two rows by eight lanes.
 __host__ __device__ constexpr int fw_pitch(int d) { return (d + 63) / 64 * 64 + 32; }
 
-template <bool STATS2>
+// Eight values of a row of w as the B fragments of their parts.
+template <int PARTS>
+struct Values;
+template <>
+struct Values<1> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p, bool on) {
+        v = make_uint4(0, 0, 0, 0);
+        if (on) v = __ldcs(reinterpret_cast<const uint4 *>(p));
+    }
+    __device__ __forceinline__ void get(uint4 (&o)[1]) const { o[0] = v; }
+};
+template <>
+struct Values<3> {
+    float4 v[2];
+    __device__ __forceinline__ void load(const float *p, bool on) {
+        v[0] = v[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (on) v[0] = __ldcs(reinterpret_cast<const float4 *>(p)), v[1] = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+    }
+    __device__ __forceinline__ void get(uint4 (&o)[3]) const {
+        const float f[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+        uint32_t w[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a = f[2 * i], b = f[2 * i + 1];
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                w[q][i] = pack_bf16x2(a, b);
+                const float2 h = unpk2(bf16x2_to_f32x2(w[q][i]));
+                a -= h.x;
+                b -= h.y;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) o[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+    }
+};
+
+template <bool STATS2, int PARTS, typename W>
 __global__ void __launch_bounds__(FW_THREADS, 2)
-head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_bfloat16 *__restrict__ w) {
-    extern __shared__ __align__(16) __nv_bfloat16 fw_z[];  // [16][pitch]
+head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const W *__restrict__ w) {
+    constexpr int NT = fw_tiles(PARTS), ROWS = 8 * NT;
+    extern __shared__ __align__(16) __nv_bfloat16 fw_z[];  // [parts][16][pitch]
     __shared__ float2 joined[2][FW_WARPS][HEAD_FEW];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
     const int d = args.d, V = args.V, pitch = fw_pitch(d);
-    const __nv_bfloat16 *wt = w + (long long)t * V * d;
+    const W *wt = w + (long long)t * V * d;
     // The warp's first rows, a lane each, on their way into L2 while head_pack runs: at most 120 MB of its 129 (2432 warps).
     // A pass of 4 tokens, 128000 entries, d 1024: 60.7 us without, 58.9 with 256 bytes a row, 57.4 with 512, 54.4 with 1024,
     // 52.2 with 1536 or 1792.  Fetched ahead all the way, a block's rows under the products of the last: 62.
-    const int first = (blockIdx.x * FW_WARPS + warp) * FW_ROWS + lane;
-    if (first < V)
+    const int first = (blockIdx.x * FW_WARPS + warp) * ROWS + lane;
+    if (lane < ROWS && first < V)
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(__cvta_generic_to_global(wt + (long long)first * d)),
-                     "r"(min(d * 2, FW_AHEAD))
+                     "r"(min(d * (int)sizeof(W), fw_ahead(PARTS)))
                      : "memory");
     pdl_wait();
     pdl_launch_dependents();
-    for (int i = tid; i < HEAD_FEW * (pitch / 8); i += FW_THREADS) {
+    const long long plane = (long long)args.T * args.Np * d;
+    for (int i = tid; i < PARTS * HEAD_FEW * (pitch / 8); i += FW_THREADS) {
         const int r = i / (pitch / 8), c = (i - r * (pitch / 8)) * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (c < d) v = __ldg(reinterpret_cast<const uint4 *>(z + ((long long)t * args.Np + r) * d + c));
+        if (c < d) v = __ldg(reinterpret_cast<const uint4 *>(z + r / HEAD_FEW * plane + ((long long)t * args.Np + r % HEAD_FEW) * d + c));
         *reinterpret_cast<uint4 *>(fw_z + r * pitch + c) = v;
     }
     if (args.rows[t] == 0) return;  // nothing was packed, and nothing is read
@@ -67,46 +111,58 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
     const int lab[2] = {args.label ? __ldg(args.label + at) : -1, args.label ? __ldg(args.label + at + 8) : -1};
     const __nv_bfloat16 *za = fw_z + g * pitch + 8 * q, *zb = za + 8 * pitch;
     Sum one[2], two[2];
-    const int blocks = (V + FW_ROWS - 1) / FW_ROWS;
+    const int blocks = (V + ROWS - 1) / ROWS;
     for (int b = blockIdx.x * FW_WARPS + warp; b < blocks; b += gridDim.x * FW_WARPS) {
-        const int v0 = b * FW_ROWS;
-        const __nv_bfloat16 *row[4];
+        const int v0 = b * ROWS;
+        const W *row[NT];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) row[n] = wt + (long long)min(V - 1, v0 + 8 * n + g) * d + 8 * q;
-        float sum[4][4] = {};
+        for (int n = 0; n < NT; ++n) row[n] = wt + (long long)min(V - 1, v0 + 8 * n + g) * d + 8 * q;
+        float sum[NT][4] = {};
         constexpr int U = 4;  // steps of 32 k in flight: 8 KB a warp
         for (int k0 = 0; k0 < d; k0 += 32 * U) {
-            uint4 x[U][4];
+            Values<PARTS> x[U][NT];
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    x[u][n] = make_uint4(0, 0, 0, 0);
-                    if (k0 + 32 * u + 8 * q < d) x[u][n] = __ldcs(reinterpret_cast<const uint4 *>(row[n] + k0 + 32 * u));
-                }
-            // 128 k at a time: the products cut every step of their sums towards zero (all 1024 in one: ce off by 1.1e-6; so 1e-7)
-            float acc[4][4] = {};
+                for (int n = 0; n < NT; ++n) x[u][n].load(row[n] + k0 + 32 * u, k0 + 32 * u + 8 * q < d);
+            // 128 k at a time: the products cut every step of their sums towards zero (all 1024 in one: ce off by 1.1e-6; so 1e-7);
+            // fp32: the five small products of parts apart from the large one
+            float acc[NT][4] = {}, low[NT][4] = {};
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (k0 + 32 * u >= d) break;
-                const uint4 a = *reinterpret_cast<const uint4 *>(za + k0 + 32 * u), c = *reinterpret_cast<const uint4 *>(zb + k0 + 32 * u);
+                uint4 a[PARTS], c[PARTS];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    mma_bf16_16816(acc[n], a.x, c.x, a.y, c.y, x[u][n].x, x[u][n].y);
-                    mma_bf16_16816(acc[n], a.z, c.z, a.w, c.w, x[u][n].z, x[u][n].w);
+                for (int p = 0; p < PARTS; ++p) {
+                    a[p] = *reinterpret_cast<const uint4 *>(za + p * HEAD_FEW * pitch + k0 + 32 * u);
+                    c[p] = *reinterpret_cast<const uint4 *>(zb + p * HEAD_FEW * pitch + k0 + 32 * u);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint4 w8[PARTS];
+                    x[u][n].get(w8);
+                    auto product = [&](float(&o)[4], int i, int j) {
+                        mma_bf16_16816(o, a[i].x, c[i].x, a[i].y, c[i].y, w8[j].x, w8[j].y);
+                        mma_bf16_16816(o, a[i].z, c[i].z, a[i].w, c[i].w, w8[j].z, w8[j].w);
+                    };
+                    if constexpr (PARTS == 3) {
+                        product(low[n], 2, 0), product(low[n], 0, 2), product(low[n], 1, 1);
+                        product(low[n], 1, 0), product(low[n], 0, 1);
+                    }
+                    product(acc[n], 0, 0);
                 }
             }
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[n][i] += acc[n][i];
+                for (int i = 0; i < 4; ++i) sum[n][i] += PARTS == 3 ? acc[n][i] + low[n][i] : acc[n][i];
         }
         // columns v0 + 8 n + 2 q, + 1 of tokens g (0, 1) and g + 8 (2, 3)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float l[8], top = -INFINITY;
+            float l[2 * NT], top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 2 * NT; ++i) {
                 const int col = v0 + 8 * (i >> 1) + 2 * q + (i & 1);
                 l[i] = sum[i >> 1][2 * h + (i & 1)];
                 if (col == lab[h]) args.picked[at + 8 * h] = l[i];
@@ -118,7 +174,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
                 const float m = fmaxf(s.m, top * c);
                 float v = s.s * ex2(s.m - m);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v += ex2(fmaf(l[i], c, -m));
+                for (int i = 0; i < 2 * NT; ++i) v += ex2(fmaf(l[i], c, -m));
                 s.m = m;
                 s.s = v;
             };
@@ -150,22 +206,30 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const __nv_b
     if (STATS2) args.part2[o] = make_float2(s2.m, s2.s);
 }
 
+template <bool STATS2, int PARTS, typename W>
+int launch_few(const HeadPlan &h, const HeadGemm &g, const __nv_bfloat16 *z, const void *w, cudaStream_t s) {
+    const size_t smem = (size_t)PARTS * HEAD_FEW * fw_pitch(h.d) * 2;
+    static std::atomic<int> limit[64];
+    auto kern = head_few_kernel<STATS2, PARTS, W>;
+    if (smem > 40 * 1024)
+        if (const int st = raise_smem_limit((const void *)kern, limit, (int)smem)) return st;
+    return launch_kernel(kern, dim3(h.few, h.T), dim3(FW_THREADS), smem, s, g, z, (const W *)w);
+}
+
 }  // namespace
 
-int launch_head_few(const HeadPlan &h, const HeadGemm &in, const __nv_bfloat16 *z, const __nv_bfloat16 *w, cudaStream_t s) {
+int launch_head_few(const HeadPlan &h, const HeadGemm &in, const __nv_bfloat16 *z, const void *w, cudaStream_t s) {
     HeadGemm g = in;
+    g.T = h.T;
     g.Np = h.Np;
     g.V = h.V;
     g.d = h.d;
     g.c1 = h.c1;
     g.c2 = h.c2;
-    const size_t smem = (size_t)HEAD_FEW * fw_pitch(h.d) * 2;
-    static std::atomic<int> limit[2][64];
-    auto kern = h.stats == 2 ? head_few_kernel<true> : head_few_kernel<false>;
-    if (smem > 40 * 1024)
-        if (const int st = raise_smem_limit((const void *)kern, limit[h.stats == 2], (int)smem)) return st;
     trace_before(s, "head_few");
-    const int st = launch_kernel(kern, dim3(h.few, h.T), dim3(FW_THREADS), smem, s, g, z, w);
+    const int st = h.parts == 1 ? (h.stats == 2 ? launch_few<true, 1, __nv_bfloat16>(h, g, z, w, s)
+                                                : launch_few<false, 1, __nv_bfloat16>(h, g, z, w, s))
+                                : (h.stats == 2 ? launch_few<true, 3, float>(h, g, z, w, s) : launch_few<false, 3, float>(h, g, z, w, s));
     trace_after(s);
     return st;
 }

@@ -257,6 +257,18 @@ def test_nan_token(N, dtype, tau):
         assert torch.equal(torch.isnan(o[n]).cpu(), bad), n
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("size", [(1, 5, 90001, 40, 0, 1.0), (3, 16, 30010, 136, 9, 2.0), (1, 9, 700, 1032, 3, 0.5), (2, 2, 5000, 2048, 0, 1.0)],
+                         ids=str)
+def test_few_tokens(size, dtype):
+    """At most 16 tokens: more entries than all warps take at a time, widths around what they are taken up to."""
+    T, N, V, d, K, tau = size
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, dtype), vm.head_config(V, K, tau)
+    z, w, s = _inputs(T, N, V, d, K, dtype, False, True, True, seed=6)
+    o = _forward(p, head, z, w, s)
+    _check(o, z, w, dict(s, dce=None, dlse=None, dkl=None), tau, dtype)
+
+
 @pytest.mark.parametrize("N", (5, 40))
 def test_entries_out_of_reach(N):
     """Weights of -inf against tokens of positive values: logits of -inf, whole half tiles of them, add nothing."""
