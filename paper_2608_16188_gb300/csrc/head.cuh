@@ -17,6 +17,7 @@ struct HeadPlan {
     int T, N, d, V, K;   // heads, tokens of a head (all tasks' with a shared one), width, vocabulary, teacher's entries
     int Np;              // N in whole tiles: row pitch of what holds tokens
     int parts;           // bf16 parts of a value: 1, or 3 (fp32)
+    int two;             // 1: rows 16 .. 31 of dl hold what rounding has taken from rows 0 .. 15, of z the same tokens again
     int stats;           // sums of a row: 1, or 2 (labels and a teacher at another temperature)
     int piece;           // backward: columns of a piece of the vocabulary, whole tiles
     int pairs;           // backward: SM pairs, at most, that dz is shared out to; 0: in pieces of the vocabulary
@@ -33,6 +34,7 @@ struct HeadPlan {
 enum { HEAD_STATS = 0, HEAD_DLOGITS = 1, HEAD_DZ = 2, HEAD_DW = 3 };
 struct HeadGemm {
     int T, Np, V, d, parts, np;   // np: products of parts
+    int two;
     const int *rows;              // [T] tokens that take part
     int v0, vn;                   // the piece: first column, columns
     int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows

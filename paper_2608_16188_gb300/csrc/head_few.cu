@@ -7,7 +7,7 @@
 // k of one row, which the products take in an order of their own (two of four k each: any order of the sum will do, if A
 // has the same); the tokens, 16 rows, are A, from shared memory.  A lane keeps the running maximum and sum of its two
 // tokens, a CTA leaves one of each.
-// 4 tokens, 128000 entries, d 1024 (262 MB, 38.6 us at the copy rate): 51 us, and 52 for the whole pass, whose packing runs
+// 4 tokens, 128000 entries, d 1024 (262 MB, 38.6 us at the copy rate): 48 us, and 46 for the whole pass, whose packing runs
 // under the first rows' way from DRAM; as 256 x 256 tiles of head_tc.cu, whose 128-byte pieces of 19000 rows at a time lose
 // DRAM's pages, 57.
 // fp32: a lane's eight values are split into three bf16 parts on their way, 16 rows at a time, for six products each; nothing

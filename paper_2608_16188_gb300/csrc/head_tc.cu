@@ -398,6 +398,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
             }
             if (!ok) break;
+            if (MODE == HEAD_DZ && PARTS == 1 && args.two && row - lane == 0) {  // their products, joined
+#pragma unroll
+                for (int i = 0; i < 128; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], HEAD_FEW);
+            }
             if (MODE == HEAD_STATS && PARTS > 1) {
                 for (; ent < ents; ++ent) {
                     const unsigned what = __ldg(list + ent);
@@ -447,9 +451,12 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     args.part2[o] = make_float2(ref2, (s2[0] + s2[1]) + (s2[2] + s2[3]));
                 }
             } else if (MODE == HEAD_DLOGITS) {
-                const bool live = row < x.rows;
-                const float4 cf = live ? __ldg(args.coef + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                const int lab = live && args.label ? __ldg(args.label + at) - args.v0 - col : -1;
+                // with `two` rows 16 .. 31 are the tokens again, and take what rounding leaves of their values
+                const bool again = PARTS == 1 && args.two && row >= HEAD_FEW && row < 2 * HEAD_FEW;
+                const long long me = at - (again ? HEAD_FEW : 0);
+                const bool live = row - (again ? HEAD_FEW : 0) < x.rows;
+                const float4 cf = live ? __ldg(args.coef + me) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                const int lab = live && args.label ? __ldg(args.label + me) - args.v0 - col : -1;
                 if (live) {
                     float there = 0.0f;  // the value at the label, whose first term cancels where it is formed as the others are
                     if (lab >= 0 && lab < 128) {
@@ -457,7 +464,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 #pragma unroll
                         for (int i = 0; i < 128; ++i)
                             if (i == lab) l = v[i];
-                        there = __ldg(args.at_label + at);
+                        there = __ldg(args.at_label + me);
                         if (STATS2) there = fmaf(cf.z, ex2(fmaf(l, args.c2, -cf.w)), there);
                     }
 #pragma unroll
@@ -481,6 +488,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     for (int i = 0; i < 128; ++i) v[i] = 0.0f;
                 }
                 const int r0 = row - lane;
+                if (again) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) v[i] -= __bfloat162float(__float2bfloat16_rn(v[i]));
+                }
 #pragma unroll
                 for (int part = 0; part < PARTS; ++part) {
                     store64<(PARTS > 1)>(&tmD, v, stg, col, r0, x.t + args.T * part);
@@ -604,6 +615,7 @@ int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat1
     g.V = h.V;
     g.d = h.d;
     g.parts = h.parts;
+    g.two = h.two;
     g.np = h.parts == 1 ? 1 : 6;
     g.c1 = h.c1;
     g.c2 = h.c2;

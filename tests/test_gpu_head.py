@@ -81,7 +81,7 @@ def _run(p, head, z, w, s, nbytes=None, stream=None, train=True, dz=True):
     return o
 
 
-def _check(o, z, w, s, tau, dtype):
+def _check(o, z, w, s, tau, dtype, few=False):
     r = ref.loss(z, w, s["label"], s["tidx"], s["tlogit"], tau)
     part = r["has"] | r["taught"]
     T, N, V = r["logits"].shape
@@ -108,7 +108,7 @@ def _check(o, z, w, s, tau, dtype):
         assert np.all(np.abs(np64(o["kl"]) - r["kl"]) <= qt + 2e-6 * r["taught"])
     dl, size = ref.dlogits(r, s["label"], s["tidx"], tau, s["dce"], s["dlse"], s["dkl"])
     dz, dw = ref.back(dl, z, w, part)
-    err = size_err[..., None] * size + (2.0 ** -23 if f32 else 2.0 ** -8) * np.abs(dl)
+    err = size_err[..., None] * size + (2.0 ** -23 if f32 else 2.0 ** -16 if few else 2.0 ** -8) * np.abs(dl)
     steps = 6 if f32 else 1
     if o.get("dz") is not None:
         got = np64(o["dz"])
@@ -287,3 +287,13 @@ def test_entries_out_of_reach(N):
     D = (d / 16 + 4) * 2.0 ** -23 * np.einsum("tnd,tvd->tnv", np64(z), np.abs(np64(few))).max(axis=2)
     assert np.all(np.abs(np64(o["lse"]) - r["lse"]) <= D + 1e-6 + 2.0 ** -23 * np.abs(r["lse"]))
     assert np.all(np.abs(np64(o["ce"]) - r["ce"]) <= 2 * D + 2e-6 + 2.0 ** -22 * np.abs(r["ce"]))
+
+
+@pytest.mark.parametrize("size", [(1, 1, 700, 128, 0, 1.0), (2, 3, 5003, 72, 9, 2.0), (90, 16, 600, 264, 5, 1.0)], ids=str)
+def test_few_tokens_gradients(size):
+    """At most 16 tokens a head: dl, of which few values make most of the gradient, is kept to 2^-16 in bf16 problems."""
+    T, N, V, d, K, tau = size
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, "bf16"), vm.head_config(V, K, tau)
+    z, w, s = _inputs(T, N, V, d, K, "bf16", False, True, True, seed=7)
+    _check(_run(p, head, z, w, s), z, w, s, tau, "bf16", few=True)
+    _check(_run(p, head, z, w, s, vm.vmoe_head_min_workspace_size(p, head)), z, w, s, tau, "bf16", few=True)
