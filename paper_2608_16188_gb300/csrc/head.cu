@@ -170,20 +170,26 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
     before = total = 0;
 #pragma unroll
     for (int i = 0; i < HG_THREADS / 32; ++i) before += sum[0][i], total += sum[1][i];
-    if (blockIdx.x == 0 && tid == 0) f.rows[t] = total;
+    const int whole = (total + HEAD_HALF - 1) / HEAD_HALF * HEAD_HALF, rows = f.two ? two_row(whole) : total;
+    if (blockIdx.x == 0 && tid == 0) f.rows[t] = rows;
     const int n = n0 + tid;
     if (tid < HP_TOKENS) to[tid] = -1;
     if (tid < HP_TOKENS && n < z.N) {  // a token a thread
         const unsigned word = either[n >> 5];
         const long long tn = t0 + n;
         const bool in = word >> (n & 31) & 1u;
-        const int r = before + __popc(word & ((1u << (n & 31)) - 1u));
+        int r = before + __popc(word & ((1u << (n & 31)) - 1u));
+        if (f.two) r = two_row(r);
         const int y = f.label && label_ok(z, f.label[tn]) ? f.label[tn] : -1;
         f.pos[tn] = to[tid] = in ? r : -1;
         const long long at = (long long)t * z.Np + r;
         if (in) {
             f.map[at] = n;
             if (f.out_label) f.out_label[at] = y;
+            if (f.two) {
+                f.map[at + HEAD_HALF] = -1;
+                if (f.out_label) f.out_label[at + HEAD_HALF] = y;
+            }
         } else {
             if (f.ce) f.ce[tn] = f.lse[tn] = 0.0f;
             if (f.kl) f.kl[tn] = f.tlse[tn] = 0.0f;
@@ -210,6 +216,10 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
             }
             f.coef[at] = c;
             f.at_label[at] = there;
+            if (f.two) {
+                f.coef[at + HEAD_HALF] = c;
+                f.at_label[at + HEAD_HALF] = there;
+            }
         }
     }
     __syncthreads();
@@ -242,7 +252,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
             __nv_bfloat16 *o = f.out + ((long long)t * z.Np + r[u]) * z.d + at[u] % z.d;
             if constexpr (sizeof(T) == 2) {
                 *reinterpret_cast<uint4 *>(o) = v[u][0];
-                if (f.two) *reinterpret_cast<uint4 *>(o + HEAD_FEW * z.d) = v[u][0];
+                if (f.two) *reinterpret_cast<uint4 *>(o + HEAD_HALF * z.d) = v[u][0];
             } else {
                 const float *x = reinterpret_cast<const float *>(v[u]);
                 __align__(16) __nv_bfloat16 p[3][8];
@@ -258,11 +268,20 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
             if (to[i / z.K] < 0) f.logp[(t0 + n0) * z.K + i] = 0.0f;
     // the rest of HEAD_DW's last block of tokens, whose sum has zeros times these; elsewhere a row reaches nothing but what is
     // its own, and nobody reads that.  (Whole tiles for everybody: a head of 8 tokens, d 1024, fp32, 30 us a call.)
+    if (f.two)  // rows without a token among the first
+        for (int r = 2 * total + blockIdx.x * (HG_THREADS / 32) + warp; r < 2 * whole; r += gridDim.x * (HG_THREADS / 32)) {
+            const long long at = (long long)t * z.Np + two_row(r >> 1) + (r & 1) * HEAD_HALF;
+            if (lane == 0) {
+                f.map[at] = -1;
+                if (f.out_label) f.out_label[at] = -1;
+                f.coef[at] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            for (int c = lane * 8; c < z.d; c += 256) *reinterpret_cast<uint4 *>(f.out + at * z.d + c) = make_uint4(0, 0, 0, 0);
+        }
     if (!f.fill) return;
-    const int end = (total + HEAD_BLOCK - 1) / HEAD_BLOCK * HEAD_BLOCK;
-    for (int r = total + blockIdx.x * (HG_THREADS / 32) + warp; r < end; r += gridDim.x * (HG_THREADS / 32)) {
+    const int end = (rows + HEAD_BLOCK - 1) / HEAD_BLOCK * HEAD_BLOCK;
+    for (int r = rows + blockIdx.x * (HG_THREADS / 32) + warp; r < end; r += gridDim.x * (HG_THREADS / 32)) {
         const long long at = (long long)t * z.Np + r;
-        if (f.two && r >= HEAD_FEW && r < HEAD_FEW + total) continue;  // the tokens again
         for (int q = 0; q < (sizeof(T) == 2 ? 1 : 3); ++q)
             for (int c = lane * 8; c < z.d; c += 256)
                 *reinterpret_cast<uint4 *>(f.out + q * plane + at * z.d + c) = make_uint4(0, 0, 0, 0);
@@ -535,13 +554,14 @@ __global__ void __launch_bounds__(HG_THREADS) head_patch_kernel(Patch f) {
     pdl_launch_dependents();
     if (r >= f.rows[t]) return;
     const long long at = (long long)t * z.Np + r, tn = (long long)t * z.N + f.map[at];
+    if (f.map[at] < 0) return;
     Teacher q;
     q.load(z, f.tidx, f.tlogit, f.inv_tau, tn);
     if (!q.any) return;
     const int y = f.label && label_ok(z, f.label[tn]) ? f.label[tn] : -1;
     const float dce = y >= 0 && f.dce ? f.dce[tn] : 0.0f, dlse = y >= 0 && f.dlse ? f.dlse[tn] : 0.0f;
     const float b = f.dkl[tn] * f.inv_tau, lse = y >= 0 ? f.lse[tn] : 0.0f, tlse = f.tlse[tn];
-    const long long plane = (f.parts == 2 ? HEAD_FEW : (long long)z.T * z.Np) * f.piece;
+    const long long plane = (f.parts == 2 ? HEAD_HALF : (long long)z.T * z.Np) * f.piece;
     __nv_bfloat16 *row = f.dl + at * f.piece;
 #pragma unroll
     for (int m = 0; m < Teacher::M; ++m) {
@@ -610,7 +630,7 @@ head_dz_join_kernel(Sizes z, int pairs, int kb, int least, int tiles_n, const in
     }
     const int in = blockIdx.y * 8 + (threadIdx.x >> 5), r = local / tiles_n * HEAD_TILE + in;
     const int c0 = (threadIdx.x & 31) * 8, col = local % tiles_n * HEAD_TILE + c0;
-    if (r >= n || col >= z.d) return;
+    if (r >= n || col >= z.d || map[(long long)t * z.Np + r] < 0) return;
     T *o = dz + ((long long)t * z.N + map[(long long)t * z.Np + r]) * z.d + col;
     const float *p = parts + ((long long)tile * HEAD_TILE + in) * HEAD_TILE + c0;
     const long long step = (long long)s.left * HEAD_TILE * HEAD_TILE;
@@ -693,9 +713,8 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.Np = (h.N + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
     h.parts = p.bf16 ? 1 : 3;
     // A gradient of few tokens hangs on few values of dl, the labels' among them, whose rounding to bf16 (up to 2^-8) does not
-    // average out: one token's dw was off by 0.0029 in the mean, where its own rounding is 0.0018.  A second part of them takes
-    // rows of a tile that are empty otherwise, and no time.
-    h.two = p.bf16 && h.N <= HEAD_FEW;
+    // average out: one token's dw was off by 0.0029 in the mean, where its own rounding is 0.0018.
+    h.two = p.bf16 && h.N <= HEAD_TILE / 2;
     // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM
     if (h.N <= HEAD_FEW && h.d <= (p.bf16 ? 2048 : 1024))
         h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));
@@ -894,7 +913,7 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             f.dkl = dkl;
             f.dl = dl;
             trace_before(s, "head_patch");
-            st = launch_kernel(head_patch_kernel, dim3((h.N + 7) / 8, h.T), dim3(HG_THREADS), 0, s, f);
+            st = launch_kernel(head_patch_kernel, dim3(((h.two ? two_row(h.N - 1) + 1 : h.N) + 7) / 8, h.T), dim3(HG_THREADS), 0, s, f);
             trace_after(s);
             if (st != VMOE_OK) return st;
         }

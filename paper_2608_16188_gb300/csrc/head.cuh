@@ -9,6 +9,11 @@ namespace vmoe {
 constexpr int HEAD_K = 128;     // entries of a teacher's list at most
 constexpr int HEAD_V = 1 << 20;  // entries of a vocabulary at most, with a teacher
 constexpr int HEAD_FEW = 16;    // tokens of a head at most for head_few
+// Up to 128 bf16 tokens a head, which leave half of a tile's rows empty, have two rows each in the backward: token r (packed) row
+// 32 (r / 16) + r % 16 and the one 16 behind it, which a warp of an epilogue has both of.  z is the same in both, dl in the
+// second what rounding takes from the first: it is then kept to 2^-16, and the sums need no other code.  map is -1 for the second.
+constexpr int HEAD_HALF = 16;
+__host__ __device__ constexpr int two_row(int r) { return 2 * HEAD_HALF * (r / HEAD_HALF) + r % HEAD_HALF; }
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
 constexpr int HEAD_BLOCK = 64;  // of its sum that are loaded at a time
 
@@ -17,7 +22,7 @@ struct HeadPlan {
     int T, N, d, V, K;   // heads, tokens of a head (all tasks' with a shared one), width, vocabulary, teacher's entries
     int Np;              // N in whole tiles: row pitch of what holds tokens
     int parts;           // bf16 parts of a value: 1, or 3 (fp32)
-    int two;             // 1: rows 16 .. 31 of dl hold what rounding has taken from rows 0 .. 15, of z the same tokens again
+    int two;             // backward, 1: two rows a token, see HEAD_HALF
     int stats;           // sums of a row: 1, or 2 (labels and a teacher at another temperature)
     int piece;           // backward: columns of a piece of the vocabulary, whole tiles
     int pairs;           // backward: SM pairs, at most, that dz is shared out to; 0: in pieces of the vocabulary

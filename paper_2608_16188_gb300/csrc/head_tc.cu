@@ -398,9 +398,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 if (lane == 0) mbar_arrive_remote(mapa_shared(bar_tempty(acc), 0));
             }
             if (!ok) break;
-            if (MODE == HEAD_DZ && PARTS == 1 && args.two && row - lane == 0) {  // their products, joined
+            if (MODE == HEAD_DZ && PARTS == 1 && args.two) {  // a token's two rows
 #pragma unroll
-                for (int i = 0; i < 128; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], HEAD_FEW);
+                for (int i = 0; i < 128; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], HEAD_HALF);
             }
             if (MODE == HEAD_STATS && PARTS > 1) {
                 for (; ent < ents; ++ent) {
@@ -451,12 +451,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     args.part2[o] = make_float2(ref2, (s2[0] + s2[1]) + (s2[2] + s2[3]));
                 }
             } else if (MODE == HEAD_DLOGITS) {
-                // with `two` rows 16 .. 31 are the tokens again, and take what rounding leaves of their values
-                const bool again = PARTS == 1 && args.two && row >= HEAD_FEW && row < 2 * HEAD_FEW;
-                const long long me = at - (again ? HEAD_FEW : 0);
-                const bool live = row - (again ? HEAD_FEW : 0) < x.rows;
-                const float4 cf = live ? __ldg(args.coef + me) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                const int lab = live && args.label ? __ldg(args.label + me) - args.v0 - col : -1;
+                const bool live = row < x.rows;
+                const float4 cf = live ? __ldg(args.coef + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                const int lab = live && args.label ? __ldg(args.label + at) - args.v0 - col : -1;
                 if (live) {
                     float there = 0.0f;  // the value at the label, whose first term cancels where it is formed as the others are
                     if (lab >= 0 && lab < 128) {
@@ -464,7 +461,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 #pragma unroll
                         for (int i = 0; i < 128; ++i)
                             if (i == lab) l = v[i];
-                        there = __ldg(args.at_label + me);
+                        there = __ldg(args.at_label + at);
                         if (STATS2) there = fmaf(cf.z, ex2(fmaf(l, args.c2, -cf.w)), there);
                     }
 #pragma unroll
@@ -488,7 +485,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     for (int i = 0; i < 128; ++i) v[i] = 0.0f;
                 }
                 const int r0 = row - lane;
-                if (again) {
+                if (PARTS == 1 && args.two && (lane & HEAD_HALF)) {  // the token's second row: what rounding leaves of the first
 #pragma unroll
                     for (int i = 0; i < 128; ++i) v[i] -= __bfloat162float(__float2bfloat16_rn(v[i]));
                 }
@@ -499,8 +496,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 }
             } else if (MODE == HEAD_DZ && args.dz && x.part < 0) {
                 // straight into the tokens' rows
-                if (row < x.rows) {
-                    const long long o = ((long long)x.t * args.N + __ldg(args.map + at)) * args.d + col;
+                const int to = row < x.rows ? __ldg(args.map + at) : -1;
+                if (to >= 0) {
+                    const long long o = ((long long)x.t * args.N + to) * args.d + col;
 #pragma unroll
                     for (int i = 0; i < 128; i += 8) {
                         if (col + i >= args.d) break;

@@ -289,9 +289,10 @@ def test_entries_out_of_reach(N):
     assert np.all(np.abs(np64(o["ce"]) - r["ce"]) <= 2 * D + 2e-6 + 2.0 ** -22 * np.abs(r["ce"]))
 
 
-@pytest.mark.parametrize("size", [(1, 1, 700, 128, 0, 1.0), (2, 3, 5003, 72, 9, 2.0), (90, 16, 600, 264, 5, 1.0)], ids=str)
+@pytest.mark.parametrize("size", [(1, 1, 700, 128, 0, 1.0), (2, 3, 5003, 72, 9, 2.0), (90, 16, 600, 264, 5, 1.0), (2, 17, 5003, 136, 9, 2.0),
+                                  (1, 31, 700, 72, 0, 1.0), (3, 128, 2000, 64, 3, 1.0), (1, 97, 40000, 264, 4, 0.5)], ids=str)
 def test_few_tokens_gradients(size):
-    """At most 16 tokens a head: dl, of which few values make most of the gradient, is kept to 2^-16 in bf16 problems."""
+    """At most 128 tokens a head: dl, of which few values make most of the gradient, is kept to 2^-16 in bf16 problems."""
     T, N, V, d, K, tau = size
     p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, "bf16"), vm.head_config(V, K, tau)
     z, w, s = _inputs(T, N, V, d, K, "bf16", False, True, True, seed=7)
