@@ -33,12 +33,14 @@ constexpr int HB = HEAD_TILE;
 static_assert(BK == HEAD_BLOCK, "HEAD_DW's last block of tokens");
 constexpr int HG_ROWS = 32;  // row tiles that share a column tile
 
-// Blocks of 64 of a tile's sum that the tensor cores add up by themselves: all, or in fp32 the five small products of
-// parts and then two at a time of the large one.
-template <int PARTS>
-__device__ __forceinline__ int sums_of(int kb) { return kb == 0 ? 0 : PARTS == 1 ? 1 : 1 + (kb + 1) / 2; }
-template <int PARTS>
-__device__ __forceinline__ int sum_end(int kb, int i) { return PARTS == 1 ? kb : min(6 * kb, 5 * kb + 2 * i); }
+// Blocks of 64 of a tile's sum that the tensor cores add up by themselves: all, with SHORT two at a time, or in fp32 the five
+// small products of parts and then two at a time of the large one.
+template <int PARTS, bool SHORT>
+__device__ __forceinline__ int sums_of(int kb) { return kb == 0 ? 0 : SHORT ? (kb + 1) / 2 : PARTS == 1 ? 1 : 1 + (kb + 1) / 2; }
+template <int PARTS, bool SHORT>
+__device__ __forceinline__ int sum_end(int kb, int i) {
+    return SHORT ? min(kb, 2 * i + 2) : PARTS == 1 ? kb : min(6 * kb, 5 * kb + 2 * i);
+}
 
 struct HeadShape {
     static constexpr uint32_t A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
@@ -156,8 +158,8 @@ __device__ __forceinline__ float ex2(float v) {
     return v;
 }
 
-// STATS2: labels and a teacher at another temperature.  PARTS: 1 or 3.
-template <int MODE, bool STATS2, int PARTS>
+// STATS2: labels and a teacher at another temperature.  PARTS: 1 or 3.  SHORT: see sums_of.
+template <int MODE, bool STATS2, int PARTS, bool SHORT = false>
 __global__ void __launch_bounds__(THREADS, 1)
 head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                  const __grid_constant__ CUtensorMap tmD, HeadGemm args) {
@@ -290,9 +292,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             Cursor<MODE> cur(args, cid, ncl);
             HTile x;
             while (ok && cur.next(args, x)) {
-                const int kb = x.kb1 - x.kb0, sums = sums_of<PARTS>(kb);  // none without a token: the epilogue writes zeros
+                const int kb = x.kb1 - x.kb0, sums = sums_of<PARTS, SHORT>(kb);  // none without a token: the epilogue writes zeros
                 for (int i = 0, k = 0; i < sums && ok; ++i, ++it) {
-                    const int acc = it & 1, end = sum_end<PARTS>(kb, i);
+                    const int acc = it & 1, end = sum_end<PARTS, SHORT>(kb, i);
                     if (!wait_phase(bar_tempty(acc), (uint32_t)((it >> 1) & 1) ^ 1u, abort_flag, args.status)) {
                         ok = false;
                         break;
@@ -346,8 +348,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             float v[128];
             const int row = x.m * HB + (int)rank * 128 + q * 32 + lane, col = x.n * HB + half * 128;
             const long long at = (long long)x.t * args.Np + row;
-            const int sums = sums_of<PARTS>(x.kb1 - x.kb0);
-            if (PARTS > 1 || sums == 0) {
+            const int sums = sums_of<PARTS, SHORT>(x.kb1 - x.kb0);
+            if (PARTS > 1 || SHORT || sums == 0) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] = 0.0f;
             }
@@ -367,7 +369,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                 if (!(ok = wait_phase(bar_tfull(acc), (uint32_t)((it >> 1) & 1), abort_flag, args.status))) break;
                 tc_fence_after();
                 const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * HB + half * 128);
-                if (PARTS == 1) {
+                if (PARTS == 1 && !SHORT) {
                     if (MODE == HEAD_STATS) {
                         for (; ent < ents; ent += 32) {  // their columns, by the column
                             const unsigned mine = ent + lane < ents ? __ldg(list + ent + lane) : 0u;
@@ -402,7 +404,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], HEAD_HALF);
             }
-            if (MODE == HEAD_STATS && PARTS > 1) {
+            if (MODE == HEAD_STATS && (PARTS > 1 || SHORT)) {
                 for (; ent < ents; ++ent) {
                     const unsigned what = __ldg(list + ent);
                     if (lane != (int)(what & 31u)) continue;
@@ -551,9 +553,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
 }
 
 // SM pairs that run the kernel at once on the current device, its shared memory granted first; 0: the query fails.
-template <int MODE, bool STATS2, int PARTS>
+template <int MODE, bool STATS2, int PARTS, bool SHORT = false>
 int pairs_of(cudaLaunchConfig_t *cfg, cudaLaunchAttribute (&attr)[2]) {
-    auto kern = head_gemm_kernel<MODE, STATS2, PARTS>;
+    auto kern = head_gemm_kernel<MODE, STATS2, PARTS, SHORT>;
     static std::atomic<int> smem_limit[64], fits[64];
     if (raise_smem_limit((const void *)kern, smem_limit, (int)HeadShape::SMEM_BYTES) != VMOE_OK) return 0;
     int dev = 0;
@@ -578,19 +580,19 @@ int pairs_of(cudaLaunchConfig_t *cfg, cudaLaunchAttribute (&attr)[2]) {
     return n;
 }
 
-template <int MODE, bool STATS2, int PARTS>
+template <int MODE, bool STATS2, int PARTS, bool SHORT = false>
 int launch(const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &md, const HeadGemm &g, long long tiles,
            cudaStream_t s, const char *name) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    const int fits = pairs_of<MODE, STATS2, PARTS>(&cfg, attr);
+    const int fits = pairs_of<MODE, STATS2, PARTS, SHORT>(&cfg, attr);
     if (!fits) return VMOE_ERR_CUDA;
     const int pairs = g.pairs ? g.pairs : (int)(tiles < fits ? tiles : fits);
     cfg.stream = s;
     cfg.gridDim = dim3((unsigned)(2 * pairs));
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
     trace_before(s, name);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, STATS2, PARTS>, ma, mb, md, g);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, head_gemm_kernel<MODE, STATS2, PARTS, SHORT>, ma, mb, md, g);
     trace_after(s);
     return e == cudaSuccess ? VMOE_OK : VMOE_ERR_CUDA;
 }
@@ -626,6 +628,12 @@ int launch_head_gemm(int mode, const HeadPlan &h, HeadGemm g, const __nv_bfloat1
     if (mode == HEAD_STATS || mode == HEAD_DLOGITS) {
         g.tiles_n = tn_v;
         if (!make_map(&ma, z, h.d, h.Np, batches, 128) || !make_map(&mb, w, h.d, h.V, batches, 128)) return VMOE_ERR_CUDA;
+        // No more than a tile a pair: short sums cost half a microsecond, and what the tensor cores cut from a long one does not
+        // reach the losses: kl of 46 tokens, 9055 entries, d 840, is off by 3e-7 instead of 1.75e-6.  With more tiles their reads
+        // do not hide behind the next tile's products: 17 tasks of 1576 tokens, 6 and 4 blocks at a time, 809 and 876 us for 726.
+        if (mode == HEAD_STATS && !f32 && tm * tn_v <= num_sms() / 2)
+            return h.stats == 2 ? launch<HEAD_STATS, true, 1, true>(ma, mb, ma, g, tm * tn_v, s, "head_stats")
+                                : launch<HEAD_STATS, false, 1, true>(ma, mb, ma, g, tm * tn_v, s, "head_stats");
         if (mode == HEAD_STATS)
             return h.stats == 2 ? (f32 ? launch<HEAD_STATS, true, 3>(ma, mb, ma, g, tm * tn_v, s, "head_stats")
                                        : launch<HEAD_STATS, true, 1>(ma, mb, ma, g, tm * tn_v, s, "head_stats"))
