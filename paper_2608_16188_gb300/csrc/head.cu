@@ -403,7 +403,7 @@ struct Finish {
     Sizes z;
     int halves, pitch;  // half tiles of the vocabulary, and as the sums are laid out
     int stats;
-    float inv_tau, c1;
+    float inv_tau, c1, c2;  // c2: of the teacher's sum
     const int *rows, *map, *label;
     const float2 *part, *part2;
     const float *picked, *tl;
@@ -453,6 +453,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
     constexpr int SHARES = HG_THREADS / ROWS;  // threads of a row
     __shared__ float2 sm[2][HG_THREADS / 32][ROWS];
     __shared__ float tl[ROWS];
+    __shared__ float2 top[ROWS];  // the teacher's sum, in units of log2: largest logit, logarithm
     constexpr bool DOT = !std::is_void<DOTS>::value;
     __shared__ float dots[DOT ? ROWS : 1][DOT ? HEAD_K : 1];
     const int t = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row_in = lane % ROWS;
@@ -485,8 +486,9 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
             join(m, s, sm[0][q][lane]);
             join(m2, s2, sm[1][q][lane]);
         }
-        const float ls = log2f(s), a = (m + ls) * LN2, b = p2 ? (m2 + log2f(s2)) * LN2 : a;
-        tl[lane] = b;
+        const float ls = log2f(s), a = (m + ls) * LN2;
+        top[lane] = p2 ? make_float2(m2, log2f(s2)) : make_float2(m, ls);
+        tl[lane] = (top[lane].x + top[lane].y) * LN2;
         if (row < n && f.ce) {
             const long long at = (long long)t * z.Np + row, tn = (long long)t * z.N + f.map[at];
             const bool has = f.label[at] >= 0;
@@ -522,7 +524,8 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
             float l = 0.0f;
             if (j < z.K && q.i[mm] >= 0) l = DOT ? dots[DOT ? i : 0][DOT ? j : 0] : f.tl[at * z.K + j];
             if (j >= z.K) continue;
-            const float lp = q.i[mm] >= 0 ? l * f.inv_tau - tl[i] : 0.0f;
+            // not l / tau - tlse, whose difference of large numbers is off by 2e-6 where a sure teacher and a sure model leave p - q
+            const float lp = q.i[mm] >= 0 ? (fmaf(l, f.c2, -top[i].x) - top[i].y) * LN2 : 0.0f;
             f.logp[tn * z.K + j] = lp;
             // an entry of no weight adds nothing, whatever its logarithm
             if (q.q[mm] > 0.0f || q.q[mm] != q.q[mm]) loss += q.q[mm] * (q.lq[mm] - lp);
@@ -821,6 +824,7 @@ int launch_head_loss(const Dims &p, const HeadPlan &h, const HeadIn &in, float *
     f.stats = h.stats;
     f.inv_tau = 1.0f / h.tau;
     f.c1 = h.c1;
+    f.c2 = h.stats == 2 ? h.c2 : h.c1;
     f.rows = g.rows;
     f.map = at<int>(ws, h.map);
     f.label = at<int>(ws, h.label);
