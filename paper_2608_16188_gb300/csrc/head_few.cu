@@ -126,7 +126,7 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const W *__r
 #pragma unroll
                 for (int n = 0; n < NT; ++n) x[u][n].load(row[n] + k0 + 32 * u, k0 + 32 * u + 8 * q < d);
             // 128 k at a time: the products cut every step of their sums towards zero (all 1024 in one: ce off by 1.1e-6; so 1e-7);
-            // fp32: the five small products of parts apart from the large one
+            // fp32: the large product 32 at a time (128: logits off by 3e-7 of themselves), the five small ones apart
             float acc[NT][4] = {}, low[NT][4] = {};
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -150,12 +150,19 @@ head_few_kernel(HeadGemm args, const __nv_bfloat16 *__restrict__ z, const W *__r
                         product(low[n], 1, 0), product(low[n], 0, 1);
                     }
                     product(acc[n], 0, 0);
+                    if constexpr (PARTS == 3) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sum[n][i] += acc[n][i];
+                            acc[n][i] = 0.0f;
+                        }
+                    }
                 }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[n][i] += PARTS == 3 ? acc[n][i] + low[n][i] : acc[n][i];
+                for (int i = 0; i < 4; ++i) sum[n][i] += PARTS == 3 ? low[n][i] : acc[n][i];
         }
         // columns v0 + 8 n + 2 q, + 1 of tokens g (0, 1) and g + 8 (2, 3)
 #pragma unroll
