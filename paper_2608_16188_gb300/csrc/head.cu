@@ -195,7 +195,9 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
             if (f.kl) f.kl[tn] = f.tlse[tn] = 0.0f;
         }
         if (in && f.coef) {
-            float4 c = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            // a term that the token does not have: weight 0, and a logarithm that takes its exponential to 0 whatever the logit (from
+            // 0 it would be infinite at logits over 88, and 0 times it NaN)
+            float4 c = make_float4(0.0f, INFINITY, 0.0f, INFINITY);
             float there = 0.0f;
             if (y >= 0) {
                 const float dce = f.dce ? f.dce[tn] : 0.0f, dlse = f.dlse ? f.dlse[tn] : 0.0f;

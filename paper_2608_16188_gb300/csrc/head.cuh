@@ -54,7 +54,7 @@ struct HeadGemm {
     const int *off;               // [T][Np / 32][2 tiles_n + 1] where each half tile's entries of 32 rows begin in list
     const unsigned *list;         // [T][Np / 32][32 K] row | column in the half tile << 5 | entry << 12
     float *tl;
-    const float4 *coef;           // HEAD_DLOGITS: a, lse times log2(e), b, tlse times log2(e) of a row
+    const float4 *coef;           // HEAD_DLOGITS: a, lse times log2(e), b, tlse times log2(e) of a row; infinite logarithms where a, b is 0
     const float *at_label;        // the first sum's share of the gradient there
     float *out;                   // HEAD_DZ: in pieces [T][Np][d], else [pairs][256][256] parts of tiles; HEAD_DW, fp32: [T][V][d]
     void *dz;                     // HEAD_DZ in one go: [T][N][d], row map[t][r] of it

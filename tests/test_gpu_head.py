@@ -81,7 +81,7 @@ def _run(p, head, z, w, s, nbytes=None, stream=None, train=True, dz=True):
     return o
 
 
-def _check(o, z, w, s, tau, dtype, few=False):
+def _check(o, z, w, s, tau, dtype, few=False, flushed=0.0):
     r = ref.loss(z, w, s["label"], s["tidx"], s["tlogit"], tau)
     part = r["has"] | r["taught"]
     T, N, V = r["logits"].shape
@@ -108,7 +108,7 @@ def _check(o, z, w, s, tau, dtype, few=False):
         assert np.all(np.abs(np64(o["kl"]) - r["kl"]) <= qt + 2e-6 * r["taught"])
     dl, size = ref.dlogits(r, s["label"], s["tidx"], tau, s["dce"], s["dlse"], s["dkl"])
     dz, dw = ref.back(dl, z, w, part)
-    err = size_err[..., None] * size + (2.0 ** -23 if f32 else 2.0 ** -16 if few else 2.0 ** -8) * np.abs(dl)
+    err = size_err[..., None] * size + (2.0 ** -23 if f32 else 2.0 ** -16 if few else 2.0 ** -8) * np.abs(dl) + flushed
     steps = 6 if f32 else 1
     if o.get("dz") is not None:
         got = np64(o["dz"])
@@ -192,6 +192,30 @@ def test_wide_logits():
     p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, "bf16"), vm.head_config(V, 6, 2.0)
     r = _check(_run(p, head, z, w, s), z, w, s, 2.0, "bf16")
     assert r["ce"].max() > 100 and r["ce"].min() < 1e-3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("N", [40, 200])
+def test_wide_logits_of_tokens_without_a_label_or_a_teacher(N, tau, dtype):
+    """Logits of hundreds, a third of the tokens with a label alone, a third with a teacher alone, a third with both: all
+    gradients together, each by itself, and each left out.  exp of a logit that nothing is taken from is infinite here.
+
+    Of logits so wide many p lie at the end of fp32's range: an exponential below 2^-126 is 0 (ex2.approx.ftz), and its weight
+    is below 1, so a dl of two of them is off by up to 2 * 2^-126; its parts and their products with z or w, where they are
+    that small, by as much again: 2^-124 a dl, beside the relative bounds."""
+    T, V, d, K = 2, 900, 64, 6
+    z, w, s = _inputs(T, N, V, d, K, dtype, N == 200, True, False, seed=8)
+    z = z * 40
+    s["label"][:, 0::3], s["tidx"][:, 1::3] = -1, -1
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, dtype), vm.head_config(V, K, tau, N == 200)
+    r = ref.loss(z, w, s["label"], s["tidx"], s["tlogit"], tau)
+    assert np.abs(r["logits"]).max(axis=(1, 2)).min() > 200 and (r["has"] != r["taught"]).mean() > 0.6
+    for given in (("dce", "dlse", "dkl"), ("dce",), ("dlse",), ("dkl",), ("dce", "dkl"), ("dce", "dlse")):
+        one = dict(s, **{n: s[n] if n in given else None for n in ("dce", "dlse", "dkl")})
+        o = _run(p, head, z, w, one)
+        assert torch.isfinite(o["dz"]).all() and torch.isfinite(o["dw"]).all(), given
+        _check(o, z, w, one, tau, dtype, flushed=2.0 ** -124)
 
 
 def test_stream_graph_and_two_at_once():
