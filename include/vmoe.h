@@ -374,10 +374,11 @@ typedef struct {
  * Equal values go to the lower index, and what is larger is decided in exact
  * arithmetic (64 bits), not by fp32 roundings of s.  The bias acts on the choice
  * alone.  An expert whose logit or bias is not finite (-inf, say) is switched off: never
- * chosen, 0 in a softmax.  Where fewer than k experts can be chosen, the rest of the
- * token's choices have expert_idx -1, gate 0 and slot -1 and take no capacity; the
- * other entry points pass over them.  So it is for all choices of a token whose
- * token_mask is 0, whose logits may hold anything.
+ * chosen; a logit that is not finite is 0 in a softmax too, a bias takes nothing from the
+ * softmax, whose sum keeps the expert.  Where fewer than k experts can be chosen, the
+ * rest of the token's choices have expert_idx -1, gate 0 and slot -1 and take no
+ * capacity; the other entry points pass over them.  So it is for all choices of a token
+ * whose token_mask is 0, whose logits may hold anything.
  *   x, w_router, logit_bias, logits, expert_idx, gate, slot, load as for vmoe_route;
  *   select_bias [T,E] fp32 nullable; token_mask [T,N] uint8 nullable;
  *   demand [T,E] int32 out, nullable: choices of each expert, dropped ones too;

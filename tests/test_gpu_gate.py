@@ -93,6 +93,39 @@ def test_padding_ties_and_switched_off_experts(shape, score):
         _check(o, ref)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k", [2, 6])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_experts_switched_off_by_a_bias(score, k, dtype):
+    """Gates without renormalisation: an expert whose bias is -inf or NaN is not chosen and stays in a softmax's sum, one whose
+    logit is -inf does not; the gradient by the logits is that of these gates."""
+    T, N, E, d = 2, 90, 16, 64
+    g = torch.Generator().manual_seed(k)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    logits, bias = torch.randn(T, N, E, generator=g), 0.1 * torch.randn(T, E, generator=g)
+    logits[:, :, 3] += 3.0  # most of the softmax's sum
+    bias[:, 3], bias[1, 5] = float("-inf"), float("nan")
+    logits[:, :, 7] = float("-inf")
+    p = vm.problem(T, N, d, 8, E, k, 1.5, dtype, vm.VMOE_LOGITS_IN | vm.VMOE_NO_RENORM)
+    C, cfg = vm.vmoe_problem_capacity(p), vm.gating(score, scale=1.5)
+    o = _run(p, cfg, logits.cuda(), bias.cuda(), None)
+    ref = gating.choose(logits, bias, None, k, C, score, renorm=False, scale=1.5)
+    _check(o, ref)
+    assert not np.isin(ref["idx"], (3, 7)).any() and not (ref["idx"][1] == 5).any()
+    if score == "softmax":  # the sum of all gates would be 1.5 without the expert that is off
+        assert ref["gate"].sum(axis=2).max() < 1.3
+    x, dy, dx_in = (torch.randn(T, N, d, generator=g).to(dt) for _ in range(3))
+    ye, wr = torch.randn(T, E, C, d, generator=g).to(dt), torch.randn(T, d, E, generator=g) / d ** 0.5
+    r = _bwd(p, cfg, o, x.cuda(), wr.cuda(), dy.cuda(), ye.cuda(), dx_in.cuda())
+    b = gating.choose_bwd(ref, logits, x, wr, dy, ye, score, False, 1.5)
+    size = (np.linalg.norm(np64(dy), axis=2) * np.linalg.norm(np64(ye), axis=3).max()).max()  # at least sum |dy ye|
+    tol = 4e-6 * (np.abs(b["dgate"]).max(axis=2) + np.abs(ref["share"] * b["dgate"]).sum(axis=2)) + 2 * (d / 32 + 8) * 2.0 ** -24 * size
+    assert np.all(np.abs(np64(r["dlogits"]) - b["dlogits"]) <= 1.5 * tol[:, :, None])
+    assert rel_err(r["dw_router"], b["dw_router"], groups=T) <= F32_TOL
+    assert (np64(r["dlogits"])[:, :, 7] == 0).all()
+    assert (np64(r["dlogits"])[:, :, 3] != 0).any() == (score == "softmax")
+
+
 @pytest.mark.parametrize("groups", [1, 4])
 def test_choices_closer_than_fp32(groups):
     """s + b of two experts apart by less than a step of fp32: the larger one in exact arithmetic comes first."""
