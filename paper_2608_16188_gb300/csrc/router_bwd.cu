@@ -938,7 +938,7 @@ router_dw_mma_kernel(Dims p, const __nv_bfloat16 *__restrict__ x,
         sm.bias_sum[tid] = b;
     }
     cluster.sync();
-    // rank r writes rows [32 r, 32 r + 32) of the tile, summing ranks 0..3 in order
+    // rank r writes rows [ROWS r, ROWS r + ROWS) of the tile, summing the SPLIT ranks in order
     float *dwt = dw + (long long)t * d * E;
     constexpr int ROWS = DW_BD / SPLIT;
     for (int v = tid; v < ROWS * DW_BE; v += DW_THREADS) {
@@ -1090,28 +1090,44 @@ int launch_router_dw_simt(const Dims &p, const float *x, const float *dl, float 
 }
 
 template <int SPLIT>
-int launch_dw_mma(const Dims &p, const __nv_bfloat16 *x, const float *dl, float *dw, float *dbias, cudaStream_t s) {
+cudaLaunchConfig_t dw_config(const Dims &p, cudaLaunchAttribute (&attr)[1], cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(SPLIT, (p.d + DW_BD - 1) / DW_BD, p.T * ((p.E + DW_BE - 1) / DW_BE));
     cfg.blockDim = dim3(DW_THREADS);
     cfg.stream = s;
-    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = SPLIT;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (SPLIT > 8) {  // above the portable size
-        static std::atomic<int> allowed[64];
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return VMOE_ERR_CUDA;
-        if (!allowed[dev].load(std::memory_order_relaxed)) {
-            if (cudaFuncSetAttribute(router_dw_mma_kernel<SPLIT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-                return VMOE_ERR_CUDA;
-            allowed[dev].store(1, std::memory_order_relaxed);
-        }
+    return cfg;
+}
+
+// Whether the current device can place a cluster of 16: that is above the portable size, and a device may have no 16 SMs
+// left that lie together.  Asked once a device.
+bool dw_fits_16(const Dims &p) {
+    static std::atomic<int> known[64];  // 1: it can, 2: it cannot
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    int v = known[dev].load(std::memory_order_relaxed);
+    if (!v) {
+        auto kern = router_dw_mma_kernel<16>;
+        cudaLaunchAttribute attr[1];
+        const cudaLaunchConfig_t cfg = dw_config<16>(p, attr, nullptr);
+        int n = 0;
+        const bool ok = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0;
+        if (!ok) cudaGetLastError();
+        known[dev].store(v = ok ? 1 : 2, std::memory_order_relaxed);
     }
+    return v == 1;
+}
+
+template <int SPLIT>
+int launch_dw_mma(const Dims &p, const __nv_bfloat16 *x, const float *dl, float *dw, float *dbias, cudaStream_t s) {
+    cudaLaunchAttribute attr[1];
+    const cudaLaunchConfig_t cfg = dw_config<SPLIT>(p, attr, s);
     return cudaLaunchKernelEx(&cfg, router_dw_mma_kernel<SPLIT>, p, x, dl, dw, dbias) == cudaSuccess ? VMOE_OK : VMOE_ERR_CUDA;
 }
 
@@ -1130,6 +1146,7 @@ int launch_router_dw(const Dims &p, const void *x, const float *dlogits, float *
         const long long tiles = (long long)((p.d + DW_BD - 1) / DW_BD) * p.T * ((p.E + DW_BE - 1) / DW_BE);
         int split = DW_SPLIT;
         while (split < splits && tiles * split < 2LL * num_sms() && p.N >= split * 16 * DW_KC) split *= 2;
+        if (split > 8 && !dw_fits_16(p)) split = 8;
         const __nv_bfloat16 *xb = (const __nv_bfloat16 *)x;
         st = split <= 4   ? launch_dw_mma<4>(p, xb, dlogits, dw, dbias, s)
              : split <= 8 ? launch_dw_mma<8>(p, xb, dlogits, dw, dbias, s)

@@ -200,6 +200,24 @@ def test_gate_bwd_parity(shape, score, renorm, dtype):
     assert torch.equal(r2["dlogits"], more + r["dlogits"])
 
 
+@pytest.mark.parametrize("N", [2047, 2048, 4095, 4097, 9001])
+def test_router_gradient_of_many_tokens_in_few_tiles(N):
+    """A tile's tokens over 4, 8 and 16 CTAs, with an odd rest."""
+    T, d, E, k = 1, 136, 8, 2
+    g = torch.Generator().manual_seed(N)
+    p = vm.problem(T, N, d, 8, E, k, 1.0, "bf16", vm.VMOE_LOGITS_IN)
+    C, cfg = vm.vmoe_problem_capacity(p), vm.gating("sigmoid")
+    logits = torch.randn(T, N, E, generator=g)
+    x, dy, dx_in = (torch.randn(T, N, d, generator=g).to(torch.bfloat16) for _ in range(3))
+    ye, wr = torch.randn(T, E, C, d, generator=g).to(torch.bfloat16), torch.randn(T, d, E, generator=g) / d ** 0.5
+    o = _run(p, cfg, logits.cuda(), None, None)
+    ref = gating.choose(logits, None, None, k, C, "sigmoid")
+    _check(o, ref)
+    r = _bwd(p, cfg, o, x.cuda(), wr.cuda(), dy.cuda(), ye.cuda(), dx_in.cuda())
+    b = gating.choose_bwd(ref, logits, x, wr, dy, ye, "sigmoid")
+    assert rel_err(r["dw_router"], b["dw_router"]) <= F32_TOL and rel_err(r["dbias"], b["dbias"]) <= F32_TOL
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 384), ("f32", 200)])
 def test_from_tokens_and_through_the_layer(dtype, d):
     """Logits from tokens are vmoe_route's bit for bit; dispatch and combine pass over choices that there are not."""
