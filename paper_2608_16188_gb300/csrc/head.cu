@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
 #pragma unroll
     for (int i = 0; i < HG_THREADS / 32; ++i) before += sum[0][i], total += sum[1][i];
     const int whole = (total + HEAD_HALF - 1) / HEAD_HALF * HEAD_HALF, rows = f.two ? two_row(whole) : total;
-    if (blockIdx.x == 0 && tid == 0) f.rows[t] = rows;
+    if (blockIdx.x == 0 && tid == 0) f.rows[t] = rows, f.rows[z.T + t] = total;
     const int n = n0 + tid;
     if (tid < HP_TOKENS) to[tid] = -1;
     if (tid < HP_TOKENS && n < z.N) {  // a token a thread
@@ -270,14 +270,10 @@ __global__ void __launch_bounds__(HG_THREADS) head_pack_kernel(Pack f, const T *
             if (to[i / z.K] < 0) f.logp[(t0 + n0) * z.K + i] = 0.0f;
     // the rest of HEAD_DW's last block of tokens, whose sum has zeros times these; elsewhere a row reaches nothing but what is
     // its own, and nobody reads that.  (Whole tiles for everybody: a head of 8 tokens, d 1024, fp32, 30 us a call.)
-    if (f.two)  // rows without a token among the first
+    if (f.two)  // rows without a token among the first; HEAD_DLOGITS leaves zeros there
         for (int r = 2 * total + blockIdx.x * (HG_THREADS / 32) + warp; r < 2 * whole; r += gridDim.x * (HG_THREADS / 32)) {
             const long long at = (long long)t * z.Np + two_row(r >> 1) + (r & 1) * HEAD_HALF;
-            if (lane == 0) {
-                f.map[at] = -1;
-                if (f.out_label) f.out_label[at] = -1;
-                f.coef[at] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
+            if (lane == 0) f.map[at] = -1;
             for (int c = lane * 8; c < z.d; c += 256) *reinterpret_cast<uint4 *>(f.out + at * z.d + c) = make_uint4(0, 0, 0, 0);
         }
     if (!f.fill) return;
@@ -734,7 +730,7 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
         o += (n + 255) & ~(size_t)255;
         return a;
     };
-    h.rows = take((size_t)h.T * 4);
+    h.rows = take((size_t)h.T * 8);
     h.mark = take((size_t)h.T * ((h.N + 31) / 32) * 8);
     h.pos = take((size_t)h.T * h.N * 4);
     h.map = take(rowsp * 4);

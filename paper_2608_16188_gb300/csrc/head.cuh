@@ -14,6 +14,7 @@ constexpr int HEAD_FEW = 16;    // tokens of a head at most for head_few
 // second what rounding takes from the first: it is then kept to 2^-16, and the sums need no other code.  map is -1 for the second.
 constexpr int HEAD_HALF = 16;
 __host__ __device__ constexpr int two_row(int r) { return 2 * HEAD_HALF * (r / HEAD_HALF) + r % HEAD_HALF; }
+__host__ __device__ constexpr int two_token(int row) { return HEAD_HALF * (row / (2 * HEAD_HALF)) + row % HEAD_HALF; }
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
 constexpr int HEAD_BLOCK = 64;  // of its sum that are loaded at a time
 
@@ -40,7 +41,7 @@ enum { HEAD_STATS = 0, HEAD_DLOGITS = 1, HEAD_DZ = 2, HEAD_DW = 3 };
 struct HeadGemm {
     int T, Np, V, d, parts, np;   // np: products of parts
     int two;
-    const int *rows;              // [T] tokens that take part
+    const int *rows;              // [2][T] rows of tokens that take part, and those tokens
     int v0, vn;                   // the piece: first column, columns
     int tiles_n, tiles_m;         // tiles of columns; HEAD_DW: of rows
     int pairs, first;             // HEAD_DZ: SM pairs; whether this is the first piece

@@ -454,7 +454,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                     args.part2[o] = make_float2(ref2, (s2[0] + s2[1]) + (s2[2] + s2[3]));
                 }
             } else if (MODE == HEAD_DLOGITS) {
-                const bool live = row < x.rows;
+                // a row of zeros among those of two a token is none: times an infinite weight it has a logit of NaN
+                const bool live = PARTS == 1 && args.two ? two_token(row) < __ldcg(args.rows + args.T + x.t) : row < x.rows;
                 const float4 cf = live ? __ldg(args.coef + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 const int lab = live && args.label ? __ldg(args.label + at) - args.v0 - col : -1;
                 if (live) {

@@ -322,3 +322,23 @@ def test_few_tokens_gradients(size):
     z, w, s = _inputs(T, N, V, d, K, "bf16", False, True, True, seed=7)
     _check(_run(p, head, z, w, s), z, w, s, tau, "bf16", few=True)
     _check(_run(p, head, z, w, s, vm.vmoe_head_min_workspace_size(p, head)), z, w, s, tau, "bf16", few=True)
+
+
+@pytest.mark.parametrize("value", ["-inf", "lowest"])
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("N", [5, 40, 150])
+def test_entries_switched_off(N, dtype, value):
+    """Weights of -inf, and of the type's lowest value, against tokens of positive values: losses and gradients are those of the
+    other entries alone.  dz of bf16 weights of -inf is 0 times them, which the header leaves out."""
+    T, V, d, K, tau = 2, 600, 64, 4, 2.0
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, dtype), vm.head_config(V, K, tau)
+    z, w, s = _inputs(T, N, V, d, K, dtype, False, True, False, seed=5)
+    z = z.abs() + 1
+    s["label"], s["tidx"] = s["label"] % 100, s["tidx"] % 100
+    cut = torch.zeros(V, dtype=torch.bool)
+    cut[128:256] = cut[500:] = True
+    lost = w.clone()
+    lost[:, cut] = float("-inf") if value == "-inf" else torch.finfo(w.dtype).min
+    o = _run(p, head, z, lost, s, dz=dtype == "f32" or value == "lowest")
+    assert torch.all(o["dw"][:, cut] == 0)
+    _check(dict(o, dw=o["dw"][:, ~cut]), z, w[:, ~cut].contiguous(), s, tau, dtype, flushed=2.0 ** -124)
