@@ -444,6 +444,9 @@ typedef struct {
  *   vmoe_head_workspace_size(p, head) bytes for this call and the backward, or of any
  *   size from vmoe_head_min_workspace_size(p, head) on (else VMOE_ERR_INVALID): the
  *   backward then takes the vocabulary in more pieces.
+ * An entry may be switched off by weights of the type's lowest value, or -inf, where the
+ * tokens that take part have positive values: it then adds nothing to the sums.  dz takes
+ * 0 times them, so bf16 weights have to be finite in the backward.
  * Sums in fp32; fp32 operands are taken as three bf16 parts each, six products of
  * parts (2^-24).  T*N < 2^31 - 256, V <= 2^30, d_model <= 65536 (else
  * VMOE_ERR_UNSUPPORTED).  Of p only T, N, d_model, dtype and the checks matter. */

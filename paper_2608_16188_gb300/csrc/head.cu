@@ -348,11 +348,10 @@ head_split_kernel(long long n, const float *__restrict__ src, __nv_bfloat16 *__r
     for (long long i = ((long long)blockIdx.x * HG_THREADS + threadIdx.x) * 8; i < n; i += (long long)gridDim.x * HG_THREADS * 8) {
         const float4 a = __ldg(reinterpret_cast<const float4 *>(src + i)), b = __ldg(reinterpret_cast<const float4 *>(src + i) + 1);
         const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        __align__(16) __nv_bfloat16 p[3][8];
+        uint4 p[3];
+        split_weights(v, p);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) split3(v[q], p[0][q], p[1][q], p[2][q]);
-#pragma unroll
-        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(out + q * n + i) = *reinterpret_cast<const uint4 *>(p[q]);
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4 *>(out + q * n + i) = p[q];
     }
 }
 

@@ -18,6 +18,25 @@ __host__ __device__ constexpr int two_token(int row) { return HEAD_HALF * (row /
 constexpr int HEAD_TILE = 256;  // rows and columns of a product's tile
 constexpr int HEAD_BLOCK = 64;  // of its sum that are loaded at a time
 
+// Eight fp32 weights as three bf16 parts each.  A part that would round to infinity is the largest finite value: of fp32's lowest
+// value, and of -inf, the usual weights of entries that are switched off, plain rounding leaves -inf and then -inf - -inf, NaN.
+__device__ __forceinline__ void split_weights(const float (&f)[8], uint4 (&o)[3]) {
+    uint32_t w[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a = f[2 * i], b = f[2 * i + 1];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w[q][i]) : "f"(b), "f"(a));
+            const float2 h = unpk2(bf16x2_to_f32x2(w[q][i]));
+            a -= h.x;
+            b -= h.y;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) o[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+}
+
 // Sizes of a call, and where its scratch lies in the workspace (byte offsets).
 struct HeadPlan {
     int T, N, d, V, K;   // heads, tokens of a head (all tasks' with a shared one), width, vocabulary, teacher's entries

@@ -62,20 +62,7 @@ struct Values<3> {
     }
     __device__ __forceinline__ void get(uint4 (&o)[3]) const {
         const float f[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
-        uint32_t w[3][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float a = f[2 * i], b = f[2 * i + 1];
-#pragma unroll
-            for (int q = 0; q < 3; ++q) {
-                w[q][i] = pack_bf16x2(a, b);
-                const float2 h = unpk2(bf16x2_to_f32x2(w[q][i]));
-                a -= h.x;
-                b -= h.y;
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 3; ++q) o[q] = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+        split_weights(f, o);
     }
 };
 

@@ -325,7 +325,7 @@ def test_few_tokens_gradients(size):
 
 
 @pytest.mark.parametrize("value", ["-inf", "lowest"])
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N", [5, 40, 150])
 def test_entries_switched_off(N, dtype, value):
     """Weights of -inf, and of the type's lowest value, against tokens of positive values: losses and gradients are those of the
