@@ -400,8 +400,9 @@ size_t vmoe_gate_workspace_size(const vmoe_problem *p);
  *   softmax: dlogit_{e_j} = gate_j (dgate_j - m); VMOE_NO_RENORM: dlogit_e =
  *   scale s_e (dgate_e - m) for every e, dgate_e 0 unless chosen
  *   dW_r = x^T dlogits, dbias = sum_n dlogits (of logit_bias), dX = dX_in + dlogits W_r^T
- * Other dlogits, and those of a token without choices, are 0.  logits and select_bias
- * have no other part in it.  VMOE_DLOGITS_ADD as for vmoe_router_bwd.
+ * Other dlogits, and those of a token without choices, are 0.  dW_r takes 0 times such a
+ * token's x, which has to be finite; its logits and dY may hold anything.  logits and
+ * select_bias have no other part in it.  VMOE_DLOGITS_ADD as for vmoe_router_bwd.
  *   dx_in, dx [T,N,d] p->dtype, both or neither; dx_in may be dx.  The rest as for
  *   vmoe_router_bwd (w_router is needed with dx, logits always). */
 int vmoe_gate_bwd(const vmoe_problem *p, const vmoe_gating *gating, const void *x, const float *w_router,

@@ -31,7 +31,8 @@ class BlockStack:
     ``balance``: the balance losses' weights, see BalanceBuffers; each block computes its own.
     ``token_mask`` [T,N] uint8: 0 for padding that the losses leave out.  ``gating``: a VmoeGating
     (gating(...)) for experts that are chosen by vmoe_gate, each block with a bias of its own, in
-    ``gates``, which ``update_gates(rate)`` moves; token_mask's padding then goes nowhere.
+    ``gates``, which ``update_gates(rate)`` moves; token_mask's padding then goes nowhere, but passes
+    through the norms and has to be finite.
 
     ``forward(x)`` returns z [T,N,d]; ``backward(dz)`` returns dx and leaves every parameter's
     gradient in ``grads[l][name]``.  Both run on the current stream, or on ``stream``, and write the

@@ -116,7 +116,8 @@ class StepRunner:
     ``b.dlogits`` before each backward.  With ``gating`` (a VmoeGating, or
     GateBuffers with a bias of the caller's) the experts are chosen by vmoe_gate, in
     ``self.gating``; a token whose token_mask is 0 then goes nowhere and takes no
-    capacity.
+    capacity (its x has to be finite all the same: the router's gradient takes 0
+    times it).
     """
 
     def __init__(self, p, inputs, bufs: Buffers | None = None, router_grad: bool = False, balance=None, gating=None):

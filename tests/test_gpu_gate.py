@@ -200,6 +200,31 @@ def test_gate_bwd_parity(shape, score, renorm, dtype):
     assert torch.equal(r2["dlogits"], more + r["dlogits"])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k,renorm", [(1, True), (2, False), (4, True), (6, False)])
+def test_gradient_beside_padding_of_nan(k, renorm, dtype):
+    """Logits, dY and dX_in of NaN at masked tokens: all else is what it is with numbers there."""
+    T, N, d, E = 2, 90, 64, 8
+    g = torch.Generator().manual_seed(k)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    p = vm.problem(T, N, d, 8, E, k, 1.0, dtype, vm.VMOE_LOGITS_IN | (0 if renorm else vm.VMOE_NO_RENORM))
+    C, cfg = vm.vmoe_problem_capacity(p), vm.gating("softmax")
+    mask = torch.rand(T, N, generator=g) < 0.7
+    logits = torch.randn(T, N, E, generator=g)
+    x, dy, dx_in = (torch.randn(T, N, d, generator=g).to(dt) for _ in range(3))
+    ye, wr = torch.randn(T, E, C, d, generator=g).to(dt).cuda(), (torch.randn(T, d, E, generator=g) / d ** 0.5).cuda()
+    out = []
+    for value in (0.0, float("nan")):
+        for t in (logits, dy, dx_in):
+            t[~mask] = value
+        o = _run(p, cfg, logits.cuda(), None, mask.to(torch.uint8).cuda())
+        out.append(dict(o, **_bwd(p, cfg, o, x.cuda(), wr, dy.cuda(), ye, dx_in.cuda())))
+    for n in ("idx", "gate", "slot", "load", "demand", "dgate", "dlogits", "dw_router", "dbias"):
+        assert torch.equal(out[0][n], out[1][n]), n
+    on = mask.cuda()
+    assert torch.equal(out[0]["dx"][on], out[1]["dx"][on]) and torch.isnan(out[1]["dx"][~on]).all()
+
+
 @pytest.mark.parametrize("N", [2047, 2048, 4095, 4097, 9001])
 def test_router_gradient_of_many_tokens_in_few_tiles(N):
     """A tile's tokens over 4, 8 and 16 CTAs, with an odd rest."""
