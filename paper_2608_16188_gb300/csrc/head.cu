@@ -29,6 +29,7 @@ namespace {
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LN2 = 0.6931471805599453f, LOG2E = 1.4426950408889634f;
 constexpr int HG_THREADS = 256, HP_TOKENS = 32, HP_SELF = 2048, HF_DOTS = 16384;
+constexpr float PATCH_TAU = 8.0f;
 static_assert(HP_TOKENS == 32, "a CTA of head_pack has one word of marks");
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -538,6 +539,9 @@ __global__ void __launch_bounds__(HG_THREADS) head_finish_kernel(Finish f) {
 // The teacher's entries in a piece of dl: the whole value, from the stored logarithms, so that neither the order of
 // equal entries nor a label among them matters.  A warp a packed row.  605000 entries of the six-task step: 28 us, single
 // values written into rows that L2 no longer holds.
+// The other softmax at an entry, exp(l - lse), has l from tau (logp + tlse), whose roundings tau multiplies: p is off by
+// tau 2^-24 (|logp| + |tlse|) of itself: 1e-5 at PATCH_TAU, all of it at 10^6.  Above PATCH_TAU l is formed again as a dot product
+// (DOTS: the type of z and w, else void), which reads a row of w an entry: the six-task step's backward 900 -> 1023 us.
 struct Patch {
     Sizes z;
     int v0, vn, piece, parts;
@@ -545,9 +549,12 @@ struct Patch {
     const int *rows, *map;
     const int32_t *label, *tidx;
     const float *tlogit, *ce, *lse, *tlse, *logp, *dce, *dlse, *dkl;
+    const void *dot_z, *dot_w;
     __nv_bfloat16 *dl;
 };
+template <typename DOTS>
 __global__ void __launch_bounds__(HG_THREADS) head_patch_kernel(Patch f) {
+    constexpr bool DOT = !std::is_void<DOTS>::value;
     const int t = blockIdx.y, lane = threadIdx.x & 31, r = blockIdx.x * (HG_THREADS / 32) + (threadIdx.x >> 5);
     const Sizes z = f.z;
     pdl_wait();
@@ -577,10 +584,22 @@ __global__ void __launch_bounds__(HG_THREADS) head_patch_kernel(Patch f) {
                 if (oi == i) all += oq;
             }
         }
-        if (i < f.v0 || i >= f.v0 + f.vn) continue;
+        const bool here = i >= f.v0 && i < f.v0 + f.vn;
+        float l = 0.0f;
+        if constexpr (DOT) {  // eight entries at a time
+            if (y >= 0)
+                for (int j = 0; j < 4; ++j) {
+                    if (!__any_sync(FULL, here && lane / 8 == j)) continue;
+                    const float each = entries_logits(z.d, (const DOTS *)f.dot_z + tn * z.d, (const DOTS *)f.dot_w + (long long)t * z.V * z.d,
+                                                      __shfl_sync(FULL, i, 8 * j + (lane & 7)));
+                    const float mine = __shfl_sync(FULL, each, lane & 7);
+                    if (lane / 8 == j) l = mine;
+                }
+        }
+        if (!here) continue;
         const float lp = f.logp[tn * z.K + lane + 32 * m];
         float v = b * (expf(lp) - all);
-        if (y >= 0) v += i == y ? label_value(f.ce[tn], dce, dlse) : (dce + dlse) * expf(f.tau * (lp + tlse) - lse);
+        if (y >= 0) v += i == y ? label_value(f.ce[tn], dce, dlse) : (dce + dlse) * expf((DOT ? l : f.tau * (lp + tlse)) - lse);
         __nv_bfloat16 *o = row + (i - f.v0);
         if (f.parts < 3) {
             const __nv_bfloat16 hi = __float2bfloat16_rn(v);
@@ -913,8 +932,13 @@ int launch_head_loss_bwd(const Dims &p, const HeadPlan &h, const HeadIn &in, con
             f.dlse = dlse;
             f.dkl = dkl;
             f.dl = dl;
+            f.dot_z = in.z;
+            f.dot_w = in.w;
+            auto kern = !(in.label && h.tau > PATCH_TAU) ? head_patch_kernel<void>
+                        : p.bf16                         ? head_patch_kernel<__nv_bfloat16>
+                                                         : head_patch_kernel<float>;
             trace_before(s, "head_patch");
-            st = launch_kernel(head_patch_kernel, dim3(((h.two ? two_row(h.N - 1) + 1 : h.N) + 7) / 8, h.T), dim3(HG_THREADS), 0, s, f);
+            st = launch_kernel(kern, dim3(((h.two ? two_row(h.N - 1) + 1 : h.N) + 7) / 8, h.T), dim3(HG_THREADS), 0, s, f);
             trace_after(s);
             if (st != VMOE_OK) return st;
         }

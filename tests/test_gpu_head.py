@@ -342,3 +342,20 @@ def test_entries_switched_off(N, dtype, value):
     o = _run(p, head, z, lost, s, dz=dtype == "f32" or value == "lowest")
     assert torch.all(o["dw"][:, cut] == 0)
     _check(dict(o, dw=o["dw"][:, ~cut]), z, w[:, ~cut].contiguous(), s, tau, dtype, flushed=2.0 ** -124)
+
+
+@pytest.mark.parametrize("tau", [30.0, 1e3, 1e6])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,K", [(40, 3), (150, 40)])
+def test_high_temperatures(N, K, dtype, tau):
+    """A model that is sure of an entry in the teacher's list that is not the label: its part of the gradient of ce does not pass
+    through the logarithm at the temperature, whose roundings it would multiply."""
+    T, V, d = 2, 700, 72
+    z, w, s = _inputs(T, N, V, d, K, dtype, True, True, False, seed=9)
+    s["tidx"][..., K - 1] = (s["label"] + 1) % V
+    z = (z.double() + 6 * w.double()[s["tidx"][..., K - 1].long()]).to(w.dtype)
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, dtype), vm.head_config(V, K, tau, True)
+    for nbytes in (None, vm.vmoe_head_min_workspace_size(p, head)):
+        r = _check(_run(p, head, z, w, s, nbytes), z, w, s, tau, dtype)
+    at = np.take_along_axis(r["logits"], s["tidx"][..., K - 1:].numpy().astype(np.int64), 2)[..., 0]
+    assert np.median(np.exp(at - r["lse"])) > 0.5
