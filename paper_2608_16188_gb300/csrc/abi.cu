@@ -460,7 +460,7 @@ static int check_head(const vmoe_problem *p, const vmoe_head *h, Dims *d) {
     int st = check_problem(p, d);
     if (st != VMOE_OK) return st;
     if (!h || h->V < 1 || h->teacher_k < 0 || !(h->temperature > 0.0f) || !isfinite(h->temperature) ||
-        !isfinite(1.0f / h->temperature) || (h->flags & ~(uint32_t)VMOE_HEAD_SHARED))
+        !isfinite((float)(1.4426950408889634 / (double)h->temperature)) || (h->flags & ~(uint32_t)VMOE_HEAD_SHARED))
         return VMOE_ERR_INVALID;
     // offsets within a CTA's tokens (32 rows of d, of several tasks with a shared head) and token numbers are 32 bits
     if (d->d > (1 << 16) || h->V > (1 << 30) || h->teacher_k > HEAD_K || (h->teacher_k > 0 && h->V > HEAD_V) ||

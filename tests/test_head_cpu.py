@@ -88,3 +88,12 @@ def test_head_and_gate_buffers_refuse_what_does_not_fit():
     for bias in (torch.zeros(2, 7), torch.zeros(2, 8, dtype=torch.float64), torch.zeros(8, 2).t()):
         with pytest.raises(ValueError):
             vm.GateBuffers(vm.problem(2, 64, 64, 8, 8, 2, 1.0), vm.gating(), bias, device="cpu")
+
+
+def test_a_temperature_whose_factor_is_infinite():
+    """log2(e) / temperature is what logits are taken times: past fp32's range a logit of 0 would be NaN."""
+    lib, least = vm.library(), vm.vmoe_head_min_workspace_size(_p(), vm.head_config(100, 8, 4.5e-39))
+    assert least > 0
+    for head in (vm.head_config(100, 8, 4e-39), vm.head_config(100, 8, 1e-42)):
+        assert vm.vmoe_head_min_workspace_size(_p(), head) == 0
+        assert _call(lib.vmoe_head_loss, FWD, head) == INVALID and _call(lib.vmoe_head_loss_bwd, BWD, head) == INVALID
