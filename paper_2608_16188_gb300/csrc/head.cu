@@ -731,9 +731,16 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.K = head->teacher_k;
     h.Np = (h.N + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
     h.parts = p.bf16 ? 1 : 3;
-    // A gradient of few tokens hangs on few values of dl, the labels' among them, whose rounding to bf16 (up to 2^-8) does not
-    // average out: one token's dw was off by 0.0029 in the mean, where its own rounding is 0.0018.
-    h.two = p.bf16 && h.N <= HEAD_TILE / 2;
+    // dl is an operand of the tensor cores and in bf16 problems a bf16 value, off by up to 2^-8, 1.6e-3 in the mean, which sums
+    // of independent roundings keep: dz and dw are 2.3e-3 off where their own rounding alone is 1.66e-3.  Two rows a token keep it to
+    // 2^-16 and take twice the products.  That costs nothing up to 128 tokens, which leave half of a tile's rows empty, and little
+    // while the logits' tiles, doubled, are still one a pair (forward and backward, one row a token and two, us: 197 tokens, 1000 entries
+    // 72 and 71, 9000 77 and 84); beyond, it is a choice for the time that bf16 training makes (197 x 128000 236 and 298; 1024 x 40000
+    // 212 and 311; 1024 x 128000 520 and 841).
+    const size_t rows2 = ((size_t)two_row((h.N + HEAD_HALF - 1) / HEAD_HALF * HEAD_HALF) + HEAD_TILE - 1) / HEAD_TILE * HEAD_TILE;
+    h.two = p.bf16 && h.N <= HEAD_TILE &&
+            (h.N <= HEAD_TILE / 2 || (size_t)h.T * (rows2 / HEAD_TILE) * ((h.V + HEAD_TILE - 1) / HEAD_TILE) <= (size_t)num_sms() / 2);
+    if (h.two) h.Np = (int)rows2;
     // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM
     if (h.N <= HEAD_FEW && h.d <= (p.bf16 ? 2048 : 1024))
         h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));

@@ -9,9 +9,9 @@ namespace vmoe {
 constexpr int HEAD_K = 128;     // entries of a teacher's list at most
 constexpr int HEAD_V = 1 << 20;  // entries of a vocabulary at most, with a teacher
 constexpr int HEAD_FEW = 16;    // tokens of a head at most for head_few
-// Up to 128 bf16 tokens a head, which leave half of a tile's rows empty, have two rows each in the backward: token r (packed) row
-// 32 (r / 16) + r % 16 and the one 16 behind it, which a warp of an epilogue has both of.  z is the same in both, dl in the
-// second what rounding takes from the first: it is then kept to 2^-16, and the sums need no other code.  map is -1 for the second.
+// A few bf16 tokens a head (head_plan has the rule) have two rows each in the backward: token r (packed) row 32 (r / 16) + r % 16
+// and the one 16 behind it, which a warp of an epilogue has both of.  z is the same in both, dl in the second what rounding
+// takes from the first: it is then kept to 2^-16, and the sums need no other code.  map is -1 for the second.
 constexpr int HEAD_HALF = 16;
 __host__ __device__ constexpr int two_row(int r) { return 2 * HEAD_HALF * (r / HEAD_HALF) + r % HEAD_HALF; }
 __host__ __device__ constexpr int two_token(int row) { return HEAD_HALF * (row / (2 * HEAD_HALF)) + row % HEAD_HALF; }

@@ -359,3 +359,15 @@ def test_high_temperatures(N, K, dtype, tau):
         r = _check(_run(p, head, z, w, s, nbytes), z, w, s, tau, dtype)
     at = np.take_along_axis(r["logits"], s["tidx"][..., K - 1:].numpy().astype(np.int64), 2)[..., 0]
     assert np.median(np.exp(at - r["lse"])) > 0.5
+
+
+@pytest.mark.parametrize("size", [(1, 197, 1000, 384, 8, 2.0), (1, 129, 9001, 72, 0, 1.0), (1, 256, 5000, 264, 5, 0.5), (5, 193, 1500, 136, 0, 1.0)],
+                         ids=str)
+def test_gradients_of_an_image(size):
+    """Up to 256 tokens a head against a small vocabulary, one image's as a rule: dl is kept to 2^-16 as well."""
+    T, N, V, d, K, tau = size
+    p, head = vm.problem(T, N, d, 8, 1, 1, 1.0, "bf16"), vm.head_config(V, K, tau)
+    for ragged in (False, True):
+        z, w, s = _inputs(T, N, V, d, K, "bf16", False, True, ragged, seed=7)
+        _check(_run(p, head, z, w, s), z, w, s, tau, "bf16", few=True)
+        _check(_run(p, head, z, w, s, vm.vmoe_head_min_workspace_size(p, head)), z, w, s, tau, "bf16", few=True)
