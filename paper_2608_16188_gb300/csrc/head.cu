@@ -15,7 +15,8 @@
 //
 // Forward: [head_mark] head_pack [head_list] HEAD_STATS or head_few, head_finish; backward: [head_mark] head_pack, then for
 // each piece of the vocabulary HEAD_DLOGITS [head_patch] HEAD_DZ HEAD_DW, then [head_dz_join].  17 x 1576 tokens, 32000
-// entries, d 768, a head each: 3.4 ms, of it the products 725, 860, 810 and 755 us, packing 28 and 22, joining the sums 23.
+// entries, d 768, a head each: 3.4 ms on the same inputs in a row, of it the products 725, 860, 810 and 755 us, packing 28 and 22,
+// joining the sums 23; 3.75 on inputs that change, at the power limit.
 #include <math.h>
 
 #include <algorithm>
@@ -741,7 +742,9 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.two = p.bf16 && h.N <= HEAD_TILE &&
             (h.N <= HEAD_TILE / 2 || (size_t)h.T * (rows2 / HEAD_TILE) * ((h.V + HEAD_TILE - 1) / HEAD_TILE) <= (size_t)num_sms() / 2);
     if (h.two) h.Np = (int)rows2;
-    // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM
+    // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM, while two hold the tokens.  4 tokens, us so and as tiles:
+    // 128000 entries in bf16, d 2048 110 and 116, 2560 137 and 137, 4096 (one CTA) 218 and 199; 50000 in fp32, d 1024 98 and 212, 2048
+    // (one CTA) 149 and 407
     if (h.N <= HEAD_FEW && h.d <= (p.bf16 ? 2048 : 1024))
         h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));
     h.tau = head->temperature;
@@ -774,7 +777,8 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.coef = take(rowsp * 16);
     h.at_label = take(rowsp * 4);
     const size_t fixed = o, column = rowsp * HEAD_TILE * 2 * h.parts;  // a tile of columns of dl
-    // the whole vocabulary at once where there is room: dz is then shared out to the SM pairs
+    // the whole vocabulary at once where there is room: dz is then shared out to the SM pairs.  Backward in pieces and at once, us,
+    // d 1024: 16384 tokens, 128000 entries 7990 and 7870; 2304 tokens, 500000 entries, whose tiles of dz leave pairs idle, 4980 and 4170
     const size_t tiles_d = rowsp / HEAD_TILE * ((h.d + HEAD_TILE - 1) / HEAD_TILE), blocks = ((size_t)h.V + 63) / 64;
     const size_t pairs = std::min<size_t>(std::max(1, num_sms() / 2), std::max(tiles_d, tiles_d * blocks / dz_least(h.parts)));
     const size_t whole = pairs * HEAD_TILE * HEAD_TILE * 4, sums = (rowsp * h.d * 4 + 255) & ~(size_t)255;
