@@ -742,9 +742,9 @@ bool head_plan(const Dims &p, const vmoe_head *head, bool label, size_t bytes, H
     h.two = p.bf16 && h.N <= HEAD_TILE &&
             (h.N <= HEAD_TILE / 2 || (size_t)h.T * (rows2 / HEAD_TILE) * ((h.V + HEAD_TILE - 1) / HEAD_TILE) <= (size_t)num_sms() / 2);
     if (h.two) h.Np = (int)rows2;
-    // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM, while two hold the tokens.  4 tokens, us so and as tiles:
-    // 128000 entries in bf16, d 2048 110 and 116, 2560 137 and 137, 4096 (one CTA) 218 and 199; 50000 in fp32, d 1024 98 and 212, 2048
-    // (one CTA) 149 and 407
+    // a warp 32 (fp32: 16) entries at a time, two CTAs of eight warps an SM.  4 tokens, us so and as tiles: 128000 entries in bf16, d 2048
+    // 110 and 116, 2560 137 and 137, 4096, where an SM holds the tokens once, 218 and 199; 50000 in fp32, d 1024 98 and 212; wider ones
+    // (1536, held once: 116 and 309) are still tiles
     if (h.N <= HEAD_FEW && h.d <= (p.bf16 ? 2048 : 1024))
         h.few = std::max(1, std::min((h.V + 255) / 256, std::max(1, 2 * num_sms() / h.T)));
     h.tau = head->temperature;
